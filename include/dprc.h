@@ -41,7 +41,8 @@
  * rows 32w..32w+31 of a layer's probe matrix in stream s is word (w mod 4) of
  * Philox(counter = (w div 4, j, layer_id, s), key = (seed lo, seed hi)); bit b
  * gives row 32w+b, 0 -> +1, 1 -> -1.  Streams: 0 = Hutchinson probes (also
- * the Hutch++ residual probes), 1 = Hutch++ sketch, 2 = Gaussian noise.
+ * the Hutch++ residual probes), 1 = Hutch++ sketch, 2 = Gaussian noise, 3 =
+ * Gaussian probes, 4 = dropout.
  */
 #ifndef DPRC_H
 #define DPRC_H
@@ -238,6 +239,92 @@ dprc_status dprc_private_adamw(float* theta, float* m, float* v, int64_t ldt, co
                                uint32_t tensor_id, float inv_batch, const dprc_adamw_params* hp,
                                uint16_t* w, int64_t ldw, hipStream_t stream);
 
+/* ---- Dropout, residual sum and norm -------------------------------------------------
+ * What lies between two linear layers of a decoder block, and the private
+ * gradient of the norm's own weight and bias.
+ *
+ * Dropout's mask is never stored: it is a function of (seed, site_id, row, column),
+ * so the backward pass makes it again.  Row r of a call is token row i*T + t.  The
+ * 16 bits of element (r, c) are half (c mod 2) (0 = the low one) of word
+ * (c mod 8) div 2 of Philox(counter = (c div 8, r, site_id, 4), key = (seed lo,
+ * seed hi)); with q = floor(65536 p + 1/2) it is dropped iff these bits are below q
+ * (p acts in steps of 2^-16).  A dropped element counts as exactly 0, also where the
+ * input is infinite or NaN; a kept one is multiplied by 65536 / (65536 - q).
+ * q = 0 leaves the input as it is, q = 65536 drops everything.  The caller folds
+ * the training step into `seed` and gives each place in the model its site_id.
+ *
+ * All arithmetic is in fp32 on inputs of either type, each output rounded once.  Rows
+ * may lie at any alignment of their element (16-byte boundaries are fastest).
+ * B, T, n >= 1; B * T <= 2^31 and n <= 2^30, else DPRC_ERROR_NOT_SUPPORTED, as is a
+ * pointer that is not aligned to its element.  An output may be the very tensor (same
+ * pointer and row stride) that an input of the call is, where it says so; no other
+ * overlap is allowed.
+ *
+ * dprc_dropout: out = res + dropout(x) (res may be NULL: none).  The backward pass is
+ * the same call on the gradient, without res.  out may be x or res. */
+dprc_status dprc_dropout(const void* x, int64_t ldx, const void* res, int64_t ldr, void* out, int64_t ldo,
+                         int64_t rows, int64_t n, dprc_dtype dtype, float p, uint64_t seed, uint32_t site_id,
+                         hipStream_t stream);
+
+typedef enum { DPRC_LAYERNORM = 0, DPRC_RMSNORM = 1 } dprc_ln_kind;
+
+/* One norm over the last axis of [B, T, n] rows, and the dropout before it. */
+typedef struct {
+  int64_t B, T, n;
+  dprc_dtype dtype;     /* x, res, sum, y and their gradients                   */
+  dprc_dtype wdtype;    /* weight, bias                                         */
+  dprc_ln_kind kind;
+  float eps;            /* > 0, finite (forward)                                */
+  const void* weight;   /* [n], NULL = ones                                     */
+  const void* bias;     /* [n], NULL = zeros (forward only)                     */
+  float p;              /* dropout rate in [0, 1]                               */
+  uint32_t site_id;
+  uint64_t seed;
+} dprc_ln;
+
+/* Forward, per row:  s = res + dropout(x);  y = (s - mu) * rstd * weight + bias
+ *   LAYERNORM: mu = mean(s), rstd = 1 / sqrt(mean((s - mu)^2) + eps)
+ *   RMSNORM:   mu = 0,       rstd = 1 / sqrt(mean(s^2) + eps)
+ * The norm is taken of s in fp32, before s is rounded for `sum`.  res may be NULL
+ * (none); sum may be NULL (s is not wanted, or is x itself); mean (LAYERNORM only) and
+ * rstd, [B*T] fp32, may be NULL (no backward pass follows).  y may be x or res,
+ * sum may be x or res (y and sum must differ). */
+dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const void* res, int64_t ldr, void* sum,
+                           int64_t lds, void* y, int64_t ldy, float* mean, float* rstd, hipStream_t stream);
+
+/* Backward, from dy = dL/dy, s (the forward's `sum`, or x where there was none) and its
+ * statistics.  With xh = (s - mu) * rstd and g = dy * weight, per row:
+ *   dx = ds + rstd * (g - mean(g) - xh * mean(g * xh))       (RMSNORM: no mean(g))
+ *   dh = dropout(dx)                                         (from dx before rounding)
+ *   dw[i] = sum_t dy * xh,   db[i] = sum_t dy                of each sample i, [B, n] fp32
+ * ds (may be NULL: zero) is the gradient that reaches s past the norm, dx is the
+ * gradient with respect to s (and so res), dh that with respect to x.  Each of dx, dh,
+ * dw, db may be NULL; one at least is not.  dw and db have row stride ldg >= n.  dx or dh
+ * may be dy, s or ds (dx and dh must differ).  mean is read for LAYERNORM only; L->bias
+ * and L->eps are not read.  Workspace (needed with dw or db):
+ * dprc_layernorm_backward_workspace() bytes (0 when the arguments are invalid). */
+size_t dprc_layernorm_backward_workspace(const dprc_ln* L);
+dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t lddy, const void* s, int64_t lds,
+                                    const float* mean, const float* rstd, const void* ds, int64_t ldds, void* dx,
+                                    int64_t lddx, void* dh, int64_t lddh, float* dw, float* db, int64_t ldg,
+                                    void* ws, size_t ws_bytes, hipStream_t stream);
+
+/* ---- per-sample vector gradients (norm weights, biases) ------------------------------
+ * G [B, n] fp32 (row stride ldg >= n) holds every sample's gradient of a vector parameter,
+ * or of all of a model's side by side.  dprc_norm_vectors adds their exact squared
+ * norms to the estimates of the linear layers:  n2[i] (=|+=) sum_j G[i,j]^2  (the sum
+ * in fp64).  dprc_clip_accumulate_vectors is the clipped sum:
+ * grad[j] (=|+=) sum_i c[i] G[i,j], samples with c[i] == 0 skipped entirely.
+ * 1 <= B, n; B <= 2^24 and n <= 2^40, else DPRC_ERROR_NOT_SUPPORTED.  Workspaces: the
+ * matching queries (0 bytes: none needed, ws may be NULL; also 0 for invalid sizes). */
+size_t dprc_norm_vectors_workspace(int64_t B, int64_t n);
+dprc_status dprc_norm_vectors(const float* G, int64_t ldg, int64_t B, int64_t n, float* n2, int32_t accumulate,
+                              void* ws, size_t ws_bytes, hipStream_t stream);
+size_t dprc_clip_accumulate_vectors_workspace(int64_t B, int64_t n);
+dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const float* c, int64_t B, int64_t n,
+                                         float* grad, int32_t accumulate, void* ws, size_t ws_bytes,
+                                         hipStream_t stream);
+
 /* ---- Envelope CDF of the Hutchinson estimate (privacy accounting) ------------------
  * Proposition on the extremal envelope and the appendix algorithms cdf-grid and
  * binary-search-xplus.  dprc_envelope_middle evaluates MiddleRegionCDF at nx
@@ -353,7 +440,12 @@ typedef enum {
   DPRC_KERNEL_ADAMW = 20,             /* private AdamW step                      */
   DPRC_KERNEL_ENVELOPE = 21,          /* MiddleRegionCDF candidates and reduction */
   DPRC_KERNEL_CHI2_CDF = 22,          /* chi-squared CDF values                  */
-  DPRC_KERNEL_PLD = 23                /* accountant: bins, step PLD, fold, delta */
+  DPRC_KERNEL_PLD = 23,               /* accountant: bins, step PLD, fold, delta */
+  DPRC_KERNEL_DROPOUT = 24,           /* dropout and residual sum                */
+  DPRC_KERNEL_LAYERNORM = 25,         /* dropout, residual sum and norm          */
+  DPRC_KERNEL_LAYERNORM_BACKWARD = 26,
+  DPRC_KERNEL_VECTOR_NORMS = 27,      /* squared norms of per-sample vectors     */
+  DPRC_KERNEL_VECTOR_SUMS = 28        /* clipped sums of per-sample vectors, sums of their token splits */
 } dprc_kernel_kind;
 dprc_status dprc_trace_launches(hipEvent_t* events, int32_t* kinds, int32_t capacity,
                                 int32_t* count);

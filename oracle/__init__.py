@@ -11,6 +11,8 @@ LLMs with Randomized Clipping" (Ullah, Aketi, Gupta, Zhang, Razaviyayn):
                     Algorithm 2, the clip factors, the clipped accumulation and
                     the Gaussian noise of Algorithm 1, and the FLOP model of the
                     appendix table on FLOPs.
+* ``junction``   -- dropout, residual sum and norm between two linear layers, their
+                    gradients, and the per-sample gradients of the norm's weight and bias.
 
 Only ``tests/``, ``__graft_entry__.smoke()`` and the ``cpu_baseline`` leg of
 ``bench.py`` may import anything from here.  The library under
@@ -19,4 +21,4 @@ from the library: the two share no code.  The seeded input generators live in
 ``workloads/``, which holds none of the method's arithmetic.
 """
 
-from . import philox, estimators  # noqa: F401
+from . import philox, estimators, junction  # noqa: F401

@@ -24,7 +24,8 @@ definition independently):
   layer_id, s)).  Bit ``b`` of the word is row ``32w+b``; bit 0 means +1 and
   bit 1 means -1.
 * streams: 0 = Hutchinson probes P (also the Hutch++ residual probes),
-  1 = Hutch++ sketch S, 2 = Gaussian noise, 3 = Gaussian Hutchinson probes.
+  1 = Hutch++ sketch S, 2 = Gaussian noise, 3 = Gaussian Hutchinson probes,
+  4 = dropout (``junction``).
 * Gaussian probe entry of row ``u`` and column ``j`` (the Gaussian probes of
   Algorithm 2, standard normal here and divided by k in the estimate): block
   q = u div 4, counter = (q, j, layer_id, 3); words (x0,x1) give rows 4q, 4q+1

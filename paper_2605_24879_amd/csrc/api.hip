@@ -1602,3 +1602,162 @@ dprc_status dprc_probe_gaussian(uint64_t seed, uint32_t layer_id, int64_t m, int
 }
 
 }  // extern "C"
+
+// ---- dropout, norm, per-sample vectors -------------------------------------------------------
+namespace {
+
+bool dtype_ok(dprc_dtype t) { return t == DPRC_F32 || t == DPRC_BF16; }
+size_t elem_bytes(dprc_dtype t) { return t == DPRC_BF16 ? 2 : 4; }
+
+bool drop_args(float p, uint64_t seed, uint32_t site, DropArgs& d) {
+  if (!(p >= 0.f && p <= 1.f)) return false;
+  const uint32_t q = (uint32_t)std::floor(65536.0 * (double)p + 0.5);
+  d.on = q > 0;
+  d.lim = (q << 16) - 1u;
+  d.scale = q < 65536u ? (float)(65536.0 / (65536.0 - q)) : 0.f;
+  key_of(seed, d.key0, d.key1);
+  d.site = site;
+  return true;
+}
+
+dprc_status check_ln(const dprc_ln* L) {
+  if (!L || L->B < 1 || L->T < 1 || L->n < 1 || !dtype_ok(L->dtype) || !dtype_ok(L->wdtype))
+    return DPRC_ERROR_INVALID_VALUE;
+  if (L->kind != DPRC_LAYERNORM && L->kind != DPRC_RMSNORM) return DPRC_ERROR_INVALID_VALUE;
+  if (!(L->p >= 0.f && L->p <= 1.f)) return DPRC_ERROR_INVALID_VALUE;
+  if (L->n > (1LL << 30) || L->B > (1LL << 31) || L->T > (1LL << 31) || L->B * L->T > (1LL << 31))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  return DPRC_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+dprc_status dprc_dropout(const void* x, int64_t ldx, const void* res, int64_t ldr, void* out, int64_t ldo,
+                         int64_t rows, int64_t n, dprc_dtype dtype, float p, uint64_t seed, uint32_t site_id,
+                         hipStream_t stream) {
+  DropoutArgs a;
+  if (!x || !out || rows < 1 || n < 1 || !dtype_ok(dtype) || ldx < n || ldo < n || (res && ldr < n) ||
+      !drop_args(p, seed, site_id, a.drop))
+    return DPRC_ERROR_INVALID_VALUE;
+  const size_t e = elem_bytes(dtype);
+  if (rows > (1LL << 31) || n > (1LL << 30) || !aligned(x, e) || !aligned(res, e) || !aligned(out, e))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  a.x = x; a.res = res; a.out = out;
+  a.ldx = ldx; a.ldr = ldr; a.ldo = ldo;
+  a.rows = rows; a.n = n; a.bf16 = dtype == DPRC_BF16;
+  return hip_status(traced(DPRC_KERNEL_DROPOUT, stream, [&] { return launch_dropout(a, stream); }));
+}
+
+dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const void* res, int64_t ldr, void* sum,
+                           int64_t lds, void* y, int64_t ldy, float* mean, float* rstd, hipStream_t stream) {
+  dprc_status st = check_ln(L);
+  if (st == DPRC_ERROR_INVALID_VALUE) return st;
+  if (!x || !y || ldx < L->n || ldy < L->n || (res && ldr < L->n) || (sum && lds < L->n) || sum == y ||
+      !(L->eps > 0.f) || !std::isfinite(L->eps))
+    return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  const size_t e = elem_bytes(L->dtype), we = elem_bytes(L->wdtype);
+  if (!aligned(x, e) || !aligned(res, e) || !aligned(sum, e) || !aligned(y, e) || !aligned(L->weight, we) ||
+      !aligned(L->bias, we) || !aligned(mean, 4) || !aligned(rstd, 4))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  NormArgs a;
+  drop_args(L->p, L->seed, L->site_id, a.drop);
+  a.x = x; a.res = res; a.sum = sum; a.y = y;
+  a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
+  a.w = L->weight; a.b = L->bias;
+  a.rms = L->kind == DPRC_RMSNORM;
+  a.mean = a.rms ? nullptr : mean; a.rstd = rstd;
+  a.rows = L->B * L->T; a.n = L->n;
+  a.eps = L->eps; a.inv_n = (float)(1.0 / (double)L->n);
+  a.bf16 = L->dtype == DPRC_BF16; a.wbf16 = L->wdtype == DPRC_BF16;
+  return hip_status(traced(DPRC_KERNEL_LAYERNORM, stream, [&] { return launch_norm(a, stream); }));
+}
+
+size_t dprc_layernorm_backward_workspace(const dprc_ln* L) {
+  if (check_ln(L) != DPRC_SUCCESS) return 0;
+  const int S = norm_back_splits(L->B, L->T, L->n);
+  return S > 1 ? (size_t)round_up(L->B * S * 2 * L->n * (int64_t)sizeof(float), kAlign) : 0;
+}
+
+dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t lddy, const void* s, int64_t lds,
+                                    const float* mean, const float* rstd, const void* ds, int64_t ldds, void* dx,
+                                    int64_t lddx, void* dh, int64_t lddh, float* dw, float* db, int64_t ldg,
+                                    void* ws, size_t ws_bytes, hipStream_t stream) {
+  dprc_status st = check_ln(L);
+  if (st == DPRC_ERROR_INVALID_VALUE) return st;
+  const bool grads = dw || db;
+  if (!dy || !s || !rstd || (L->kind == DPRC_LAYERNORM && !mean) || (!dx && !dh && !grads) || lddy < L->n ||
+      lds < L->n || (ds && ldds < L->n) || (dx && lddx < L->n) || (dh && lddh < L->n) || (grads && ldg < L->n) ||
+      (dx && dx == dh) || (dw && dw == db))
+    return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  const size_t e = elem_bytes(L->dtype);
+  if (!aligned(dy, e) || !aligned(s, e) || !aligned(ds, e) || !aligned(dx, e) || !aligned(dh, e) ||
+      !aligned(L->weight, elem_bytes(L->wdtype)) || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(dw, 4) ||
+      !aligned(db, 4))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  const size_t need = grads ? dprc_layernorm_backward_workspace(L) : 0;
+  if (ws_bytes < need) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (need && (!ws || !aligned(ws, kAlign))) return DPRC_ERROR_INVALID_VALUE;
+  NormBackArgs a;
+  drop_args(L->p, L->seed, L->site_id, a.drop);
+  a.dy = dy; a.s = s; a.ds = ds; a.dx = dx; a.dh = dh;
+  a.lddy = lddy; a.lds = lds; a.ldds = ldds; a.lddx = lddx; a.lddh = lddh;
+  a.w = L->weight; a.mean = mean; a.rstd = rstd;
+  a.dw = dw; a.db = db; a.ldg = ldg;
+  a.B = L->B; a.T = L->T; a.n = L->n;
+  a.inv_n = (float)(1.0 / (double)L->n);
+  a.bf16 = L->dtype == DPRC_BF16; a.wbf16 = L->wdtype == DPRC_BF16; a.rms = L->kind == DPRC_RMSNORM;
+  a.S = norm_back_splits(L->B, L->T, L->n);
+  a.part = static_cast<float*>(ws);
+  st = hip_status(traced(DPRC_KERNEL_LAYERNORM_BACKWARD, stream, [&] { return launch_norm_back(a, stream); }));
+  if (st != DPRC_SUCCESS || !grads || a.S == 1) return st;
+  return hip_status(traced(DPRC_KERNEL_VECTOR_SUMS, stream, [&] { return launch_norm_back_sums(a, stream); }));
+}
+
+static dprc_status check_vectors(const float* G, int64_t ldg, int64_t B, int64_t n, const void* out) {
+  if (!G || !out || B < 1 || n < 1 || ldg < n) return DPRC_ERROR_INVALID_VALUE;
+  if (B > (1LL << 24) || n > (1LL << 40) || !aligned(G, 4) || !aligned(out, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  return DPRC_SUCCESS;
+}
+
+size_t dprc_norm_vectors_workspace(int64_t B, int64_t n) {
+  if (B < 1 || n < 1 || B > (1LL << 24) || n > (1LL << 40)) return 0;
+  const int S = vector_norm_splits(B, n);
+  return S > 1 ? (size_t)round_up(B * S * (int64_t)sizeof(double), kAlign) : 0;
+}
+
+dprc_status dprc_norm_vectors(const float* G, int64_t ldg, int64_t B, int64_t n, float* n2, int32_t accumulate,
+                              void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dprc_status st = check_vectors(G, ldg, B, n, n2);
+  if (st != DPRC_SUCCESS) return st;
+  const size_t need = dprc_norm_vectors_workspace(B, n);
+  if (ws_bytes < need) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (need && (!ws || !aligned(ws, kAlign))) return DPRC_ERROR_INVALID_VALUE;
+  const VectorArgs a{G, ldg, B, n, nullptr, n2, accumulate, vector_norm_splits(B, n), ws};
+  return hip_status(traced(DPRC_KERNEL_VECTOR_NORMS, stream, [&] { return launch_vector_norms(a, stream); }));
+}
+
+size_t dprc_clip_accumulate_vectors_workspace(int64_t B, int64_t n) {
+  if (B < 1 || n < 1 || B > (1LL << 24) || n > (1LL << 40)) return 0;
+  const int S = vector_sum_splits(B, n);
+  return S > 1 ? (size_t)round_up(S * n * (int64_t)sizeof(float), kAlign) : 0;
+}
+
+dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const float* c, int64_t B, int64_t n,
+                                         float* grad, int32_t accumulate, void* ws, size_t ws_bytes,
+                                         hipStream_t stream) {
+  const dprc_status st = check_vectors(G, ldg, B, n, grad);
+  if (st == DPRC_ERROR_INVALID_VALUE || !c) return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(c, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  const size_t need = dprc_clip_accumulate_vectors_workspace(B, n);
+  if (ws_bytes < need) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (need && (!ws || !aligned(ws, kAlign))) return DPRC_ERROR_INVALID_VALUE;
+  const VectorArgs a{G, ldg, B, n, c, grad, accumulate, vector_sum_splits(B, n), ws};
+  return hip_status(traced(DPRC_KERNEL_VECTOR_SUMS, stream, [&] { return launch_vector_sums(a, stream); }));
+}
+
+}  // extern "C"

@@ -44,7 +44,7 @@ __device__ __forceinline__ u32x4 philox4x32_10(u32x4 c, uint32_t k0, uint32_t k1
   return c;
 }
 
-enum : uint32_t { kStreamProbe = 0, kStreamSketch = 1, kStreamNoise = 2, kStreamGaussProbe = 3 };
+enum : uint32_t { kStreamProbe = 0, kStreamSketch = 1, kStreamNoise = 2, kStreamGaussProbe = 3, kStreamDropout = 4 };
 enum : int { kProbeRademacher = 0, kProbeHadamard = 1 };
 
 // Four consecutive probe words (rows 128*blk .. 128*blk+127) of column j.

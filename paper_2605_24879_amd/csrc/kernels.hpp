@@ -360,6 +360,83 @@ struct AdamArgs {
 };
 hipError_t launch_private_adamw(const AdamArgs& a, hipStream_t st);
 
+// Dropout of a site (see dprc_dropout).  With q = floor(65536 p + 1/2), an element is kept iff
+// its 16 bits u are not below q, that is (u << 16) > (q << 16) - 1 in unsigned arithmetic, also
+// for q = 65536 (never).
+struct DropArgs {
+  int32_t on;              // q > 0
+  uint32_t lim;            // (q << 16) - 1
+  float scale;             // 65536 / (65536 - q); 0 for q = 65536
+  uint32_t key0, key1, site;
+};
+struct DropoutArgs {
+  const void* x;
+  const void* res;         // may be null
+  void* out;
+  int64_t ldx, ldr, ldo;
+  int64_t rows, n;
+  int32_t bf16;
+  DropArgs drop;
+};
+hipError_t launch_dropout(const DropoutArgs& a, hipStream_t st);
+
+// Norm of token rows and its backward pass (see dprc_layernorm).
+struct NormArgs {
+  const void* x;
+  const void* res;         // may be null
+  void* sum;               // may be null
+  void* y;
+  int64_t ldx, ldr, lds, ldy;
+  const void* w;           // null: ones
+  const void* b;           // null: zeros
+  float* mean;             // may be null
+  float* rstd;             // may be null
+  int64_t rows, n;
+  float eps, inv_n;
+  int32_t bf16, wbf16, rms;
+  DropArgs drop;
+};
+hipError_t launch_norm(const NormArgs& a, hipStream_t st);
+
+struct NormBackArgs {
+  const void* dy;
+  const void* s;
+  const void* ds;          // may be null
+  void* dx;                // may be null
+  void* dh;                // may be null
+  int64_t lddy, lds, ldds, lddx, lddh;
+  const void* w;           // null: ones
+  const float* mean;       // layer norm
+  const float* rstd;
+  float* dw;               // [B][ldg], may be null
+  float* db;               // [B][ldg], may be null
+  int64_t ldg;
+  int64_t B, T, n;
+  float inv_n;
+  int32_t bf16, wbf16, rms;
+  int32_t S;               // token splits of a sample (of ceil(T / S) rows each)
+  float* part;             // [B][S][2][n] (S > 1)
+  DropArgs drop;
+};
+int norm_back_splits(int64_t B, int64_t T, int64_t n);
+hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t st);
+hipError_t launch_norm_back_sums(const NormBackArgs& a, hipStream_t st);   // S > 1: dw and db from part
+
+// Per-sample vectors G [B][ldg] (see dprc_norm_vectors).
+struct VectorArgs {
+  const float* G;
+  int64_t ldg, B, n;
+  const float* c;          // clipped sums
+  float* out;              // n2 [B] or grad [n]
+  int32_t accumulate;
+  int32_t S;               // splits: of the columns (norms) or of the samples (sums)
+  void* part;              // S > 1: [B][S] double (norms), [S][n] float (sums)
+};
+int vector_norm_splits(int64_t B, int64_t n);
+int vector_sum_splits(int64_t B, int64_t n);
+hipError_t launch_vector_norms(const VectorArgs& a, hipStream_t st);
+hipError_t launch_vector_sums(const VectorArgs& a, hipStream_t st);
+
 // Gaussian probe columns, column j at [j*ld .. j*ld + ld) (rows >= m zero);
 // any of hi/lo (both or neither) and f32 may be null.
 hipError_t launch_gauss_probe(uint32_t key0, uint32_t key1, uint32_t layer, int64_t m, int32_t k, int64_t ld,

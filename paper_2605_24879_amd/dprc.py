@@ -20,14 +20,17 @@ SUCCESS = 0
 F32, BF16 = 0, 1
 SIDE_OUT, SIDE_IN, SIDE_AUTO = 0, 1, 2
 PROBE_RADEMACHER, PROBE_HADAMARD, PROBE_GAUSSIAN = 0, 1, 2
-STREAM_PROBE, STREAM_SKETCH, STREAM_NOISE = 0, 1, 2
+STREAM_PROBE, STREAM_SKETCH, STREAM_NOISE, STREAM_GAUSS_PROBE, STREAM_DROPOUT = 0, 1, 2, 3, 4
+LAYERNORM, RMSNORM = 0, 1
 
 EXPORTS = ["dprc_norm_hutch_workspace", "dprc_norm_hutch", "dprc_norm_hutch_clip", "dprc_norm_hutch_clip_static", "dprc_norm_hutchpp_workspace",
            "dprc_norm_hutchpp", "dprc_clip_scale", "dprc_clip_accumulate_workspace",
            "dprc_clip_accumulate", "dprc_clip_accumulate_layers", "dprc_add_noise", "dprc_probe_bits", "dprc_probe_gaussian", "dprc_private_adamw", "dprc_envelope_middle_workspace",
            "dprc_envelope_middle", "dprc_chi2_cdf", "dprc_envelope_bins", "dprc_pld_step_workspace",
            "dprc_pld_step", "dprc_pld_fold", "dprc_pld_delta", "dprc_status_string",
-           "dprc_version", "dprc_trace_launches"]
+           "dprc_version", "dprc_trace_launches", "dprc_dropout", "dprc_layernorm",
+           "dprc_layernorm_backward_workspace", "dprc_layernorm_backward", "dprc_norm_vectors_workspace",
+           "dprc_norm_vectors", "dprc_clip_accumulate_vectors_workspace", "dprc_clip_accumulate_vectors"]
 
 
 class Layer(ctypes.Structure):
@@ -42,6 +45,14 @@ class AdamWParams(ctypes.Structure):
     """Mirror of dprc_adamw_params."""
     _fields_ = [("lr", ctypes.c_float), ("beta1", ctypes.c_float), ("beta2", ctypes.c_float),
                 ("eps", ctypes.c_float), ("weight_decay", ctypes.c_float), ("step", ctypes.c_int32)]
+
+
+class LN(ctypes.Structure):
+    """Mirror of dprc_ln."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("dtype", ctypes.c_int), ("wdtype", ctypes.c_int), ("kind", ctypes.c_int), ("eps", ctypes.c_float),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
+                ("p", ctypes.c_float), ("site_id", ctypes.c_uint32), ("seed", ctypes.c_uint64)]
 
 
 _lib = None
@@ -84,6 +95,15 @@ def lib():
             "dprc_pld_delta": (ctypes.c_int, [P, I64, ctypes.c_double, P, P, I32, P, P]),
             "dprc_private_adamw": (ctypes.c_int, [P, P, P, I64, P, I64, I64, I64, F, F, U64, U32, F,
                                                   ctypes.POINTER(AdamWParams), P, I64, P]),
+            "dprc_dropout": (ctypes.c_int, [P, I64, P, I64, P, I64, I64, I64, ctypes.c_int, F, U64, U32, P]),
+            "dprc_layernorm": (ctypes.c_int, [P, P, I64, P, I64, P, I64, P, I64, P, P, P]),
+            "dprc_layernorm_backward_workspace": (SZ, [P]),
+            "dprc_layernorm_backward": (ctypes.c_int, [P, P, I64, P, I64, P, P, P, I64, P, I64, P, I64, P, P, I64, P,
+                                                       SZ, P]),
+            "dprc_norm_vectors_workspace": (SZ, [I64, I64]),
+            "dprc_norm_vectors": (ctypes.c_int, [P, I64, I64, I64, P, I32, P, SZ, P]),
+            "dprc_clip_accumulate_vectors_workspace": (SZ, [I64, I64]),
+            "dprc_clip_accumulate_vectors": (ctypes.c_int, [P, I64, P, I64, I64, P, I32, P, SZ, P]),
             "dprc_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "dprc_version": (ctypes.c_char_p, []),
             "dprc_trace_launches": (ctypes.c_int, [P, P, I32, P]),
@@ -403,6 +423,179 @@ def dprc_probe_gaussian(seed, layer_id, m, k, device="cuda", out=None):
     return out
 
 
+def _token_rows(x, name, shape=None, dtype=None, dev=None):
+    """The row stride of [B, T, n] token rows, after checks of the tensor's shape, dtype, device and strides."""
+    if x.dim() != 3:
+        raise ValueError(f"{name} must be [B, T, n]")
+    if shape is not None:
+        if x.shape != shape:
+            raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
+        if x.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
+        if x.device != dev:
+            raise ValueError(f"{name} must be on {dev}, not {x.device}")
+    B, T, n = x.shape
+    s0, s1, s2 = x.stride()
+    if T == 1:
+        s1 = s0 if B > 1 else n
+    elif B > 1 and s0 != T * s1:
+        s2 = 0
+    if s2 != 1 and (n > 1 or s2 == 0):
+        raise ValueError(f"{name} must have contiguous features, token rows of stride ld, samples of stride T*ld")
+    return s1
+
+
+def _vector(x, name, n, dev, dtype=torch.float32):
+    """The pointer of a contiguous vector of n entries (None for no vector)."""
+    if x is None:
+        return None
+    if x.device != dev:
+        raise ValueError(f"{name} must be on {dev}, not {x.device}")
+    if x.dtype != dtype or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous entries of {dtype}")
+    return x.data_ptr()
+
+
+def _ln(x, kind, weight, bias, eps, p, seed, site_id):
+    """dprc_ln of the norm of x [B, T, n]."""
+    B, T, n = x.shape
+    wd = weight if weight is not None else bias
+    wdtype = wd.dtype if wd is not None else torch.float32
+    return LN(B, T, n, _dtype_code(x), F32 if wdtype == torch.float32 else _dtype_code(wd), kind, eps,
+              _vector(weight, "weight", n, x.device, wdtype), _vector(bias, "bias", n, x.device, wdtype), p,
+              site_id, seed)
+
+
+def dprc_dropout(x, p, seed, site_id, res=None, out=None):
+    """res + dropout(x) (res may be None) of [B, T, n] token rows.  The same call on a gradient, with the same
+    seed and site and without res, is dropout's backward pass."""
+    ldx = _token_rows(x, "x")
+    dev, dtype = x.device, x.dtype
+    ldr = 0 if res is None else _token_rows(res, "res", x.shape, dtype, dev)
+    B, T, n = x.shape
+    if out is None:
+        out = torch.empty((B, T, n), dtype=dtype, device=dev)
+        ldo = n
+    else:
+        ldo = _token_rows(out, "out", x.shape, dtype, dev)
+    _check(lib().dprc_dropout(x.data_ptr(), ldx, None if res is None else res.data_ptr(), ldr, out.data_ptr(), ldo,
+                              B * T, n, _dtype_code(x), p, seed, site_id, _stream(dev)))
+    return out
+
+
+def dprc_layernorm(x, weight=None, bias=None, eps=1e-5, kind=LAYERNORM, res=None, p=0.0, seed=0, site_id=0,
+                   stats=True, y=None, s=None):
+    """s = res + dropout(x) and its norm y over the last axis of [B, T, n]: returns (y, s, mean, rstd).
+
+    s is x itself where there is neither res nor dropout.  mean (None for RMSNORM) and rstd are [B*T] fp32,
+    what the backward pass needs besides s; with stats=False both are None."""
+    ldx = _token_rows(x, "x")
+    dev, dtype, shape = x.device, x.dtype, x.shape
+    B, T, n = shape
+    ldr = 0 if res is None else _token_rows(res, "res", shape, dtype, dev)
+    L = _ln(x, kind, weight, bias, eps, p, seed, site_id)
+    lds = ldy = n
+    if s is not None:
+        lds = _token_rows(s, "s", shape, dtype, dev)
+    elif res is not None or p > 0.0:
+        s = torch.empty((B, T, n), dtype=dtype, device=dev)
+    if y is None:
+        y = torch.empty((B, T, n), dtype=dtype, device=dev)
+    else:
+        ldy = _token_rows(y, "y", shape, dtype, dev)
+    mean = rstd = None
+    if stats:
+        rstd = torch.empty(B * T, dtype=torch.float32, device=dev)
+        if kind == LAYERNORM:
+            mean = torch.empty(B * T, dtype=torch.float32, device=dev)
+    _check(lib().dprc_layernorm(ctypes.byref(L), x.data_ptr(), ldx, None if res is None else res.data_ptr(), ldr,
+                                None if s is None else s.data_ptr(), lds, y.data_ptr(), ldy,
+                                None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(),
+                                _stream(dev)))
+    return y, x if s is None else s, mean, rstd
+
+
+def dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=LAYERNORM, ds=None, p=0.0, seed=0, site_id=0,
+                            weight_grad=True, bias_grad=True, dx=None, dh=None, dw=None, db=None, ws=None):
+    """Gradients of dprc_layernorm from dy = dL/dy, s and its statistics: returns (dx, dh, dw, db).
+
+    dx = dL/ds (ds, the gradient that reaches s past the norm, included), dh = dL/dx through the dropout (None
+    where p = 0, then it is dx), dw and db [B, n] fp32: every sample's own weight and bias gradient (None where
+    not wanted).  dw and db may be given as column slices of one buffer; they share a row stride."""
+    ldd = _token_rows(dy, "dy")
+    dev, dtype, shape = dy.device, dy.dtype, dy.shape
+    B, T, n = shape
+    lds = _token_rows(s, "s", shape, dtype, dev)
+    ldds = 0 if ds is None else _token_rows(ds, "ds", shape, dtype, dev)
+    L = _ln(dy, kind, weight, None, 0.0, p, seed, site_id)
+    lddx = lddh = n
+    if dx is None:
+        dx = torch.empty((B, T, n), dtype=dtype, device=dev)
+    else:
+        lddx = _token_rows(dx, "dx", shape, dtype, dev)
+    if dh is not None:
+        lddh = _token_rows(dh, "dh", shape, dtype, dev)
+    elif p > 0.0:
+        dh = torch.empty((B, T, n), dtype=dtype, device=dev)
+    if dw is None and weight_grad:
+        dw = torch.empty((B, n), dtype=torch.float32, device=dev) if db is None else torch.empty_like(db)
+    if db is None and bias_grad:
+        db = (torch.empty((B, n), dtype=torch.float32, device=dev) if dw is None or dw.stride(0) == n
+              else torch.empty_strided(dw.shape, dw.stride(), dtype=torch.float32, device=dev))
+    ldg = 0
+    for g, name in ((dw, "dw"), (db, "db")):
+        if g is None:
+            continue
+        if g.shape != (B, n) or g.dtype != torch.float32 or g.device != dev or (n > 1 and g.stride(1) != 1):
+            raise ValueError(f"{name} must be [B, n] fp32 on {dev} with contiguous rows")
+        ld = g.stride(0) if B > 1 else max(n, ldg)
+        if ldg and ld != ldg:
+            raise ValueError("dw and db must share a row stride")
+        ldg = ld
+    need = 0
+    if ldg:
+        need = lib().dprc_layernorm_backward_workspace(ctypes.byref(L))
+        ws = _workspace(need, dev, ws) if need else None
+    ptr = lambda t: None if t is None else t.data_ptr()
+    _check(lib().dprc_layernorm_backward(ctypes.byref(L), dy.data_ptr(), ldd, s.data_ptr(), lds,
+                                         _vector(mean, "mean", B * T, dev), _vector(rstd, "rstd", B * T, dev),
+                                         ptr(ds), ldds, ptr(dx), lddx, ptr(dh), lddh, ptr(dw), ptr(db), ldg,
+                                         ptr(ws) if need else None, need, _stream(dev)))
+    return dx, dh, dw, db
+
+
+def _sample_vectors(G):
+    if G.dim() != 2 or G.dtype != torch.float32 or (G.shape[1] > 1 and G.stride(1) != 1):
+        raise ValueError("G must be fp32 [B, n] with contiguous rows")
+    B, n = G.shape
+    return B, n, G.stride(0) if B > 1 else n, G.device
+
+
+def dprc_norm_vectors(G, n2=None, accumulate=False, ws=None):
+    """Squared norms of the per-sample vectors G [B, n] (fp32): n2 [B] (=|+=) sum_j G[i, j]^2."""
+    B, n, ldg, dev = _sample_vectors(G)
+    if n2 is None:
+        n2 = _new_n2(B, dev, accumulate)
+    need = lib().dprc_norm_vectors_workspace(B, n)
+    ws = _workspace(need, dev, ws) if need else None
+    _check(lib().dprc_norm_vectors(G.data_ptr(), ldg, B, n, _vector(n2, "n2", B, dev), int(bool(accumulate)),
+                                   ws.data_ptr() if need else None, need, _stream(dev)))
+    return n2
+
+
+def dprc_clip_accumulate_vectors(G, c, grad=None, accumulate=False, ws=None):
+    """Clipped sum of the per-sample vectors G [B, n] (fp32): grad [n] (=|+=) sum_i c_i G[i]."""
+    B, n, ldg, dev = _sample_vectors(G)
+    if grad is None:
+        grad = (torch.zeros if accumulate else torch.empty)(n, dtype=torch.float32, device=dev)
+    need = lib().dprc_clip_accumulate_vectors_workspace(B, n)
+    ws = _workspace(need, dev, ws) if need else None
+    _check(lib().dprc_clip_accumulate_vectors(G.data_ptr(), ldg, _vector(c, "c", B, dev), B, n,
+                                              _vector(grad, "grad", n, dev), int(bool(accumulate)),
+                                              ws.data_ptr() if need else None, need, _stream(dev)))
+    return grad
+
+
 def dprc_version():
     return lib().dprc_version().decode()
 
@@ -411,7 +604,8 @@ KERNEL_NAMES = {1: "project", 2: "token_reduce", 3: "qr", 4: "hutchpp_final", 5:
                 6: "accumulate", 7: "splitk_reduce", 8: "noise", 9: "probe_bits", 10: "project_f32",
                 11: "token_reduce_f32", 12: "sample_sq", 13: "accumulate_f32",
                 14: "token_splits", 15: "sample_sum", 16: "qr_combine", 17: "qr_expand", 18: "hutchpp_sum",
-                19: "probe_gauss", 20: "adamw", 21: "envelope", 22: "chi2_cdf", 23: "pld"}
+                19: "probe_gauss", 20: "adamw", 21: "envelope", 22: "chi2_cdf", 23: "pld", 24: "dropout",
+                25: "layernorm", 26: "layernorm_backward", 27: "vector_norms", 28: "vector_sums"}
 
 
 def dprc_trace_launches(events_ptr, kinds_ptr, capacity, count_ptr):
