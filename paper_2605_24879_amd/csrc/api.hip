@@ -1677,7 +1677,7 @@ dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const v
 
 size_t dprc_layernorm_backward_workspace(const dprc_ln* L) {
   if (check_ln(L) != DPRC_SUCCESS) return 0;
-  const int S = norm_back_splits(L->B, L->T, L->n);
+  const int S = norm_back_splits(L->B, L->T, L->n, L->dtype == DPRC_BF16);
   return S > 1 ? (size_t)round_up(L->B * S * 2 * L->n * (int64_t)sizeof(float), kAlign) : 0;
 }
 
@@ -1710,7 +1710,7 @@ dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t ld
   a.B = L->B; a.T = L->T; a.n = L->n;
   a.inv_n = (float)(1.0 / (double)L->n);
   a.bf16 = L->dtype == DPRC_BF16; a.wbf16 = L->wdtype == DPRC_BF16; a.rms = L->kind == DPRC_RMSNORM;
-  a.S = norm_back_splits(L->B, L->T, L->n);
+  a.S = norm_back_splits(L->B, L->T, L->n, L->dtype == DPRC_BF16);
   a.part = static_cast<float*>(ws);
   st = hip_status(traced(DPRC_KERNEL_LAYERNORM_BACKWARD, stream, [&] { return launch_norm_back(a, stream); }));
   if (st != DPRC_SUCCESS || !grads || a.S == 1) return st;

@@ -6,30 +6,69 @@
 
 namespace dprc {
 
-// One thread takes 8 columns of a row (one Philox block of mask bits) at a time.
-template <class E>
-__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int64_t chunks) {
-  const int64_t total = a.rows * chunks;
-  for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (int64_t)gridDim.x * 256) {
-    const int64_t r = q / chunks, c = 8 * (q - r * chunks);
-    const int m = (int)std::min<int64_t>(8, a.n - c);
-    float x[8], z[8];
-    load8((const E*)a.x + r * a.ldx + c, m, x);
-    drop8(a.drop, (uint32_t)r, (uint32_t)(c >> 3), x);
-    if (a.res) {
-      load8((const E*)a.res + r * a.ldr + c, m, z);
+constexpr int kDropPieces = 4;   // pieces per thread, all loaded before the first is worked on
+
+// A workgroup takes 256 * kDropPieces consecutive pieces of the rows laid end to end (per_row
+// pieces each), a thread every 256th of them: one division finds its first row, steps of
+// 256 pieces are (step_rows, step_pieces) with a carry.
+template <class E, int M, class I>
+__global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int per_row, int step_rows, int step_pieces) {
+  constexpr int EP = kPiece<E>;
+  const int n = (int)a.n;
+  const I q = (I)((int64_t)flat_block() * (256 * kDropPieces) + threadIdx.x);
+  int64_t r = (int64_t)(q / (I)per_row);
+  int c = (int)(q - (I)r * (I)per_row);
+  uint4 x[kDropPieces], z[kDropPieces];
+  int64_t row[kDropPieces];
+  int col[kDropPieces];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] += z[j];
+  for (int k = 0; k < kDropPieces; ++k) {
+    row[k] = r;
+    col[k] = r < a.rows ? c * EP : -1;
+    if (col[k] >= 0) {
+      x[k] = load_row<E, M>((const E*)a.x + r * a.ldx, col[k], n);
+      if (a.res) z[k] = load_row<E, M>((const E*)a.res + r * a.ldr, col[k], n);
     }
-    store8((E*)a.out + r * a.ldo + c, m, x);
+    r += step_rows;
+    c += step_pieces;
+    if (c >= per_row) {
+      c -= per_row;
+      ++r;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kDropPieces; ++k) {
+    if (col[k] < 0) continue;
+    float v[EP], u[EP];
+    unpack_row<E, M>(x[k], col[k], n, v);
+    if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)row[k], col[k], v);
+    if (a.res) {
+      unpack_row<E, M>(z[k], col[k], n, u);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) v[j] += u[j];
+    }
+    store_row<E, M>((E*)a.out + row[k] * a.ldo, col[k], n, v);
   }
 }
 
+template <class E>
+static void launch_dropout_of(const DropoutArgs& a, hipStream_t st) {
+  constexpr int EP = kPiece<E>;
+  const int64_t per_row = ceil_div(a.n, EP), total = a.rows * per_row;
+  const dim3 grid = flat_grid(ceil_div(total, 256 * kDropPieces));
+  const int sr = (int)(256 / per_row), sp = (int)(256 % per_row);
+  const bool small = total < ((int64_t)1 << 31);
+  auto go = [&](auto kernel) { DPRC_LAUNCH(kernel, grid, dim3(256), 0, st, a, (int)per_row, sr, sp); };
+  if (a.n < EP) go(dropout_kernel<E, kTiny, uint64_t>);
+  else if (a.n % EP == 0 && small) go(dropout_kernel<E, kWhole, uint32_t>);
+  else if (a.n % EP == 0) go(dropout_kernel<E, kWhole, uint64_t>);
+  else if (small) go(dropout_kernel<E, kTail, uint32_t>);
+  else go(dropout_kernel<E, kTail, uint64_t>);
+}
+
 hipError_t launch_dropout(const DropoutArgs& a, hipStream_t st) {
-  const int64_t chunks = ceil_div(a.n, 8);
-  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(a.rows * chunks, 256), 65536));
-  if (a.bf16) DPRC_LAUNCH((dropout_kernel<uint16_t>), grid, dim3(256), 0, st, a, chunks);
-  else DPRC_LAUNCH((dropout_kernel<float>), grid, dim3(256), 0, st, a, chunks);
+  if (a.bf16) launch_dropout_of<uint16_t>(a, st);
+  else launch_dropout_of<float>(a, st);
   return hipGetLastError();
 }
 

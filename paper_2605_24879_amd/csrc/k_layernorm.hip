@@ -1,4 +1,7 @@
-// Dropout, residual sum and norm of token rows, and the backward pass.
+// Dropout, residual sum and norm of token rows (forward).
+//
+// Bounded by memory: a row is read once and held in registers from the sum through its mean,
+// its variance about that mean and the output.
 #include <algorithm>
 #include "device.hpp"
 #include "kernels.hpp"
@@ -6,49 +9,143 @@
 
 namespace dprc {
 
-template <class E>
-__device__ __forceinline__ void sum_piece(const NormArgs& a, int64_t r, int64_t c, int m, float (&x)[8]) {
-  load8((const E*)a.x + r * a.ldx + c, m, x);
-  drop8(a.drop, (uint32_t)r, (uint32_t)(c >> 3), x);
-  if (!a.res) return;
-  float z[8];
-  load8((const E*)a.res + r * a.ldr + c, m, z);
+constexpr int64_t kNormBlocks = 512;
+
+// TPR threads hold a row of at most TPR * C columns, C each; a workgroup of max(256, TPR)
+// threads works on 256 / TPR rows at a time and walks the rows with the grid, the next row's
+// pieces loading while this one is reduced.  Weight and bias stay in registers for all rows.
+template <class E, int M, int TPR, int C>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a) {
+  constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
+  constexpr bool kHold = TPR < 1024;
+  typedef RowSum<TPR, 1, BLK> Sum;
+  __shared__ typename Sum::Buffer buf;
+  int turn = 0;
+  const int t = threadIdx.x % TPR, n = (int)a.n;
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+
+  uint4 x[V], z[V];
+  auto load = [&](int64_t row) {
+    row = std::min(row, a.rows - 1);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] += z[j];
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * TPR + t) * EP;
+      x[v] = load_row<E, M>((const E*)a.x + row * a.ldx, c, n);
+      if (a.res) z[v] = load_row<E, M>((const E*)a.res + row * a.ldr, c, n);
+    }
+  };
+  load(r);
+  float w[C], b[C];
+  auto load_wb = [&](int v) {
+    const int c = (v * TPR + t) * EP;
+    load_vec<EP>(a.w, a.wbf16, c, n, 1.f, w + v * EP);
+    load_vec<EP>(a.b, a.wbf16, c, n, 0.f, b + v * EP);
+  };
+  if (kHold)
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_wb(v);
+  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, r += step) {
+    float s[C], u[EP], red[1] = {0.f}, mu = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * TPR + t) * EP;
+#pragma unroll
+      for (int k = v * EP; k < v * EP + EP; ++k) s[k] = 0.f;
+      if (c >= n) continue;
+      unpack_row<E, M>(x[v], c, n, s + v * EP);
+      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, s + v * EP);
+      if (!a.res) continue;
+      unpack_row<E, M>(z[v], c, n, u);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) s[v * EP + j] += u[j];
+    }
+    load(r + step);
+    if (!a.rms) {
+#pragma unroll
+      for (int k = 0; k < C; ++k) red[0] += s[k];
+      Sum::run(red, buf, turn);
+      mu = red[0] * a.inv_n;
+      red[0] = 0.f;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * TPR + t) * EP;
+#pragma unroll
+      for (int j = 0; j < EP; ++j) {
+        const float d = (M == kWhole ? c : c + j) < n ? s[v * EP + j] - mu : 0.f;
+        red[0] = fmaf(d, d, red[0]);
+      }
+    }
+    Sum::run(red, buf, turn);
+    const float rstd = 1.f / sqrtf(fmaf(red[0], a.inv_n, a.eps));
+    if (r >= a.rows) continue;
+    if (t == 0) {
+      if (a.mean) a.mean[r] = mu;
+      if (a.rstd) a.rstd[r] = rstd;
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+      const int c = (v * TPR + t) * EP;
+      if (c >= n) continue;
+      if (a.sum) store_row<E, M>((E*)a.sum + r * a.lds, c, n, s + v * EP);
+      if (!kHold) load_wb(v);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) u[j] = fmaf((s[v * EP + j] - mu) * rstd, w[v * EP + j], b[v * EP + j]);
+      store_row<E, M>((E*)a.y + r * a.ldy, c, n, u);
+    }
+  }
 }
 
-// One workgroup per row, three passes over it: mean, variance, output.
-template <class E>
-__global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
-  __shared__ float buf[4];
+// Rows longer than a workgroup's registers hold: three passes over the row (mean, variance,
+// output), the sum made again in each.
+template <class E, int M>
+__global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
+  constexpr int EP = kPiece<E>;
+  typedef RowSum<1024, 1, 1024> Sum;
+  __shared__ typename Sum::Buffer buf;
+  int turn = 0;
+  const int n = (int)a.n;
   for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
-    float x[8], mu = 0.f, t = 0.f;
-    if (!a.rms) {
-      for (int64_t c = 8 * threadIdx.x; c < a.n; c += 8 * 256) {
-        sum_piece<E>(a, r, c, (int)std::min<int64_t>(8, a.n - c), x);
+    auto piece = [&](int c, float* s) {
+      float u[EP];
+      unpack_row<E, M>(load_row<E, M>((const E*)a.x + r * a.ldx, c, n), c, n, s);
+      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, s);
+      if (a.res) {
+        unpack_row<E, M>(load_row<E, M>((const E*)a.res + r * a.ldr, c, n), c, n, u);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) t += x[j];
+        for (int j = 0; j < EP; ++j) s[j] += u[j];
       }
-      mu = block_sum(t, buf) * a.inv_n;
-      t = 0.f;
-    }
-    for (int64_t c = 8 * threadIdx.x; c < a.n; c += 8 * 256) {
-      const int m = (int)std::min<int64_t>(8, a.n - c);
-      sum_piece<E>(a, r, c, m, x);
+    };
+    float s[EP], w[EP], b[EP], red[1] = {0.f}, mu = 0.f;
+    if (!a.rms) {
+      for (int c = threadIdx.x * EP; c < n; c += 1024 * EP) {
+        piece(c, s);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < m) t = fmaf(x[j] - mu, x[j] - mu, t);
+        for (int j = 0; j < EP; ++j) red[0] += (M == kWhole || c + j < n) ? s[j] : 0.f;
+      }
+      Sum::run(red, buf, turn);
+      mu = red[0] * a.inv_n;
+      red[0] = 0.f;
     }
-    const float rstd = 1.f / sqrtf(fmaf(block_sum(t, buf), a.inv_n, a.eps));
-    for (int64_t c = 8 * threadIdx.x; c < a.n; c += 8 * 256) {
-      const int m = (int)std::min<int64_t>(8, a.n - c);
-      sum_piece<E>(a, r, c, m, x);
-      if (a.sum) store8((E*)a.sum + r * a.lds + c, m, x);
+    for (int c = threadIdx.x * EP; c < n; c += 1024 * EP) {
+      piece(c, s);
 #pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (j < m)
-          x[j] = fmaf((x[j] - mu) * rstd, vec_entry(a.w, a.wbf16, c + j, 1.f), vec_entry(a.b, a.wbf16, c + j, 0.f));
-      store8((E*)a.y + r * a.ldy + c, m, x);
+      for (int j = 0; j < EP; ++j) {
+        const float d = (M == kWhole || c + j < n) ? s[j] - mu : 0.f;
+        red[0] = fmaf(d, d, red[0]);
+      }
+    }
+    Sum::run(red, buf, turn);
+    const float rstd = 1.f / sqrtf(fmaf(red[0], a.inv_n, a.eps));
+    for (int c = threadIdx.x * EP; c < n; c += 1024 * EP) {
+      piece(c, s);
+      if (a.sum) store_row<E, M>((E*)a.sum + r * a.lds, c, n, s);
+      load_vec<EP>(a.w, a.wbf16, c, n, 1.f, w);
+      load_vec<EP>(a.b, a.wbf16, c, n, 0.f, b);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) s[j] = fmaf((s[j] - mu) * rstd, w[j], b[j]);
+      store_row<E, M>((E*)a.y + r * a.ldy, c, n, s);
     }
     if (threadIdx.x == 0) {
       if (a.mean) a.mean[r] = mu;
@@ -57,123 +154,50 @@ __global__ __launch_bounds__(256) void norm_kernel(NormArgs a) {
   }
 }
 
+// Threads per row: a power of two with 16 columns each (two bf16 or four fp32 pieces of every
+// tensor in flight per thread), and two workgroups per CU.  32768 rows of 2048 bf16 with
+// residual, dropout and statistics took 98 us so, 106 with four or eight per CU, 98 to 107
+// with 32 columns per thread (196 registers) and, in the plain form, 92 against 49 with
+// 8 columns (half as much in flight).
+template <class E, int M>
+static void launch_norm_of(const NormArgs& a, hipStream_t st) {
+  auto go = [&](auto kernel, int block, int rows_per_block) {
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, rows_per_block), kNormBlocks);
+    DPRC_LAUNCH(kernel, dim3((unsigned)blocks), dim3(block), 0, st, a);
+  };
+  const int64_t n = a.n;
+  if (n <= 64) return go(norm_kernel<E, M, 8, 8>, 256, 32);
+  if constexpr (M != kTiny) {
+    // At most one row per workgroup: a row's latency counts, 8 columns per thread (one row of 2048:
+    // 2.9 us against 3.5, 512 rows: 4.1 against 4.5; from 1024 rows on it is slower).  Past
+    // 4096 columns the two are alike.
+    if (a.rows <= kNormBlocks && n > 512 && n <= 4096) {
+      if (n <= 1024) return go(norm_kernel<E, M, 128, 8>, 256, 2);
+      if (n <= 2048) return go(norm_kernel<E, M, 256, 8>, 256, 1);
+      return go(norm_kernel<E, M, 512, 8>, 512, 1);
+    }
+    if (n <= 128) return go(norm_kernel<E, M, 8, 16>, 256, 32);
+    if (n <= 256) return go(norm_kernel<E, M, 16, 16>, 256, 16);
+    if (n <= 512) return go(norm_kernel<E, M, 32, 16>, 256, 8);
+    if (n <= 1024) return go(norm_kernel<E, M, 64, 16>, 256, 4);
+    if (n <= 2048) return go(norm_kernel<E, M, 128, 16>, 256, 2);
+    if (n <= 4096) return go(norm_kernel<E, M, 256, 16>, 256, 1);
+    if (n <= 8192) return go(norm_kernel<E, M, 512, 16>, 512, 1);
+    if (n <= 16384) return go(norm_kernel<E, M, 1024, 16>, 1024, 1);
+    go(norm_long_kernel<E, M>, 1024, 1);
+  }
+}
+
+template <class E>
+static void launch_norm_width(const NormArgs& a, hipStream_t st) {
+  if (a.n < kPiece<E>) launch_norm_of<E, kTiny>(a, st);
+  else if (a.n % kPiece<E> == 0) launch_norm_of<E, kWhole>(a, st);
+  else launch_norm_of<E, kTail>(a, st);
+}
+
 hipError_t launch_norm(const NormArgs& a, hipStream_t st) {
-  const dim3 grid((unsigned)std::min<int64_t>(a.rows, 65536));
-  if (a.bf16) DPRC_LAUNCH((norm_kernel<uint16_t>), grid, dim3(256), 0, st, a);
-  else DPRC_LAUNCH((norm_kernel<float>), grid, dim3(256), 0, st, a);
-  return hipGetLastError();
-}
-
-// ---- backward ---------------------------------------------------------------------------------
-
-// xh and g = dy w of 8 columns of row r
-template <class E>
-__device__ __forceinline__ void back_piece(const NormBackArgs& a, int64_t r, int64_t c, int m, float mu, float rstd,
-                                           float (&dy)[8], float (&xh)[8], float (&g)[8]) {
-  load8((const E*)a.dy + r * a.lddy + c, m, dy);
-  load8((const E*)a.s + r * a.lds + c, m, xh);
-#pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    xh[j] = j < m ? (xh[j] - mu) * rstd : 0.f;
-    g[j] = j < m ? dy[j] * vec_entry(a.w, a.wbf16, c + j, 1.f) : 0.f;
-  }
-}
-
-// dx and dh: one workgroup per row, two passes over it.
-template <class E>
-__global__ __launch_bounds__(256) void norm_back_rows_kernel(NormBackArgs a) {
-  __shared__ float buf[4];
-  const int64_t rows = a.B * a.T;
-  for (int64_t r = blockIdx.x; r < rows; r += gridDim.x) {
-    const float mu = a.rms ? 0.f : a.mean[r], rstd = a.rstd[r];
-    float dy[8], xh[8], g[8], sg = 0.f, sgx = 0.f;
-    for (int64_t c = 8 * threadIdx.x; c < a.n; c += 8 * 256) {
-      back_piece<E>(a, r, c, (int)std::min<int64_t>(8, a.n - c), mu, rstd, dy, xh, g);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        sg += g[j];
-        sgx = fmaf(g[j], xh[j], sgx);
-      }
-    }
-    sg = a.rms ? 0.f : block_sum(sg, buf) * a.inv_n;
-    sgx = block_sum(sgx, buf) * a.inv_n;
-    for (int64_t c = 8 * threadIdx.x; c < a.n; c += 8 * 256) {
-      const int m = (int)std::min<int64_t>(8, a.n - c);
-      back_piece<E>(a, r, c, m, mu, rstd, dy, xh, g);
-      float z[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      if (a.ds) load8((const E*)a.ds + r * a.ldds + c, m, z);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) z[j] = fmaf(rstd, (g[j] - sg) - xh[j] * sgx, z[j]);
-      if (a.dx) store8((E*)a.dx + r * a.lddx + c, m, z);
-      drop8(a.drop, (uint32_t)r, (uint32_t)(c >> 3), z);
-      if (a.dh) store8((E*)a.dh + r * a.lddh + c, m, z);
-    }
-  }
-}
-
-// dw and db: one thread per column and token split.
-template <class E>
-__global__ __launch_bounds__(256) void norm_back_cols_kernel(NormBackArgs a, int64_t col_blocks, int64_t blocks) {
-  const int64_t blk = flat_block();
-  if (blk >= blocks) return;
-  const int64_t c = (blk % col_blocks) * 256 + threadIdx.x, is = blk / col_blocks;
-  if (c >= a.n) return;
-  const int64_t i = is / a.S, per = (a.T + a.S - 1) / a.S;
-  const int64_t t0 = (is % a.S) * per, t1 = std::min<int64_t>(a.T, t0 + per);
-  float dw = 0.f, db = 0.f;
-  for (int64_t t = t0; t < t1; ++t) {
-    const int64_t r = i * a.T + t;
-    const float dy = to_f32(((const E*)a.dy)[r * a.lddy + c]);
-    const float xh = (to_f32(((const E*)a.s)[r * a.lds + c]) - (a.rms ? 0.f : a.mean[r])) * a.rstd[r];
-    dw = fmaf(dy, xh, dw);
-    db += dy;
-  }
-  if (a.S > 1) {
-    a.part[(is * 2 + 0) * a.n + c] = dw;
-    a.part[(is * 2 + 1) * a.n + c] = db;
-  } else {
-    if (a.dw) a.dw[i * a.ldg + c] = dw;
-    if (a.db) a.db[i * a.ldg + c] = db;
-  }
-}
-
-int norm_back_splits(int64_t B, int64_t T, int64_t n) {
-  const int64_t base = B * ceil_div(n, 256);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(1024, base), T / 16));
-}
-
-hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t st) {
-  if (a.dw || a.db) {
-    const int64_t cb = ceil_div(a.n, 256), blocks = a.B * a.S * cb;
-    if (a.bf16) DPRC_LAUNCH((norm_back_cols_kernel<uint16_t>), flat_grid(blocks), dim3(256), 0, st, a, cb, blocks);
-    else DPRC_LAUNCH((norm_back_cols_kernel<float>), flat_grid(blocks), dim3(256), 0, st, a, cb, blocks);
-  }
-  if (a.dx || a.dh) {
-    const dim3 grid((unsigned)std::min<int64_t>(a.B * a.T, 65536));
-    if (a.bf16) DPRC_LAUNCH((norm_back_rows_kernel<uint16_t>), grid, dim3(256), 0, st, a);
-    else DPRC_LAUNCH((norm_back_rows_kernel<float>), grid, dim3(256), 0, st, a);
-  }
-  return hipGetLastError();
-}
-
-// the token splits' partial sums of a sample, in their order
-__global__ __launch_bounds__(256) void norm_back_sums_kernel(NormBackArgs a, int64_t col_blocks, int64_t blocks) {
-  const int64_t blk = flat_block();
-  if (blk >= blocks) return;
-  const int64_t c = (blk % col_blocks) * 256 + threadIdx.x, i = blk / col_blocks;
-  if (c >= a.n) return;
-  float dw = 0.f, db = 0.f;
-  for (int k = 0; k < a.S; ++k) {
-    dw += a.part[((i * a.S + k) * 2 + 0) * a.n + c];
-    db += a.part[((i * a.S + k) * 2 + 1) * a.n + c];
-  }
-  if (a.dw) a.dw[i * a.ldg + c] = dw;
-  if (a.db) a.db[i * a.ldg + c] = db;
-}
-
-hipError_t launch_norm_back_sums(const NormBackArgs& a, hipStream_t st) {
-  const int64_t cb = ceil_div(a.n, 256), blocks = a.B * cb;
-  DPRC_LAUNCH(norm_back_sums_kernel, flat_grid(blocks), dim3(256), 0, st, a, cb, blocks);
+  if (a.bf16) launch_norm_width<uint16_t>(a, st);
+  else launch_norm_width<float>(a, st);
   return hipGetLastError();
 }
 

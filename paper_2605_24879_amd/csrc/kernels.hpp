@@ -418,7 +418,7 @@ struct NormBackArgs {
   float* part;             // [B][S][2][n] (S > 1)
   DropArgs drop;
 };
-int norm_back_splits(int64_t B, int64_t T, int64_t n);
+int norm_back_splits(int64_t B, int64_t T, int64_t n, bool bf16);
 hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t st);
 hipError_t launch_norm_back_sums(const NormBackArgs& a, hipStream_t st);   // S > 1: dw and db from part
 

@@ -1,55 +1,282 @@
-// Token rows in 8-column pieces: loads, stores, dropout masks and sums over a workgroup.
+// Token rows in 16-byte pieces: loads, stores, dropout masks and sums over a row's threads.
+//
+// A row of n elements is dealt to TPR threads in pieces of 16 bytes (EP = 8 bf16 or 4 fp32
+// columns): thread t holds the pieces t, TPR + t, 2 TPR + t, ..., so a wave's loads are
+// consecutive.  Rows may start at any alignment of their element (gfx950 takes 16-byte accesses at
+// any address).  The width's kind M:
+//   kWhole  n is a multiple of EP;
+//   kTail   it is not, and the row's last piece is part of one: its thread loads the row's last EP
+//           elements instead (they lie within the row), shifts them down when it comes to use
+//           them, and stores 8, 4 and 2 bytes;
+//   kTiny   n < EP: element loads.  (A kind of its own: beside the others these loads made
+//           every load of a loop wait for the one before.)
 #pragma once
+#include <type_traits>
 #include "device.hpp"
 #include "kernels.hpp"
 
 namespace dprc {
 
-__device__ __forceinline__ float to_f32(uint16_t h) { return bf16_to_f32(h); }
-__device__ __forceinline__ float to_f32(float f) { return f; }
-__device__ __forceinline__ void from_f32(float f, uint16_t& h) { h = (uint16_t)f32_to_bf16(f); }
-__device__ __forceinline__ void from_f32(float f, float& h) { h = f; }
-
-// the first m (at most 8) elements at p, zeros after them
-template <class E>
-__device__ __forceinline__ void load8(const E* p, int m, float (&x)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j) x[j] = j < m ? to_f32(p[j]) : 0.f;
-}
+enum : int { kWhole = 0, kTail = 1, kTiny = 2 };
 
 template <class E>
-__device__ __forceinline__ void store8(E* p, int m, const float (&x)[8]) {
-#pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (j < m) from_f32(x[j], p[j]);
+constexpr int kPiece = 16 / (int)sizeof(E);
+
+typedef uint32_t piece2_t __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t piece4_t __attribute__((ext_vector_type(4), aligned(4)));
+template <class E>
+using piece_t = std::conditional_t<sizeof(E) == 2, piece2_t, piece4_t>;
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef float f32x2_t __attribute__((ext_vector_type(2)));
+
+template <class E>
+__device__ __forceinline__ uint4 load_piece(const E* p) {
+  const piece_t<E> v = *reinterpret_cast<const piece_t<E>*>(p);
+  return uint4{v[0], v[1], v[2], v[3]};
 }
 
-// entry c of a weight or bias (fp32 or bf16), `none` without one
-__device__ __forceinline__ float vec_entry(const void* v, int bf16, int64_t c, float none) {
-  if (!v) return none;
-  return bf16 ? bf16_to_f32(((const uint16_t*)v)[c]) : ((const float*)v)[c];
+template <class E>
+__device__ __forceinline__ void store_piece(E* p, const uint4& v) {
+  *reinterpret_cast<piece_t<E>*>(p) = piece_t<E>{v.x, v.y, v.z, v.w};
 }
 
-// x (columns 8 blk .. 8 blk + 7 of row r) through the site's dropout; a dropped element is 0
-// whatever it was
-__device__ __forceinline__ void drop8(const DropArgs& d, uint32_t r, uint32_t blk, float (&x)[8]) {
-  if (!d.on) return;
-  const u32x4 w = philox4x32_10(u32x4{blk, r, d.site, kStreamDropout}, d.key0, d.key1);
-  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+// The piece of `row` at column c, for unpack_row at the same column.  Past the row's end it is the
+// last piece again: the loads of a loop have no conditions, whose merges (a value or zero) would
+// make the compiler wait for a load where it is issued.
+template <class E, int M>
+__device__ __forceinline__ uint4 load_row(const E* row, int c, int n) {
+  constexpr int EP = kPiece<E>;
+  if constexpr (M != kTiny) return load_piece(row + min(c, n - EP));
+  uint32_t h[EP];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const uint32_t u = (j & 1) ? word[j >> 1] & 0xFFFF0000u : word[j >> 1] << 16;
-    x[j] = u > d.lim ? x[j] * d.scale : 0.f;
+  for (int j = 0; j < EP; ++j) {
+    h[j] = 0;
+    if (c + j < n) {
+      if constexpr (sizeof(E) == 2) h[j] = row[c + j];
+      else h[j] = __float_as_uint(row[c + j]);
+    }
+  }
+  if constexpr (EP == 8) return uint4{h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16};
+  else return uint4{h[0], h[1], h[2], h[3]};
+}
+
+template <class E>
+__device__ __forceinline__ void unpack(const uint4& v, float* x) {
+  if constexpr (sizeof(E) == 2) {
+    const uint32_t d[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      x[2 * j] = __uint_as_float(d[j] << 16);
+      x[2 * j + 1] = __uint_as_float(d[j] & 0xFFFF0000u);
+    }
+  } else {
+    x[0] = __uint_as_float(v.x); x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z); x[3] = __uint_as_float(v.w);
   }
 }
 
-// sum over a workgroup of 256 threads, in every thread; `buf` is 4 floats of LDS
-__device__ __forceinline__ float block_sum(float v, float* buf) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return (buf[0] + buf[1]) + (buf[2] + buf[3]);
+// The columns c .. c + EP - 1 (c < n) of what load_row returned, zeros past the row's end.  (The
+// shift is made here and not at the load, which it would have to wait for.)
+template <class E, int M>
+__device__ __forceinline__ void unpack_row(uint4 v, int c, int n, float* x) {
+  constexpr int EP = kPiece<E>;
+  const int over = c + EP - n;
+  if (M == kTail && over > 0) {
+    if constexpr (EP == 8) v = shr_elems(v, over);
+    else {
+      if (over & 2) v = uint4{v.z, v.w, 0u, 0u};
+      if (over & 1) v = uint4{v.y, v.z, v.w, 0u};
+    }
+  }
+  unpack<E>(v, x);
 }
+
+// to E, nearest even
+template <class E>
+__device__ __forceinline__ uint4 pack(const float* x) {
+  if constexpr (sizeof(E) == 2) {
+    uint32_t d[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      d[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{x[2 * j], x[2 * j + 1]}, bf16x2_t));
+    return uint4{d[0], d[1], d[2], d[3]};
+  } else {
+    return uint4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+  }
+}
+
+// 8 or 4 bytes at any address that is aligned to an element
+typedef uint32_t u32_any2 __attribute__((aligned(2)));
+typedef uint32_t u32x2_any2 __attribute__((ext_vector_type(2), aligned(2)));
+__device__ __forceinline__ void store_part(void* p, uint32_t v) { *reinterpret_cast<u32_any2*>(p) = v; }
+__device__ __forceinline__ void store_part(void* p, uint2 v) { *reinterpret_cast<u32x2_any2*>(p) = u32x2_any2{v.x, v.y}; }
+
+// Piece at column c < n of an output row.
+template <class E, int M>
+__device__ __forceinline__ void store_row(E* row, int c, int n, const float* x) {
+  constexpr int EP = kPiece<E>;
+  const uint4 v = pack<E>(x);
+  if (M == kWhole || c + EP <= n) {
+    store_piece(row + c, v);
+    return;
+  }
+  // n - c < EP elements, as 8, 4 and 2 bytes
+  const int m = n - c;
+  E* p = row + c;
+  uint2 d{v.x, v.y};
+  if (m * (int)sizeof(E) & 8) {
+    store_part(p, d);
+    d = uint2{v.z, v.w};
+    p += 8 / sizeof(E);
+  }
+  if (m * (int)sizeof(E) & 4) {
+    store_part(p, d.x);
+    d.x = d.y;
+    p += 4 / sizeof(E);
+  }
+  if constexpr (sizeof(E) == 2)
+    if (m & 1) *p = (uint16_t)d.x;
+}
+
+// Entries c .. c + N - 1 of a weight or bias (fp32 or bf16), `none` without one and past its end.
+template <int N>
+__device__ __forceinline__ void load_vec(const void* v, int bf16, int c, int n, float none, float* x) {
+#pragma unroll
+  for (int j = 0; j < N; ++j) x[j] = none;
+  if (!v || c >= n) return;
+  if (bf16) {
+    const uint16_t* p = (const uint16_t*)v + c;
+    if (N == 8 && c + 8 <= n) {
+      unpack<uint16_t>(load_piece(p), x);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (c + j < n) x[j] = bf16_to_f32(p[j]);
+  } else {
+    const float* p = (const float*)v + c;
+#pragma unroll
+    for (int q = 0; q < N; q += 4) {
+      if (c + q + 4 <= n) {
+        unpack<float>(load_piece(p + q), x + q);
+        continue;
+      }
+#pragma unroll
+      for (int j = q; j < q + 4; ++j)
+        if (c + j < n) x[j] = p[j];
+    }
+  }
+}
+
+// Philox4x32-10 with each round's two products taken whole (one v_mad_u64_u32 each, where high
+// and low halves apart take two multiplies): 6.6e11 blocks/s against 5.2e11, in a loop of
+// nothing else.
+__device__ __forceinline__ u32x4 philox_mask(u32x4 c, uint32_t k0, uint32_t k1) {
+#pragma unroll
+  for (int round = 0; round < 10; ++round) {
+    if (round) {
+      k0 += 0x9E3779B9u;
+      k1 += 0xBB67AE85u;
+    }
+    const uint64_t a = (uint64_t)0xD2511F53u * c.x, b = (uint64_t)0xCD9E8D57u * c.z;
+    c = u32x4{(uint32_t)(b >> 32) ^ c.y ^ k0, (uint32_t)b, (uint32_t)(a >> 32) ^ c.w ^ k1, (uint32_t)a};
+  }
+  return c;
+}
+
+// The mask words of a piece (columns c .. c + EP - 1 of row r): 8 columns share a Philox block, two
+// fp32 pieces half of it each.
+template <class E>
+__device__ __forceinline__ u32x4 drop_words(const DropArgs& d, uint32_t r, int c) {
+  const u32x4 w = philox_mask(u32x4{(uint32_t)c >> 3, r, d.site, kStreamDropout}, d.key0, d.key1);
+  if constexpr (sizeof(E) == 2) return w;
+  else return (c & 4) ? u32x4{w.z, w.w, 0u, 0u} : u32x4{w.x, w.y, 0u, 0u};
+}
+
+// The piece through the site's dropout.  A dropped element is 0 whatever it was: it is replaced
+// before the product with the scale.
+template <class E>
+__device__ __forceinline__ void drop_apply(const DropArgs& d, const u32x4& w, float* x) {
+  const uint32_t word[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+  for (int j = 0; j < kPiece<E>; ++j)
+    x[j] = (((j & 1) ? word[j >> 1] : word[j >> 1] << 16) > d.lim ? x[j] : 0.f) * d.scale;
+}
+
+template <class E>
+__device__ __forceinline__ void drop_piece(const DropArgs& d, uint32_t r, int c, float* x) {
+  drop_apply<E>(d, drop_words<E>(d, r, c), x);
+}
+
+// ---- sums over groups of lanes ----------------------------------------------------------------
+// Butterflies in vector registers: quad permutes for lanes 1 and 2 apart; the mirrors of 8 and of
+// 16 lanes reach the other half of a group whose halves are uniform already; the lane swaps of
+// gfx950 exchange rows of 16 and halves of 32.
+template <int CTRL>
+__device__ __forceinline__ float dpp_mov(float v) {
+  return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
+}
+constexpr int kDppXor1 = 0xB1, kDppXor2 = 0x4E, kDppMirror8 = 0x141, kDppMirror16 = 0x140, kDppRotate8 = 0x128;
+
+// v of this lane plus v of the lane 16 (32) away
+__device__ __forceinline__ float add_xor16(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto s = __builtin_amdgcn_permlane16_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+__device__ __forceinline__ float add_xor32(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const auto s = __builtin_amdgcn_permlane32_swap(u, u, false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// sum over aligned groups of L lanes (8, 16, 32 or 64), in every lane
+template <int L>
+__device__ __forceinline__ float lane_sum(float v) {
+  v += dpp_mov<kDppXor1>(v);
+  v += dpp_mov<kDppXor2>(v);
+  v += dpp_mov<kDppMirror8>(v);
+  if (L >= 16) v += dpp_mov<kDppMirror16>(v);
+  if (L >= 32) v = add_xor16(v);
+  if (L >= 64) v = add_xor32(v);
+  return v;
+}
+
+// sum over the lanes of a wave that hold the same place in groups of L lanes, in every lane
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+  if (L <= 8) v += dpp_mov<kDppRotate8>(v);
+  if (L <= 16) v = add_xor16(v);
+  if (L <= 32) v = add_xor32(v);
+  return v;
+}
+
+// Sums over a row's TPR threads, N values at once, in every thread.  Rows of several waves
+// meet in LDS with one barrier a call: the calls of a kernel alternate between two buffers
+// (`turn`), and a buffer is written again only after the barrier of the call between.
+template <int TPR, int N, int BLK>
+struct RowSum {
+  static constexpr int kWaves = BLK / 64, kPer = TPR / 64;
+  typedef float Buffer[2][N][TPR > 64 ? kWaves : 1];
+  __device__ static __forceinline__ void run(float (&v)[N], Buffer& buf, int& turn) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = lane_sum<(TPR < 64 ? TPR : 64)>(v[k]);
+    if constexpr (TPR > 64) {
+      const int wave = threadIdx.x >> 6, w0 = wave / kPer * kPer;
+      if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < N; ++k) buf[turn][k][wave] = v[k];
+      __syncthreads();
+#pragma unroll
+      for (int k = 0; k < N; ++k) {
+        float t = 0.f;
+#pragma unroll
+        for (int q = 0; q < kPer; ++q) t += buf[turn][k][w0 + q];
+        v[k] = t;
+      }
+      turn ^= 1;
+    }
+  }
+};
 
 }  // namespace dprc
