@@ -172,6 +172,8 @@ def _layers(pairs):
 
 def _workspace(nbytes, dev, ws):
     if ws is not None:
+        if not ws.is_cuda:
+            raise ValueError("the workspace must be a GPU tensor")
         if ws.numel() * ws.element_size() < nbytes:
             raise ValueError("workspace too small")
         return ws
@@ -423,19 +425,17 @@ def dprc_probe_gaussian(seed, layer_id, m, k, device="cuda", out=None):
     return out
 
 
-def _token_rows(x, name, shape=None, dtype=None, dev=None):
-    """The row stride of [B, T, n] token rows, after checks of the tensor's shape, dtype, device and strides."""
+def _token_rows(x, name, like=None):
+    """The row stride of [B, T, n] token rows, after checks of the tensor's strides and, with `like`, of its
+    shape, dtype and device."""
+    if like is not None and (x.shape != like.shape or x.dtype != like.dtype or x.get_device() != like.get_device()):
+        raise ValueError(f"{name} must be {list(like.shape)} {like.dtype} on {like.device}, not {list(x.shape)} "
+                         f"{x.dtype} on {x.device}")
     if x.dim() != 3:
         raise ValueError(f"{name} must be [B, T, n]")
-    if shape is not None:
-        if x.shape != shape:
-            raise ValueError(f"{name} must be {list(shape)}, not {list(x.shape)}")
-        if x.dtype != dtype:
-            raise TypeError(f"{name} must be {dtype}, not {x.dtype}")
-        if x.device != dev:
-            raise ValueError(f"{name} must be on {dev}, not {x.device}")
-    B, T, n = x.shape
-    s0, s1, s2 = x.stride()
+    if x.is_contiguous():
+        return x.size(2)
+    (B, T, n), (s0, s1, s2) = x.shape, x.stride()
     if T == 1:
         s1 = s0 if B > 1 else n
     elif B > 1 and s0 != T * s1:
@@ -445,41 +445,58 @@ def _token_rows(x, name, shape=None, dtype=None, dev=None):
     return s1
 
 
-def _vector(x, name, n, dev, dtype=torch.float32):
-    """The pointer of a contiguous vector of n entries (None for no vector)."""
+def _vector(x, name, n, device, dtype=torch.float32):
+    """The pointer of a contiguous vector of n entries on the GPU of index `device` (None for no vector)."""
     if x is None:
         return None
-    if x.device != dev:
-        raise ValueError(f"{name} must be on {dev}, not {x.device}")
-    if x.dtype != dtype or x.numel() != n or not x.is_contiguous():
-        raise ValueError(f"{name} must be {n} contiguous entries of {dtype}")
+    if x.get_device() != device or x.dtype != dtype or x.numel() != n or not x.is_contiguous():
+        raise ValueError(f"{name} must be {n} contiguous entries of {dtype} on the other tensors' GPU")
     return x.data_ptr()
+
+
+def _sample_rows(g, name, B, n, device):
+    """The row stride of per-sample gradients [B, n] (0: any)."""
+    if g.shape != (B, n) or g.dtype != torch.float32 or g.get_device() != device or (n > 1 and g.stride(1) != 1):
+        raise ValueError(f"{name} must be [{B}, {n}] fp32 with contiguous rows on the other tensors' GPU")
+    return g.stride(0) if B > 1 else 0
 
 
 def _ln(x, kind, weight, bias, eps, p, seed, site_id):
     """dprc_ln of the norm of x [B, T, n]."""
     B, T, n = x.shape
-    wd = weight if weight is not None else bias
-    wdtype = wd.dtype if wd is not None else torch.float32
-    return LN(B, T, n, _dtype_code(x), F32 if wdtype == torch.float32 else _dtype_code(wd), kind, eps,
-              _vector(weight, "weight", n, x.device, wdtype), _vector(bias, "bias", n, x.device, wdtype), p,
-              site_id, seed)
+    wdtype = torch.float32
+    if weight is not None:
+        wdtype = weight.dtype
+    elif bias is not None:
+        wdtype = bias.dtype
+    if wdtype is not torch.float32 and wdtype is not torch.bfloat16:
+        raise TypeError(f"unsupported weight dtype {wdtype}; use bfloat16 or float32")
+    dev = x.get_device()
+    return LN(B, T, n, _dtype_code(x), BF16 if wdtype is torch.bfloat16 else F32, kind, eps,
+              _vector(weight, "weight", n, dev, wdtype), _vector(bias, "bias", n, dev, wdtype), p, site_id, seed)
+
+
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
+def _rows_like(x, ld):
+    """New contiguous rows of x's shape (ld: x's row stride)."""
+    return torch.empty_like(x) if ld == x.size(2) else torch.empty(x.shape, dtype=x.dtype, device=x.device)
 
 
 def dprc_dropout(x, p, seed, site_id, res=None, out=None):
     """res + dropout(x) (res may be None) of [B, T, n] token rows.  The same call on a gradient, with the same
-    seed and site and without res, is dropout's backward pass."""
+    seed and site and without res, is dropout's backward pass.  out may be x or res."""
     ldx = _token_rows(x, "x")
-    dev, dtype = x.device, x.dtype
-    ldr = 0 if res is None else _token_rows(res, "res", x.shape, dtype, dev)
+    ldr = 0 if res is None else _token_rows(res, "res", x)
     B, T, n = x.shape
     if out is None:
-        out = torch.empty((B, T, n), dtype=dtype, device=dev)
-        ldo = n
+        out, ldo = _rows_like(x, ldx), n
     else:
-        ldo = _token_rows(out, "out", x.shape, dtype, dev)
-    _check(lib().dprc_dropout(x.data_ptr(), ldx, None if res is None else res.data_ptr(), ldr, out.data_ptr(), ldo,
-                              B * T, n, _dtype_code(x), p, seed, site_id, _stream(dev)))
+        ldo = _token_rows(out, "out", x)
+    _check(lib().dprc_dropout(x.data_ptr(), ldx, _ptr(res), ldr, out.data_ptr(), ldo, B * T, n, _dtype_code(x), p,
+                              seed, site_id, _stream(x.device)))
     return out
 
 
@@ -488,30 +505,27 @@ def dprc_layernorm(x, weight=None, bias=None, eps=1e-5, kind=LAYERNORM, res=None
     """s = res + dropout(x) and its norm y over the last axis of [B, T, n]: returns (y, s, mean, rstd).
 
     s is x itself where there is neither res nor dropout.  mean (None for RMSNORM) and rstd are [B*T] fp32,
-    what the backward pass needs besides s; with stats=False both are None."""
+    what the backward pass needs besides s; with stats=False both are None.  y and s may be x or res."""
     ldx = _token_rows(x, "x")
-    dev, dtype, shape = x.device, x.dtype, x.shape
-    B, T, n = shape
-    ldr = 0 if res is None else _token_rows(res, "res", shape, dtype, dev)
+    ldr = 0 if res is None else _token_rows(res, "res", x)
     L = _ln(x, kind, weight, bias, eps, p, seed, site_id)
-    lds = ldy = n
+    lds = ldy = L.n
     if s is not None:
-        lds = _token_rows(s, "s", shape, dtype, dev)
+        lds = _token_rows(s, "s", x)
     elif res is not None or p > 0.0:
-        s = torch.empty((B, T, n), dtype=dtype, device=dev)
+        s = _rows_like(x, ldx)
     if y is None:
-        y = torch.empty((B, T, n), dtype=dtype, device=dev)
+        y = _rows_like(x, ldx)
     else:
-        ldy = _token_rows(y, "y", shape, dtype, dev)
+        ldy = _token_rows(y, "y", x)
     mean = rstd = None
+    dev = x.device
     if stats:
-        rstd = torch.empty(B * T, dtype=torch.float32, device=dev)
+        rstd = torch.empty(L.B * L.T, dtype=torch.float32, device=dev)
         if kind == LAYERNORM:
-            mean = torch.empty(B * T, dtype=torch.float32, device=dev)
-    _check(lib().dprc_layernorm(ctypes.byref(L), x.data_ptr(), ldx, None if res is None else res.data_ptr(), ldr,
-                                None if s is None else s.data_ptr(), lds, y.data_ptr(), ldy,
-                                None if mean is None else mean.data_ptr(), None if rstd is None else rstd.data_ptr(),
-                                _stream(dev)))
+            mean = torch.empty_like(rstd)
+    _check(lib().dprc_layernorm(ctypes.byref(L), x.data_ptr(), ldx, _ptr(res), ldr, _ptr(s), lds, y.data_ptr(), ldy,
+                                _ptr(mean), _ptr(rstd), _stream(dev)))
     return y, x if s is None else s, mean, rstd
 
 
@@ -521,46 +535,39 @@ def dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=LAYERNORM, ds=None, 
 
     dx = dL/ds (ds, the gradient that reaches s past the norm, included), dh = dL/dx through the dropout (None
     where p = 0, then it is dx), dw and db [B, n] fp32: every sample's own weight and bias gradient (None where
-    not wanted).  dw and db may be given as column slices of one buffer; they share a row stride."""
+    not wanted).  dw and db may be given as column slices of one buffer; they share a row stride.  dx and dh may
+    be dy, s or ds."""
     ldd = _token_rows(dy, "dy")
-    dev, dtype, shape = dy.device, dy.dtype, dy.shape
-    B, T, n = shape
-    lds = _token_rows(s, "s", shape, dtype, dev)
-    ldds = 0 if ds is None else _token_rows(ds, "ds", shape, dtype, dev)
+    lds = _token_rows(s, "s", dy)
+    ldds = 0 if ds is None else _token_rows(ds, "ds", dy)
     L = _ln(dy, kind, weight, None, 0.0, p, seed, site_id)
+    B, n, dev, index = L.B, L.n, dy.device, dy.get_device()
     lddx = lddh = n
     if dx is None:
-        dx = torch.empty((B, T, n), dtype=dtype, device=dev)
+        dx = _rows_like(dy, ldd)
     else:
-        lddx = _token_rows(dx, "dx", shape, dtype, dev)
+        lddx = _token_rows(dx, "dx", dy)
     if dh is not None:
-        lddh = _token_rows(dh, "dh", shape, dtype, dev)
+        lddh = _token_rows(dh, "dh", dy)
     elif p > 0.0:
-        dh = torch.empty((B, T, n), dtype=dtype, device=dev)
+        dh = _rows_like(dy, ldd)
+    given = [_sample_rows(g, name, B, n, index) for g, name in ((dw, "dw"), (db, "db")) if g is not None]
+    ldg = max(given, default=n) or n
+    if len(given) == 2 and given[0] != given[1]:
+        raise ValueError("dw and db must share a row stride")
     if dw is None and weight_grad:
-        dw = torch.empty((B, n), dtype=torch.float32, device=dev) if db is None else torch.empty_like(db)
+        dw = torch.empty_strided((B, n), (ldg, 1), dtype=torch.float32, device=dev)
     if db is None and bias_grad:
-        db = (torch.empty((B, n), dtype=torch.float32, device=dev) if dw is None or dw.stride(0) == n
-              else torch.empty_strided(dw.shape, dw.stride(), dtype=torch.float32, device=dev))
-    ldg = 0
-    for g, name in ((dw, "dw"), (db, "db")):
-        if g is None:
-            continue
-        if g.shape != (B, n) or g.dtype != torch.float32 or g.device != dev or (n > 1 and g.stride(1) != 1):
-            raise ValueError(f"{name} must be [B, n] fp32 on {dev} with contiguous rows")
-        ld = g.stride(0) if B > 1 else max(n, ldg)
-        if ldg and ld != ldg:
-            raise ValueError("dw and db must share a row stride")
-        ldg = ld
+        db = torch.empty_strided((B, n), (ldg, 1), dtype=torch.float32, device=dev)
     need = 0
-    if ldg:
+    if dw is not None or db is not None:
         need = lib().dprc_layernorm_backward_workspace(ctypes.byref(L))
-        ws = _workspace(need, dev, ws) if need else None
-    ptr = lambda t: None if t is None else t.data_ptr()
+    ws = _workspace(need, dev, ws) if need else None
+    rows = B * L.T
     _check(lib().dprc_layernorm_backward(ctypes.byref(L), dy.data_ptr(), ldd, s.data_ptr(), lds,
-                                         _vector(mean, "mean", B * T, dev), _vector(rstd, "rstd", B * T, dev),
-                                         ptr(ds), ldds, ptr(dx), lddx, ptr(dh), lddh, ptr(dw), ptr(db), ldg,
-                                         ptr(ws) if need else None, need, _stream(dev)))
+                                         _vector(mean, "mean", rows, index), _vector(rstd, "rstd", rows, index),
+                                         _ptr(ds), ldds, dx.data_ptr(), lddx, _ptr(dh), lddh, _ptr(dw), _ptr(db), ldg,
+                                         _ptr(ws), need, _stream(dev)))
     return dx, dh, dw, db
 
 
@@ -578,8 +585,8 @@ def dprc_norm_vectors(G, n2=None, accumulate=False, ws=None):
         n2 = _new_n2(B, dev, accumulate)
     need = lib().dprc_norm_vectors_workspace(B, n)
     ws = _workspace(need, dev, ws) if need else None
-    _check(lib().dprc_norm_vectors(G.data_ptr(), ldg, B, n, _vector(n2, "n2", B, dev), int(bool(accumulate)),
-                                   ws.data_ptr() if need else None, need, _stream(dev)))
+    _check(lib().dprc_norm_vectors(G.data_ptr(), ldg, B, n, _vector(n2, "n2", B, G.get_device()),
+                                   int(bool(accumulate)), _ptr(ws), need, _stream(dev)))
     return n2
 
 
@@ -590,9 +597,10 @@ def dprc_clip_accumulate_vectors(G, c, grad=None, accumulate=False, ws=None):
         grad = (torch.zeros if accumulate else torch.empty)(n, dtype=torch.float32, device=dev)
     need = lib().dprc_clip_accumulate_vectors_workspace(B, n)
     ws = _workspace(need, dev, ws) if need else None
-    _check(lib().dprc_clip_accumulate_vectors(G.data_ptr(), ldg, _vector(c, "c", B, dev), B, n,
-                                              _vector(grad, "grad", n, dev), int(bool(accumulate)),
-                                              ws.data_ptr() if need else None, need, _stream(dev)))
+    index = G.get_device()
+    _check(lib().dprc_clip_accumulate_vectors(G.data_ptr(), ldg, _vector(c, "c", B, index), B, n,
+                                              _vector(grad, "grad", n, index), int(bool(accumulate)), _ptr(ws), need,
+                                              _stream(dev)))
     return grad
 
 
