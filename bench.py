@@ -54,6 +54,8 @@ def parse():
                     help="skip the context measurements (vendor GEMM and read references)")
     ap.add_argument("--graph", action="store_true",
                     help="replay a captured HIP graph per step instead of launching from the host")
+    ap.add_argument("--junctions", action="store_true",
+                    help="llama_step: residual sums and norms as fused junctions whose weights are trained too")
     ap.add_argument("--copy-calibration", type=float, default=0.0, metavar="BYTES",
                     help="only run 5 device copies of BYTES bytes (calibrates FETCH_SIZE / WRITE_SIZE counters)")
     return ap.parse_args()
@@ -580,9 +582,10 @@ def run_llama_step(args, torch, D):
     B, T, k, C, sigma = cfg["B"], cfg["T"], cfg["k"], cfg["C"], cfg["sigma"]
     steps, warmup = min(args.steps, 10), max(1, min(args.warmup, 3))
     print(f"[bench] workload=llama_step B={B} T={T}: building the model", file=sys.stderr, flush=True)
-    model = llama.build(seed=0, device="cuda")
+    model = llama.build(seed=0, device="cuda", junctions=args.junctions)
     tok = llama.tokens(B, T, llama.LLAMA_3_2_1B["vocab"], device="cuda")
-    drv = dpsgd.DPSGDRC(model.linears(), C=C, sigma=sigma, k=k, lr=cfg["lr"])
+    drv = dpsgd.DPSGDRC(model.linears(), C=C, sigma=sigma, k=k, lr=cfg["lr"],
+                        norms=model.norms() if args.junctions else ())
     loss_fn = lambda: llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:])
     layer_shapes = [(lin.in_features, lin.out_features) for lin in drv.linears]
     Ev = lambda: torch.cuda.Event(enable_timing=True)
@@ -593,7 +596,7 @@ def run_llama_step(args, torch, D):
         losses, pairs = drv.capture(loss_fn)
         mark(1)
         key = dpsgd.step_seed(0, drv.steps)
-        n2, c = D.dprc_norm_hutch_clip(pairs, k, key, C)
+        n2, c = drv.estimate(pairs, key)
         mark(2)
         grads = drv.clipped_sums(pairs, c)
         mark(3)
@@ -644,7 +647,7 @@ def run_llama_step(args, torch, D):
     extra = {"stages_ms": {"forward_and_capture": round(stage[0], 3), "norms_and_clip": round(stage[1], 3),
                            "clipped_gemm": round(stage[2], 3), "noise_and_adamw_fused": round(stage[3], 3)},
              "library_kernels": kernels}
-    if not args.no_extra:
+    if not args.no_extra and not args.junctions:
         extra.update(llama_context_steps(torch, D, dpsgd, drv, loss_fn, model, B, T, k, C, sigma, steps))
     rec = {"metric": "DP-SGD-RC training-step tokens/s, Llama-3.2-1B-shaped stack",
            "value": round(B * T / (ms_per_step * 1e-3), 1), "unit": "tokens/s", "n_gpus": 1,
@@ -652,7 +655,7 @@ def run_llama_step(args, torch, D):
            "scaling": "weak", "vs_baseline": None, "dtype": "bf16",
            "data": "synthetic (seeded tokens; random-init Llama-3.2-1B-shaped weights)",
            "config": {"workload": "llama_step", "B": B, "T": T, "blocks": 16, "hidden": 2048, "mlp": 8192,
-                      "heads": "32q/8kv", "vocab": 128256, "trained": "all 113 linear layers",
+                      "heads": "32q/8kv", "vocab": 128256, "trained": "all 113 linear layers" + (" and 33 norms" if args.junctions else ""),
                       "estimator": "hutch", "probes": k, "C": C, "sigma": sigma, "optimizer": "AdamW",
                       "steps_include": ["forward", "capture E (autograd to layer outputs)", "norm-hutch",
                                         "clip_scale", "clip_accumulate", "private_adamw (noise + AdamW)"]},

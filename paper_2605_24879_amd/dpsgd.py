@@ -24,9 +24,17 @@ Per step:
    and the transposed bf16 weight write); ``fused_adamw=False`` runs
    ``dprc_add_noise`` and ``torch.optim.AdamW`` instead.
 
-Only the listed linear layers are trained; every other parameter (embedding,
-norms) is held fixed.  Probes and noise are keyed by a per-step seed derived
-from (seed, step), so they are fresh every step.
+Only the listed linear layers are trained, and the norms given as ``norms``;
+every other parameter (embedding, other norms) is held fixed.  Probes, noise
+and the norms' dropout masks are keyed by a per-step seed derived from (seed,
+step), so they are fresh every step.
+
+With ``norms`` (``junction.Junction`` modules), step 2 goes on through the first
+norm; the backward calls write every sample's weight and bias gradients side by
+side into one [B, N] matrix; step 3 starts from its rows' exact squared norms
+(``dprc_norm_vectors``), step 5 adds its clipped sum
+(``dprc_clip_accumulate_vectors``), and steps 6 and 7 treat all of them as one
+more layer, without weight decay.
 """
 
 import torch
@@ -54,11 +62,13 @@ class DPSGDRC:
     "hutch" (k probes, ``probe`` "rademacher" or "gaussian") or "hutchpp"
     (sketch s, residual probes r).  ``C``: clipping threshold; ``sigma``:
     noise multiplier.  AdamW hyper-parameters as in ``torch.optim.AdamW``.
+    ``norms``: the ``junction.Junction`` modules whose weights and biases are
+    trained too (parameters of one dtype; they become views of one buffer).
     """
 
     def __init__(self, linears, C, sigma, estimator="hutch", k=16, probe="rademacher", s=16, r=32,
                  side=D.SIDE_OUT, seed=0, lr=1e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
-                 fused_adamw=True):
+                 fused_adamw=True, norms=()):
         self.linears = list(linears)
         for lin in self.linears:
             if lin.bias is not None:
@@ -71,19 +81,59 @@ class DPSGDRC:
         self.master = [lin.weight.detach().t().float().contiguous() for lin in self.linears]
         for lin in self.linears:
             lin.weight.requires_grad_(True)
+        self.norms = list(norms)
+        self._gather_vectors()
         self.hp = dict(lr=lr, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay)
         self.fused = bool(fused_adamw)
+        masters = self.master + ([self.vec_master] if self.norms else [])
         if self.fused:
-            self.m = [torch.zeros_like(x) for x in self.master]
-            self.v = [torch.zeros_like(x) for x in self.master]
+            self.m = [torch.zeros_like(x) for x in masters]
+            self.v = [torch.zeros_like(x) for x in masters]
         else:
-            self.opt = torch.optim.AdamW(self.master, lr=lr, betas=betas, eps=eps, weight_decay=weight_decay)
+            groups = [dict(params=self.master)]
+            if self.norms:
+                groups.append(dict(params=[self.vec_master], weight_decay=0.0))
+            self.opt = torch.optim.AdamW(groups, lr=lr, betas=betas, eps=eps, weight_decay=weight_decay)
         self.steps = 0
         self._A = [None] * len(self.linears)
         self._S = [None] * len(self.linears)
         self._hooks = [lin.register_forward_hook(self._tap(j)) for j, lin in enumerate(self.linears)]
         self._ws_acc = None
         self.last = {}
+
+    def _gather_vectors(self):
+        """Lay the norms' parameters side by side: vec_master [1, N] fp32, and for bf16 parameters vec_w [N],
+        which the parameters become views of (fp32 ones become views of the master)."""
+        params = [q for m in self.norms for q in m.parameters_in_order()]
+        self._G = None
+        if not params:
+            return
+        if len({q.dtype for q in params}) != 1:
+            raise ValueError("the norms' parameters must share a dtype")
+        flat = torch.cat([q.detach().reshape(-1) for q in params])
+        self.vec_master = flat.float().view(1, -1)
+        self.vec_w = flat if flat.dtype == torch.bfloat16 else None
+        store = self.vec_master.view(-1) if self.vec_w is None else self.vec_w
+        at = 0
+        for m in self.norms:
+            cols = []
+            for q in m.parameters_in_order():
+                q.data = store[at:at + q.numel()]
+                q.requires_grad_(True)
+                cols.append(slice(at, at + q.numel()))
+                at += q.numel()
+            m.sink = self._sink(m, cols)
+
+    def _sink(self, m, cols):
+        def rows(B):
+            if self._G is None:
+                self._G = torch.empty(B, self.vec_master.shape[1], dtype=torch.float32, device=self.vec_master.device)
+                self._filled = set()
+            if id(m) in self._filled:
+                raise RuntimeError("a trained norm ran twice in one step")
+            self._filled.add(id(m))
+            return self._G[:, cols[0]], self._G[:, cols[1]] if len(cols) > 1 else None
+        return rows
 
     def _tap(self, j):
         def hook(mod, inputs, output):
@@ -94,13 +144,24 @@ class DPSGDRC:
     def remove_hooks(self):
         for h in self._hooks:
             h.remove()
+        for m in self.norms:
+            m.sink = None
 
     def capture(self, loss_fn):
         """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs."""
+        for m in self.norms:
+            m.seed = step_seed(self.seed, self.steps)
+        self._G = None
         losses = loss_fn()
         if losses.dim() != 1:
             raise ValueError("loss_fn must return per-sample losses [B]")
-        E = torch.autograd.grad(losses.sum(), self._S)
+        # the norms' weights are listed for the backward pass to reach every norm; their own
+        # gradients go to the rows of self._G
+        E = torch.autograd.grad(losses.sum(), self._S + [m.weight for m in self.norms], allow_unused=bool(self.norms))
+        if self.norms:
+            E = E[:len(self._S)]
+            if any(e is None for e in E) or self._G is None or len(self._filled) < len(self.norms):
+                raise RuntimeError("a trained layer or norm has no part in the loss")
         # token-row layouts for the library (no copy when already so; layers fed the
         # same activations keep one pointer, so they share a pass over A)
         pairs = [(_rows(self._A[j].detach()), _rows(E[j]), j) for j in range(len(self.linears))]
@@ -108,29 +169,41 @@ class DPSGDRC:
         self._S = [None] * len(self.linears)
         return losses.detach(), pairs
 
-    def private_grads(self, pairs, key, noise=True):
-        """Steps 3-6: n2 [B], c [B] and the clipped gradients ([d, p] fp32 per layer), with
-        the noise added unless ``noise`` is false."""
+    def estimate(self, pairs, key):
+        """Steps 3-4: n2 [B] and c [B]."""
+        n2 = D.dprc_norm_vectors(self._G) if self.norms else None
+        more = n2 is not None
         if self.estimator == "hutch":
-            n2, c = D.dprc_norm_hutch_clip(pairs, self.k, key, self.C, side=self.side, probe=self.probe)
-        else:
-            n2 = D.dprc_norm_hutchpp(pairs, self.s, self.r, key, side=self.side)
-            c = D.dprc_clip_scale(n2, self.C)
+            return D.dprc_norm_hutch_clip(pairs, self.k, key, self.C, side=self.side, probe=self.probe, n2=n2,
+                                          accumulate=more)
+        n2 = D.dprc_norm_hutchpp(pairs, self.s, self.r, key, side=self.side, n2=n2, accumulate=more)
+        return n2, D.dprc_clip_scale(n2, self.C)
+
+    def private_grads(self, pairs, key, noise=True):
+        """Steps 3-6: n2 [B], c [B] and the clipped gradients ([d, p] fp32 per layer, then [1, N] of
+        the norms if any are trained), with the noise added unless ``noise`` is false."""
+        n2, c = self.estimate(pairs, key)
         grads = self.clipped_sums(pairs, c)
         if noise and self.sigma > 0:
-            for (A, E, j), g in zip(pairs, grads):
+            for j, g in enumerate(grads):
                 D.dprc_add_noise(g, self.sigma, self.C, key, j)
         return n2, c, grads
 
     def clipped_sums(self, pairs, c):
         """Step 5 for every layer: one call when all are bf16 (the small layers share
-        launches), else one call per layer."""
+        launches), else one call per layer; then for the norms, whose per-sample
+        gradients it releases."""
         if all(A.dtype == torch.bfloat16 and E.dtype == torch.bfloat16 for (A, E, _) in pairs):
-            return D.dprc_clip_accumulate_layers(pairs, c)
-        need = max(D.dprc_clip_accumulate_workspace(A, E) for (A, E, _) in pairs)
-        if self._ws_acc is None or self._ws_acc.numel() < need:
-            self._ws_acc = torch.empty(max(need, 1), dtype=torch.uint8, device=c.device)
-        return [D.dprc_clip_accumulate(A, E, c, ws=self._ws_acc) for (A, E, _) in pairs]
+            grads = D.dprc_clip_accumulate_layers(pairs, c)
+        else:
+            need = max(D.dprc_clip_accumulate_workspace(A, E) for (A, E, _) in pairs)
+            if self._ws_acc is None or self._ws_acc.numel() < need:
+                self._ws_acc = torch.empty(max(need, 1), dtype=torch.uint8, device=c.device)
+            grads = [D.dprc_clip_accumulate(A, E, c, ws=self._ws_acc) for (A, E, _) in pairs]
+        if self.norms:
+            grads.append(D.dprc_clip_accumulate_vectors(self._G, c).view(1, -1))
+            self._G = None
+        return grads
 
     def update(self, clipped, batch, key):
         """Steps 6-7 fused: per layer, noise + 1/batch + AdamW + bf16 weight write in one pass."""
@@ -139,17 +212,24 @@ class DPSGDRC:
             D.dprc_private_adamw(th, self.m[j], self.v[j], G, self.sigma, self.C, key, j, 1.0 / batch,
                                  step=t, w=lin.weight.detach(), **self.hp)
             lin.weight.grad = None
+        if self.norms:
+            j = len(self.linears)
+            D.dprc_private_adamw(self.vec_master, self.m[j], self.v[j], clipped[j], self.sigma, self.C, key, j,
+                                 1.0 / batch, step=t, w=None if self.vec_w is None else self.vec_w.view(-1, 1),
+                                 **dict(self.hp, weight_decay=0.0))
         self.steps = t
 
     def apply(self, grads, batch):
         """Step 7 with torch's AdamW (noisy grads / batch), then refresh the model weights."""
-        for m, g in zip(self.master, grads):
+        for m, g in zip(self.master + ([self.vec_master] if self.norms else []), grads):
             m.grad = g.div_(batch)
         self.opt.step()
         with torch.no_grad():
             for lin, m in zip(self.linears, self.master):
                 lin.weight.copy_(m.t())
                 lin.weight.grad = None
+            if self.norms and self.vec_w is not None:
+                self.vec_w.copy_(self.vec_master[0])
         self.opt.zero_grad(set_to_none=True)
         self.steps += 1
 

@@ -1,0 +1,88 @@
+"""The junction between two linear layers of a block as a torch module around libdprc.
+
+``Junction`` computes ``s = res + dropout(x)`` and ``y = norm(s)`` in one call and hands both on:
+``y`` to the next layer, ``s`` to the next residual sum.  Its backward pass is one call too, and
+forms the gradient of the norm's weight and bias for every sample by itself.  Under a private
+training step (``dpsgd.DPSGDRC`` with ``norms=``) these per-sample gradients go to the step, which
+adds their squared norms to the estimates and takes their clipped sum; otherwise their sum is the
+parameters' ordinary gradient.
+
+The dropout mask is a function of (seed, site, row, column) and is made again in the backward pass.
+``seed`` is an attribute: the step sets it to its key; without a step the caller changes it from one
+training step to the next.
+"""
+
+import torch
+import torch.nn as nn
+
+from . import dprc as D
+
+_KINDS = {"layer": D.LAYERNORM, "rms": D.RMSNORM}
+
+
+def token_rows(x):
+    """x [B, T, n] itself where its token rows have one stride, else a contiguous copy."""
+    B, T, n = x.shape
+    return x if x.stride(2) == 1 and x.stride(0) == T * x.stride(1) and x.stride(1) >= n else x.contiguous()
+
+
+class _JunctionFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, res, weight, bias, mod, p):
+        y, s, mean, rstd = D.dprc_layernorm(x, weight, bias, eps=mod.eps, kind=mod.kind, res=res, p=p, seed=mod.seed,
+                                            site_id=mod.site_id)
+        ctx.save_for_backward(s, weight, mean, rstd)
+        ctx.mod, ctx.p, ctx.seed, ctx.has_res, ctx.has_bias = mod, p, mod.seed, res is not None, bias is not None
+        ctx.set_materialize_grads(False)
+        return (y,) if s is x else (y, s)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, ds=None):
+        s, weight, mean, rstd = ctx.saved_tensors
+        mod, B = ctx.mod, s.shape[0]
+        dy = torch.zeros_like(s) if dy is None else token_rows(dy)
+        ds = None if ds is None else token_rows(ds)
+        dw = db = gw = gb = None
+        want_w, want_b = ctx.needs_input_grad[2], ctx.has_bias and ctx.needs_input_grad[3]
+        if mod.sink is not None:
+            dw, db = mod.sink(B)
+            want_w, want_b = True, ctx.has_bias
+        dx, dh, dw, db = D.dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=mod.kind, ds=ds, p=ctx.p,
+                                                   seed=ctx.seed, site_id=mod.site_id, weight_grad=want_w,
+                                                   bias_grad=want_b, dw=dw, db=db)
+        if mod.sink is None and (want_w or want_b):
+            ones = torch.ones(B, dtype=torch.float32, device=s.device)
+            gw = D.dprc_clip_accumulate_vectors(dw, ones).to(weight.dtype) if want_w else None
+            gb = D.dprc_clip_accumulate_vectors(db, ones).to(weight.dtype) if want_b else None
+        return dx if dh is None else dh, dx if ctx.has_res else None, gw, gb, None, None
+
+
+class Junction(nn.Module):
+    """Dropout, residual sum and norm of [B, T, n] token rows: ``y, s = junction(x, res)``.
+
+    ``kind``: "layer" (with a bias unless ``bias`` is false) or "rms" (none).  ``p``: dropout rate,
+    in training only.  ``site_id``: the place in the model, part of the mask's key.
+    """
+
+    def __init__(self, n, kind="layer", eps=1e-5, bias=True, p=0.0, site_id=0):
+        super().__init__()
+        self.kind, self.eps, self.p, self.site_id = _KINDS[kind], float(eps), float(p), int(site_id)
+        self.weight = nn.Parameter(torch.ones(n))
+        self.bias = nn.Parameter(torch.zeros(n)) if kind == "layer" and bias else None
+        self.seed = 0
+        self.sink = None                  # a private step's: B -> (dw, db) rows to write
+
+    def parameters_in_order(self):
+        return [self.weight] if self.bias is None else [self.weight, self.bias]
+
+    def forward(self, x, res=None):
+        p = self.p if self.training else 0.0
+        x = token_rows(x)
+        res = None if res is None else token_rows(res)
+        if not torch.is_grad_enabled():
+            y, s, _, _ = D.dprc_layernorm(x, self.weight, self.bias, eps=self.eps, kind=self.kind, res=res, p=p,
+                                          seed=self.seed, site_id=self.site_id, stats=False)
+            return y, s
+        out = _JunctionFn.apply(x, res, self.weight, self.bias, self, p)
+        return out if len(out) == 2 else (out[0], x)

@@ -12,10 +12,16 @@ Attention scores, softmax and the value product run in fp32 on contiguous
 operands; the projections run in the weights' dtype (bf16 by default).  q, k
 and v read the same normed activations, as do gate and up.
 
+With ``junctions`` the norms, the residual sums before them and a dropout of rate
+``dropout`` on every branch run as ``paper_2605_24879_amd.junction.Junction``
+(``norm``: "rms" or "layer"), whose parameters ``norms()`` lists for private
+training.
+
 ``linears()`` lists the projections in model order (per block q, k, v, o,
 gate, up, down; then lm_head), which keeps the shared-input layers adjacent.
 """
 
+import itertools
 import math
 
 import torch
@@ -51,23 +57,22 @@ def _rope(x, cos, sin):
 
 
 class Block(nn.Module):
-    def __init__(self, hidden, mlp, heads, kv_heads):
+    def __init__(self, hidden, mlp, heads, kv_heads, make_norm=RMSNorm):
         super().__init__()
         hd = hidden // heads
         self.heads, self.kv_heads, self.hd = heads, kv_heads, hd
-        self.norm1 = RMSNorm(hidden)
+        self.norm1 = make_norm(hidden)
         self.q = nn.Linear(hidden, heads * hd, bias=False)
         self.k = nn.Linear(hidden, kv_heads * hd, bias=False)
         self.v = nn.Linear(hidden, kv_heads * hd, bias=False)
         self.o = nn.Linear(heads * hd, hidden, bias=False)
-        self.norm2 = RMSNorm(hidden)
+        self.norm2 = make_norm(hidden)
         self.gate = nn.Linear(hidden, mlp, bias=False)
         self.up = nn.Linear(hidden, mlp, bias=False)
         self.down = nn.Linear(mlp, hidden, bias=False)
 
-    def forward(self, x, cos, sin, mask):
-        B, T, _ = x.shape
-        h = self.norm1(x)
+    def attend(self, h, cos, sin, mask):
+        B, T, _ = h.shape
         q = self.q(h).view(B, T, self.heads, self.hd).transpose(1, 2).float()
         k = self.k(h).view(B, T, self.kv_heads, self.hd).transpose(1, 2).float()
         v = self.v(h).view(B, T, self.kv_heads, self.hd).transpose(1, 2).float()
@@ -77,19 +82,42 @@ class Block(nn.Module):
         v = v.repeat_interleave(rep, dim=1).contiguous()
         s = torch.matmul(q.contiguous(), k.transpose(-1, -2).contiguous()) * (1.0 / math.sqrt(self.hd))
         p = torch.softmax(s + mask, dim=-1)
-        a = torch.matmul(p, v).transpose(1, 2).reshape(B, T, self.heads * self.hd).to(x.dtype)
-        x = x + self.o(a)
-        h = self.norm2(x)
-        return x + self.down(F.silu(self.gate(h)) * self.up(h))
+        a = torch.matmul(p, v).transpose(1, 2).reshape(B, T, self.heads * self.hd).to(h.dtype)
+        return self.o(a)
+
+    def feed(self, h):
+        return self.down(F.silu(self.gate(h)) * self.up(h))
+
+    def forward(self, x, cos, sin, mask):
+        x = x + self.attend(self.norm1(x), cos, sin, mask)
+        return x + self.feed(self.norm2(x))
+
+
+class JunctionBlock(Block):
+    """The block with each residual sum in the junction before the next norm: from a branch not yet added
+    and the residual (None before the first sum) to the next such pair."""
+
+    def forward(self, branch, x, cos, sin, mask):
+        h, x = self.norm1(branch, x)
+        h, x = self.norm2(self.attend(h, cos, sin, mask), x)
+        return self.feed(h), x
 
 
 class LlamaShaped(nn.Module):
     def __init__(self, layers=16, hidden=2048, mlp=8192, heads=32, kv_heads=8, vocab=128256,
-                 rope_base=500000.0):
+                 rope_base=500000.0, junctions=False, norm="rms", dropout=0.0):
         super().__init__()
         self.embed = nn.Embedding(vocab, hidden)
-        self.blocks = nn.ModuleList([Block(hidden, mlp, heads, kv_heads) for _ in range(layers)])
-        self.norm = RMSNorm(hidden)
+        self.junctions = bool(junctions)
+        make_norm, block = RMSNorm, Block
+        if self.junctions:
+            from paper_2605_24879_amd.junction import Junction
+            sites = itertools.count()
+            make_norm, block = lambda n: Junction(n, kind=norm, p=dropout, site_id=next(sites)), JunctionBlock
+        elif norm != "rms" or dropout:
+            raise ValueError("layer norm and dropout come with junctions")
+        self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm) for _ in range(layers)])
+        self.norm = make_norm(hidden)
         self.lm_head = nn.Linear(hidden, vocab, bias=False)
         self.rope_base = rope_base
         self.hd = hidden // heads
@@ -100,11 +128,19 @@ class LlamaShaped(nn.Module):
             out += [b.q, b.k, b.v, b.o, b.gate, b.up, b.down]
         return out + [self.lm_head]
 
+    def norms(self):
+        return [m for b in self.blocks for m in (b.norm1, b.norm2)] + [self.norm]
+
     def forward(self, tokens):
         B, T = tokens.shape
         cos, sin = _rope_tables(T, self.hd, self.rope_base, tokens.device)
         mask = torch.full((T, T), float("-inf"), device=tokens.device).triu(1)
         x = self.embed(tokens)
+        if self.junctions:
+            branch, x = x, None
+            for b in self.blocks:
+                branch, x = b(branch, x, cos, sin, mask)
+            return self.lm_head(self.norm(branch, x)[0])
         for b in self.blocks:
             x = b(x, cos, sin, mask)
         return self.lm_head(self.norm(x))
@@ -123,7 +159,7 @@ def build(seed=0, device="cuda", dtype=torch.bfloat16, **sizes):
             if prm.dim() == 2:
                 prm.normal_(0.0, 0.02, generator=g)
             else:
-                prm.fill_(1.0)
+                prm.fill_(0.0 if name.endswith("bias") else 1.0)
     return model.to(dtype)
 
 
