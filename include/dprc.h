@@ -445,7 +445,7 @@ typedef enum {
   DPRC_KERNEL_LAYERNORM = 25,         /* dropout, residual sum and norm          */
   DPRC_KERNEL_LAYERNORM_BACKWARD = 26,
   DPRC_KERNEL_VECTOR_NORMS = 27,      /* squared norms of per-sample vectors     */
-  DPRC_KERNEL_VECTOR_SUMS = 28        /* clipped sums of per-sample vectors, sums of their token splits */
+  DPRC_KERNEL_VECTOR_SUMS = 28        /* clipped sums of per-sample vectors      */
 } dprc_kernel_kind;
 dprc_status dprc_trace_launches(hipEvent_t* events, int32_t* kinds, int32_t capacity,
                                 int32_t* count);

@@ -1677,8 +1677,7 @@ dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const v
 
 size_t dprc_layernorm_backward_workspace(const dprc_ln* L) {
   if (check_ln(L) != DPRC_SUCCESS) return 0;
-  const int S = norm_back_splits(L->B, L->T, L->n, L->dtype == DPRC_BF16);
-  return S > 1 ? (size_t)round_up(L->B * S * 2 * L->n * (int64_t)sizeof(float), kAlign) : 0;
+  return (size_t)round_up(norm_back_plan(L->B, L->T, L->n, elem_bytes(L->dtype), 2).parts * 2 * L->n * (int64_t)sizeof(float), kAlign);
 }
 
 dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t lddy, const void* s, int64_t lds,
@@ -1710,11 +1709,10 @@ dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t ld
   a.B = L->B; a.T = L->T; a.n = L->n;
   a.inv_n = (float)(1.0 / (double)L->n);
   a.bf16 = L->dtype == DPRC_BF16; a.wbf16 = L->wdtype == DPRC_BF16; a.rms = L->kind == DPRC_RMSNORM;
-  a.S = norm_back_splits(L->B, L->T, L->n, L->dtype == DPRC_BF16);
+  const NormBackPlan p = norm_back_plan(L->B, L->T, L->n, e, ds ? 3 : 2);
+  a.split = p.split;
   a.part = static_cast<float*>(ws);
-  st = hip_status(traced(DPRC_KERNEL_LAYERNORM_BACKWARD, stream, [&] { return launch_norm_back(a, stream); }));
-  if (st != DPRC_SUCCESS || !grads || a.S == 1) return st;
-  return hip_status(traced(DPRC_KERNEL_VECTOR_SUMS, stream, [&] { return launch_norm_back_sums(a, stream); }));
+  return hip_status(traced(DPRC_KERNEL_LAYERNORM_BACKWARD, stream, [&] { return launch_norm_back(a, p, stream); }));
 }
 
 static dprc_status check_vectors(const float* G, int64_t ldg, int64_t B, int64_t n, const void* out) {

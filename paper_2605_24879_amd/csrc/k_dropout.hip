@@ -41,7 +41,7 @@ __global__ __launch_bounds__(256) void dropout_kernel(DropoutArgs a, int per_row
     if (col[k] < 0) continue;
     float v[EP], u[EP];
     unpack_row<E, M>(x[k], col[k], n, v);
-    if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)row[k], col[k], v);
+    if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)row[k], col[k], n, v);
     if (a.res) {
       unpack_row<E, M>(z[k], col[k], n, u);
 #pragma unroll

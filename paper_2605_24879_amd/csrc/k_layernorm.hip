@@ -9,91 +9,122 @@
 
 namespace dprc {
 
-constexpr int64_t kNormBlocks = 512;
+// What a call has besides x and y: known at compile time, because the number of loads and stores of a
+// row then is, and with it how many may still be under way when the next row is waited for.  kAny takes
+// any set.
+enum : int { kRes = 1, kSum = 2, kStats = 4, kAny = 8 };
 
 // TPR threads hold a row of at most TPR * C columns, C each; a workgroup of max(256, TPR)
-// threads works on 256 / TPR rows at a time and walks the rows with the grid, the next row's
+// threads works on 256 / TPR rows at a time and walks the rows with the grid, the next rows'
 // pieces loading while this one is reduced.  Weight and bias stay in registers for all rows.
-template <class E, int M, int TPR, int C>
+template <class E, int M, int TPR, int C, int FL>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a) {
   constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
   constexpr bool kHold = TPR < 1024;
+  constexpr int kAhead = C == 8 ? 2 : 1;                          // rows loading ahead
   typedef RowSum<TPR, 1, BLK> Sum;
   __shared__ typename Sum::Buffer buf;
   int turn = 0;
-  const int t = threadIdx.x % TPR, n = (int)a.n;
-  const int64_t step = (int64_t)gridDim.x * RPB;
-  int64_t r = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+  const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR, n = (int)a.n;
+  const bool has_res = FL & kAny ? a.res != nullptr : (FL & kRes) != 0;
+  const bool has_sum = FL & kAny ? a.sum != nullptr : (FL & kSum) != 0;
+  const int64_t step = (int64_t)gridDim.x * RPB, r_first = (int64_t)blockIdx.x * RPB;
+  // bytes from the first of the workgroup's rows to this thread's
+  const uint32_t gx = (uint32_t)(rg * a.ldx * sizeof(E)), gr = (uint32_t)(rg * a.ldr * sizeof(E));
+  const uint32_t gs = (uint32_t)(rg * a.lds * sizeof(E)), gy = (uint32_t)(rg * a.ldy * sizeof(E));
 
-  uint4 x[V], z[V];
-  auto load = [&](int64_t row) {
-    row = std::min(row, a.rows - 1);
+  struct Row {
+    uint4 x[V], z[V];
+  };
+  auto load = [&](Row& q, int64_t r0, bool live) {
+    const char* px = (const char*)a.x + r0 * a.ldx * sizeof(E);
+    const char* pr = (const char*)a.res + r0 * a.ldr * sizeof(E);
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (v * TPR + t) * EP;
-      x[v] = load_row<E, M>((const E*)a.x + row * a.ldx, c, n);
-      if (a.res) z[v] = load_row<E, M>((const E*)a.res + row * a.ldr, c, n);
+      q.x[v] = load_at<E, M>(px, live ? gx : 0u, c, n);
+      if (has_res) q.z[v] = load_at<E, M>(pr, live ? gr : 0u, c, n);
     }
   };
-  load(r);
   float w[C], b[C];
   auto load_wb = [&](int v) {
-    const int c = (v * TPR + t) * EP;
+    const int c = piece_col<E, M>((v * TPR + t) * EP, n);
     load_vec<EP>(a.w, a.wbf16, c, n, 1.f, w + v * EP);
     load_vec<EP>(a.b, a.wbf16, c, n, 0.f, b + v * EP);
   };
-  if (kHold)
-#pragma unroll
-    for (int v = 0; v < V; ++v) load_wb(v);
-  for (int64_t r0 = (int64_t)blockIdx.x * RPB; r0 < a.rows; r0 += step, r += step) {
+  int64_t r0 = r_first;
+  // a round: the rows from r0 on, and the loads of those `ahead` rounds on.  PART: rows that are `live`.
+  auto round = [&](Row& q, auto part, int64_t ahead, bool live) {
+    constexpr bool PART = decltype(part)::value;
     float s[C], u[EP], red[1] = {0.f}, mu = 0.f;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * EP;
-#pragma unroll
-      for (int k = v * EP; k < v * EP + EP; ++k) s[k] = 0.f;
-      if (c >= n) continue;
-      unpack_row<E, M>(x[v], c, n, s + v * EP);
-      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, s + v * EP);
-      if (!a.res) continue;
-      unpack_row<E, M>(z[v], c, n, u);
+      unpack<E>(q.x[v], s + v * EP);
+      if (a.drop.on)
+        drop_piece<E>(a.drop, (uint32_t)r0 + (uint32_t)rg, piece_col<E, M>((v * TPR + t) * EP, n), n, s + v * EP);
+      if (!has_res) continue;
+      unpack<E>(q.z[v], u);
 #pragma unroll
       for (int j = 0; j < EP; ++j) s[v * EP + j] += u[j];
     }
-    load(r + step);
+    if (!PART) load(q, r0 + ahead * step, true);
     if (!a.rms) {
 #pragma unroll
-      for (int k = 0; k < C; ++k) red[0] += s[k];
+      for (int k = 0; k < C; ++k) {
+        const int c = (k / EP * TPR + t) * EP;
+        red[0] += owns<M>(c, piece_col<E, M>(c, n), k % EP, n) ? s[k] : 0.f;
+      }
       Sum::run(red, buf, turn);
       mu = red[0] * a.inv_n;
       red[0] = 0.f;
     }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * EP;
-#pragma unroll
-      for (int j = 0; j < EP; ++j) {
-        const float d = (M == kWhole ? c : c + j) < n ? s[v * EP + j] - mu : 0.f;
-        red[0] = fmaf(d, d, red[0]);
-      }
+    for (int k = 0; k < C; ++k) {
+      const int c = (k / EP * TPR + t) * EP;
+      const float d = owns<M>(c, piece_col<E, M>(c, n), k % EP, n) ? s[k] - mu : 0.f;
+      red[0] = fmaf(d, d, red[0]);
     }
     Sum::run(red, buf, turn);
     const float rstd = 1.f / sqrtf(fmaf(red[0], a.inv_n, a.eps));
-    if (r >= a.rows) continue;
-    if (t == 0) {
-      if (a.mean) a.mean[r] = mu;
-      if (a.rstd) a.rstd[r] = rstd;
-    }
+    char* ps = (char*)a.sum + r0 * a.lds * sizeof(E);
+    char* py = (char*)a.y + r0 * a.ldy * sizeof(E);
+    if (!PART || live) {
+      if (FL & kAny) {
+        if (t == 0 && a.mean) a.mean[r0 + rg] = mu;
+        if (t == 0 && a.rstd) a.rstd[r0 + rg] = rstd;
+      } else if (FL & kStats) {                                   // by all of the row's threads
+        (a.rms ? a.rstd : a.mean)[r0 + rg] = a.rms ? rstd : mu;
+        a.rstd[r0 + rg] = rstd;
+      }
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-      const int c = (v * TPR + t) * EP;
-      if (c >= n) continue;
-      if (a.sum) store_row<E, M>((E*)a.sum + r * a.lds, c, n, s + v * EP);
-      if (!kHold) load_wb(v);
+      for (int v = 0; v < V; ++v) {
+        const int c = (v * TPR + t) * EP;
+        if (has_sum) store_at<E, M>(ps, gs, c, n, s + v * EP);
+        if (!kHold) load_wb(v);
 #pragma unroll
-      for (int j = 0; j < EP; ++j) u[j] = fmaf((s[v * EP + j] - mu) * rstd, w[v * EP + j], b[v * EP + j]);
-      store_row<E, M>((E*)a.y + r * a.ldy, c, n, u);
+        for (int j = 0; j < EP; ++j) u[j] = fmaf((s[v * EP + j] - mu) * rstd, w[v * EP + j], b[v * EP + j]);
+        store_at<E, M>(py, gy, c, n, u);
+      }
     }
+    r0 += step;
+  };
+  // the rounds in which every row group has a row; then, for one workgroup, the last rows
+  const int64_t whole = a.rows - r_first < RPB ? 0 : (a.rows - r_first - RPB) / step + 1;
+  Row ring[kAhead];
+  if (whole > 0)
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q) load(ring[q], r_first + std::min<int64_t>(q, whole - 1) * step, true);
+  if (kHold)
+#pragma unroll
+    for (int v = 0; v < V; ++v) load_wb(v);
+  for (int64_t left = whole; left > 0; left -= kAhead)
+#pragma unroll
+    for (int q = 0; q < kAhead; ++q)
+      if (q < left) round(ring[q], std::false_type{}, std::min<int64_t>(kAhead, left - q - 1), true);
+  if (RPB > 1 && r0 < a.rows) {
+    const bool live = r0 + rg < a.rows;
+    load(ring[0], r0, live);
+    round(ring[0], std::true_type{}, 0, live);
   }
 }
 
@@ -110,7 +141,7 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
     auto piece = [&](int c, float* s) {
       float u[EP];
       unpack_row<E, M>(load_row<E, M>((const E*)a.x + r * a.ldx, c, n), c, n, s);
-      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, s);
+      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, n, s);
       if (a.res) {
         unpack_row<E, M>(load_row<E, M>((const E*)a.res + r * a.ldr, c, n), c, n, u);
 #pragma unroll
@@ -154,45 +185,61 @@ __global__ __launch_bounds__(1024) void norm_long_kernel(NormArgs a) {
   }
 }
 
-// Threads per row: a power of two with 16 columns each (two bf16 or four fp32 pieces of every
-// tensor in flight per thread), and two workgroups per CU.  32768 rows of 2048 bf16 with
-// residual, dropout and statistics took 98 us so, 106 with four or eight per CU, 98 to 107
-// with 32 columns per thread (196 registers) and, in the plain form, 92 against 49 with
-// 8 columns (half as much in flight).
+constexpr int64_t kNormLong = 16384;
+
 template <class E, int M>
 static void launch_norm_of(const NormArgs& a, hipStream_t st) {
-  auto go = [&](auto kernel, int block, int rows_per_block) {
-    const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, rows_per_block), kNormBlocks);
-    DPRC_LAUNCH(kernel, dim3((unsigned)blocks), dim3(block), 0, st, a);
-  };
   const int64_t n = a.n;
-  if (n <= 64) return go(norm_kernel<E, M, 8, 8>, 256, 32);
-  if constexpr (M != kTiny) {
-    // At most one row per workgroup: a row's latency counts, 8 columns per thread (one row of 2048:
-    // 2.9 us against 3.5, 512 rows: 4.1 against 4.5; from 1024 rows on it is slower).  Past
-    // 4096 columns the two are alike.
-    if (a.rows <= kNormBlocks && n > 512 && n <= 4096) {
-      if (n <= 1024) return go(norm_kernel<E, M, 128, 8>, 256, 2);
-      if (n <= 2048) return go(norm_kernel<E, M, 256, 8>, 256, 1);
-      return go(norm_kernel<E, M, 512, 8>, 512, 1);
+  auto go = [&](auto tpr, auto cols) {
+    constexpr int TPR = decltype(tpr)::value, C = decltype(cols)::value, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
+    const int64_t ahead = (C == 8 ? 2 : 1) * (a.res ? 2 : 1) * RPB * n * (int64_t)sizeof(E);
+    const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, RPB), streaming_blocks(ahead));
+    auto launch = [&](auto kernel) { DPRC_LAUNCH(kernel, dim3((unsigned)blocks), dim3(BLK), 0, st, a); };
+    const bool stats = a.rstd && (a.rms || a.mean), none = !a.rstd && !a.mean;
+    if constexpr (M != kTiny) {
+      if (a.res && a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kRes | kSum | kStats>);
+      if (a.res && a.sum && none) return launch(norm_kernel<E, M, TPR, C, kRes | kSum>);
+      if (!a.res && !a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kStats>);
+      if (!a.res && !a.sum && none) return launch(norm_kernel<E, M, TPR, C, 0>);
     }
-    if (n <= 128) return go(norm_kernel<E, M, 8, 16>, 256, 32);
-    if (n <= 256) return go(norm_kernel<E, M, 16, 16>, 256, 16);
-    if (n <= 512) return go(norm_kernel<E, M, 32, 16>, 256, 8);
-    if (n <= 1024) return go(norm_kernel<E, M, 64, 16>, 256, 4);
-    if (n <= 2048) return go(norm_kernel<E, M, 128, 16>, 256, 2);
-    if (n <= 4096) return go(norm_kernel<E, M, 256, 16>, 256, 1);
-    if (n <= 8192) return go(norm_kernel<E, M, 512, 16>, 512, 1);
-    if (n <= 16384) return go(norm_kernel<E, M, 1024, 16>, 1024, 1);
-    go(norm_long_kernel<E, M>, 1024, 1);
+    launch(norm_kernel<E, M, TPR, C, kAny>);
+  };
+  using std::integral_constant;
+  const integral_constant<int, 8> c8;
+  const integral_constant<int, 16> c16;
+  const int tpr = threads_per_row(n);
+  if (tpr == 8) return go(integral_constant<int, 8>(), c8);
+  if constexpr (M != kTiny) {
+    if (tpr == 16) return go(integral_constant<int, 16>(), c8);
+    if (tpr == 32) return go(integral_constant<int, 32>(), c8);
+    if (tpr == 64) return go(integral_constant<int, 64>(), c8);
+    if (tpr == 128) return go(integral_constant<int, 128>(), c8);
+    if (tpr == 256) return go(integral_constant<int, 256>(), c8);
+    if (n <= 4096) return go(integral_constant<int, 512>(), c8);
+    if (n <= 8192) return go(integral_constant<int, 512>(), c16);
+    go(integral_constant<int, 1024>(), c16);
   }
+}
+
+template <class E, int M>
+static void launch_norm_long(const NormArgs& a, hipStream_t st) {
+  const int64_t blocks = std::min<int64_t>(a.rows, 512);
+  DPRC_LAUNCH((norm_long_kernel<E, M>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
 }
 
 template <class E>
 static void launch_norm_width(const NormArgs& a, hipStream_t st) {
-  if (a.n < kPiece<E>) launch_norm_of<E, kTiny>(a, st);
-  else if (a.n % kPiece<E> == 0) launch_norm_of<E, kWhole>(a, st);
-  else launch_norm_of<E, kTail>(a, st);
+  constexpr int EP = kPiece<E>;
+  // also rows so far apart that the 32 of a workgroup leave 32-bit offsets go the long rows' way
+  if (a.n > kNormLong || 32 * std::max({a.ldx, a.ldr, a.lds, a.ldy}) * (int64_t)sizeof(E) >= ((int64_t)1 << 31)) {
+    if (a.n < EP) launch_norm_long<E, kTiny>(a, st);
+    else if (a.n % EP == 0) launch_norm_long<E, kWhole>(a, st);
+    else launch_norm_long<E, kTail>(a, st);
+  } else if (a.n < EP) {
+    launch_norm_of<E, kTiny>(a, st);
+  } else {
+    launch_norm_of<E, kWide>(a, st);
+  }
 }
 
 hipError_t launch_norm(const NormArgs& a, hipStream_t st) {

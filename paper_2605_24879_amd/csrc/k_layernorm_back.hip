@@ -24,13 +24,20 @@ __device__ __forceinline__ void store_vec(float* p, int c, int n, const float* x
   }
 }
 
-// TPR threads hold a row as in the forward pass, 256 / TPR row groups a workgroup.  A work item is
-// a token split of a sample, whose rows its workgroup's groups take in turn, each thread summing
-// dw and db of its own columns in registers; the groups' sums meet at the item's end, in lanes
-// and in LDS.  With SOLO (samples shorter than a few rounds of the groups) an item is
-// a sample for each group, and nothing is combined.
-template <class E, int M, int TPR, int C, bool SOLO>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBackArgs a, int64_t per, int64_t items) {
+// Which of ds and dh a call has: known at compile time, because the number of loads and stores of a
+// round then is, and with it how many may still be under way when a row is waited for.  (Where a
+// branch may skip a store, the compiler has to assume that it did, and waits for later loads.)
+// kAny takes any set, dx = null too.
+enum : int { kDs = 1, kDh = 2, kAny = 4 };
+
+// TPR threads hold a row as in the forward pass, 256 / TPR row groups a workgroup; a round is a row for each
+// of them.  The samples' rounds, laid end to end, are dealt out evenly (BackSplit), so a workgroup walks
+// one sample's rounds or parts of several; each thread sums dw and db of its own columns in
+// registers over a sample's rounds, the groups' sums meet in lanes and in LDS, and go to dw and db, or as a
+// part of them to the workspace where other workgroups have the sample's other rounds.  With
+// SOLO (samples shorter than a round) every group has samples of its own, and nothing is combined.
+template <class E, int M, int TPR, int C, bool SOLO, int FL>
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBackArgs a) {
   constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
   constexpr int G = SOLO ? 1 : (TPR < 64 ? BLK / 64 : RPB);      // sums to combine in LDS
   constexpr int kAhead = V <= 2 ? 2 : 1;                          // rows loading ahead
@@ -39,93 +46,122 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
   __shared__ float comb[G > 1 ? G - 1 : 1][2][G > 1 ? C : 1][G > 1 ? TPR : 1];
   int turn = 0;
   const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR, n = (int)a.n;
+  const bool has_ds = FL & kAny ? a.ds != nullptr : (FL & kDs) != 0;
+  const bool has_dh = FL & kAny ? a.dh != nullptr : (FL & kDh) != 0;
+  const bool has_dx = FL & kAny ? a.dx != nullptr : true;
   const bool grads = a.dw || a.db;
+  const float* mean = a.rms ? a.rstd : a.mean;                    // loaded either way
+  // rows, and bytes, from the first row group's row to this one's
+  const uint32_t apart = (uint32_t)(rg * (SOLO ? a.T : 1));
+  const uint32_t gy = (uint32_t)(apart * a.lddy * sizeof(E)), gs = (uint32_t)(apart * a.lds * sizeof(E));
+  const uint32_t gd = (uint32_t)(apart * a.ldds * sizeof(E));
 
   float w[C];
 #pragma unroll
-  for (int v = 0; v < V; ++v) load_vec<EP>(a.w, a.wbf16, (v * TPR + t) * EP, n, 1.f, w + v * EP);
+  for (int v = 0; v < V; ++v) load_vec<EP>(a.w, a.wbf16, piece_col<E, M>((v * TPR + t) * EP, n), n, 1.f, w + v * EP);
 
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int64_t i = SOLO ? it * RPB + rg : it / a.S;
-    const int64_t first = SOLO ? 0 : (it - i * a.S) * per;
-    const int64_t last = SOLO ? (i < a.B ? a.T : 0) : std::min<int64_t>(a.T, first + per);
-    const int64_t trips = SOLO ? a.T : (last - first + RPB - 1) / RPB;
-    int64_t tok = first + (SOLO ? 0 : rg);
+  // this workgroup's samples (SOLO: every gridDim.x-th RPB of them) and rounds
+  const BackSplit& sp = a.split;
+  const int64_t q0 = SOLO ? 0 : sp.begin(blockIdx.x), q1 = SOLO ? 0 : sp.begin(blockIdx.x + 1);
+  const int64_t i_first = SOLO ? (int64_t)blockIdx.x * RPB : q0 / sp.rounds, i_step = SOLO ? (int64_t)gridDim.x * RPB : 1;
+  const int64_t i_end = SOLO ? a.B : (q1 + sp.rounds - 1) / sp.rounds;
+  for (int64_t i0 = i_first; i0 < i_end; i0 += i_step) {
+    const int64_t i = i0 + (SOLO ? rg : 0);
+    // its tokens, kTokStep of them a round: the rounds in which every row group has a row, then the others
     constexpr int kTokStep = SOLO ? 1 : RPB;
+    const int64_t first = SOLO ? 0 : std::max<int64_t>(q0 - i * sp.rounds, 0) * RPB;
+    const int64_t last = SOLO ? a.T : std::min<int64_t>((q1 - i * sp.rounds) * RPB, a.T);
+    const int64_t whole = SOLO ? (i0 + RPB <= a.B ? a.T : 0) : (last - first) / RPB;
+    const int64_t rest = SOLO ? a.T - whole : (last - first + RPB - 1) / RPB - whole;
+    int64_t tok = first;
 
     struct Row {
       uint4 dy[V], s[V], ds[V];
       float mu, rstd;
     };
-    auto load = [&](Row& x, int64_t token) {
-      const int64_t r = std::min(i, a.B - 1) * a.T + std::min(token, a.T - 1);
+    auto load = [&](Row& x, int64_t token, bool live) {
+      const int64_t r0 = i0 * a.T + token;
+      const char* py = (const char*)a.dy + r0 * a.lddy * sizeof(E);
+      const char* ps = (const char*)a.s + r0 * a.lds * sizeof(E);
+      const char* pd = (const char*)a.ds + r0 * a.ldds * sizeof(E);
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int c = (v * TPR + t) * EP;
-        x.dy[v] = load_row<E, M>((const E*)a.dy + r * a.lddy, c, n);
-        x.s[v] = load_row<E, M>((const E*)a.s + r * a.lds, c, n);
-        if (a.ds) x.ds[v] = load_row<E, M>((const E*)a.ds + r * a.ldds, c, n);
+        x.dy[v] = load_at<E, M>(py, live ? gy : 0u, c, n);
+        x.s[v] = load_at<E, M>(ps, live ? gs : 0u, c, n);
+        if (has_ds) x.ds[v] = load_at<E, M>(pd, live ? gd : 0u, c, n);
       }
-      if (!a.rms) x.mu = a.mean[r];
-      x.rstd = a.rstd[r];
+      x.mu = (mean + r0)[live ? apart : 0u];
+      x.rstd = (a.rstd + r0)[live ? apart : 0u];
     };
     float dw[C], db[C];
 #pragma unroll
     for (int k = 0; k < C; ++k) dw[k] = db[k] = 0.f;
-    // one round: this row's sums, the loads of the row two rounds on, the mask, then the outputs
-    auto round = [&](Row& x) {
+    // one round: this row's sums, the loads of the row kAhead rounds on (of `more` whole rounds), the
+    // mask, then the outputs.  PART: only rows that are `live`.
+    auto round = [&](Row& x, auto part, int64_t more, bool live) {
+      constexpr bool PART = decltype(part)::value;
       float g[C], xh[C], z[C], red[2] = {0.f, 0.f};
       const float rs = x.rstd, mu = a.rms ? 0.f : x.mu;
 #pragma unroll
       for (int v = 0; v < V; ++v) {
-        const int c = (v * TPR + t) * EP;
-        if (tok >= last || c >= n) continue;
-        unpack_row<E, M>(x.dy[v], c, n, g + v * EP);
-        unpack_row<E, M>(x.s[v], c, n, xh + v * EP);
-        if (a.ds) unpack_row<E, M>(x.ds[v], c, n, z + v * EP);
-        else
+        const int c = (v * TPR + t) * EP, cc = piece_col<E, M>(c, n);
+        unpack<E>(x.dy[v], g + v * EP);
+        unpack<E>(x.s[v], xh + v * EP);
+        if (has_ds) unpack<E>(x.ds[v], z + v * EP);
 #pragma unroll
-          for (int k = v * EP; k < v * EP + EP; ++k) z[k] = 0.f;
-#pragma unroll
-        for (int k = v * EP; k < v * EP + EP; ++k) {
+        for (int j = 0; j < EP; ++j) {
+          const int k = v * EP + j;
+          if (!has_ds) z[k] = 0.f;
+          if (PART) g[k] = live ? g[k] : 0.f;
           xh[k] = (xh[k] - mu) * rs;
           db[k] += g[k];
-          dw[k] = fmaf(g[k], xh[k], dw[k]);
+          dw[k] = fmaf(g[k], PART && !live ? 0.f : xh[k], dw[k]);
           g[k] *= w[k];
-          red[0] += g[k];
-          red[1] = fmaf(g[k], xh[k], red[1]);
+          const float own = owns<M>(c, cc, j, n) ? g[k] : 0.f;
+          red[0] += own;
+          red[1] = fmaf(own, owns<M>(c, cc, j, n) ? xh[k] : 0.f, red[1]);
         }
       }
-      load(x, tok + kAhead * kTokStep);
-      const int64_t r = i * a.T + tok;
+      const int64_t r0 = i0 * a.T + tok;
+      if (!PART) load(x, tok + std::min<int64_t>(kAhead, more - 1) * kTokStep, true);
       u32x4 mask[V];
-      const bool drop = a.dh && a.drop.on;
+      const bool drop = has_dh && a.drop.on;
       if (drop)
 #pragma unroll
-        for (int v = 0; v < V; ++v) mask[v] = drop_words<E>(a.drop, (uint32_t)r, (v * TPR + t) * EP);
+        for (int v = 0; v < V; ++v)
+          mask[v] = drop_words<E>(a.drop, (uint32_t)r0 + apart, piece_col<E, M>((v * TPR + t) * EP, n), n);
       Sum::run(red, buf, turn);
       const float mg = a.rms ? 0.f : red[0] * a.inv_n, mgx = red[1] * a.inv_n;
-      if (tok < last)
+      char* px = (char*)a.dx + r0 * a.lddx * sizeof(E);
+      char* ph = (char*)a.dh + r0 * a.lddh * sizeof(E);
+      if (!PART || live)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
           const int c = (v * TPR + t) * EP;
-          if (c >= n) continue;
 #pragma unroll
           for (int k = v * EP; k < v * EP + EP; ++k) z[k] = fmaf(rs, fmaf(-xh[k], mgx, g[k] - mg), z[k]);
-          if (a.dx) store_row<E, M>((E*)a.dx + r * a.lddx, c, n, z + v * EP);
-          if (!a.dh) continue;
+          if (has_dx) store_at<E, M>(px, (uint32_t)(apart * a.lddx * sizeof(E)), c, n, z + v * EP);
+          if (!has_dh) continue;
           if (drop) drop_apply<E>(a.drop, mask[v], z + v * EP);
-          store_row<E, M>((E*)a.dh + r * a.lddh, c, n, z + v * EP);
+          store_at<E, M>(ph, (uint32_t)(apart * a.lddh * sizeof(E)), c, n, z + v * EP);
         }
       tok += kTokStep;
     };
-    Row even, odd;
-    load(even, tok);
-    if constexpr (kAhead == 2) load(odd, tok + kTokStep);
-    for (int64_t trip = 0; trip < trips; ++trip) {
-      round(even);
-      if constexpr (kAhead == 2)
-        if (++trip < trips) round(odd);
+    if (whole > 0) {
+      Row ring[kAhead];
+#pragma unroll
+      for (int q = 0; q < kAhead; ++q) load(ring[q], first + std::min<int64_t>(q, whole - 1) * kTokStep, true);
+      for (int64_t left = whole; left > 0; left -= kAhead)
+#pragma unroll
+        for (int q = 0; q < kAhead; ++q)
+          if (q < left) round(ring[q], std::false_type{}, left - q, true);
+    }
+    for (int64_t k = 0; k < rest; ++k) {
+      const bool live = SOLO ? i < a.B : tok + rg < last;
+      Row x;
+      load(x, tok, live);
+      round(x, std::true_type{}, 0, live);
     }
     if (!grads) continue;
     if (!SOLO) {
@@ -137,7 +173,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
         }
       if constexpr (G > 1) {
         const int grp = TPR < 64 ? threadIdx.x >> 6 : rg;
-        __syncthreads();                                  // the item before has read its sums
+        __syncthreads();                                  // the sample before has read its sums
         if (grp > 0)
 #pragma unroll
           for (int k = 0; k < C; ++k) {
@@ -156,19 +192,19 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
       }
     }
     if (SOLO ? i >= a.B : rg > 0) continue;
-    float *pw = a.dw, *pb = a.db;
-    if (!SOLO && a.S > 1) {
-      pw = a.dw ? a.part + it * 2 * n : nullptr;
-      pb = a.db ? a.part + it * 2 * n + n : nullptr;
-    } else {
-      if (pw) pw += i * a.ldg;
-      if (pb) pb += i * a.ldg;
+    float* pw = a.dw ? a.dw + i * a.ldg : nullptr;
+    float* pb = a.db ? a.db + i * a.ldg : nullptr;
+    if (!SOLO && (first > 0 || last < a.T)) {             // part of a sample: slot blockIdx.x + i is nobody else's
+      float* part = a.part + (blockIdx.x + i) * 2 * n;
+      pw = a.dw ? part : nullptr;
+      pb = a.db ? part + n : nullptr;
     }
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (v * TPR + t) * EP;
-      if (pw) store_vec<EP>(pw, c, n, dw + v * EP);
-      if (pb) store_vec<EP>(pb, c, n, db + v * EP);
+      if (c >= n) continue;
+      if (pw) store_vec<EP>(pw, piece_col<E, M>(c, n), n, dw + v * EP);
+      if (pb) store_vec<EP>(pb, piece_col<E, M>(c, n), n, db + v * EP);
     }
   }
 }
@@ -216,67 +252,97 @@ __global__ __launch_bounds__(1024) void norm_back_rows_kernel(NormBackArgs a) {
       for (int j = 0; j < EP; ++j) z[j] = fmaf(rs, fmaf(-xh[j], mgx, g[j] - mg), z[j]);
       if (a.dx) store_row<E, M>((E*)a.dx + r * a.lddx, c, n, z);
       if (!a.dh) continue;
-      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, z);
+      if (a.drop.on) drop_piece<E>(a.drop, (uint32_t)r, c, n, z);
       store_row<E, M>((E*)a.dh + r * a.lddh, c, n, z);
     }
   }
 }
 
-// dw and db: one thread per piece of columns and token split.
+// dw and db: one thread per piece of columns and workgroup's share of the rounds (at_once rows each).
 template <class E, int M>
-__global__ __launch_bounds__(256) void norm_back_cols_kernel(NormBackArgs a, int64_t per, int64_t col_blocks,
-                                                             int64_t blocks) {
-  constexpr int EP = kPiece<E>;
-  const int64_t blk = flat_block();
-  if (blk >= blocks) return;
-  const int n = (int)a.n;
-  const int64_t it = blk / col_blocks, i = it / a.S;
-  const int64_t c64 = ((blk - it * col_blocks) * 256 + threadIdx.x) * EP;
-  if (c64 >= a.n) return;
-  const int c = (int)c64;
-  const int64_t first = (it - i * a.S) * per, last = std::min<int64_t>(a.T, first + per);
-  float dw[EP], db[EP], g[EP], xh[EP];
+__global__ __launch_bounds__(64) void norm_back_cols_kernel(NormBackArgs a, int at_once, int64_t col_blocks) {
+  constexpr int EP = kPiece<E>, kRows = 4;
+  const BackSplit& sp = a.split;
+  const int64_t blk = flat_block() / col_blocks, c64 = ((flat_block() - blk * col_blocks) * 64 + threadIdx.x) * EP;
+  if (blk >= sp.blocks || c64 >= a.n) return;
+  const int c = (int)c64, n = (int)a.n;
+  const int64_t q0 = sp.begin(blk), q1 = sp.begin(blk + 1);
+  for (int64_t i = q0 / sp.rounds; i * sp.rounds < q1; ++i) {
+    const int64_t first = std::max<int64_t>(q0 - i * sp.rounds, 0) * at_once;
+    const int64_t last = std::min<int64_t>((q1 - i * sp.rounds) * at_once, a.T);
+    float dw[EP], db[EP], g[EP], xh[EP];
 #pragma unroll
-  for (int j = 0; j < EP; ++j) dw[j] = db[j] = 0.f;
-  for (int64_t tok = first; tok < last; ++tok) {
-    const int64_t r = i * a.T + tok;
-    const float mu = a.rms ? 0.f : a.mean[r], rs = a.rstd[r];
-    unpack_row<E, M>(load_row<E, M>((const E*)a.dy + r * a.lddy, c, n), c, n, g);
-    unpack_row<E, M>(load_row<E, M>((const E*)a.s + r * a.lds, c, n), c, n, xh);
+    for (int j = 0; j < EP; ++j) dw[j] = db[j] = 0.f;
+    for (int64_t t0 = first; t0 < last; t0 += kRows) {
+      uint4 dy[kRows], s[kRows];
+      float mu[kRows], rs[kRows];
 #pragma unroll
-    for (int j = 0; j < EP; ++j) {
-      dw[j] = fmaf(g[j], (xh[j] - mu) * rs, dw[j]);
-      db[j] += g[j];
+      for (int k = 0; k < kRows; ++k) {
+        const int64_t r = i * a.T + std::min<int64_t>(t0 + k, last - 1);
+        dy[k] = load_row<E, M>((const E*)a.dy + r * a.lddy, c, n);
+        s[k] = load_row<E, M>((const E*)a.s + r * a.lds, c, n);
+        mu[k] = a.rms ? 0.f : a.mean[r];
+        rs[k] = a.rstd[r];
+      }
+#pragma unroll
+      for (int k = 0; k < kRows; ++k) {
+        if (t0 + k >= last) continue;
+        unpack_row<E, M>(dy[k], c, n, g);
+        unpack_row<E, M>(s[k], c, n, xh);
+#pragma unroll
+        for (int j = 0; j < EP; ++j) {
+          dw[j] = fmaf(g[j], (xh[j] - mu[k]) * rs[k], dw[j]);
+          db[j] += g[j];
+        }
+      }
     }
+    float* pw = a.dw ? a.dw + i * a.ldg : nullptr;
+    float* pb = a.db ? a.db + i * a.ldg : nullptr;
+    if (first > 0 || last < a.T) {
+      float* part = a.part + (blk + i) * 2 * n;
+      pw = a.dw ? part : nullptr;
+      pb = a.db ? part + n : nullptr;
+    }
+    if (pw) store_vec<EP>(pw, c, n, dw);
+    if (pb) store_vec<EP>(pb, c, n, db);
   }
-  float* pw = a.S > 1 ? a.part + it * 2 * n : a.dw + i * a.ldg;
-  float* pb = a.S > 1 ? a.part + it * 2 * n + n : a.db + i * a.ldg;
-  if (a.dw) store_vec<EP>(pw, c, n, dw);
-  if (a.db) store_vec<EP>(pb, c, n, db);
 }
 
-// ---- token splits -----------------------------------------------------------------------------
+// ---- sums of parts ----------------------------------------------------------------------------------
 
-// Sums of a sample's token splits, 64 columns a workgroup: 16 groups of lanes take every 16th
-// split, then each column's 16 sums are added in order.
+// dw and db of the samples whose rounds several workgroups had, 64 columns a workgroup: 16 groups of 16 lanes
+// (four columns each) take every 16th part, all loads of four rounds first; then each column's
+// 16 sums are added in order.
 __global__ __launch_bounds__(256) void norm_back_sums_kernel(NormBackArgs a, int64_t col_blocks, int64_t blocks) {
   __shared__ float sums[2][16][64];
   const int64_t blk = flat_block();
   if (blk >= blocks) return;
-  const int64_t i = blk / col_blocks;
+  const int64_t i = blk / col_blocks, b0 = a.split.block_of(i * a.split.rounds);
+  const int S = (int)(a.split.block_of((i + 1) * a.split.rounds - 1) - b0) + 1;
+  if (S == 1) return;                                     // written whole
   const int n = (int)a.n, c0 = (int)(blk - i * col_blocks) * 64, q = (threadIdx.x & 15) * 4, grp = threadIdx.x >> 4;
+  const int col = min(c0 + q, max(n - 4, 0)), skip = c0 + q - col;       // the last piece: `skip` columns to the left
+  const float* part = a.part + (b0 + i) * 2 * n + col;
 #pragma unroll
   for (int k = 0; k < 2; ++k) {
     if (!(k ? a.db : a.dw)) continue;
-    float t[4] = {0.f, 0.f, 0.f, 0.f}, u[4];
-#pragma unroll 4
-    for (int sp = grp; sp < a.S; sp += 16) {
-      load_vec<4>(a.part + ((i * a.S + sp) * 2 + k) * n, 0, c0 + q, n, 0.f, u);
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n < 4) {
+      for (int sp = grp; sp < S; sp += 16)
+        for (int m = 0; m < n; ++m) t[m] += part[((int64_t)sp * 2 + k) * n + m];
+    } else for (int sp = grp; sp < S; sp += 64) {
+      float u[4][4];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] += u[j];
+      for (int j = 0; j < 4; ++j) unpack<float>(load_piece(part + ((int64_t)min(sp + 16 * j, S - 1) * 2 + k) * n), u[j]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (sp + 16 * j < S)
+#pragma unroll
+          for (int m = 0; m < 4; ++m) t[m] += u[j][m];
     }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) sums[k][grp][q + j] = t[j];
+    for (int m = 0; m < 4; ++m)
+      if (m >= skip) sums[k][grp][q + m - skip] = t[m];
   }
   __syncthreads();
   const int k = threadIdx.x >> 6, c = c0 + (threadIdx.x & 63);
@@ -288,103 +354,93 @@ __global__ __launch_bounds__(256) void norm_back_sums_kernel(NormBackArgs a, int
   out[i * a.ldg + c] = t;
 }
 
-hipError_t launch_norm_back_sums(const NormBackArgs& a, hipStream_t st) {
-  const int64_t cb = ceil_div(a.n, 64), blocks = a.B * cb;
-  DPRC_LAUNCH(norm_back_sums_kernel, flat_grid(blocks), dim3(256), 0, st, a, cb, blocks);
-  return hipGetLastError();
-}
-
 // ---- launch -------------------------------------------------------------------------------------
 
 constexpr int64_t kNormBackLong = 8192;
 
-// How a width is dealt out: TPR threads of C columns.  Small and few workgroups do best where every
-// thread has two rows on their way (8 x 4096 x 2048 bf16 with ds, dropout and dh: 131 us with 256
-// workgroups of <128, 16>, 140 with 512, 137 with 512 of <256, 8>, 187 with 256 of <256, 8> and one
-// row ahead); up to 1024 columns <., 8> with 512 (n = 512: 37 us against 40 with 16 columns).
-struct BackLayout {
-  int tpr, cols;
-};
-static BackLayout back_layout(int64_t n, bool bf16) {
-  if (n > 4096) return {512, 16};
-  if (n > 2048) return {512, 8};
-  if (n > 1024) return bf16 ? BackLayout{128, 16} : BackLayout{256, 8};
-  int tpr = 8;
-  while (8 * tpr < n) tpr *= 2;
-  return {tpr, 8};
-}
-// rows that a workgroup works on at a time
-static int64_t rows_at_once(int64_t n, bool bf16) {
-  return n > kNormBackLong ? 1 : std::max(1, 256 / back_layout(n, bf16).tpr);
-}
-
-// Token splits of a sample: at least four rounds of rows each, and so many that the workgroups
-// number 256, or 512 where that is better (bf16 rows of up to 1024 columns; fewer than 16 rounds a
-// workgroup, where their latency is what counts: 16 x 333 x 1111 took 25 us with 448, 33 with 256).
-int norm_back_splits(int64_t B, int64_t T, int64_t n, bool bf16) {
-  const int64_t at_once = rows_at_once(n, bf16), rounds = ceil_div(T, at_once);
-  const int64_t blocks = (bf16 && n <= 1024) || B * rounds < 16 * 256 ? 512 : 256;
-  const int64_t S = std::max<int64_t>(1, std::min<int64_t>(ceil_div(blocks, B), rounds / 4));
-  return (int)ceil_div(rounds, ceil_div(rounds, S));
+NormBackPlan norm_back_plan(int64_t B, int64_t T, int64_t n, int64_t elem_bytes, int tensors) {
+  const bool wide = n > kNormBackLong;
+  NormBackPlan p{};
+  p.tpr = threads_per_row(n);
+  p.at_once = wide ? 1 : std::max(1, 256 / p.tpr);
+  p.solo = T < p.at_once && B > 512;
+  BackSplit& sp = p.split;
+  sp.rounds = ceil_div(T, (int64_t)p.at_once);
+  sp.total = B * sp.rounds;
+  // few rounds a sample, or many samples: none is cut (a cut costs a launch to join its parts, 3.5 us)
+  sp.samples = sp.rounds <= 8 || B >= 1024 ? B : 0;
+  if (p.solo) sp.blocks = std::min<int64_t>(ceil_div(B, (int64_t)p.at_once), 1024);
+  else if (sp.samples) sp.blocks = std::min<int64_t>(B, 1024);
+  else sp.blocks = std::min<int64_t>(streaming_blocks(2 * tensors * p.at_once * n * elem_bytes), std::max<int64_t>(B, sp.total / 4));
+  p.parts = sp.samples ? 0 : sp.blocks + B;
+  return p;
 }
 
 template <class E, int M>
-static void launch_norm_back_of(const NormBackArgs& a, hipStream_t st) {
-  const int64_t n = a.n, at_once = rows_at_once(n, a.bf16);
-  const int64_t per = ceil_div(ceil_div(a.T, at_once), (int64_t)a.S) * at_once;
-  if (n > kNormBackLong) {
-    if (a.dw || a.db) {
-      const int64_t cb = ceil_div(n, 256 * kPiece<E>), blocks = a.B * a.S * cb;
-      DPRC_LAUNCH((norm_back_cols_kernel<E, M>), flat_grid(blocks), dim3(256), 0, st, a, per, cb, blocks);
-    }
-    if (a.dx || a.dh) {
-      const int64_t blocks = std::min<int64_t>(a.B * a.T, 512);
-      DPRC_LAUNCH((norm_back_rows_kernel<E, M>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
-    }
-    return;
+static void launch_norm_back_long(const NormBackArgs& a, const NormBackPlan& p, hipStream_t st) {
+  if (a.dw || a.db) {
+    const int64_t cb = ceil_div(a.n, 64 * kPiece<E>);
+    DPRC_LAUNCH((norm_back_cols_kernel<E, M>), flat_grid(a.split.blocks * cb), dim3(64), 0, st, a, p.at_once, cb);
   }
-  // Many samples of fewer rows than a workgroup takes at a time: a sample for each row group.
-  const bool solo = a.T < at_once && a.B > 512;
-  const int64_t items = solo ? ceil_div(a.B, at_once) : a.B * a.S;
-  const int64_t blocks = std::min<int64_t>(items, 1024);
-  auto go = [&](auto kernel, int block) { DPRC_LAUNCH(kernel, dim3((unsigned)blocks), dim3(block), 0, st, a, per, items); };
+  if (a.dx || a.dh) {
+    const int64_t blocks = std::min<int64_t>(a.B * a.T, 512);
+    DPRC_LAUNCH((norm_back_rows_kernel<E, M>), dim3((unsigned)blocks), dim3(1024), 0, st, a);
+  }
+}
+
+template <class E, int M>
+static void launch_norm_back_of(const NormBackArgs& a, const NormBackPlan& p, hipStream_t st) {
+  auto go = [&](auto kernel, int block) { DPRC_LAUNCH(kernel, dim3((unsigned)p.split.blocks), dim3(block), 0, st, a); };
   auto pick = [&](auto tpr, auto cols) {
-    constexpr int TPR = decltype(tpr)::value, C = decltype(cols)::value;
+    constexpr int TPR = decltype(tpr)::value, C = decltype(cols)::value, BLK = TPR > 256 ? TPR : 256;
     if constexpr (TPR < 256) {
-      if (solo) return go(norm_back_kernel<E, M, TPR, C, true>, 256);
+      if (p.solo) return go(norm_back_kernel<E, M, TPR, C, true, kAny>, BLK);
     }
-    go(norm_back_kernel<E, M, TPR, C, false>, TPR > 256 ? TPR : 256);
+    if constexpr (M != kTiny) {
+      if (a.dx && a.ds && a.dh) return go(norm_back_kernel<E, M, TPR, C, false, kDs | kDh>, BLK);
+      if (a.dx && a.ds) return go(norm_back_kernel<E, M, TPR, C, false, kDs>, BLK);
+      if (a.dx && a.dh) return go(norm_back_kernel<E, M, TPR, C, false, kDh>, BLK);
+      if (a.dx) return go(norm_back_kernel<E, M, TPR, C, false, 0>, BLK);
+    }
+    go(norm_back_kernel<E, M, TPR, C, false, kAny>, BLK);
   };
   using std::integral_constant;
   const integral_constant<int, 8> c8;
-  const integral_constant<int, 16> c16;
-  const BackLayout lay = back_layout(n, a.bf16);
-  if (lay.tpr == 8) return pick(integral_constant<int, 8>(), c8);
+  if (p.tpr == 8) return pick(integral_constant<int, 8>(), c8);
   if constexpr (M != kTiny) {
-    if (lay.tpr == 16) return pick(integral_constant<int, 16>(), c8);
-    if (lay.tpr == 32) return pick(integral_constant<int, 32>(), c8);
-    if (lay.tpr == 64) return pick(integral_constant<int, 64>(), c8);
-    if (lay.tpr == 128 && lay.cols == 8) return pick(integral_constant<int, 128>(), c8);
-    if constexpr (sizeof(E) == 2) {
-      if (lay.tpr == 128) return pick(integral_constant<int, 128>(), c16);
-    } else {
-      if (lay.tpr == 256) return pick(integral_constant<int, 256>(), c8);
-    }
-    if (lay.cols == 8) return pick(integral_constant<int, 512>(), c8);
-    pick(integral_constant<int, 512>(), c16);
+    if (p.tpr == 16) return pick(integral_constant<int, 16>(), c8);
+    if (p.tpr == 32) return pick(integral_constant<int, 32>(), c8);
+    if (p.tpr == 64) return pick(integral_constant<int, 64>(), c8);
+    if (p.tpr == 128) return pick(integral_constant<int, 128>(), c8);
+    if (p.tpr == 256) return pick(integral_constant<int, 256>(), c8);
+    if (a.n <= 4096) return pick(integral_constant<int, 512>(), c8);
+    pick(integral_constant<int, 512>(), integral_constant<int, 16>());
   }
 }
 
 template <class E>
-static void launch_norm_back_width(const NormBackArgs& a, hipStream_t st) {
-  if (a.n < kPiece<E>) launch_norm_back_of<E, kTiny>(a, st);
-  else if (a.n % kPiece<E> == 0) launch_norm_back_of<E, kWhole>(a, st);
-  else launch_norm_back_of<E, kTail>(a, st);
+static void launch_norm_back_width(const NormBackArgs& a, const NormBackPlan& p, hipStream_t st) {
+  constexpr int EP = kPiece<E>;
+  // also rows so far apart that those of a workgroup's round leave 32-bit offsets go the long rows' way
+  const int64_t apart = p.at_once * (p.solo ? a.T : 1) * (int64_t)sizeof(E);
+  if (a.n > kNormBackLong || apart * std::max({a.lddy, a.lds, a.ldds, a.lddx, a.lddh}) >= ((int64_t)1 << 31)) {
+    if (a.n < EP) launch_norm_back_long<E, kTiny>(a, p, st);
+    else if (a.n % EP == 0) launch_norm_back_long<E, kWhole>(a, p, st);
+    else launch_norm_back_long<E, kTail>(a, p, st);
+  } else if (a.n < EP) {
+    launch_norm_back_of<E, kTiny>(a, p, st);
+  } else {
+    launch_norm_back_of<E, kWide>(a, p, st);
+  }
 }
 
-hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t st) {
-  if (a.bf16) launch_norm_back_width<uint16_t>(a, st);
-  else launch_norm_back_width<float>(a, st);
+hipError_t launch_norm_back(const NormBackArgs& a, const NormBackPlan& p, hipStream_t st) {
+  if (a.bf16) launch_norm_back_width<uint16_t>(a, p, st);
+  else launch_norm_back_width<float>(a, p, st);
+  if (p.parts > 0 && (a.dw || a.db)) {
+    const int64_t cb = ceil_div(a.n, 64), blocks = a.B * cb;
+    DPRC_LAUNCH(norm_back_sums_kernel, flat_grid(blocks), dim3(256), 0, st, a, cb, blocks);
+  }
   return hipGetLastError();
 }
 

@@ -398,6 +398,26 @@ struct NormArgs {
 };
 hipError_t launch_norm(const NormArgs& a, hipStream_t st);
 
+// How the backward pass deals the rounds of B samples (`rounds` each, `total` in all) to workgroups: laid end
+// to end and cut into `blocks` even ranges, or with `samples` > 0 whole samples to each.
+struct BackSplit {
+  int64_t rounds, total, samples, blocks;
+  __host__ __device__ int64_t begin(int64_t blk) const {
+    return samples ? blk * samples / blocks * rounds : blk * total / blocks;
+  }
+  __host__ __device__ int64_t block_of(int64_t round) const {
+    return samples ? ((round / rounds + 1) * blocks - 1) / samples : ((round + 1) * blocks - 1) / total;
+  }
+};
+struct NormBackPlan {
+  int32_t tpr, at_once;    // threads per row, rows of a round
+  int32_t solo;            // samples shorter than a round: one for each row group
+  int64_t parts;           // partial sums [parts][2][n] (0: no sample is cut)
+  BackSplit split;
+};
+// tensors: 3 with ds, 2 without (at least as many parts)
+NormBackPlan norm_back_plan(int64_t B, int64_t T, int64_t n, int64_t elem_bytes, int tensors);
+
 struct NormBackArgs {
   const void* dy;
   const void* s;
@@ -414,13 +434,11 @@ struct NormBackArgs {
   int64_t B, T, n;
   float inv_n;
   int32_t bf16, wbf16, rms;
-  int32_t S;               // token splits of a sample (of ceil(T / S) rows each)
-  float* part;             // [B][S][2][n] (S > 1)
+  BackSplit split;
+  float* part;             // [parts][2][n]
   DropArgs drop;
 };
-int norm_back_splits(int64_t B, int64_t T, int64_t n, bool bf16);
-hipError_t launch_norm_back(const NormBackArgs& a, hipStream_t st);
-hipError_t launch_norm_back_sums(const NormBackArgs& a, hipStream_t st);   // S > 1: dw and db from part
+hipError_t launch_norm_back(const NormBackArgs& a, const NormBackPlan& p, hipStream_t st);
 
 // Per-sample vectors G [B][ldg] (see dprc_norm_vectors).
 struct VectorArgs {

@@ -1,15 +1,22 @@
 // Token rows in 16-byte pieces: loads, stores, dropout masks and sums over a row's threads.
 //
-// A row of n elements is dealt to TPR threads in pieces of 16 bytes (EP = 8 bf16 or 4 fp32
-// columns): thread t holds the pieces t, TPR + t, 2 TPR + t, ..., so a wave's loads are
-// consecutive.  Rows may start at any alignment of their element (gfx950 takes 16-byte accesses at
-// any address).  The width's kind M:
+// A piece is EP = 8 bf16 or 4 fp32 columns.  Rows may start at any alignment of their element
+// (gfx950 takes 16-byte accesses at any address).
+//
+// Kernels that hold a whole row deal it to TPR threads: thread t has the pieces t, TPR + t, 2 TPR +
+// t, ..., so a wave's loads are consecutive.  A piece that would reach past the row's end lies
+// further left instead, on the row's last EP columns (piece_col), in part or wholly on columns of
+// other threads.  There it holds what they hold and stores the same bits that they store; only
+// sums over the row leave these columns out (owns).  So the loads and stores of a loop need no
+// conditions.  (Every thread has its pieces of a row before any stores to it, also in place.)
+// Rows of fewer than EP columns (kTiny) take element loads and stores, in instances of their own:
+// beside the others these loads made every load of a loop wait for the one before.
+//
+// Kernels that come back to a row, or go through it piece by piece, keep to a piece's own columns:
 //   kWhole  n is a multiple of EP;
-//   kTail   it is not, and the row's last piece is part of one: its thread loads the row's last EP
-//           elements instead (they lie within the row), shifts them down when it comes to use
-//           them, and stores 8, 4 and 2 bytes;
-//   kTiny   n < EP: element loads.  (A kind of its own: beside the others these loads made
-//           every load of a loop wait for the one before.)
+//   kTail   the row's last piece is part of one: its thread loads the row's last EP elements,
+//           shifts them down, and stores 8, 4 and 2 bytes;
+//   kTiny   as above.
 #pragma once
 #include <type_traits>
 #include "device.hpp"
@@ -17,7 +24,26 @@
 
 namespace dprc {
 
-enum : int { kWhole = 0, kTail = 1, kTiny = 2 };
+// Threads of a row held whole: a power of two with 8 columns each (16 past 4096 columns).
+inline int threads_per_row(int64_t n) {
+  int tpr = 8;
+  while (tpr < 512 && 8 * tpr < n) tpr *= 2;
+  return tpr;
+}
+
+// Workgroups of a kernel that streams rows: one, two, three or four per CU, so that about 32 KB of loads are
+// under way on each.  `ahead` bytes are those of a workgroup's rows in flight (the threads' columns within
+// n only).  Fewer leave the memory waiting, more are slower again, as they reach over more
+// pages at a time.  32768 x 2048 bf16 forwards with residual and dropout (16 KB a workgroup): 129, 97,
+// 104, 106, 108 us with 1, 2, 3, 4, 8 per CU; without (8 KB): 92, 61, 51, 53, 56; backwards (24 KB): 135,
+// 137, 144, 145, 139; 59 x 2402 x 130 fp32 backwards (25 KB): 82, 81, 82, 80; 8 x 4096 x 1111 bf16
+// backwards (13 KB): 133, 97, 93, 96.
+inline int64_t streaming_blocks(int64_t ahead) {
+  const int64_t per_cu = (32768 + ahead / 2) / ahead;
+  return 256 * (per_cu < 1 ? 1 : per_cu > 4 ? 4 : per_cu);
+}
+
+enum : int { kWide = 0, kTiny = 1, kWhole = 2, kTail = 3 };
 
 template <class E>
 constexpr int kPiece = 16 / (int)sizeof(E);
@@ -40,9 +66,7 @@ __device__ __forceinline__ void store_piece(E* p, const uint4& v) {
   *reinterpret_cast<piece_t<E>*>(p) = piece_t<E>{v.x, v.y, v.z, v.w};
 }
 
-// The piece of `row` at column c, for unpack_row at the same column.  Past the row's end it is the
-// last piece again: the loads of a loop have no conditions, whose merges (a value or zero) would
-// make the compiler wait for a load where it is issued.
+// The piece of `row` at column c < n, for unpack_row at the same column.
 template <class E, int M>
 __device__ __forceinline__ uint4 load_row(const E* row, int c, int n) {
   constexpr int EP = kPiece<E>;
@@ -76,14 +100,17 @@ __device__ __forceinline__ void unpack(const uint4& v, float* x) {
 }
 
 // The columns c .. c + EP - 1 (c < n) of what load_row returned, zeros past the row's end.  (The
-// shift is made here and not at the load, which it would have to wait for.)
+// shift is made here and not at the load, which would have to be waited for.)
 template <class E, int M>
 __device__ __forceinline__ void unpack_row(uint4 v, int c, int n, float* x) {
   constexpr int EP = kPiece<E>;
-  const int over = c + EP - n;
-  if (M == kTail && over > 0) {
-    if constexpr (EP == 8) v = shr_elems(v, over);
-    else {
+  if (M == kTail && c + EP > n) {
+    const int over = EP - n % EP;                       // the same for every row: scalar branches
+    if constexpr (EP == 8) {
+      if (over & 4) v = uint4{v.z, v.w, 0u, 0u};
+      if (over & 2) v = uint4{v.y, v.z, v.w, 0u};
+      if (over & 1) v = shr_elems(v, 1);
+    } else {
       if (over & 2) v = uint4{v.z, v.w, 0u, 0u};
       if (over & 1) v = uint4{v.y, v.z, v.w, 0u};
     }
@@ -121,7 +148,7 @@ __device__ __forceinline__ void store_row(E* row, int c, int n, const float* x) 
     return;
   }
   // n - c < EP elements, as 8, 4 and 2 bytes
-  const int m = n - c;
+  const int m = n % EP;
   E* p = row + c;
   uint2 d{v.x, v.y};
   if (m * (int)sizeof(E) & 8) {
@@ -136,6 +163,33 @@ __device__ __forceinline__ void store_row(E* row, int c, int n, const float* x) 
   }
   if constexpr (sizeof(E) == 2)
     if (m & 1) *p = (uint16_t)d.x;
+}
+
+// ---- pieces of rows held whole: kWide or kTiny ------------------------------------------------
+
+// where the piece of column c lies, and whether its j-th column is its own
+template <class E, int M>
+__device__ __forceinline__ int piece_col(int c, int n) { return M == kTiny ? c : min(c, n - kPiece<E>); }
+template <int M>
+__device__ __forceinline__ bool owns(int c, int cc, int j, int n) { return M == kTiny ? c + j < n : cc + j >= c; }
+
+// The piece of column c of the row `off` bytes after a base that the whole workgroup shares (the base
+// stays in scalar registers, the offset in one vector register for a whole loop).
+template <class E, int M>
+__device__ __forceinline__ uint4 load_at(const void* base, uint32_t off, int c, int n) {
+  const char* p = static_cast<const char*>(base);
+  if constexpr (M == kTiny) return load_row<E, kTiny>(reinterpret_cast<const E*>(p + off), c, n);
+  else return load_piece(reinterpret_cast<const E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))));
+}
+
+template <class E, int M>
+__device__ __forceinline__ void store_at(void* base, uint32_t off, int c, int n, const float* x) {
+  char* p = static_cast<char*>(base);
+  if constexpr (M == kTiny) {
+    if (c < n) store_row<E, kTiny>(reinterpret_cast<E*>(p + off), c, n, x);
+  } else {
+    store_piece(reinterpret_cast<E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))), pack<E>(x));
+  }
 }
 
 // Entries c .. c + N - 1 of a weight or bias (fp32 or bf16), `none` without one and past its end.
@@ -184,13 +238,26 @@ __device__ __forceinline__ u32x4 philox_mask(u32x4 c, uint32_t k0, uint32_t k1) 
   return c;
 }
 
-// The mask words of a piece (columns c .. c + EP - 1 of row r): 8 columns share a Philox block, two
-// fp32 pieces half of it each.
+// The mask words of the piece at column c of row r: 8 columns share a Philox block, two fp32 pieces half of
+// it each.  A piece that was moved left (c no multiple of EP; all of a row's at the same place, n - EP)
+// takes its words from two blocks.
 template <class E>
-__device__ __forceinline__ u32x4 drop_words(const DropArgs& d, uint32_t r, int c) {
-  const u32x4 w = philox_mask(u32x4{(uint32_t)c >> 3, r, d.site, kStreamDropout}, d.key0, d.key1);
-  if constexpr (sizeof(E) == 2) return w;
-  else return (c & 4) ? u32x4{w.z, w.w, 0u, 0u} : u32x4{w.x, w.y, 0u, 0u};
+__device__ __forceinline__ u32x4 drop_words(const DropArgs& d, uint32_t r, int c, int n) {
+  constexpr int EP = kPiece<E>;
+  u32x4 w = philox_mask(u32x4{(uint32_t)c >> 3, r, d.site, kStreamDropout}, d.key0, d.key1);
+  if (c % EP == 0) {
+    if (EP == 4 && (c & 4)) w = u32x4{w.z, w.w, 0u, 0u};
+    return w;
+  }
+  u32x4 x = philox_mask(u32x4{((uint32_t)c >> 3) + 1u, r, d.site, kStreamDropout}, d.key0, d.key1);
+  const int s = (n - EP) & 7;
+  if (s & 4) w = u32x4{w.z, w.w, x.x, x.y}, x = u32x4{x.z, x.w, 0u, 0u};
+  if (s & 2) w = u32x4{w.y, w.z, w.w, x.x}, x.x = x.y;
+  if (s & 1) {
+    auto join = [](uint32_t lo, uint32_t hi) { return lo >> 16 | hi << 16; };
+    w = u32x4{join(w.x, w.y), join(w.y, w.z), join(w.z, w.w), join(w.w, x.x)};
+  }
+  return w;
 }
 
 // The piece through the site's dropout.  A dropped element is 0 whatever it was: it is replaced
@@ -204,8 +271,8 @@ __device__ __forceinline__ void drop_apply(const DropArgs& d, const u32x4& w, fl
 }
 
 template <class E>
-__device__ __forceinline__ void drop_piece(const DropArgs& d, uint32_t r, int c, float* x) {
-  drop_apply<E>(d, drop_words<E>(d, r, c), x);
+__device__ __forceinline__ void drop_piece(const DropArgs& d, uint32_t r, int c, int n, float* x) {
+  drop_apply<E>(d, drop_words<E>(d, r, c, n), x);
 }
 
 // ---- sums over groups of lanes ----------------------------------------------------------------

@@ -507,3 +507,45 @@ def test_graph_replays(D):
         got = [o.clone() for o in outs]
         for a, b in zip(got, step()):
             assert torch.equal(a, b), k
+
+
+# ---- many short samples, rows of every remainder in place ---------------------------------------------
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,n", [(700, 1, 5), (700, 5, 64), (1100, 3, 100), (520, 7, 300), (600, 2, 520), (1500, 1, 1024),
+                                   (1030, 4, 1100), (2100, 9, 66)])
+def test_many_short_samples(D, B, T, n, dtype):
+    # more samples than workgroups, and samples of fewer tokens than a workgroup takes at a time
+    dy, s, ds = rows(B, T, n, dtype, 1), rows(B, T, n, dtype, 2, shift=0.5), rows(B, T, n, dtype, 3)
+    check_backward(D, dy, s, vec(n, dtype, 4, shift=1.0), D.LAYERNORM, ds, 0.25)
+    check_backward(D, dy, s, None, D.RMSNORM, None, 0.0, bias_grad=False)
+
+
+@pytest.mark.parametrize("B,T", [(1, 1000), (3, 777), (37, 61), (255, 40), (300, 33)])
+@pytest.mark.parametrize("n", [40, 300])
+def test_samples_cut_at_any_token(D, B, T, n):
+    # the rows of all samples are dealt out evenly, so workgroups end and begin within samples
+    dy, s = rows(B, T, n, "f32", 1), rows(B, T, n, "f32", 2, shift=0.5)
+    check_backward(D, dy, s, vec(n, "f32", 4, shift=1.0), D.LAYERNORM, None, 0.0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n", [9, 67, 130, 257, 1111, 2047, 4099, 8190, 9001])
+def test_in_place_at_every_remainder(D, n, dtype):
+    # a row's last piece overlaps others' columns: in place it still sees the row as it was
+    B, T = 3, 45
+    x, z, w = rows(B, T, n, dtype, 1), rows(B, T, n, dtype, 2), vec(n, dtype, 3, shift=1.0)
+    y, s, mean, rstd = D.dprc_layernorm(x, w, res=z, p=0.1, seed=SEED, site_id=SITE)
+    a, b = x.clone(), z.clone()
+    D.dprc_layernorm(a, w, res=b, p=0.1, seed=SEED, site_id=SITE, y=a, s=b)
+    assert torch.equal(a, y) and torch.equal(b, s)
+    dy, ds = rows(B, T, n, dtype, 4), rows(B, T, n, dtype, 5)
+    call = lambda dy, s, ds, **kw: D.dprc_layernorm_backward(dy, s, w, mean, rstd, ds=ds, p=0.1, seed=SEED, site_id=SITE, **kw)
+    dx, dh, dw, db = call(dy, s, ds)
+    for which in (0, 1, 2):
+        ins = [dy.clone(), s.clone(), ds.clone()]
+        got = call(*ins, dx=ins[which], dh=ins[(which + 1) % 3])
+        for u, v in zip(got, (dx, dh, dw, db)):
+            assert torch.equal(u, v), which
+    a = x.clone()
+    assert torch.equal(D.dprc_dropout(a, 0.1, SEED, SITE, res=z, out=a), D.dprc_dropout(x, 0.1, SEED, SITE, res=z))
