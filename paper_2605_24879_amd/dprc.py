@@ -482,7 +482,8 @@ def _ptr(x):
 
 def _rows_like(x, ld):
     """New contiguous rows of x's shape (ld: x's row stride)."""
-    return torch.empty_like(x) if ld == x.size(2) else torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    B, T, n = x.shape
+    return torch.empty_like(x) if ld == n else x.new_empty((B, T, n))
 
 
 def dprc_dropout(x, p, seed, site_id, res=None, out=None):
@@ -551,10 +552,12 @@ def dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=LAYERNORM, ds=None, 
         lddh = _token_rows(dh, "dh", dy)
     elif p > 0.0:
         dh = _rows_like(dy, ldd)
-    given = [_sample_rows(g, name, B, n, index) for g, name in ((dw, "dw"), (db, "db")) if g is not None]
-    ldg = max(given, default=n) or n
-    if len(given) == 2 and given[0] != given[1]:
-        raise ValueError("dw and db must share a row stride")
+    ldg = n
+    if dw is not None or db is not None:
+        given = [_sample_rows(g, name, B, n, index) for g, name in ((dw, "dw"), (db, "db")) if g is not None]
+        if len(given) == 2 and given[0] != given[1]:
+            raise ValueError("dw and db must share a row stride")
+        ldg = given[0] or n
     if dw is None and weight_grad:
         dw = torch.empty_strided((B, n), (ldg, 1), dtype=torch.float32, device=dev)
     if db is None and bias_grad:
