@@ -1645,7 +1645,7 @@ dprc_status dprc_dropout(const void* x, int64_t ldx, const void* res, int64_t ld
   if (rows > (1LL << 31) || n > (1LL << 30) || !aligned(x, e) || !aligned(res, e) || !aligned(out, e))
     return DPRC_ERROR_NOT_SUPPORTED;
   a.x = x; a.res = res; a.out = out;
-  a.ldx = ldx; a.ldr = ldr; a.ldo = ldo;
+  a.ldx = ldx; a.ldr = res ? ldr : 0; a.ldo = ldo;
   a.rows = rows; a.n = n; a.bf16 = dtype == DPRC_BF16;
   return hip_status(traced(DPRC_KERNEL_DROPOUT, stream, [&] { return launch_dropout(a, stream); }));
 }
@@ -1665,7 +1665,7 @@ dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const v
   NormArgs a;
   drop_args(L->p, L->seed, L->site_id, a.drop);
   a.x = x; a.res = res; a.sum = sum; a.y = y;
-  a.ldx = ldx; a.ldr = ldr; a.lds = lds; a.ldy = ldy;
+  a.ldx = ldx; a.ldr = res ? ldr : 0; a.lds = sum ? lds : 0; a.ldy = ldy;
   a.w = L->weight; a.b = L->bias;
   a.rms = L->kind == DPRC_RMSNORM;
   a.mean = a.rms ? nullptr : mean; a.rstd = rstd;
@@ -1703,7 +1703,7 @@ dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t ld
   NormBackArgs a;
   drop_args(L->p, L->seed, L->site_id, a.drop);
   a.dy = dy; a.s = s; a.ds = ds; a.dx = dx; a.dh = dh;
-  a.lddy = lddy; a.lds = lds; a.ldds = ldds; a.lddx = lddx; a.lddh = lddh;
+  a.lddy = lddy; a.lds = lds; a.ldds = ds ? ldds : 0; a.lddx = dx ? lddx : 0; a.lddh = dh ? lddh : 0;
   a.w = L->weight; a.mean = mean; a.rstd = rstd;
   a.dw = dw; a.db = db; a.ldg = ldg;
   a.B = L->B; a.T = L->T; a.n = L->n;
