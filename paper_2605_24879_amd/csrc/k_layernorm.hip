@@ -202,6 +202,7 @@ static void launch_norm_of(const NormArgs& a, hipStream_t st) {
     if constexpr (M != kTiny) {
       if (a.res && a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kRes | kSum | kStats>);
       if (a.res && a.sum && none) return launch(norm_kernel<E, M, TPR, C, kRes | kSum>);
+      if (!a.res && a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kSum | kStats>);
       if (!a.res && !a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kStats>);
       if (!a.res && !a.sum && none) return launch(norm_kernel<E, M, TPR, C, 0>);
     }

@@ -105,7 +105,7 @@ class DPSGDRC:
         """Lay the norms' parameters side by side: vec_master [1, N] fp32, and for bf16 parameters vec_w [N],
         which the parameters become views of (fp32 ones become views of the master)."""
         params = [q for m in self.norms for q in m.parameters_in_order()]
-        self._G = None
+        self._G, self._sinks = None, []
         if not params:
             return
         if len({q.dtype for q in params}) != 1:
@@ -122,9 +122,10 @@ class DPSGDRC:
                 q.requires_grad_(True)
                 cols.append(slice(at, at + q.numel()))
                 at += q.numel()
-            m.sink = self._sink(m, cols)
+            self._sinks.append(self._sink(m, cols))
 
     def _sink(self, m, cols):
+        """What the backward call of norm m writes its per-sample gradients to, during a capture."""
         def rows(B):
             if self._G is None:
                 self._G = torch.empty(B, self.vec_master.shape[1], dtype=torch.float32, device=self.vec_master.device)
@@ -144,20 +145,23 @@ class DPSGDRC:
     def remove_hooks(self):
         for h in self._hooks:
             h.remove()
-        for m in self.norms:
-            m.sink = None
 
     def capture(self, loss_fn):
         """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs."""
-        for m in self.norms:
-            m.seed = step_seed(self.seed, self.steps)
         self._G = None
-        losses = loss_fn()
-        if losses.dim() != 1:
-            raise ValueError("loss_fn must return per-sample losses [B]")
-        # the norms' weights are listed for the backward pass to reach every norm; their own
-        # gradients go to the rows of self._G
-        E = torch.autograd.grad(losses.sum(), self._S + [m.weight for m in self.norms], allow_unused=bool(self.norms))
+        for m, sink in zip(self.norms, self._sinks):
+            m.seed, m.sink = step_seed(self.seed, self.steps), sink
+        try:
+            losses = loss_fn()
+            if losses.dim() != 1:
+                raise ValueError("loss_fn must return per-sample losses [B]")
+            # the norms' weights are listed for the backward pass to reach every norm; their own
+            # gradients go to the rows of self._G
+            E = torch.autograd.grad(losses.sum(), self._S + [m.weight for m in self.norms],
+                                    allow_unused=bool(self.norms))
+        finally:
+            for m in self.norms:
+                m.sink = None
         if self.norms:
             E = E[:len(self._S)]
             if any(e is None for e in E) or self._G is None or len(self._filled) < len(self.norms):

@@ -149,8 +149,13 @@ def test_captured_norm_gradients_are_each_samples_own(mods):
         li = llama.per_sample_loss(plain(tok[i:i + 1, :-1]), tok[i:i + 1, 1:])[0]
         ref = torch.cat(torch.autograd.grad(li, [m.weight for m in plain.norms()]))
         assert (drv._G[i] - ref).abs().max() <= 1e-4 * ref.abs().max(), i
-    drv.remove_hooks()
+    # outside a step the modules give ordinary gradients, as often as wanted
     assert all(m.sink is None for m in model.norms())
+    for _ in range(2):
+        gw = torch.autograd.grad(llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:]).sum(), [m.weight for m in model.norms()])
+        ref = drv._G.sum(0)
+        assert (torch.cat(gw) - ref).abs().max() <= 1e-5 * ref.abs().max()
+    drv.remove_hooks()
 
 
 def test_dropout_is_fresh_every_step_and_training_stays_finite(mods):
