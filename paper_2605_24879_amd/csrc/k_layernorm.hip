@@ -3,7 +3,7 @@
 // Bounded by memory: a row is read once and held in registers from the sum through its mean, its
 // variance about that mean (two sums one after the other: mean(s^2) - mu^2 would cancel) and the
 // output.  Everything is fp32; y and s are rounded once, y from the unrounded s.  8 x 4096 x 2048 bf16
-// with residual, dropout, statistics and bias takes 95 to 97 us, 5.6 TB/s (a copy reaches 5.4); one row of
+// with residual, dropout, statistics and bias takes 91 us, 5.9 TB/s (a copy reaches 5.4); one row of
 // 2048 takes 2.7 us, a launch's latency.
 #include <algorithm>
 #include "device.hpp"
@@ -20,7 +20,7 @@ enum : int { kRes = 1, kSum = 2, kStats = 4, kAny = 8 };
 // TPR threads hold a row of at most TPR * C columns, C each; a workgroup of max(256, TPR)
 // threads works on 256 / TPR rows at a time and walks the rows with the grid, the next rows'
 // pieces loading while this one is reduced.  Weight and bias stay in registers for all rows.
-template <class E, int M, int TPR, int C, int FL>
+template <class E, int M, int TPR, int C, int FL, bool NT = false>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a) {
   constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
   constexpr bool kHold = TPR < 1024;
@@ -45,8 +45,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
 #pragma unroll
     for (int v = 0; v < V; ++v) {
       const int c = (v * TPR + t) * EP;
-      q.x[v] = load_at<E, M>(px, live ? gx : 0u, c, n);
-      if (has_res) q.z[v] = load_at<E, M>(pr, live ? gr : 0u, c, n);
+      q.x[v] = load_at<E, M, NT>(px, live ? gx : 0u, c, n);
+      if (has_res) q.z[v] = load_at<E, M, NT>(pr, live ? gr : 0u, c, n);
     }
   };
   float w[C], b[C];
@@ -102,11 +102,11 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int c = (v * TPR + t) * EP;
-        if (has_sum) store_at<E, M>(ps, gs, c, n, s + v * EP);
+        if (has_sum) store_at<E, M, NT>(ps, gs, c, n, s + v * EP);
         if (!kHold) load_wb(v);
 #pragma unroll
         for (int j = 0; j < EP; ++j) u[j] = fmaf((s[v * EP + j] - mu) * rstd, w[v * EP + j], b[v * EP + j]);
-        store_at<E, M>(py, gy, c, n, u);
+        store_at<E, M, NT>(py, gy, c, n, u);
       }
     }
     r0 += step;
@@ -199,6 +199,18 @@ static void launch_norm_of(const NormArgs& a, hipStream_t st) {
     const int64_t blocks = std::min<int64_t>(ceil_div(a.rows, RPB), streaming_blocks(ahead));
     auto launch = [&](auto kernel) { DPRC_LAUNCH(kernel, dim3((unsigned)blocks), dim3(BLK), 0, st, a); };
     const bool stats = a.rstd && (a.rms || a.mean), none = !a.rstd && !a.mean;
+    if constexpr (M != kTiny && TPR >= 64) {                      // (narrower rows: not worth their instances)
+      StreamRows stream(n * (int64_t)sizeof(E));
+      stream.add(a.x, a.rows, a.ldx * sizeof(E));
+      stream.add(a.res, a.rows, a.ldr * sizeof(E));
+      stream.add(a.sum, a.rows, a.lds * sizeof(E));
+      stream.add(a.y, a.rows, a.ldy * sizeof(E));
+      if (stats && stream.yes()) {
+        if (a.res && a.sum) return launch(norm_kernel<E, M, TPR, C, kRes | kSum | kStats, true>);
+        if (!a.res && a.sum) return launch(norm_kernel<E, M, TPR, C, kSum | kStats, true>);
+        if (!a.res && !a.sum) return launch(norm_kernel<E, M, TPR, C, kStats, true>);
+      }
+    }
     if constexpr (M != kTiny) {
       if (a.res && a.sum && stats) return launch(norm_kernel<E, M, TPR, C, kRes | kSum | kStats>);
       if (a.res && a.sum && none) return launch(norm_kernel<E, M, TPR, C, kRes | kSum>);

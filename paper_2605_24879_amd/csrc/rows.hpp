@@ -43,6 +43,24 @@ inline int64_t streaming_blocks(int64_t ahead) {
   return 256 * (per_cu < 1 ? 1 : per_cu > 4 ? 4 : per_cu);
 }
 
+// Whether a call streams past the caches.  8 x 4096 x 2048 bf16: dropout (403 MB) 68 us with non-temporal
+// accesses, 74 without; the fused norm (537 MB) 91 and 96, and a product with y that follows takes no
+// longer.  4 x 4096 x 2048: the norm (268 MB) 45.5 and 44; 4 x 2048 x 2048 (134 MB): 26 and 23.6.  Not for
+// rows that share lines (97 fp32 columns backwards, 533 MB: 128 us and 109), and not for the backward pass,
+// whose five streams took 133 to 157 us with them and 133 to 140 without, by where the tensors lay.
+constexpr int64_t kStreamRowsBytes = (int64_t)300 << 20;
+struct StreamRows {
+  int64_t width, total = 0;      // bytes of a row's columns; of all tensors
+  bool lines;
+  explicit StreamRows(int64_t row_bytes) : width(row_bytes), lines(row_bytes % 128 == 0) {}
+  void add(const void* p, int64_t rows, int64_t ld_bytes) {
+    if (!p) return;
+    total += rows * width;
+    lines = lines && reinterpret_cast<uintptr_t>(p) % 128 == 0 && ld_bytes % 128 == 0;
+  }
+  bool yes() const { return lines && total >= kStreamRowsBytes; }
+};
+
 enum : int { kWide = 0, kTiny = 1, kWhole = 2, kTail = 3 };
 
 template <class E>
@@ -55,22 +73,28 @@ using piece_t = std::conditional_t<sizeof(E) == 2, piece2_t, piece4_t>;
 typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 
-template <class E>
+// NT: non-temporal accesses, for calls whose tensors together are far larger than the 256 MB Infinity
+// Cache and whose rows are whole 128-byte lines (StreamRows).
+template <class E, bool NT = false>
 __device__ __forceinline__ uint4 load_piece(const E* p) {
-  const piece_t<E> v = *reinterpret_cast<const piece_t<E>*>(p);
+  const piece_t<E>* q = reinterpret_cast<const piece_t<E>*>(p);
+  const piece_t<E> v = NT ? __builtin_nontemporal_load(q) : *q;
   return uint4{v[0], v[1], v[2], v[3]};
 }
 
-template <class E>
+template <class E, bool NT = false>
 __device__ __forceinline__ void store_piece(E* p, const uint4& v) {
-  *reinterpret_cast<piece_t<E>*>(p) = piece_t<E>{v.x, v.y, v.z, v.w};
+  const piece_t<E> d = {v.x, v.y, v.z, v.w};
+  piece_t<E>* q = reinterpret_cast<piece_t<E>*>(p);
+  if (NT) __builtin_nontemporal_store(d, q);
+  else *q = d;
 }
 
 // The piece of `row` at column c < n, for unpack_row at the same column.
-template <class E, int M>
+template <class E, int M, bool NT = false>
 __device__ __forceinline__ uint4 load_row(const E* row, int c, int n) {
   constexpr int EP = kPiece<E>;
-  if constexpr (M != kTiny) return load_piece(row + min(c, n - EP));
+  if constexpr (M != kTiny) return load_piece<E, NT>(row + min(c, n - EP));
   uint32_t h[EP];
 #pragma unroll
   for (int j = 0; j < EP; ++j) {
@@ -139,12 +163,12 @@ __device__ __forceinline__ void store_part(void* p, uint32_t v) { *reinterpret_c
 __device__ __forceinline__ void store_part(void* p, uint2 v) { *reinterpret_cast<u32x2_any2*>(p) = u32x2_any2{v.x, v.y}; }
 
 // Piece at column c < n of an output row.
-template <class E, int M>
+template <class E, int M, bool NT = false>
 __device__ __forceinline__ void store_row(E* row, int c, int n, const float* x) {
   constexpr int EP = kPiece<E>;
   const uint4 v = pack<E>(x);
   if (M == kWhole || c + EP <= n) {
-    store_piece(row + c, v);
+    store_piece<E, NT>(row + c, v);
     return;
   }
   // n - c < EP elements, as 8, 4 and 2 bytes
@@ -175,20 +199,20 @@ __device__ __forceinline__ bool owns(int c, int cc, int j, int n) { return M == 
 
 // The piece of column c of the row `off` bytes after a base that the whole workgroup shares (the base
 // stays in scalar registers, the offset in one vector register for a whole loop).
-template <class E, int M>
+template <class E, int M, bool NT = false>
 __device__ __forceinline__ uint4 load_at(const void* base, uint32_t off, int c, int n) {
   const char* p = static_cast<const char*>(base);
   if constexpr (M == kTiny) return load_row<E, kTiny>(reinterpret_cast<const E*>(p + off), c, n);
-  else return load_piece(reinterpret_cast<const E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))));
+  else return load_piece<E, NT>(reinterpret_cast<const E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))));
 }
 
-template <class E, int M>
+template <class E, int M, bool NT = false>
 __device__ __forceinline__ void store_at(void* base, uint32_t off, int c, int n, const float* x) {
   char* p = static_cast<char*>(base);
   if constexpr (M == kTiny) {
     if (c < n) store_row<E, kTiny>(reinterpret_cast<E*>(p + off), c, n, x);
   } else {
-    store_piece(reinterpret_cast<E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))), pack<E>(x));
+    store_piece<E, NT>(reinterpret_cast<E*>(p + (off + (uint32_t)piece_col<E, M>(c, n) * (uint32_t)sizeof(E))), pack<E>(x));
   }
 }
 

@@ -118,3 +118,33 @@ def test_every_launch_is_recorded(D, name):
     make, kinds = CALLS[name]
     got, ms = _trace(D, make(D))
     assert got == kinds and all(t > 0 for t in ms)
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 512), ("bf16", 1024), ("bf16", 2048), ("bf16", 4096), ("bf16", 8192), ("f32", 512),
+                                     ("f32", 1024), ("f32", 2048), ("f32", 4096), ("f32", 8192), ("bf16", 16384)])
+def test_calls_that_stream_past_the_caches_give_the_same_bits(D, dtype, n):
+    # tensors of 320 MiB together take non-temporal accesses; rows of the same call in pieces do not
+    dt = {"bf16": torch.bfloat16, "f32": torch.float32}[dtype]
+    R = (320 << 20) // (2 * n * (2 if dtype == "bf16" else 4)) + 3
+    g = torch.Generator(device="cuda").manual_seed(n)
+    x, z = (torch.randn(1, R, n, generator=g, device="cuda").to(dt) for _ in range(2))
+    w = (1 + 0.1 * torch.randn(n, generator=g, device="cuda")).to(dt)
+    cut = [(0, 100), (R // 2, R // 2 + 57), (R - 33, R)]
+    for kw in (dict(res=z, p=0.0), dict(p=0.0), dict(res=z, p=0.1, seed=SEED, site_id=SITE), dict(p=0.1, seed=SEED, site_id=SITE)):
+        y, s, mean, rstd = D.dprc_layernorm(x, w, **kw)
+        for a, b in cut:
+            # the mask goes by the row: the piece starts at row 0, so it is compared where there is none
+            if kw["p"] == 0.0:
+                part = dict(kw, res=z[:, a:b]) if "res" in kw else kw
+                for u, v in zip((y[:, a:b], s[:, a:b], mean[a:b], rstd[a:b]), D.dprc_layernorm(x[:, a:b], w, **part)):
+                    assert torch.equal(u, v)
+        if kw["p"] > 0.0:
+            for u, v in zip((y[:, :100], s[:, :100]), D.dprc_layernorm(x[:, :100], w, **dict(kw, **({"res": z[:, :100]} if "res" in kw else {})))):
+                assert torch.equal(u, v)
+            f = torch.from_numpy(J.dropout_factors(SEED, SITE, 33, n, 0.1, row0=R - 33)).cuda()
+            tail = f.float() * x[0, R - 33:].float() + (z[0, R - 33:].float() if "res" in kw else 0.0)
+            assert torch.allclose(s[0, R - 33:].float(), tail, rtol=2.0 ** -8, atol=1e-6)
+    for res in (z, None):
+        out = D.dprc_dropout(x, 0.1, SEED, SITE, res=res)
+        assert torch.equal(out[:, :100], D.dprc_dropout(x[:, :100], 0.1, SEED, SITE, res=None if res is None else res[:, :100]))
+        assert torch.equal(out, D.dprc_layernorm(x, w, res=res, p=0.1, seed=SEED, site_id=SITE)[1])
