@@ -25,6 +25,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
   constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
   constexpr bool kHold = TPR < 1024;
   constexpr int kAhead = C == 8 ? 2 : 1;                          // rows loading ahead
+  // fp32 rows of 1024 threads: 128 registers are too few for a row ahead (2048 x 16384 with residual and
+  // sum 103 us without, 113 with it and spilled registers; bf16, which has them, 94 with it)
+  constexpr bool kLean = TPR == 1024 && sizeof(E) == 4;
   typedef RowSum<TPR, 1, BLK> Sum;
   __shared__ typename Sum::Buffer buf;
   int turn = 0;
@@ -111,8 +114,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
     }
     r0 += step;
   };
-  // the rounds in which every row group has a row; then, for one workgroup, the last rows
-  const int64_t whole = a.rows - r_first < RPB ? 0 : (a.rows - r_first - RPB) / step + 1;
+  // the rounds in which every row group has a row; then, for one workgroup, the last rows (or, without a
+  // row ahead, all)
+  const int64_t whole = kLean || a.rows - r_first < RPB ? 0 : (a.rows - r_first - RPB) / step + 1;
   Row ring[kAhead];
   if (whole > 0)
 #pragma unroll
@@ -124,7 +128,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
 #pragma unroll
     for (int q = 0; q < kAhead; ++q)
       if (q < left) round(ring[q], std::false_type{}, std::min<int64_t>(kAhead, left - q - 1), true);
-  if (RPB > 1 && r0 < a.rows) {
+  while ((RPB > 1 || kLean) && r0 < a.rows) {
     const bool live = r0 + rg < a.rows;
     load(ring[0], r0, live);
     round(ring[0], std::true_type{}, 0, live);

@@ -46,8 +46,14 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
   constexpr int EP = kPiece<E>, V = C / EP, BLK = TPR > 256 ? TPR : 256, RPB = BLK / TPR;
   constexpr int G = SOLO ? 1 : (TPR < 64 ? BLK / 64 : RPB);      // sums to combine in LDS
   constexpr int kAhead = V <= 2 ? 2 : 1;                          // rows loading ahead
+  // Rows of 1024 threads have 128 registers each, too few for dw and db, which lie in LDS (every thread its
+  // own words), for the weights and for a row ahead.  4096 x 16384 bf16 (dy, s, dx) takes 104 us and
+  // 2048 x 16384 fp32 99, where two passes over the rows took 168 and 167 (9000 columns: 137 and 99
+  // against 182 and 164).
+  constexpr bool kLean = TPR == 1024;
   typedef RowSum<TPR, 2, BLK> Sum;
   __shared__ typename Sum::Buffer buf;
+  __shared__ float acc[2][kLean ? C : 1][kLean ? TPR : 1];
   __shared__ float comb[G > 1 ? G - 1 : 1][2][G > 1 ? C : 1][G > 1 ? TPR : 1];
   int turn = 0;
   const int t = threadIdx.x % TPR, rg = threadIdx.x / TPR, n = (int)a.n;
@@ -62,8 +68,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
   const uint32_t gd = (uint32_t)(apart * a.ldds * sizeof(E));
 
   float w[C];
+  auto load_w = [&](int v) { load_vec<EP>(a.w, a.wbf16, piece_col<E, M>((v * TPR + t) * EP, n), n, 1.f, w + v * EP); };
+  if (!kLean)
 #pragma unroll
-  for (int v = 0; v < V; ++v) load_vec<EP>(a.w, a.wbf16, piece_col<E, M>((v * TPR + t) * EP, n), n, 1.f, w + v * EP);
+    for (int v = 0; v < V; ++v) load_w(v);
 
   // this workgroup's samples (SOLO: every gridDim.x-th RPB of them) and rounds
   const BackSplit& sp = a.split;
@@ -76,7 +84,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
     constexpr int kTokStep = SOLO ? 1 : RPB;
     const int64_t first = SOLO ? 0 : std::max<int64_t>(q0 - i * sp.rounds, 0) * RPB;
     const int64_t last = SOLO ? a.T : std::min<int64_t>((q1 - i * sp.rounds) * RPB, a.T);
-    const int64_t whole = SOLO ? (i0 + RPB <= a.B ? a.T : 0) : (last - first) / RPB;
+    const int64_t whole = kLean ? 0 : SOLO ? (i0 + RPB <= a.B ? a.T : 0) : (last - first) / RPB;
     const int64_t rest = SOLO ? a.T - whole : (last - first + RPB - 1) / RPB - whole;
     int64_t tok = first;
 
@@ -101,7 +109,10 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
     };
     float dw[C], db[C];
 #pragma unroll
-    for (int k = 0; k < C; ++k) dw[k] = db[k] = 0.f;
+    for (int k = 0; k < C; ++k) {
+      dw[k] = db[k] = 0.f;
+      if constexpr (kLean) acc[0][k][t] = acc[1][k][t] = 0.f;
+    }
     // one round: this row's sums, the loads of the row kAhead rounds on (of `more` whole rounds), the
     // mask, then the outputs.  PART: only rows that are `live`.
     auto round = [&](Row& x, auto part, int64_t more, bool live) {
@@ -111,6 +122,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
 #pragma unroll
       for (int v = 0; v < V; ++v) {
         const int c = (v * TPR + t) * EP, cc = piece_col<E, M>(c, n);
+        if (kLean) load_w(v);
         unpack<E>(x.dy[v], g + v * EP);
         unpack<E>(x.s[v], xh + v * EP);
         if (has_ds) unpack<E>(x.ds[v], z + v * EP);
@@ -120,8 +132,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
           if (!has_ds) z[k] = 0.f;
           if (PART) g[k] = live ? g[k] : 0.f;
           xh[k] = (xh[k] - mu) * rs;
-          db[k] += g[k];
-          dw[k] = fmaf(g[k], PART && !live ? 0.f : xh[k], dw[k]);
+          if constexpr (kLean) {
+            acc[0][k][t] = fmaf(g[k], xh[k], acc[0][k][t]);
+            acc[1][k][t] += g[k];
+          } else {
+            db[k] += g[k];
+            dw[k] = fmaf(g[k], PART && !live ? 0.f : xh[k], dw[k]);
+          }
           g[k] *= w[k];
           const float own = owns<M>(c, cc, j, n) ? g[k] : 0.f;
           red[0] += own;
@@ -169,6 +186,12 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
       round(x, std::true_type{}, 0, live);
     }
     if (!grads) continue;
+    if constexpr (kLean)
+#pragma unroll
+      for (int k = 0; k < C; ++k) {
+        dw[k] = acc[0][k][t];
+        db[k] = acc[1][k][t];
+      }
     if (!SOLO) {
       if (TPR < 64)
 #pragma unroll
@@ -361,12 +384,13 @@ __global__ __launch_bounds__(256) void norm_back_sums_kernel(NormBackArgs a, int
 
 // ---- launch -------------------------------------------------------------------------------------
 
-constexpr int64_t kNormBackLong = 8192;
+// columns that a workgroup of 1024 threads holds; longer rows are read twice
+constexpr int64_t kNormBackLong = 16384;
 
 NormBackPlan norm_back_plan(int64_t B, int64_t T, int64_t n, int64_t elem_bytes, int tensors) {
   const bool wide = n > kNormBackLong;
   NormBackPlan p{};
-  p.tpr = threads_per_row(n);
+  p.tpr = n > 8192 ? 1024 : threads_per_row(n);
   p.at_once = wide ? 1 : std::max(1, 256 / p.tpr);
   p.solo = T < p.at_once && B > 512;
   BackSplit& sp = p.split;
@@ -378,7 +402,9 @@ NormBackPlan norm_back_plan(int64_t B, int64_t T, int64_t n, int64_t elem_bytes,
   sp.samples = sp.rounds <= 12 || B >= 1024 ? B : 0;
   if (p.solo) sp.blocks = std::min<int64_t>(ceil_div(B, (int64_t)p.at_once), 1024);
   else if (sp.samples) sp.blocks = std::min<int64_t>(B, 1024);
-  else sp.blocks = std::min<int64_t>(streaming_blocks(2 * tensors * p.at_once * n * elem_bytes), std::max<int64_t>(B, sp.total / 4));
+  // two rows of loads in flight, of more than 8192 columns one
+  else sp.blocks = std::min<int64_t>(streaming_blocks((n > 8192 ? 1 : 2) * tensors * p.at_once * n * elem_bytes),
+                                     std::max<int64_t>(B, sp.total / 4));
   p.parts = sp.samples ? 0 : sp.blocks + B;
   return p;
 }
@@ -421,7 +447,8 @@ static void launch_norm_back_of(const NormBackArgs& a, const NormBackPlan& p, hi
     if (p.tpr == 128) return pick(integral_constant<int, 128>(), c8);
     if (p.tpr == 256) return pick(integral_constant<int, 256>(), c8);
     if (a.n <= 4096) return pick(integral_constant<int, 512>(), c8);
-    pick(integral_constant<int, 512>(), integral_constant<int, 16>());
+    if (p.tpr == 512) return pick(integral_constant<int, 512>(), integral_constant<int, 16>());
+    pick(integral_constant<int, 1024>(), integral_constant<int, 16>());
   }
 }
 

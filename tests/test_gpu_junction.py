@@ -153,6 +153,20 @@ def test_norm_widths(D, n, dtype, kind):
     check_forward(D, x, None, w, None, 0.0, getattr(D, kind))
 
 
+@pytest.mark.parametrize("dtype,wdtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
+@pytest.mark.parametrize("B,T,n,pad", [(2, 13, 8193, 0), (1, 1, 8200, 1), (3, 20, 9001, 3), (5, 12, 12288, 0), (1, 40, 16383, 5),
+                                       (1030, 1, 8196, 0)])
+def test_backward_rows_of_a_whole_workgroup(D, B, T, n, pad, dtype, wdtype):
+    # a row takes all threads of a workgroup; samples whole and cut, more of them than workgroups
+    dy, s, ds = rows(B, T, n, dtype, 1, pad), rows(B, T, n, dtype, 2, pad, shift=0.5), rows(B, T, n, dtype, 3, pad)
+    w = vec(n, wdtype, 4, shift=1.0)
+    for k in (D.LAYERNORM, D.RMSNORM):
+        check_backward(D, dy, s, w, k, ds, 0.25)
+    check_backward(D, dy, s, None, D.LAYERNORM, None, 0.5, bias_grad=False)
+    check_backward(D, dy, s, w, D.LAYERNORM, ds, 0.0, weight_grad=False)
+    check_backward(D, dy, s, w, D.RMSNORM, None, 0.0, weight_grad=False, bias_grad=False)
+
+
 @pytest.mark.parametrize("kind", ["LAYERNORM", "RMSNORM"])
 @pytest.mark.parametrize("dtype,wdtype", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("f32", "f32")])
 @pytest.mark.parametrize("B,T,n,pad", [(1, 1, 64, 0), (1, 1, 2048, 0), (64, 1, 2048, 3), (1, 700, 64, 0), (5, 333, 111, 1),

@@ -102,8 +102,10 @@ CALLS = {
     "norm, long rows": (lambda D: lambda: D.dprc_layernorm(torch.ones(1, 2, 20001, device="cuda")), ["layernorm"]),
     "backward, whole samples": (lambda D: _back(D, 3, 9, 300), ["layernorm_backward"]),
     "backward, cut samples": (lambda D: _back(D, 3, 900, 300), ["layernorm_backward"] * 2),
-    "backward, long rows": (lambda D: _back(D, 2, 5, 9000), ["layernorm_backward"] * 2),
-    "backward, long rows, cut samples": (lambda D: _back(D, 2, 50, 9000), ["layernorm_backward"] * 3),
+    "backward, a workgroup's rows": (lambda D: _back(D, 2, 5, 9000), ["layernorm_backward"]),
+    "backward, a workgroup's rows, cut samples": (lambda D: _back(D, 2, 50, 9000), ["layernorm_backward"] * 2),
+    "backward, long rows": (lambda D: _back(D, 2, 5, 20000), ["layernorm_backward"] * 2),
+    "backward, long rows, cut samples": (lambda D: _back(D, 2, 50, 20000), ["layernorm_backward"] * 3),
     "vector norms": (lambda D: lambda: D.dprc_norm_vectors(torch.ones(4, 300, device="cuda")), ["vector_norms"]),
     "vector norms, split": (lambda D: lambda: D.dprc_norm_vectors(torch.ones(4, 300000, device="cuda")), ["vector_norms"] * 2),
     "vector sums": (lambda D: lambda: D.dprc_clip_accumulate_vectors(torch.ones(4, 300, device="cuda"), torch.ones(4, device="cuda")),
