@@ -21,9 +21,11 @@ _KINDS = {"layer": D.LAYERNORM, "rms": D.RMSNORM}
 
 
 def token_rows(x):
-    """x [B, T, n] itself where its token rows have one stride, else a contiguous copy."""
-    B, T, n = x.shape
-    return x if x.stride(2) == 1 and x.stride(0) == T * x.stride(1) and x.stride(1) >= n else x.contiguous()
+    """x [B, T, n] itself where its token rows have one stride, else a contiguous copy.  (The last token of
+    every sample, x[:, -1:], is such rows: one token has no stride of its own, and neither has one sample.)"""
+    (B, T, n), (s0, s1, s2) = x.shape, x.stride()
+    ld = s1 if T > 1 else s0 if B > 1 else n
+    return x if s2 == 1 and ld >= n and (B == 1 or s0 == T * ld) else x.contiguous()
 
 
 class _JunctionFn(torch.autograd.Function):

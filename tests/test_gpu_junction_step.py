@@ -92,6 +92,45 @@ def test_module_gradients(mods, kind):
     assert torch.equal(s, x.cuda())
 
 
+@pytest.mark.parametrize("p", [0.0, 0.25])
+def test_module_without_a_residual(mods, p):
+    # as above, s handed on as the next residual; with p = 0 s is x itself
+    D, _, junction = mods
+    B, T, n = 2, 19, 72
+    mod = junction.Junction(n, p=p, site_id=4).cuda()
+    mod.seed = 5
+    g = torch.Generator().manual_seed(4)
+    x, ty, ts = (torch.randn(B, T, n, generator=g) for _ in range(3))
+    f = torch.from_numpy(J.dropout_factors(5, 4, B * T, n, p)).view(B, T, n)
+    x64 = x.double().requires_grad_()
+    s64 = f * x64
+    d = s64 - s64.mean(-1, keepdim=True)
+    y64 = d / torch.sqrt((d * d).mean(-1, keepdim=True) + float(np.float32(1e-5)))
+    ref = torch.autograd.grad((y64 * ty.double()).sum() + (s64 * ts.double()).sum(), x64)[0]
+    xc = x.cuda().requires_grad_()
+    y, s = mod(xc)
+    got = torch.autograd.grad((y * ty.cuda()).sum() + (s * ts.cuda()).sum(), [xc, *mod.parameters()])
+    assert (got[0].cpu().double() - ref).abs().max() <= 1e-5 * max(1.0, ref.abs().max().item())
+    for q in mod.parameters():                                        # the weights alone, then neither
+        assert torch.equal(torch.autograd.grad((mod(x.cuda())[0] * ty.cuda()).sum(), q)[0], got[1 if q is mod.weight else 2])
+    for q in mod.parameters():
+        q.requires_grad_(False)
+    y2, s2 = mod(xc)
+    alone = torch.autograd.grad((y2 * ty.cuda()).sum() + (s2 * ts.cuda()).sum(), xc)[0]
+    assert torch.equal(alone, got[0]) and torch.equal(y2, y) and not mod(x.cuda())[0].requires_grad
+
+
+def test_module_on_each_samples_last_token(mods):
+    D, _, junction = mods
+    mod = junction.Junction(80, kind="rms").cuda().eval()
+    x, z = torch.randn(3, 7, 80, device="cuda"), torch.randn(3, 7, 80, device="cuda")
+    with torch.no_grad():
+        y, s = mod(x, z)
+        for cut in (slice(-1, None), slice(2, 3), slice(2, 5)):
+            y1, s1 = mod(x[:, cut], z[:, cut])
+            assert torch.equal(y1, y[:, cut]) and torch.equal(s1, s[:, cut])
+
+
 def test_step_trains_the_norms(mods):
     D, dpsgd, _ = mods
     C, sigma, k, lr, wd = 0.05, 0.6, 16, 1e-3, 0.01

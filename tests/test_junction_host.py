@@ -9,6 +9,7 @@ import pytest
 import torch
 
 from paper_2605_24879_amd import dprc
+from paper_2605_24879_amd.junction import token_rows
 
 pytestmark = pytest.mark.skipif(not os.path.exists(dprc.LIB_PATH), reason="libdprc.so not built")
 
@@ -138,3 +139,18 @@ def test_the_binding_refuses_what_the_kernels_cannot_take(no_launch):
         with pytest.raises((ValueError, TypeError)):
             call()
             pytest.fail(f"call {k} was taken")
+
+
+def test_token_rows_copies_only_what_has_no_row_stride():
+    x = torch.randn(4, 6, 10)
+    keeps = {"whole": x, "last tokens": x[:, -1:], "one sample's part": x[1:2, 2:5], "one row": x[3:, 5:], "columns": x[:, :, 2:7],
+             "last tokens' columns": x[:, -1:, 3:], "every other sample's token": x[::2, :1]}
+    copies = {"cut tokens": x[:, 1:4], "features apart": x[:, :, ::2], "tokens first": x.transpose(0, 1), "spread": x[:1, :1].expand(4, 6, 10),
+              "spread samples": x[:1, :1].expand(4, 1, 10)}
+    for name, v in keeps.items():
+        assert token_rows(v) is v, name
+    for name, v in copies.items():
+        got = token_rows(v)
+        assert got is not v and got.is_contiguous() and torch.equal(got, v), name
+    for v in (*keeps.values(), *map(token_rows, copies.values())):
+        assert dprc._token_rows(v, "x") >= v.shape[2]
