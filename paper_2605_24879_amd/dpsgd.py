@@ -26,8 +26,8 @@ Per step:
 
 Only the listed linear layers are trained, and the norms given as ``norms``;
 every other parameter (embedding, other norms) is held fixed.  Probes, noise
-and the norms' dropout masks are keyed by a per-step seed derived from (seed,
-step), so they are fresh every step.
+and the dropout masks of the norms and of the ``dropouts`` are keyed by a
+per-step seed derived from (seed, step), so they are fresh every step.
 
 With ``norms`` (``junction.Junction`` modules), step 2 goes on through the first
 norm; the backward calls write every sample's weight and bias gradients side by
@@ -64,11 +64,12 @@ class DPSGDRC:
     noise multiplier.  AdamW hyper-parameters as in ``torch.optim.AdamW``.
     ``norms``: the ``junction.Junction`` modules whose weights and biases are
     trained too (parameters of one dtype; they become views of one buffer).
+    ``dropouts``: ``junction.Dropout`` modules, whose masks change with the step.
     """
 
     def __init__(self, linears, C, sigma, estimator="hutch", k=16, probe="rademacher", s=16, r=32,
                  side=D.SIDE_OUT, seed=0, lr=1e-4, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0,
-                 fused_adamw=True, norms=()):
+                 fused_adamw=True, norms=(), dropouts=()):
         self.linears = list(linears)
         for lin in self.linears:
             if lin.bias is not None:
@@ -81,7 +82,7 @@ class DPSGDRC:
         self.master = [lin.weight.detach().t().float().contiguous() for lin in self.linears]
         for lin in self.linears:
             lin.weight.requires_grad_(True)
-        self.norms = list(norms)
+        self.norms, self.dropouts = list(norms), list(dropouts)
         self._gather_vectors()
         self.hp = dict(lr=lr, beta1=betas[0], beta2=betas[1], eps=eps, weight_decay=weight_decay)
         self.fused = bool(fused_adamw)
@@ -151,6 +152,8 @@ class DPSGDRC:
         self._G = None
         for m, sink in zip(self.norms, self._sinks):
             m.seed, m.sink = step_seed(self.seed, self.steps), sink
+        for m in self.dropouts:
+            m.seed = step_seed(self.seed, self.steps)
         try:
             losses = loss_fn()
             if losses.dim() != 1:

@@ -7,6 +7,8 @@ training step (``dpsgd.DPSGDRC`` with ``norms=``) these per-sample gradients go 
 adds their squared norms to the estimates and takes their clipped sum; otherwise their sum is the
 parameters' ordinary gradient.
 
+``Dropout`` is the same dropout on its own, inside a branch or with a residual that no norm follows.
+
 The dropout mask is a function of (seed, site, row, column) and is made again in the backward pass.
 ``seed`` is an attribute: the step sets it to its key; without a step the caller changes it from one
 training step to the next.
@@ -88,3 +90,36 @@ class Junction(nn.Module):
             return y, s
         out = _JunctionFn.apply(x, res, self.weight, self.bias, self, p)
         return out if len(out) == 2 else (out[0], x)
+
+
+class _DropoutFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, res, p, seed, site_id):
+        ctx.args, ctx.has_res = (p, seed, site_id), res is not None
+        return D.dprc_dropout(x, p, seed, site_id, res=res)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        dx = D.dprc_dropout(token_rows(dy), *ctx.args) if ctx.needs_input_grad[0] else None
+        return dx, dy if ctx.has_res else None, None, None, None
+
+
+class Dropout(nn.Module):
+    """Dropout of [B, T, n] token rows, and the residual added: ``res + dropout(x)`` (x itself where there is
+    neither).  Nothing is kept for the backward pass.  ``p``, in training only, ``site_id`` and ``seed`` as in
+    ``Junction``."""
+
+    def __init__(self, p, site_id=0):
+        super().__init__()
+        self.p, self.site_id, self.seed = float(p), int(site_id), 0
+
+    def forward(self, x, res=None):
+        p = self.p if self.training else 0.0
+        if res is None and p == 0.0:
+            return x
+        x = token_rows(x)
+        res = None if res is None else token_rows(res)
+        if not torch.is_grad_enabled():
+            return D.dprc_dropout(x, p, self.seed, self.site_id, res=res)
+        return _DropoutFn.apply(x, res, p, self.seed, self.site_id)

@@ -229,3 +229,54 @@ def test_norms_that_a_step_cannot_train_are_refused(mods):
     with pytest.raises(RuntimeError):                                 # twice in one step
         drv.capture(lambda: llama.per_sample_loss(model(tok[:, :-1]) + model(tok[:, :-1]), tok[:, 1:]))
     drv.remove_hooks()
+
+
+@pytest.mark.parametrize("res", [False, True])
+def test_dropout_module(mods, res):
+    # outputs and gradients are the mask's factors, bit for bit in fp32 (one product, one sum)
+    D, _, junction = mods
+    B, T, n, p = 3, 17, 75, 0.3
+    mod = junction.Dropout(p, site_id=6)
+    mod.seed = 31
+    x, z, t = (torch.randn(B, T, n, device="cuda") for _ in range(3))
+    f = torch.from_numpy(J.dropout_factors(31, 6, B * T, n, p)).view(B, T, n).float().cuda()
+    ins = [x.clone().requires_grad_()] + ([z.clone().requires_grad_()] if res else [])
+    y = mod(*ins)
+    want = torch.addcmul(z.double(), f.double(), x.double()) if res else (f * x).double()
+    assert (y.double() - want).abs().max() <= 2.0 ** -24 * 2 * ((f * x).abs().max() + want.abs().max())
+    grads = torch.autograd.grad((y * t).sum(), ins)
+    assert torch.equal(grads[0], f * t) and (not res or torch.equal(grads[1], t))
+    spread = torch.autograd.grad(mod(*ins).sum(), ins)                # a gradient without strides of its own
+    assert torch.equal(spread[0], f) and (not res or torch.equal(spread[1], torch.ones_like(z)))
+    part = mod(x[:, :1], *([z[:, :1]] if res else []))
+    assert not part.requires_grad and part.shape == (B, 1, n)
+    mod.eval()
+    assert mod(x) is x and torch.equal(mod(x, z), x + z)
+    with torch.no_grad():
+        assert torch.equal(mod(x, z), x + z)
+
+
+def test_step_keys_the_dropouts(mods):
+    # what a step captures as input of the layer after a dropout is zero exactly where that step's mask is
+    D, dpsgd, _ = mods
+    p = 0.25
+    model = _model(junctions=True, dropout=p)
+    tok = _tokens()
+    drv = dpsgd.DPSGDRC(model.linears(), C=1.0, sigma=0.0, seed=4, norms=model.norms(), dropouts=model.dropouts())
+    sites = [m.site_id for m in model.norms() + model.dropouts()]
+    assert len(set(sites)) == len(sites)
+    seen = []
+    for _ in range(2):
+        seen_now = []
+        hooks = [b.down.register_forward_hook(lambda m, i, o: seen_now.append(i[0].detach())) for b in model.blocks]
+        drv.step(lambda: llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:]))
+        for h in hooks:
+            h.remove()
+        assert len({m.seed for m in model.norms() + model.dropouts()}) == 1
+        for a, m in zip(seen_now, model.dropouts()):
+            B, T, n = a.shape
+            f = torch.from_numpy(J.dropout_factors(m.seed, m.site_id, B * T, n, p)).view(B, T, n)
+            assert (a.cpu()[f == 0] == 0).all() and (a.cpu()[f != 0] != 0).float().mean() > 0.99
+        seen.append((model.dropouts()[0].seed, seen_now))
+    assert seen[0][0] != seen[1][0]
+    drv.remove_hooks()

@@ -14,8 +14,8 @@ and v read the same normed activations, as do gate and up.
 
 With ``junctions`` the norms, the residual sums before them and a dropout of rate
 ``dropout`` on every branch run as ``paper_2605_24879_amd.junction.Junction``
-(``norm``: "rms" or "layer"), whose parameters ``norms()`` lists for private
-training.
+(``norm``: "rms" or "layer"), which ``norms()`` lists for private training, and a
+dropout of the same rate inside the MLP as ``junction.Dropout`` (``dropouts()``).
 
 ``linears()`` lists the projections in model order (per block q, k, v, o,
 gate, up, down; then lm_head), which keeps the shared-input layers adjacent.
@@ -57,7 +57,7 @@ def _rope(x, cos, sin):
 
 
 class Block(nn.Module):
-    def __init__(self, hidden, mlp, heads, kv_heads, make_norm=RMSNorm):
+    def __init__(self, hidden, mlp, heads, kv_heads, make_norm=RMSNorm, make_drop=nn.Identity):
         super().__init__()
         hd = hidden // heads
         self.heads, self.kv_heads, self.hd = heads, kv_heads, hd
@@ -70,6 +70,7 @@ class Block(nn.Module):
         self.gate = nn.Linear(hidden, mlp, bias=False)
         self.up = nn.Linear(hidden, mlp, bias=False)
         self.down = nn.Linear(mlp, hidden, bias=False)
+        self.act_drop = make_drop()
 
     def attend(self, h, cos, sin, mask):
         B, T, _ = h.shape
@@ -86,7 +87,7 @@ class Block(nn.Module):
         return self.o(a)
 
     def feed(self, h):
-        return self.down(F.silu(self.gate(h)) * self.up(h))
+        return self.down(self.act_drop(F.silu(self.gate(h)) * self.up(h)))
 
     def forward(self, x, cos, sin, mask):
         x = x + self.attend(self.norm1(x), cos, sin, mask)
@@ -109,14 +110,15 @@ class LlamaShaped(nn.Module):
         super().__init__()
         self.embed = nn.Embedding(vocab, hidden)
         self.junctions = bool(junctions)
-        make_norm, block = RMSNorm, Block
+        make_norm, make_drop, block = RMSNorm, nn.Identity, Block
         if self.junctions:
-            from paper_2605_24879_amd.junction import Junction
+            from paper_2605_24879_amd.junction import Dropout, Junction
             sites = itertools.count()
             make_norm, block = lambda n: Junction(n, kind=norm, p=dropout, site_id=next(sites)), JunctionBlock
+            make_drop = lambda: Dropout(dropout, site_id=next(sites))
         elif norm != "rms" or dropout:
             raise ValueError("layer norm and dropout come with junctions")
-        self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm) for _ in range(layers)])
+        self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm, make_drop) for _ in range(layers)])
         self.norm = make_norm(hidden)
         self.lm_head = nn.Linear(hidden, vocab, bias=False)
         self.rope_base = rope_base
@@ -130,6 +132,9 @@ class LlamaShaped(nn.Module):
 
     def norms(self):
         return [m for b in self.blocks for m in (b.norm1, b.norm2)] + [self.norm]
+
+    def dropouts(self):
+        return [b.act_drop for b in self.blocks] if self.junctions else []
 
     def forward(self, tokens):
         B, T = tokens.shape
