@@ -455,10 +455,11 @@ def _vector(x, name, n, device, dtype=torch.float32):
 
 
 def _sample_rows(g, name, B, n, device):
-    """The row stride of per-sample gradients [B, n] (0: any)."""
-    if g.shape != (B, n) or g.dtype != torch.float32 or g.get_device() != device or (n > 1 and g.stride(1) != 1):
-        raise ValueError(f"{name} must be [{B}, {n}] fp32 with contiguous rows on the other tensors' GPU")
-    return g.stride(0) if B > 1 else 0
+    """The row stride of per-sample gradients [B, n] (None for one sample: any will do)."""
+    if (g.shape != (B, n) or g.dtype != torch.float32 or g.get_device() != device or (n > 1 and g.stride(1) != 1)
+            or (B > 1 and g.stride(0) < n)):
+        raise ValueError(f"{name} must be [{B}, {n}] fp32 with contiguous rows of their own on the other tensors' GPU")
+    return g.stride(0) if B > 1 else None
 
 
 def _ln(x, kind, weight, bias, eps, p, seed, site_id):
@@ -557,7 +558,7 @@ def dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=LAYERNORM, ds=None, 
         given = [_sample_rows(g, name, B, n, index) for g, name in ((dw, "dw"), (db, "db")) if g is not None]
         if len(given) == 2 and given[0] != given[1]:
             raise ValueError("dw and db must share a row stride")
-        ldg = given[0] or n
+        ldg = n if given[0] is None else given[0]
     if dw is None and weight_grad:
         dw = torch.empty_strided((B, n), (ldg, 1), dtype=torch.float32, device=dev)
     if db is None and bias_grad:
