@@ -180,9 +180,20 @@ def _workspace(nbytes, dev, ws):
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=dev)
 
 
+def _entries(x, name, n, dev):
+    """The pointer of a given fp32 tensor of which a call reads or writes the first n entries."""
+    if x.numel() < n or x.dtype != torch.float32 or x.device != dev or not x.is_contiguous():
+        raise ValueError(f"{name} must hold {n} contiguous fp32 entries on {dev}, not {list(x.shape)} {x.dtype} on {x.device}")
+    return x.data_ptr()
+
+
 def _new_n2(B, dev, accumulate):
     """Estimates to start from: zeros to add to, else left to the call, which writes all of them."""
     return (torch.zeros if accumulate else torch.empty)(B, dtype=torch.float32, device=dev)
+
+
+def _layer_entries(n2_layers, n, dev):
+    return None if n2_layers is None else _entries(n2_layers, "n2_layers", n, dev)
 
 
 def dprc_norm_hutch_workspace(pairs, k, side=SIDE_OUT, probe=PROBE_RADEMACHER):
@@ -196,10 +207,12 @@ def dprc_norm_hutch(pairs, k, seed, side=SIDE_OUT, probe=PROBE_RADEMACHER, n2=No
     arr, nl, B, dev = _layers(pairs)
     if n2 is None:
         n2 = _new_n2(B, dev, accumulate)
+    else:
+        _entries(n2, "n2", B, dev)
     need = lib().dprc_norm_hutch_workspace(arr, nl, k, probe, side)
     ws = _workspace(need, dev, ws)
     _check(lib().dprc_norm_hutch(arr, nl, k, probe, seed, side, n2.data_ptr(),
-                                 n2_layers.data_ptr() if n2_layers is not None else None,
+                                 _layer_entries(n2_layers, nl * B, dev),
                                  int(bool(accumulate)), ws.data_ptr(), need, _stream(dev)))
     return n2
 
@@ -210,12 +223,16 @@ def dprc_norm_hutch_clip(pairs, k, seed, C, side=SIDE_OUT, probe=PROBE_RADEMACHE
     arr, nl, B, dev = _layers(pairs)
     if n2 is None:
         n2 = _new_n2(B, dev, accumulate)
+    else:
+        _entries(n2, "n2", B, dev)
     if c is None:
         c = torch.empty(B, dtype=torch.float32, device=dev)
+    else:
+        _entries(c, "c", B, dev)
     need = lib().dprc_norm_hutch_workspace(arr, nl, k, probe, side)
     ws = _workspace(need, dev, ws)
     _check(lib().dprc_norm_hutch_clip(arr, nl, k, probe, seed, side, C, n2.data_ptr(), c.data_ptr(),
-                                      n2_layers.data_ptr() if n2_layers is not None else None,
+                                      _layer_entries(n2_layers, nl * B, dev),
                                       int(bool(accumulate)), ws.data_ptr(), need, _stream(dev)))
     return n2, c
 
@@ -233,10 +250,14 @@ def dprc_norm_hutch_clip_static(pairs, k, seed, C, side=SIDE_OUT, probe=PROBE_RA
     arr, nl, B, dev = _layers(pairs)
     if n2 is None:
         n2 = _new_n2(B, dev, accumulate)
+    else:
+        _entries(n2, "n2", B, dev)
     if c is None:
         c = torch.empty(B, dtype=torch.float32, device=dev)
+    else:
+        _entries(c, "c", B, dev)
     _check(lib().dprc_norm_hutch_clip_static(arr, nl, k, probe, seed, side, C, n2.data_ptr(), c.data_ptr(),
-                                             n2_layers.data_ptr() if n2_layers is not None else None,
+                                             _layer_entries(n2_layers, nl * B, dev),
                                              int(bool(accumulate)), _stream(dev)))
     return n2, c
 
@@ -246,18 +267,24 @@ def dprc_norm_hutchpp(pairs, s, r, seed, side=SIDE_OUT, n2=None, n2_layers=None,
     arr, nl, B, dev = _layers(pairs)
     if n2 is None:
         n2 = _new_n2(B, dev, accumulate)
+    else:
+        _entries(n2, "n2", B, dev)
     need = lib().dprc_norm_hutchpp_workspace(arr, nl, s, r, side)
     ws = _workspace(need, dev, ws)
     _check(lib().dprc_norm_hutchpp(arr, nl, s, r, seed, side, n2.data_ptr(),
-                                   n2_layers.data_ptr() if n2_layers is not None else None,
+                                   _layer_entries(n2_layers, nl * B, dev),
                                    int(bool(accumulate)), ws.data_ptr(), need, _stream(dev)))
     return n2
 
 
 def dprc_clip_scale(n2, C, c=None):
+    B, dev = n2.numel(), n2.device
+    src = _entries(n2, "n2", B, dev)
     if c is None:
         c = torch.empty_like(n2)
-    _check(lib().dprc_clip_scale(n2.data_ptr(), n2.numel(), float(C), c.data_ptr(), _stream(n2.device)))
+    else:
+        _entries(c, "c", B, dev)
+    _check(lib().dprc_clip_scale(src, B, float(C), c.data_ptr(), _stream(dev)))
     return c
 
 
@@ -274,7 +301,7 @@ def dprc_clip_accumulate(A, E, c, grad=None, accumulate=False, ws=None):
         raise ValueError("grad must have contiguous rows")
     need = lib().dprc_clip_accumulate_workspace(ctypes.byref(L))
     ws = _workspace(need, A.device, ws) if need else None
-    _check(lib().dprc_clip_accumulate(ctypes.byref(L), c.data_ptr(), grad.data_ptr(), grad.stride(0),
+    _check(lib().dprc_clip_accumulate(ctypes.byref(L), _entries(c, "c", A.shape[0], A.device), grad.data_ptr(), grad.stride(0),
                                       int(bool(accumulate)), ws.data_ptr() if ws is not None else None,
                                       need, _stream(A.device)))
     return grad
@@ -296,6 +323,7 @@ def dprc_clip_accumulate_layers(pairs, c, grads=None, accumulate=False):
     ptrs = (ctypes.c_void_p * n)(*[g.data_ptr() for g in grads])
     lds = (ctypes.c_int64 * n)(*[g.stride(0) for g in grads])
     dev = pairs[0][0].device if n else c.device
+    _entries(c, "c", pairs[0][0].shape[0] if n else 0, dev)
     _check(lib().dprc_clip_accumulate_layers(arr, n, c.data_ptr(), ptrs, lds, int(bool(accumulate)), _stream(dev)))
     return grads
 

@@ -41,3 +41,46 @@ def test_per_sample_gradients_need_a_row_each(calls):
     for dw in (one, one.expand(1, 8), G[1:2, 3:11], torch.zeros(64).as_strided((1, 8), (0, 1))):
         dprc.dprc_layernorm_backward(x, x, None, st, st, dw=dw)
         assert calls[-1][1][15] == 8
+
+
+@pytest.fixture
+def layers(monkeypatch):
+    """Two layers' (A, E) of four samples as the binding sees them, host tensors for device ones."""
+    monkeypatch.setattr(dprc, "make_layer", lambda A, E, layer_id: dprc.Layer())
+    return [(torch.zeros(4, 2, 6), torch.zeros(4, 2, 5), j) for j in range(2)]
+
+
+def test_per_sample_values_need_an_entry_each(calls, layers):
+    full, A, E = torch.zeros(4), layers[0][0], layers[0][1]
+    uses = {
+        "n2": [lambda v: dprc.dprc_norm_hutch(layers, 4, 0, n2=v), lambda v: dprc.dprc_norm_hutch(layers, 4, 0, n2=v, accumulate=True),
+               lambda v: dprc.dprc_norm_hutch_clip(layers, 4, 0, 1.0, n2=v, accumulate=True),
+               lambda v: dprc.dprc_norm_hutch_clip_static(layers, 4, 0, 1.0, n2=v),
+               lambda v: dprc.dprc_norm_hutchpp(layers, 4, 4, 0, n2=v, accumulate=True)],
+        "c": [lambda v: dprc.dprc_norm_hutch_clip(layers, 4, 0, 1.0, c=v), lambda v: dprc.dprc_norm_hutch_clip_static(layers, 4, 0, 1.0, c=v),
+              lambda v: dprc.dprc_clip_scale(full, 1.0, c=v), lambda v: dprc.dprc_clip_accumulate(A, E, v),
+              lambda v: dprc.dprc_clip_accumulate_layers(layers, v)],
+    }
+    for name, fs in uses.items():
+        for k, f in enumerate(fs):
+            for bad in (torch.zeros(1), torch.zeros(3), torch.zeros(1).expand(4), torch.zeros(8)[::2], full.double(), full.bfloat16(),
+                        torch.zeros(4, device="meta")):
+                with pytest.raises(ValueError):
+                    f(bad)
+                    pytest.fail(f"{name} use {k} was taken")
+    for f in (lambda v: dprc.dprc_norm_hutch(layers, 4, 0, n2_layers=v), lambda v: dprc.dprc_norm_hutch_clip(layers, 4, 0, 1.0, n2_layers=v),
+              lambda v: dprc.dprc_norm_hutch_clip_static(layers, 4, 0, 1.0, n2_layers=v),
+              lambda v: dprc.dprc_norm_hutchpp(layers, 4, 4, 0, n2_layers=v)):
+        for bad in (torch.zeros(7), torch.zeros(4, 2).t(), torch.zeros(2, 4).double()):
+            with pytest.raises(ValueError):
+                f(bad)
+    for bad in (torch.zeros(8)[::2], full.double()):                  # the estimates that clip factors are made from
+        with pytest.raises(ValueError):
+            dprc.dprc_clip_scale(bad, 1.0)
+    assert not calls
+    for ok in (full, torch.zeros(9), torch.zeros(9)[2:6], torch.zeros(2, 2)):
+        for f in uses["n2"] + uses["c"]:
+            f(ok)
+    assert len(calls) == 40
+    dprc.dprc_norm_hutch(layers, 4, 0, n2_layers=torch.zeros(2, 4))
+    assert calls[-1][0] == "dprc_norm_hutch"
