@@ -31,7 +31,7 @@ per-step seed derived from (seed, step), so they are fresh every step.
 
 With ``norms`` (``junction.Junction`` modules), step 2 goes on through the first
 norm; the backward calls write every sample's weight and bias gradients side by
-side into one [B, N] matrix; step 3 starts from its rows' exact squared norms
+side into one [B, N] matrix, which goes with the layers' pairs; step 3 starts from its rows' exact squared norms
 (``dprc_norm_vectors``), step 5 adds its clipped sum
 (``dprc_clip_accumulate_vectors``), and steps 6 and 7 treat all of them as one
 more layer, without weight decay.
@@ -52,6 +52,16 @@ def _rows(x):
 def step_seed(seed, step):
     """The key of step ``step``: seed + step * 0x9E3779B97F4A7C15 mod 2^64."""
     return (int(seed) + int(step) * _GOLDEN) & 0xFFFFFFFFFFFFFFFF
+
+
+class Pairs(list):
+    """What a capture gives: (A, E, layer) of every trained layer, and in ``vectors`` the per-sample
+    gradients [B, N] of the trained norms (None where there are none).  Whoever makes another list of
+    them for a step with norms hands ``vectors`` on."""
+
+    def __init__(self, items=(), vectors=None):
+        super().__init__(items)
+        self.vectors = vectors
 
 
 class DPSGDRC:
@@ -148,7 +158,8 @@ class DPSGDRC:
             h.remove()
 
     def capture(self, loss_fn):
-        """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs."""
+        """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs, with the norms' per-sample gradients
+        beside them (``Pairs``)."""
         self._G = None
         for m, sink in zip(self.norms, self._sinks):
             m.seed, m.sink = step_seed(self.seed, self.steps), sink
@@ -171,14 +182,22 @@ class DPSGDRC:
                 raise RuntimeError("a trained layer or norm has no part in the loss")
         # token-row layouts for the library (no copy when already so; layers fed the
         # same activations keep one pointer, so they share a pass over A)
-        pairs = [(_rows(self._A[j].detach()), _rows(E[j]), j) for j in range(len(self.linears))]
+        pairs = Pairs(((_rows(self._A[j].detach()), _rows(E[j]), j) for j in range(len(self.linears))), self._G)
         self._A = [None] * len(self.linears)
         self._S = [None] * len(self.linears)
         return losses.detach(), pairs
 
+    @staticmethod
+    def _vectors(pairs):
+        """The norms' per-sample gradients that were captured with these layers."""
+        G = getattr(pairs, "vectors", None)
+        if G is None:
+            raise ValueError("pairs must be what capture returned, the norms' per-sample gradients with the layers'")
+        return G
+
     def estimate(self, pairs, key):
         """Steps 3-4: n2 [B] and c [B]."""
-        n2 = D.dprc_norm_vectors(self._G) if self.norms else None
+        n2 = D.dprc_norm_vectors(self._vectors(pairs)) if self.norms else None
         more = n2 is not None
         if self.estimator == "hutch":
             return D.dprc_norm_hutch_clip(pairs, self.k, key, self.C, side=self.side, probe=self.probe, n2=n2,
@@ -198,8 +217,8 @@ class DPSGDRC:
 
     def clipped_sums(self, pairs, c):
         """Step 5 for every layer: one call when all are bf16 (the small layers share
-        launches), else one call per layer; then for the norms, whose per-sample
-        gradients it releases."""
+        launches), else one call per layer; then for the norms."""
+        G = self._vectors(pairs) if self.norms else None
         if all(A.dtype == torch.bfloat16 and E.dtype == torch.bfloat16 for (A, E, _) in pairs):
             grads = D.dprc_clip_accumulate_layers(pairs, c)
         else:
@@ -208,8 +227,9 @@ class DPSGDRC:
                 self._ws_acc = torch.empty(max(need, 1), dtype=torch.uint8, device=c.device)
             grads = [D.dprc_clip_accumulate(A, E, c, ws=self._ws_acc) for (A, E, _) in pairs]
         if self.norms:
-            grads.append(D.dprc_clip_accumulate_vectors(self._G, c).view(1, -1))
-            self._G = None
+            grads.append(D.dprc_clip_accumulate_vectors(G, c).view(1, -1))
+            if G is self._G:                # from here on only `pairs` holds them
+                self._G = None
         return grads
 
     def update(self, clipped, batch, key):

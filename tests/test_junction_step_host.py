@@ -1,0 +1,114 @@
+"""Host logic of junctions in the private training step (no GPU): the library's calls are played by
+the oracle on host tensors, so the step's own bookkeeping is what is tested.
+
+The estimates of the linear layers are their exact squared norms here.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import estimators as est
+from oracle import junction as J
+from paper_2605_24879_amd import dprc, dpsgd, junction
+from workloads import llama
+
+SIZES = dict(layers=2, hidden=16, mlp=24, heads=4, kv_heads=2, vocab=19)
+f32 = lambda x: torch.from_numpy(np.ascontiguousarray(x)).float()
+
+
+def layernorm(x, weight=None, bias=None, eps=1e-5, kind=dprc.LAYERNORM, res=None, p=0.0, seed=0, site_id=0, stats=True):
+    s64 = J.dropout(x, seed, site_id, p, res=res)
+    y, mean, rstd = J.norm(s64, weight, bias, eps=eps, rms=kind == dprc.RMSNORM)
+    s = x if res is None and p == 0.0 else f32(s64)
+    return f32(y), s, None if mean is None else f32(mean), f32(rstd)
+
+
+def layernorm_backward(dy, s, weight, mean, rstd, kind=dprc.LAYERNORM, ds=None, p=0.0, seed=0, site_id=0, weight_grad=True,
+                       bias_grad=True, dw=None, db=None):
+    assert (mean is None) == (kind == dprc.RMSNORM)
+    dx, w, b = J.norm_backward(dy, s, weight, mean, rstd, ds=ds)
+    out = []
+    for given, want, g in ((dw, weight_grad, w), (db, bias_grad, b)):
+        out.append(f32(g) if given is None and want else given)
+        if given is not None:
+            assert given.shape == g.shape
+            given.copy_(f32(g))
+    return f32(dx), f32(J.dropout(dx, seed, site_id, p)) if p > 0.0 else None, *out
+
+
+def norm_vectors(G):
+    return f32(J.norm_vectors(G))
+
+
+def sample_norms(pairs):
+    return sum(np.array([((est.as_f64(A[i]).T @ est.as_f64(E[i])) ** 2).sum() for i in range(len(A))]) for (A, E, _) in pairs)
+
+
+def norm_hutch_clip(pairs, k, seed, C, side=0, probe=0, n2=None, accumulate=False):
+    n2 = f32(sample_norms(pairs) + (est.as_f64(n2) if accumulate else 0.0))
+    return n2, f32(est.clip_scale(est.as_f64(n2), C))
+
+
+def add_noise(g, sigma, C, seed, tensor_id):
+    return g.copy_(f32(est.add_noise(est.as_f64(g), sigma, C, seed, tensor_id)))
+
+
+@pytest.fixture(autouse=True)
+def library(monkeypatch):
+    for name, f in dict(
+            layernorm=layernorm, layernorm_backward=layernorm_backward, norm_vectors=norm_vectors, norm_hutch_clip=norm_hutch_clip,
+            dropout=lambda x, p, seed, site_id, res=None: f32(J.dropout(x, seed, site_id, p, res=res)),
+            clip_accumulate_vectors=lambda G, c: f32(J.clip_accumulate_vectors(G, c)), clip_accumulate_workspace=lambda A, E: 0,
+            clip_accumulate=lambda A, E, c, ws=None: torch.einsum("btd,b,btp->dp", A, c, E), add_noise=add_noise).items():
+        monkeypatch.setattr(dprc, "dprc_" + name, f)
+
+
+def stack(**kw):
+    return llama.build(seed=3, device="cpu", dtype=torch.float32, **dict(SIZES, junctions=True, **kw))
+
+
+def loss_of(model, tok):
+    return lambda: llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:])
+
+
+def tokens(B=3, seed=1):
+    return llama.tokens(B, 7, SIZES["vocab"], seed=seed, device="cpu")
+
+
+def driver(model, **kw):
+    return dpsgd.DPSGDRC(model.linears(), **dict(dict(C=0.5, sigma=0.0, norms=model.norms()), **kw))
+
+
+def reference(model, tok):
+    """Per-sample gradients of the norms' parameters [B, N], each sample alone through torch's autograd."""
+    params = [q for m in model.norms() for q in m.parameters_in_order()]
+    rows = [torch.cat([g.reshape(-1) for g in torch.autograd.grad(loss_of(model, tok[i:i + 1])()[0], params)]) for i in range(len(tok))]
+    return torch.stack(rows)
+
+
+def test_each_capture_keeps_its_own_norm_gradients():
+    # what a capture returns stands on its own: other captures between it and its use change nothing, and it
+    # can be used again
+    model = stack(norm="layer")
+    drv = driver(model)
+    toks = tokens(3, 1), tokens(2, 2)
+    refs = [reference(model, t) for t in toks]
+    alone = [drv.private_grads(drv.capture(loss_of(model, t))[1], 7) for t in toks]
+    both = [drv.capture(loss_of(model, t))[1] for t in toks]
+    for use in (0, 1, 0):
+        n2, c, grads = drv.private_grads(both[use], 7)
+        for a, b in zip((n2, c, *grads), (*alone[use][:2], *alone[use][2])):
+            assert torch.equal(a, b)
+        G = refs[use]
+        want = sample_norms(both[use]) + (G.double() ** 2).sum(1).numpy()
+        assert np.all(np.abs(n2.numpy() - want) <= 1e-4 * want)
+        assert torch.allclose(grads[-1][0], (c[:, None] * G).sum(0), rtol=1e-3, atol=1e-5 * G.abs().max().item())
+    # layers without the norms' gradients beside them are refused, not paired with some capture's
+    with pytest.raises(ValueError):
+        drv.private_grads(list(both[0]), 7)
+    with pytest.raises(ValueError):
+        drv.estimate(both[0][:3], 7)
+    same = drv.private_grads(dpsgd.Pairs(list(both[0]), both[0].vectors), 7)
+    assert torch.equal(same[0], alone[0][0])
+    drv.remove_hooks()
