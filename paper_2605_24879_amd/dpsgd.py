@@ -180,6 +180,8 @@ class DPSGDRC:
             E = E[:len(self._S)]
             if any(e is None for e in E) or self._G is None or len(self._filled) < len(self.norms):
                 raise RuntimeError("a trained layer or norm has no part in the loss")
+            if any(e.shape[0] != self._G.shape[0] for e in E):
+                raise RuntimeError(f"the norms saw a batch of {self._G.shape[0]} samples, the layers another")
         # token-row layouts for the library (no copy when already so; layers fed the
         # same activations keep one pointer, so they share a pass over A)
         pairs = Pairs(((_rows(self._A[j].detach()), _rows(E[j]), j) for j in range(len(self.linears))), self._G)
@@ -193,6 +195,8 @@ class DPSGDRC:
         G = getattr(pairs, "vectors", None)
         if G is None:
             raise ValueError("pairs must be what capture returned, the norms' per-sample gradients with the layers'")
+        if any(A.shape[0] != G.shape[0] for (A, _, _) in pairs):
+            raise ValueError(f"the norms' batch of {G.shape[0]} samples is not the layers'")
         return G
 
     def estimate(self, pairs, key):

@@ -112,3 +112,39 @@ def test_each_capture_keeps_its_own_norm_gradients():
     same = drv.private_grads(dpsgd.Pairs(list(both[0]), both[0].vectors), 7)
     assert torch.equal(same[0], alone[0][0])
     drv.remove_hooks()
+
+
+class Flattened(torch.nn.Module):
+    """A junction that is handed all samples' rows as one sample's."""
+
+    def __init__(self, inner):
+        super().__init__()
+        self.inner = inner
+
+    def forward(self, x, res=None):
+        B, T, n = x.shape
+        y, s = self.inner(x.reshape(1, B * T, n), None if res is None else res.reshape(1, B * T, n))
+        return y.view(B, T, n), s.view(B, T, n)
+
+
+def test_norms_that_see_another_batch_are_refused():
+    # their per-sample gradients would have one row for three samples, and so would n2
+    model = stack()
+    norms, tok = model.norms(), tokens()
+    for b in model.blocks:
+        b.norm1, b.norm2 = Flattened(b.norm1), Flattened(b.norm2)
+    model.norm = Flattened(model.norm)
+    drv = driver(model, norms=norms)
+    with pytest.raises(RuntimeError, match="batch"):
+        drv.capture(loss_of(model, tok))
+    assert all(m.sink is None for m in norms)
+    with pytest.raises(RuntimeError, match="batch"):
+        drv.step(loss_of(model, tok))
+    drv.remove_hooks()
+    model = stack()
+    drv = driver(model)
+    three, two = (drv.capture(loss_of(model, tokens(B)))[1] for B in (3, 2))
+    for f in (lambda pairs: drv.estimate(pairs, 7), lambda pairs: drv.clipped_sums(pairs, torch.ones(3))):
+        with pytest.raises(ValueError, match="batch"):
+            f(dpsgd.Pairs(three, two.vectors))
+    drv.remove_hooks()
