@@ -215,7 +215,7 @@ class DPSGDRC:
         n2, c = self.estimate(pairs, key)
         grads = self.clipped_sums(pairs, c)
         if noise and self.sigma > 0:
-            for j, g in enumerate(grads):
+            for j, g in zip([j for (_, _, j) in pairs] + [len(self.linears)], grads):
                 D.dprc_add_noise(g, self.sigma, self.C, key, j)
         return n2, c, grads
 

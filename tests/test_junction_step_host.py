@@ -148,3 +148,21 @@ def test_norms_that_see_another_batch_are_refused():
         with pytest.raises(ValueError, match="batch"):
             f(dpsgd.Pairs(three, two.vectors))
     drv.remove_hooks()
+
+
+@pytest.mark.parametrize("norms", [False, True])
+def test_noise_goes_by_the_layer(norms):
+    # the noise of a layer is keyed by its number, whichever layers a call has and in whatever order: parts of a
+    # step must not share their noise
+    model = stack()
+    drv = driver(model, sigma=0.7, **({} if norms else dict(norms=())))
+    _, pairs = drv.capture(loss_of(model, tokens()))
+    nl = len(pairs)
+    for order in ([4], [2, 0, 7], list(range(nl))[::-1]):
+        part = dpsgd.Pairs([pairs[j] for j in order], pairs.vectors)
+        _, c, noisy = drv.private_grads(part, 9)
+        for g, clean, j in zip(noisy, drv.clipped_sums(part, c), order + [nl] * norms):
+            want = est.add_noise(est.as_f64(clean), 0.7, 0.5, 9, j)
+            assert np.max(np.abs(est.as_f64(g) - want)) <= 1e-6 * np.max(np.abs(want)), j
+        assert len(noisy) == len(order) + norms
+    drv.remove_hooks()
