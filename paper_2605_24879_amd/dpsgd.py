@@ -121,6 +121,8 @@ class DPSGDRC:
             return
         if len({q.dtype for q in params}) != 1:
             raise ValueError("the norms' parameters must share a dtype")
+        if len({id(q) for q in params}) != len(params):
+            raise ValueError("a parameter is listed twice: norms that share parameters cannot be trained")
         flat = torch.cat([q.detach().reshape(-1) for q in params])
         self.vec_master = flat.float().view(1, -1)
         self.vec_w = flat if flat.dtype == torch.bfloat16 else None

@@ -166,3 +166,16 @@ def test_noise_goes_by_the_layer(norms):
             assert np.max(np.abs(est.as_f64(g) - want)) <= 1e-6 * np.max(np.abs(want)), j
         assert len(noisy) == len(order) + norms
     drv.remove_hooks()
+
+
+def test_shared_norm_parameters_are_refused():
+    # each listed parameter has gradients and a master of its own: one that two modules share would be trained
+    # on half of its gradient and count wrongly in the norms
+    a, b = junction.Junction(8), junction.Junction(8)
+    b.weight = a.weight
+    held = a.weight.data_ptr()
+    for norms in ([a, b], [a, a]):
+        with pytest.raises(ValueError):
+            dpsgd.DPSGDRC([], C=1.0, sigma=0.0, norms=norms)
+    assert a.weight.data_ptr() == held
+    dpsgd.DPSGDRC([], C=1.0, sigma=0.0, norms=[a, junction.Junction(8)])
