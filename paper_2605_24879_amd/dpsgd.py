@@ -26,7 +26,7 @@ Per step:
 
 Only the listed linear layers are trained, and the norms given as ``norms``;
 every other parameter (embedding, other norms) is held fixed.  Probes, noise
-and the dropout masks of the norms and of the ``dropouts`` are keyed by a
+and the masks of every ``junction`` module that the loss runs are keyed by a
 per-step seed derived from (seed, step), so they are fresh every step.
 
 With ``norms`` (``junction.Junction`` modules), step 2 goes on through the first
@@ -40,6 +40,7 @@ more layer, without weight decay.
 import torch
 
 from . import dprc as D
+from . import junction
 
 _GOLDEN = 0x9E3779B97F4A7C15
 
@@ -74,7 +75,8 @@ class DPSGDRC:
     noise multiplier.  AdamW hyper-parameters as in ``torch.optim.AdamW``.
     ``norms``: the ``junction.Junction`` modules whose weights and biases are
     trained too (parameters of one dtype; they become views of one buffer).
-    ``dropouts``: ``junction.Dropout`` modules, whose masks change with the step.
+    ``junction`` modules that run in a step take its key for their masks; those in
+    ``dropouts`` (and ``norms``) do so also where a caller has set their ``seed``.
     """
 
     def __init__(self, linears, C, sigma, estimator="hutch", k=16, probe="rademacher", s=16, r=32,
@@ -163,18 +165,20 @@ class DPSGDRC:
         """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs, with the norms' per-sample gradients
         beside them (``Pairs``)."""
         self._G = None
-        for m, sink in zip(self.norms, self._sinks):
-            m.seed, m.sink = step_seed(self.seed, self.steps), sink
-        for m in self.dropouts:
-            m.seed = step_seed(self.seed, self.steps)
+        key = step_seed(self.seed, self.steps)
         try:
-            losses = loss_fn()
-            if losses.dim() != 1:
-                raise ValueError("loss_fn must return per-sample losses [B]")
-            # the norms' weights are listed for the backward pass to reach every norm; their own
-            # gradients go to the rows of self._G
-            E = torch.autograd.grad(losses.sum(), self._S + [m.weight for m in self.norms],
-                                    allow_unused=bool(self.norms))
+            with junction.step_key(key):
+                for m, sink in zip(self.norms, self._sinks):
+                    m.seed, m.sink = key, sink
+                for m in self.dropouts:
+                    m.seed = key
+                losses = loss_fn()
+                if losses.dim() != 1:
+                    raise ValueError("loss_fn must return per-sample losses [B]")
+                # the norms' weights are listed for the backward pass to reach every norm; their own
+                # gradients go to the rows of self._G
+                E = torch.autograd.grad(losses.sum(), self._S + [m.weight for m in self.norms],
+                                        allow_unused=bool(self.norms))
         finally:
             for m in self.norms:
                 m.sink = None

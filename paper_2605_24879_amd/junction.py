@@ -10,9 +10,12 @@ parameters' ordinary gradient.
 ``Dropout`` is the same dropout on its own, inside a branch or with a residual that no norm follows.
 
 The dropout mask is a function of (seed, site, row, column) and is made again in the backward pass.
-``seed`` is an attribute: the step sets it to its key; without a step the caller changes it from one
-training step to the next.
+``seed`` is an attribute: every module that runs in a private step takes the step's key, unless its
+caller has set another; without a step the caller changes it from one training step to the next.
 """
+
+import contextlib
+import threading
 
 import torch
 import torch.nn as nn
@@ -20,6 +23,39 @@ import torch.nn as nn
 from . import dprc as D
 
 _KINDS = {"layer": D.LAYERNORM, "rms": D.RMSNORM}
+
+
+_step = threading.local()               # key: that of the private step under way on this thread
+
+
+@contextlib.contextmanager
+def step_key(key):
+    """Within: the key of every module's mask, but those whose seed the caller has set."""
+    outer, _step.key = getattr(_step, "key", None), key
+    try:
+        yield
+    finally:
+        _step.key = outer
+
+
+class _Keyed(nn.Module):
+    """A module with a dropout mask of key ``seed``."""
+
+    _seed, _own = 0, False              # the key; whether the caller has set it
+
+    @property
+    def seed(self):
+        return self._seed
+
+    @seed.setter
+    def seed(self, value):
+        self._seed, self._own = value, value != getattr(_step, "key", None)
+
+    def mask_seed(self):
+        key = getattr(_step, "key", None)
+        if key is not None and not self._own:
+            self._seed = key
+        return self._seed
 
 
 def token_rows(x):
@@ -33,10 +69,11 @@ def token_rows(x):
 class _JunctionFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, res, weight, bias, mod, p):
-        y, s, mean, rstd = D.dprc_layernorm(x, weight, bias, eps=mod.eps, kind=mod.kind, res=res, p=p, seed=mod.seed,
+        seed = mod.mask_seed()
+        y, s, mean, rstd = D.dprc_layernorm(x, weight, bias, eps=mod.eps, kind=mod.kind, res=res, p=p, seed=seed,
                                             site_id=mod.site_id)
         ctx.save_for_backward(s, weight, mean, rstd)
-        ctx.mod, ctx.p, ctx.seed, ctx.has_res, ctx.has_bias = mod, p, mod.seed, res is not None, bias is not None
+        ctx.mod, ctx.p, ctx.seed, ctx.has_res, ctx.has_bias = mod, p, seed, res is not None, bias is not None
         ctx.set_materialize_grads(False)
         return (y,) if s is x else (y, s)
 
@@ -62,7 +99,7 @@ class _JunctionFn(torch.autograd.Function):
         return dx if dh is None else dh, dx if ctx.has_res else None, gw, gb, None, None
 
 
-class Junction(nn.Module):
+class Junction(_Keyed):
     """Dropout, residual sum and norm of [B, T, n] token rows: ``y, s = junction(x, res)``.
 
     ``kind``: "layer" (with a bias unless ``bias`` is false) or "rms" (none).  ``p``: dropout rate,
@@ -74,7 +111,6 @@ class Junction(nn.Module):
         self.kind, self.eps, self.p, self.site_id = _KINDS[kind], float(eps), float(p), int(site_id)
         self.weight = nn.Parameter(torch.ones(n))
         self.bias = nn.Parameter(torch.zeros(n)) if kind == "layer" and bias else None
-        self.seed = 0
         self.sink = None                  # a private step's: B -> (dw, db) rows to write
 
     def parameters_in_order(self):
@@ -86,7 +122,7 @@ class Junction(nn.Module):
         res = None if res is None else token_rows(res)
         if not torch.is_grad_enabled():
             y, s, _, _ = D.dprc_layernorm(x, self.weight, self.bias, eps=self.eps, kind=self.kind, res=res, p=p,
-                                          seed=self.seed, site_id=self.site_id, stats=False)
+                                          seed=self.mask_seed(), site_id=self.site_id, stats=False)
             return y, s
         out = _JunctionFn.apply(x, res, self.weight, self.bias, self, p)
         return out if len(out) == 2 else (out[0], x)
@@ -105,14 +141,14 @@ class _DropoutFn(torch.autograd.Function):
         return dx, dy if ctx.has_res else None, None, None, None
 
 
-class Dropout(nn.Module):
+class Dropout(_Keyed):
     """Dropout of [B, T, n] token rows, and the residual added: ``res + dropout(x)`` (x itself where there is
     neither).  Nothing is kept for the backward pass.  ``p``, in training only, ``site_id`` and ``seed`` as in
     ``Junction``."""
 
     def __init__(self, p, site_id=0):
         super().__init__()
-        self.p, self.site_id, self.seed = float(p), int(site_id), 0
+        self.p, self.site_id = float(p), int(site_id)
 
     def forward(self, x, res=None):
         p = self.p if self.training else 0.0
@@ -120,6 +156,7 @@ class Dropout(nn.Module):
             return x
         x = token_rows(x)
         res = None if res is None else token_rows(res)
+        seed = self.mask_seed()
         if not torch.is_grad_enabled():
-            return D.dprc_dropout(x, p, self.seed, self.site_id, res=res)
-        return _DropoutFn.apply(x, res, p, self.seed, self.site_id)
+            return D.dprc_dropout(x, p, seed, self.site_id, res=res)
+        return _DropoutFn.apply(x, res, p, seed, self.site_id)

@@ -179,3 +179,71 @@ def test_shared_norm_parameters_are_refused():
             dpsgd.DPSGDRC([], C=1.0, sigma=0.0, norms=norms)
     assert a.weight.data_ptr() == held
     dpsgd.DPSGDRC([], C=1.0, sigma=0.0, norms=[a, junction.Junction(8)])
+
+
+class Masked(torch.nn.Module):
+    """A dropout and a frozen junction before a trained layer; ``seen`` has their outputs."""
+
+    def __init__(self):
+        super().__init__()
+        self.drop, self.junction = junction.Dropout(0.4, site_id=2), junction.Junction(16, kind="rms", p=0.3, site_id=5)
+        self.lin = torch.nn.Linear(16, 4, bias=False)
+
+    def forward(self, x):
+        d = self.drop(x)
+        y, s = self.junction(d)
+        self.seen = d.detach(), s.detach()
+        return self.lin(y).square().mean((1, 2))
+
+
+def test_every_mask_in_a_step_follows_its_key():
+    # modules that the step was not told of: their masks are the step's, other ones every step
+    model, x = Masked(), 1.0 + torch.rand(2, 5, 16)
+    drv = dpsgd.DPSGDRC([model.lin], C=1.0, sigma=0.0, seed=3)
+    masks = []
+    for step in range(3):
+        drv.steps = step
+        drv.capture(lambda: model(x))
+        key = dpsgd.step_seed(3, step)
+        kept = [torch.from_numpy(J.dropout_factors(key, site, 10, 16, p)).view(2, 5, 16) != 0 for site, p in ((2, 0.4), (5, 0.3))]
+        d, s = model.seen
+        assert torch.equal(d != 0, kept[0]) and torch.equal(s != 0, kept[0] & kept[1])
+        assert model.drop.seed == model.junction.seed == key
+        masks.append(d != 0)
+    assert not torch.equal(masks[0], masks[1]) and not torch.equal(masks[1], masks[2])
+    # a seed that the caller has set is left alone, unless the step was given the module
+    model.drop.seed = 12345
+    drv.capture(lambda: model(x))
+    assert torch.equal(model.seen[0] != 0, torch.from_numpy(J.dropout_factors(12345, 2, 10, 16, 0.4)).view(2, 5, 16) != 0)
+    assert model.drop.seed == 12345 and model.junction.seed == dpsgd.step_seed(3, 2)
+    listed = dpsgd.DPSGDRC([model.lin], C=1.0, sigma=0.0, seed=4, dropouts=[model.drop])
+    listed.capture(lambda: model(x))
+    assert model.drop.seed == model.junction.seed == 4
+    # and is the step's from then on, also in a step that was not given it
+    drv.capture(lambda: model(x))
+    assert model.drop.seed == dpsgd.step_seed(3, 2)
+    # outside a step nothing changes it
+    model.drop.seed = 0
+    model(x)
+    assert model.drop.seed == 0 and torch.equal(model.seen[0] != 0, torch.from_numpy(J.dropout_factors(0, 2, 10, 16, 0.4)).view(2, 5, 16) != 0)
+    drv.remove_hooks(), listed.remove_hooks()
+
+
+def test_a_step_keys_only_what_runs_in_it():
+    # neither another thread's forward pass during the capture, nor any after one that failed
+    import threading
+    model, other, x = Masked(), Masked(), torch.rand(2, 5, 16)
+    drv = dpsgd.DPSGDRC([model.lin], C=1.0, sigma=0.0, seed=3)
+
+    def loss():
+        t = threading.Thread(target=lambda: other(x))
+        t.start()
+        t.join()
+        return model(x)
+    drv.capture(loss)
+    assert model.drop.seed == 3 and other.drop.seed == other.junction.seed == 0
+    with pytest.raises(ZeroDivisionError):
+        drv.capture(lambda: 1 / 0)
+    other(x)
+    assert other.drop.seed == 0
+    drv.remove_hooks()
