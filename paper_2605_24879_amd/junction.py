@@ -69,11 +69,10 @@ def token_rows(x):
 class _JunctionFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, res, weight, bias, mod, p):
-        seed = mod.mask_seed()
-        y, s, mean, rstd = D.dprc_layernorm(x, weight, bias, eps=mod.eps, kind=mod.kind, res=res, p=p, seed=seed,
-                                            site_id=mod.site_id)
+        ctx.args = dict(kind=mod.kind, p=p, seed=mod.mask_seed(), site_id=mod.site_id)
+        y, s, mean, rstd = D.dprc_layernorm(x, weight, bias, eps=mod.eps, res=res, **ctx.args)
         ctx.save_for_backward(s, weight, mean, rstd)
-        ctx.mod, ctx.p, ctx.seed, ctx.has_res, ctx.has_bias = mod, p, seed, res is not None, bias is not None
+        ctx.mod, ctx.has_res, ctx.has_bias = mod, res is not None, bias is not None
         ctx.set_materialize_grads(False)
         return (y,) if s is x else (y, s)
 
@@ -89,9 +88,8 @@ class _JunctionFn(torch.autograd.Function):
         if mod.sink is not None:
             dw, db = mod.sink(B)
             want_w, want_b = True, ctx.has_bias
-        dx, dh, dw, db = D.dprc_layernorm_backward(dy, s, weight, mean, rstd, kind=mod.kind, ds=ds, p=ctx.p,
-                                                   seed=ctx.seed, site_id=mod.site_id, weight_grad=want_w,
-                                                   bias_grad=want_b, dw=dw, db=db)
+        dx, dh, dw, db = D.dprc_layernorm_backward(dy, s, weight, mean, rstd, ds=ds, weight_grad=want_w,
+                                                   bias_grad=want_b, dw=dw, db=db, **ctx.args)
         if mod.sink is None and (want_w or want_b):
             ones = torch.ones(B, dtype=torch.float32, device=s.device)
             gw = D.dprc_clip_accumulate_vectors(dw, ones).to(weight.dtype) if want_w else None

@@ -247,3 +247,27 @@ def test_a_step_keys_only_what_runs_in_it():
     other(x)
     assert other.drop.seed == 0
     drv.remove_hooks()
+
+
+def test_backward_is_of_the_call_that_was_made():
+    # the place and the kind are attributes: a caller may change them between a module's calls, and the
+    # backward pass makes the masks of each call again
+    x, t = torch.randn(2, 5, 16), torch.randn(2, 5, 16)
+    drop, junc = junction.Dropout(0.4), junction.Junction(16, kind="rms", p=0.3)
+
+    def outputs(ins):
+        out = []
+        for k, a in enumerate(ins):
+            junc.site_id, junc.seed, junc.p, junc.kind = 3 + k, 40 + k, 0.3 + 0.2 * k, (dprc.RMSNORM, dprc.LAYERNORM)[k]
+            drop.site_id, drop.seed, drop.p = 7 + k, 50 + k, 0.4 + 0.2 * k
+            out.append(junc(drop(a))[0])
+        return out
+    one_by_one = []
+    for k in range(2):
+        ins = [x.clone().requires_grad_() for _ in range(2)]
+        junc_out = outputs(ins[:k + 1])[k]
+        one_by_one.append(torch.autograd.grad((junc_out * t).sum(), ins[k])[0])
+    ins = [x.clone().requires_grad_() for _ in range(2)]
+    both = torch.autograd.grad(sum((y * t).sum() for y in outputs(ins)), ins)
+    for a, b in zip(both, one_by_one):
+        assert torch.equal(a, b)
