@@ -534,15 +534,16 @@ def dprc_layernorm(x, weight=None, bias=None, eps=1e-5, kind=LAYERNORM, res=None
                    stats=True, y=None, s=None):
     """s = res + dropout(x) and its norm y over the last axis of [B, T, n]: returns (y, s, mean, rstd).
 
-    s is x itself where there is neither res nor dropout.  mean (None for RMSNORM) and rstd are [B*T] fp32,
-    what the backward pass needs besides s; with stats=False both are None.  y and s may be x or res."""
+    s is x itself where there is neither res nor dropout (a new tensor if y is x).  mean (None for RMSNORM) and
+    rstd are [B*T] fp32, what the backward pass needs besides s; with stats=False both are None.  y and s may be
+    x or res."""
     ldx = _token_rows(x, "x")
     ldr = 0 if res is None else _token_rows(res, "res", x)
     L = _ln(x, kind, weight, bias, eps, p, seed, site_id)
     lds = ldy = L.n
     if s is not None:
         lds = _token_rows(s, "s", x)
-    elif res is not None or p > 0.0:
+    elif res is not None or p > 0.0 or (y is not None and y.data_ptr() == x.data_ptr()):
         s = _rows_like(x, ldx)
     if y is None:
         y = _rows_like(x, ldx)

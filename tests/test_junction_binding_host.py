@@ -84,3 +84,18 @@ def test_per_sample_values_need_an_entry_each(calls, layers):
     assert len(calls) == 40
     dprc.dprc_norm_hutch(layers, 4, 0, n2_layers=torch.zeros(2, 4))
     assert calls[-1][0] == "dprc_norm_hutch"
+
+
+def test_the_sum_outlives_a_norm_in_the_inputs_place(calls):
+    # without a residual and dropout s is x, unless y is written over x: then s is a tensor of its own
+    x, v = torch.randn(2, 3, 8), torch.ones(8)
+    was = x.clone()
+    _, s, _, _ = dprc.dprc_layernorm(x, v)
+    assert s is x and calls[-1][1][5] is None
+    for y in (x, x.view(2, 3, 8)):
+        got, s, _, _ = dprc.dprc_layernorm(x, v, y=y)
+        a = calls[-1][1]
+        assert got is y and s.data_ptr() != x.data_ptr() and a[5] == s.data_ptr() and a[7] == x.data_ptr()
+    given = torch.empty_like(x)
+    assert dprc.dprc_layernorm(x, v, y=x, s=given)[1] is given
+    assert torch.equal(x, was)
