@@ -19,6 +19,7 @@ import threading
 
 import torch
 import torch.nn as nn
+from torch.autograd import forward_ad
 
 from . import dprc as D
 
@@ -64,6 +65,14 @@ def token_rows(x):
     (B, T, n), (s0, s1, s2) = x.shape, x.stride()
     ld = s1 if T > 1 else s0 if B > 1 else n
     return x if s2 == 1 and ld >= n and (B == 1 or s0 == T * ld) else x.contiguous()
+
+
+def _recorded(*tensors):
+    """Whether a call goes through autograd: gradients are on, or a tensor has a forward-mode tangent, which
+    autograd refuses and a call past it would drop.  (Outside a dual level, as torch counts them, none has;
+    asking each tensor costs 0.3 us.)"""
+    return torch.is_grad_enabled() or getattr(forward_ad, "_current_level", 0) >= 0 and any(
+        t is not None and forward_ad.unpack_dual(t).tangent is not None for t in tensors)
 
 
 class _JunctionFn(torch.autograd.Function):
@@ -118,7 +127,7 @@ class Junction(_Keyed):
         p = self.p if self.training else 0.0
         x = token_rows(x)
         res = None if res is None else token_rows(res)
-        if not torch.is_grad_enabled():
+        if not _recorded(x, res, self.weight, self.bias):
             y, s, _, _ = D.dprc_layernorm(x, self.weight, self.bias, eps=self.eps, kind=self.kind, res=res, p=p,
                                           seed=self.mask_seed(), site_id=self.site_id, stats=False)
             return y, s
@@ -155,6 +164,6 @@ class Dropout(_Keyed):
         x = token_rows(x)
         res = None if res is None else token_rows(res)
         seed = self.mask_seed()
-        if not torch.is_grad_enabled():
+        if not _recorded(x, res):
             return D.dprc_dropout(x, p, seed, self.site_id, res=res)
         return _DropoutFn.apply(x, res, p, seed, self.site_id)

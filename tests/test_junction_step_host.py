@@ -271,3 +271,23 @@ def test_backward_is_of_the_call_that_was_made():
     both = torch.autograd.grad(sum((y * t).sum() for y in outputs(ins)), ins)
     for a, b in zip(both, one_by_one):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("dual", ["x", "res", "weight", "bias"])
+@pytest.mark.parametrize("grad", [True, False])
+def test_forward_mode_is_refused(dual, grad):
+    # there is no forward-mode rule: an output without its tangent would be taken for a constant
+    import torch.autograd.forward_ad as fw
+    t = dict(x=torch.randn(2, 5, 16), res=torch.randn(2, 5, 16), weight=torch.ones(16), bias=torch.zeros(16))
+    junc, drop = junction.Junction(16), junction.Dropout(0.3)
+    with fw.dual_level(), torch.set_grad_enabled(grad):
+        t[dual] = fw.make_dual(t[dual], torch.ones_like(t[dual]))
+        call = lambda: torch.func.functional_call(junc, {k: t[k] for k in ("weight", "bias")}, (t["x"], t["res"]))
+        with pytest.raises((NotImplementedError, RuntimeError)):
+            call()
+        if dual in ("x", "res"):
+            with pytest.raises((NotImplementedError, RuntimeError)):
+                drop(t["x"], t["res"])
+        plain = {k: fw.unpack_dual(v).primal for k, v in t.items()}
+        y, _ = torch.func.functional_call(junc, {k: plain[k] for k in ("weight", "bias")}, (plain["x"], plain["res"]))
+        assert fw.unpack_dual(y).tangent is None and drop(plain["x"], plain["res"]).shape == (2, 5, 16)
