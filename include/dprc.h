@@ -251,7 +251,9 @@ dprc_status dprc_private_adamw(float* theta, float* m, float* v, int64_t ldt, co
  * (p acts in steps of 2^-16).  A dropped element counts as exactly 0, also where the
  * input is infinite or NaN; a kept one is multiplied by 65536 / (65536 - q).
  * q = 0 leaves the input as it is, q = 65536 drops everything.  The caller folds
- * the training step into `seed` and gives each place in the model its site_id.
+ * the training step into `seed` and gives each place in the model its site_id.  Rows
+ * are counted from 0 in every call: calls on parts of a batch (micro-batches, ranks)
+ * need a seed each, or they share their masks.
  *
  * All arithmetic is in fp32 on inputs of either type, each output rounded once.  Rows
  * may lie at any alignment of their element (16-byte boundaries are fastest).

@@ -161,11 +161,12 @@ class DPSGDRC:
         for h in self._hooks:
             h.remove()
 
-    def capture(self, loss_fn):
+    def capture(self, loss_fn, key=None):
         """Steps 1-2: per-sample losses [B] and the layers' (A, E) pairs, with the norms' per-sample gradients
-        beside them (``Pairs``)."""
+        beside them (``Pairs``).  ``key``: that of the dropout masks, by default the step's.  Masks go by the
+        row of a call, so micro-batches of one step need a key each."""
         self._G = None
-        key = step_seed(self.seed, self.steps)
+        key = step_seed(self.seed, self.steps) if key is None else key
         try:
             with junction.step_key(key):
                 for m, sink in zip(self.norms, self._sinks):

@@ -10,6 +10,7 @@ parameters' ordinary gradient.
 ``Dropout`` is the same dropout on its own, inside a branch or with a residual that no norm follows.
 
 The dropout mask is a function of (seed, site, row, column) and is made again in the backward pass.
+Rows are counted from 0 in every call, so calls on parts of a batch need a seed each.
 ``seed`` is an attribute: every module that runs in a private step takes the step's key, unless its
 caller has set another; without a step the caller changes it from one training step to the next.
 """

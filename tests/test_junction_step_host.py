@@ -291,3 +291,21 @@ def test_forward_mode_is_refused(dual, grad):
         plain = {k: fw.unpack_dual(v).primal for k, v in t.items()}
         y, _ = torch.func.functional_call(junc, {k: plain[k] for k in ("weight", "bias")}, (plain["x"], plain["res"]))
         assert fw.unpack_dual(y).tangent is None and drop(plain["x"], plain["res"]).shape == (2, 5, 16)
+
+
+def test_micro_batches_take_keys_of_their_own():
+    # rows are counted from 0 in every call, so captures under one key have the same masks; with another key they
+    # have others, forwards and backwards
+    model, x = Masked(), 1.0 + torch.rand(2, 5, 16)
+    drv = dpsgd.DPSGDRC([model.lin], C=1.0, sigma=0.0, seed=3, norms=[model.junction])
+    model.junction.p = 0.0
+    E = []
+    for key in (None, dpsgd.step_seed(3, 0), 99):
+        _, pairs = drv.capture(lambda: model(x), **({} if key is None else dict(key=key)))
+        used = dpsgd.step_seed(3, 0) if key is None else key
+        assert model.drop.seed == model.junction.seed == used
+        kept = torch.from_numpy(J.dropout_factors(used, 2, 10, 16, 0.4)).view(2, 5, 16) != 0
+        assert torch.equal(model.seen[0] != 0, kept) and torch.equal(pairs[0][0] != 0, kept)
+        E.append(pairs.vectors)
+    assert torch.equal(E[0], E[1]) and not torch.equal(E[0], E[2])
+    drv.remove_hooks()
