@@ -303,8 +303,12 @@ dprc_status dprc_layernorm(const dprc_ln* L, const void* x, int64_t ldx, const v
  * gradient with respect to s (and so res), dh that with respect to x.  Each of dx, dh,
  * dw, db may be NULL; one at least is not.  dw and db have row stride ldg >= n.  dx or dh
  * may be dy, s or ds (dx and dh must differ).  mean is read for LAYERNORM only; L->bias
- * and L->eps are not read.  Workspace (needed with dw or db):
- * dprc_layernorm_backward_workspace() bytes (0 when the arguments are invalid). */
+ * and L->eps are not read.  With a rounded `sum` beside statistics of the unrounded row,
+ * xh is off by up to 2^-8 |s| rstd in bf16, and dx and dw with it: about their own
+ * rounding where a row's mean is within a few of its spreads, but up to a quarter of a
+ * spread where it is 64 of them.  Such rows are better kept in fp32.  Workspace (needed
+ * with dw or db): dprc_layernorm_backward_workspace() bytes (0 when the arguments are
+ * invalid). */
 size_t dprc_layernorm_backward_workspace(const dprc_ln* L);
 dprc_status dprc_layernorm_backward(const dprc_ln* L, const void* dy, int64_t lddy, const void* s, int64_t lds,
                                     const float* mean, const float* rstd, const void* ds, int64_t ldds, void* dx,

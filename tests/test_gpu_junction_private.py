@@ -1,0 +1,86 @@
+"""The norms' part in a private step's estimates, the masks of modules that a step was not given, and
+the junction's gradient in bf16, on the GPU.
+
+u = 2^-24 and r = 2^-8 are the roundings to fp32 and bf16.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import estimators as est
+from oracle import junction as J
+from oracle.estimators import as_f64
+from workloads import llama
+
+pytestmark = pytest.mark.gpu
+
+U, R = 2.0 ** -24, 2.0 ** -8
+SIZES = dict(layers=2, hidden=128, mlp=256, heads=4, kv_heads=2, vocab=200)
+
+
+@pytest.fixture(scope="module")
+def mods():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2605_24879_amd import dprc, dpsgd, junction
+    dprc.lib()
+    return dprc, dpsgd, junction
+
+
+def _stack(**kw):
+    return llama.build(seed=1, device="cuda", **dict(SIZES, junctions=True, **kw))
+
+
+def _loss(model, tok):
+    return lambda: llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:])
+
+
+def _tokens(B=3, T=40, seed=1):
+    return llama.tokens(B, T, SIZES["vocab"], seed=seed, device="cuda")
+
+
+@pytest.mark.parametrize("kind", ["layer", "rms"])
+@pytest.mark.parametrize("shift", [0.0, 4.0, 64.0])
+def test_module_gradients_in_bf16(mods, kind, shift):
+    """Against the gradient of the forward pass in 64 bits, at the sum as it is before it is rounded.
+
+    The backward pass has that sum rounded to bf16, so xh is off by at most h = r |s| rstd (and the few u of
+    fp32 arithmetic, which 2^-12 of everything covers here): beside a residual far from zero, with a small
+    spread, that is far more than the rounding of the outputs.  dx is rstd (g - mean(g) - xh mean(g xh)) and
+    moves by rstd (h |mean(g xh)| + (|xh| + h) mean(|g| h)), dw by the sum of |dy| h.  The gradients of weight
+    and bias are rounded to bf16 at the end, dx and dh too."""
+    D, _, junction = mods
+    B, T, n, p = 2, 30, 136, 0.2
+    mod = junction.Junction(n, kind=kind, p=p, site_id=3).cuda().bfloat16()
+    mod.seed = 9
+    g = torch.Generator().manual_seed(5)
+    x, res, dy, ds = (torch.randn(B, T, n, generator=g).bfloat16() for _ in range(4))
+    res = (res.float() + shift).bfloat16()
+    with torch.no_grad():
+        mod.weight.copy_(1 + 0.1 * torch.randn(n, generator=g))
+        if mod.bias is not None:
+            mod.bias.copy_(0.1 * torch.randn(n, generator=g))
+    ins = [t.cuda().requires_grad_() for t in (x, res)]
+    y, s = mod(*ins)
+    got = torch.autograd.grad((y.float() * dy.cuda().float()).sum() + (s.float() * ds.cuda().float()).sum(),
+                              ins + mod.parameters_in_order())
+    s64 = J.dropout(x, 9, 3, p, res=res)
+    w64, dy64, ds64 = as_f64(mod.weight), as_f64(dy), as_f64(ds)
+    _, mean, rstd = J.norm(s64, eps=1e-5, rms=kind == "rms")
+    dx, dw, db = J.norm_backward(dy64, s64, w64, mean, rstd, ds=ds64)
+    r3 = rstd.reshape(B, T, 1)
+    xh = (s64 - (0.0 if mean is None else mean.reshape(B, T, 1))) * r3
+    gg = dy64 * w64
+    h = R * np.abs(s64) * r3
+    off = r3 * (h * np.abs((gg * xh).mean(-1, keepdims=True)) + (np.abs(xh) + h) * (np.abs(gg) * h).mean(-1, keepdims=True))
+    small = r3 * (np.abs(gg) + np.abs(gg).mean(-1, keepdims=True) + np.abs(xh) * np.abs(gg * xh).mean(-1, keepdims=True))
+    tol = off + 2.0 ** -12 * (small + np.abs(ds64)) + R * np.abs(dx) + R * off
+    f = J.dropout_factors(9, 3, B * T, n, p).reshape(B, T, n)
+    assert np.all(np.abs(as_f64(got[1]) - dx) <= tol)
+    assert np.all(np.abs(as_f64(got[0]) - f * dx) <= f * tol * (1 + R))
+    dwo = (np.abs(dy64) * h).sum(1)
+    for grad, ref, o, mag in ((got[2], dw, dwo, np.abs(dy64 * xh).sum(1)), (got[3] if len(got) > 3 else None, db, 0.0 * dwo, np.abs(dy64).sum(1))):
+        if grad is not None:
+            ref, o, mag = ref.sum(0), o.sum(0), mag.sum(0)
+            assert np.all(np.abs(as_f64(grad) - ref) <= o * (1 + R) + 2.0 ** -12 * mag + R * np.abs(ref))
