@@ -40,6 +40,29 @@ def _tokens(B=3, T=40, seed=1):
     return llama.tokens(B, T, SIZES["vocab"], seed=seed, device="cuda")
 
 
+@pytest.mark.parametrize("estimator", ["hutch", "hutchpp"])
+@pytest.mark.parametrize("norm", ["rms", "layer"])
+def test_estimates_hold_the_norms_part(mods, norm, estimator):
+    # Beside the linear layers' the norms' squared gradients are small (3e-4 of n2 here), so they are looked for in
+    # the difference that they make: the same pairs and key with and without them.  Each side is a sum of one
+    # term a layer, every partial sum rounded once: 2 (layers + 2) u of n2.
+    D, dpsgd, _ = mods
+    model, key = _stack(norm=norm), 77
+    drv = dpsgd.DPSGDRC(model.linears(), C=0.05, sigma=0.0, k=16, s=4, r=8, estimator=estimator, norms=model.norms())
+    _, pairs = drv.capture(_loss(model, _tokens()))
+    linear = D.dprc_norm_hutch(pairs, 16, key) if estimator == "hutch" else D.dprc_norm_hutchpp(pairs, 4, 8, key)
+    linear = as_f64(linear)
+    for factor in (1.0, 100.0):                                        # as they are, and as most of n2
+        pairs.vectors.mul_(factor)
+        part = J.norm_vectors(pairs.vectors)
+        n2, c = drv.estimate(pairs, key)
+        tol = 2 * (len(pairs) + 2) * U * (linear + part)
+        assert np.all(part > 20 * tol) and (factor == 1.0 or np.all(part > linear))
+        assert np.all(np.abs(as_f64(n2) - linear - part) <= tol)
+        assert np.allclose(as_f64(c), est.clip_scale(linear + part, 0.05), rtol=1e-5)
+    drv.remove_hooks()
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("shift", [0.0, 4.0, 64.0])
 def test_module_gradients_in_bf16(mods, kind, shift):
