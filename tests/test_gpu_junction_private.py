@@ -107,3 +107,33 @@ def test_module_gradients_in_bf16(mods, kind, shift):
         if grad is not None:
             ref, o, mag = ref.sum(0), o.sum(0), mag.sum(0)
             assert np.all(np.abs(as_f64(grad) - ref) <= o * (1 + R) + 2.0 ** -12 * mag + R * np.abs(ref))
+
+
+def test_gradients_of_rows_past_32_bit_elements(mods):
+    """More than 2^32 elements: every part of dw and db counts.
+
+    2^27 + 5 rows of 40 in bf16 are dealt to 768 workgroups, 32 rows a round: 5462 rounds each.  A column's chain is
+    those, 3 sums over lanes, 3 over waves, then 48 parts and 16 groups: under 5600 roundings.  The terms are off by 4 u
+    each (xh; 8 allowed).  A part that were lost, or counted twice, is 1 / 768 of the sums, whose terms hardly
+    cancel: half of the rows are the others' negatives, and dy follows s about a mean of its own."""
+    D, _, _ = mods
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 60 << 30:
+        pytest.skip("needs 60 GiB of free memory")
+    rows, n = (1 << 27) + 5, 40
+    g = torch.Generator().manual_seed(2)
+    base = torch.randn(32, n, generator=g).bfloat16()
+    base = torch.cat([base, -base])
+    grad = (3.0 * base.float() + 3.0).bfloat16()
+    _, m64, r64 = J.norm(base.view(1, 64, n))
+    m32, r32 = torch.from_numpy(m64).float(), torch.from_numpy(r64).float()
+    tile = lambda t: t.cuda().repeat((rows + 63) // 64, *(1,) * (t.dim() - 1))[:rows]
+    dx, _, dw, db = D.dprc_layernorm_backward(tile(grad).view(1, rows, n), tile(base).view(1, rows, n), None, tile(m32), tile(r32))
+    del dx
+    xh = (as_f64(base) - as_f64(m32)[:, None]) * as_f64(r32)[:, None]
+    full, tail = rows // 64, rows % 64
+    for got, terms in ((dw, as_f64(grad) * xh), (db, as_f64(grad))):
+        want, mag = (full * t.sum(0) + t[:tail].sum(0) for t in (terms, np.abs(terms)))
+        tol = (5600 + 8) * U * mag
+        assert np.all(np.abs(want) / 768 > 1.5 * tol)
+        assert np.all(np.abs(as_f64(got)[0] - want) <= tol)
