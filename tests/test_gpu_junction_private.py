@@ -63,6 +63,58 @@ def test_estimates_hold_the_norms_part(mods, norm, estimator):
     drv.remove_hooks()
 
 
+def test_captures_do_not_mix(mods):
+    D, dpsgd, _ = mods
+    model = _stack(norm="layer")
+    drv = dpsgd.DPSGDRC(model.linears(), C=0.05, sigma=0.0, k=16, norms=model.norms())
+    toks = _tokens(3, seed=1), _tokens(2, seed=2)
+    alone = [drv.private_grads(drv.capture(_loss(model, t))[1], 5) for t in toks]
+    both = [drv.capture(_loss(model, t))[1] for t in toks]
+    for use in (0, 1, 0):
+        n2, c, grads = drv.private_grads(both[use], 5)
+        for a, b in zip((n2, c, *grads), (*alone[use][:2], *alone[use][2])):
+            assert torch.equal(a, b)
+    with pytest.raises(ValueError):
+        drv.private_grads(list(both[0]), 5)
+    drv.remove_hooks()
+
+
+def test_masks_of_modules_that_the_step_was_not_given(mods):
+    # norms= alone: the MLP's dropouts run under the step's key too, and so do junctions when nothing is listed
+    D, dpsgd, _ = mods
+    p = 0.25
+    for listed in (True, False):
+        model, tok = _stack(dropout=p), _tokens()
+        drv = dpsgd.DPSGDRC(model.linears(), C=1.0, sigma=0.0, seed=4, norms=model.norms() if listed else ())
+        seen, sums = [], []
+        hooks = [model.blocks[1].down.register_forward_hook(lambda m, i, o: seen.append(i[0].detach())),
+                 model.blocks[0].norm1.register_forward_hook(lambda m, i, o: sums.append(o[1].detach()))]
+        for step in range(2):
+            key = dpsgd.step_seed(4, step)
+            drv.step(_loss(model, tok))
+            for a, m in ((seen[-1], model.blocks[1].act_drop), (sums[-1], model.blocks[0].norm1)):
+                B, T, n = a.shape
+                dropped = torch.from_numpy(J.dropout_factors(key, m.site_id, B * T, n, p) == 0).view(B, T, n).cuda()
+                assert m.seed == key and (a[dropped] == 0).all() and (a[~dropped] != 0).float().mean() > 0.99
+        assert not torch.equal(seen[0] == 0, seen[1] == 0)
+        for h in hooks:
+            h.remove()
+        drv.remove_hooks()
+
+
+def test_norm_over_its_input(mods):
+    # y in x's place: s is kept apart, and the gradient is that of the call with y elsewhere
+    D, _, _ = mods
+    for dtype, n in ((torch.bfloat16, 200), (torch.float32, 75)):
+        x, w = torch.randn(3, 17, n, device="cuda").to(dtype), torch.randn(n, device="cuda").to(dtype)
+        y, s, mean, rstd = D.dprc_layernorm(x, w)
+        a = x.clone()
+        y1, s1, m1, r1 = D.dprc_layernorm(a, w, y=a)
+        assert y1 is a and torch.equal(y1, y) and torch.equal(s1, x) and torch.equal(m1, mean) and torch.equal(r1, rstd)
+        for u, v in zip(D.dprc_layernorm_backward(y, s, w, mean, rstd), D.dprc_layernorm_backward(y, s1, w, m1, r1)):
+            assert (u is None and v is None) or torch.equal(u, v)
+
+
 @pytest.mark.parametrize("kind", ["layer", "rms"])
 @pytest.mark.parametrize("shift", [0.0, 4.0, 64.0])
 def test_module_gradients_in_bf16(mods, kind, shift):
