@@ -26,7 +26,8 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_kernel(NormArgs a)
   constexpr bool kHold = TPR < 1024;
   constexpr int kAhead = C == 8 ? 2 : 1;                          // rows loading ahead
   // fp32 rows of 1024 threads: 128 registers are too few for a row ahead (2048 x 16384 with residual and
-  // sum 103 us without, 113 with it and spilled registers; bf16, which has them, 94 with it)
+  // sum 103 us without, 113 with it; bf16 4096 x 16384, which has them, 94 with it), and for the row itself:
+  // without one ahead these instances still spill 10 to 30 registers, bf16 ones none
   constexpr bool kLean = TPR == 1024 && sizeof(E) == 4;
   typedef RowSum<TPR, 1, BLK> Sum;
   __shared__ typename Sum::Buffer buf;

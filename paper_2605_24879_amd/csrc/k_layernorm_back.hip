@@ -3,8 +3,8 @@
 //
 // With xh = (s - mu) rstd and g = dy w: dx = ds + rstd (g - mean(g) - xh mean(g xh)), dh = m dx, and for
 // each sample dw = sum dy xh, db = sum dy.  Everything is fp32 but s itself, which the forward pass rounded
-// to the tensors' type after its statistics were taken (a second tensor of fp32 would cost as much traffic
-// as all of dy and dx in bf16): xh is off by that rounding times rstd.
+// to the tensors' type after its statistics were taken (s in fp32 would add as much traffic as dy
+// and dx have in bf16): xh is off by that rounding times rstd.
 //
 // Bounded by memory: one pass over dy, s and ds writes dx and dh and sums dw and db on the way.  8 x 4096 x
 // 2048 bf16 with everything takes 132 to 134 us, 5.1 TB/s, and 4 us to join the parts of dw and db; HBM
@@ -49,9 +49,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void norm_back_kernel(NormBa
   constexpr int G = SOLO ? 1 : (TPR < 64 ? BLK / 64 : RPB);      // sums to combine in LDS
   constexpr int kAhead = V <= 2 ? 2 : 1;                          // rows loading ahead
   // Rows of 1024 threads have 128 registers each, too few for dw and db, which lie in LDS (every thread its
-  // own words), for the weights and for a row ahead.  4096 x 16384 bf16 (dy, s, dx) takes 104 us and
-  // 2048 x 16384 fp32 99, where two passes over the rows took 168 and 167 (9000 columns: 137 and 99
-  // against 182 and 164).
+  // own words), for the weights and for a row ahead (bf16 does without one too, in 91 to 122 registers).
+  // 4096 x 16384 bf16 (dy, s, dx, dw, db) takes 104 to 109 us and 2048 x 16384 fp32 98 to 101, where two passes
+  // over the rows took 168 and 167 (as many elements in rows of 9000: 137 and 100 against 182 and 164).
+  // With more tensors, us (each once at 5.4 TB/s: 99, 99, 124):
+  //            ds     dh     both
+  //   bf16    130    133     157
+  //   fp32    128    147     178     (28 registers spill with dh, 54 with both)
   constexpr bool kLean = TPR == 1024;
   typedef RowSum<TPR, 2, BLK> Sum;
   __shared__ typename Sum::Buffer buf;
@@ -400,7 +404,9 @@ NormBackPlan norm_back_plan(int64_t B, int64_t T, int64_t n, int64_t elem_bytes,
   sp.total = B * sp.rounds;
   // Few rounds a sample, or many samples: none is cut.  (A cut costs a launch to join the parts, 3.5 us on
   // the GPU and as much on the host, as the four or five rounds that it saves: 4 x 12 x 2048 took 12.4 us
-  // whole and 9.8 cut, 4 x 8 x 2048 9.2 and 9.8.)
+  // whole and 9.8 cut, 4 x 8 x 2048 9.2 and 9.8.  Of many samples whole ones gain where they come out even over
+  // the workgroups, and lose where not, samples x 300 x 512 bf16: 1023 cut 207 us; whole 1024 194, 1025 233, 1280
+  // 294, 1500 298, 2048 382, 2049 417.)
   sp.samples = sp.rounds <= 12 || B >= 1024 ? B : 0;
   if (p.solo) sp.blocks = std::min<int64_t>(ceil_div(B, (int64_t)p.at_once), 1024);
   else if (sp.samples) sp.blocks = std::min<int64_t>(B, 1024);

@@ -45,9 +45,12 @@ inline int64_t streaming_blocks(int64_t ahead) {
 
 // Whether a call streams past the caches.  8 x 4096 x 2048 bf16: dropout (403 MB) 68 us with non-temporal
 // accesses, 74 without; the fused norm (537 MB) 91 and 96, and a product with y that follows takes no
-// longer.  4 x 4096 x 2048: the norm (268 MB) 45.5 and 44; 4 x 2048 x 2048 (134 MB): 26 and 23.6.  Not for
-// rows that share lines (97 fp32 columns backwards, 533 MB: 128 us and 109), and not for the backward pass,
-// whose five streams took 133 to 157 us with them and 133 to 140 without, by where the tensors lay.
+// longer.  4 x 4096 x 2048: the norm (268 MB) 45.5 and 44; 4 x 2048 x 2048 (134 MB): 26 and 23.6.
+// Over 320 to 1000 MiB of both types, 512 to 16384 columns, times without against times with: dropout 7 to
+// 11% longer; the norm with residual, dropout and sum 1% shorter to 9% longer; the norm alone 3% shorter
+// (bf16 of 4096 columns, either type of 16384, from 540 MiB on) to 8% longer.
+// Not for rows that share lines (97 fp32 columns backwards, 533 MB: 128 us and 109), and not for the backward
+// pass, whose five streams took 133 to 157 us with them and 133 to 140 without, by where the tensors lay.
 constexpr int64_t kStreamRowsBytes = (int64_t)300 << 20;
 struct StreamRows {
   int64_t width, total = 0;      // bytes of a row's columns; of all tensors
