@@ -174,8 +174,8 @@ def _workspace(nbytes, dev, ws):
     if ws is not None:
         if not ws.is_cuda:
             raise ValueError("the workspace must be a GPU tensor")
-        if ws.numel() * ws.element_size() < nbytes:
-            raise ValueError("workspace too small")
+        if ws.numel() * ws.element_size() < nbytes or not ws.is_contiguous():
+            raise ValueError(f"the workspace must hold {nbytes} contiguous bytes")
         return ws
     return torch.empty(max(int(nbytes), 1), dtype=torch.uint8, device=dev)
 

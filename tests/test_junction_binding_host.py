@@ -99,3 +99,13 @@ def test_the_sum_outlives_a_norm_in_the_inputs_place(calls):
     given = torch.empty_like(x)
     assert dprc.dprc_layernorm(x, v, y=x, s=given)[1] is given
     assert torch.equal(x, was)
+
+
+def test_a_workspace_has_to_hold_its_bytes(monkeypatch):
+    # many entries over few bytes are no workspace
+    monkeypatch.setattr(torch.Tensor, "is_cuda", property(lambda t: True))
+    fine = torch.zeros(64)
+    assert dprc._workspace(256, None, fine) is fine and dprc._workspace(256, None, torch.zeros(2, 40)).numel() == 80
+    for bad in (torch.zeros(1).expand(64), torch.zeros(1, 16).expand(4, 16), torch.zeros(128)[::2], torch.zeros(63)):
+        with pytest.raises(ValueError):
+            dprc._workspace(256, None, bad)
