@@ -331,6 +331,121 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
                                          float* grad, int32_t accumulate, void* ws, size_t ws_bytes,
                                          hipStream_t stream);
 
+/* ---- output head: cross entropy over a vocabulary, without its logits ---------------
+ * The loss of a bias-free head S = h W^T with V outputs (the last layer of Algorithm 1's model) and the
+ * gradients that it starts, with the logits l_tv = <h_t, W_v> formed in matrix-core tiles only:
+ *   lse_t = log sum_v exp l_tv,  loss_t = lse_t - l_t,y(t)                        (dprc_head_loss)
+ *   E_tv = g_t (exp(l_tv - lse_t) - [v = y(t)]),  g_t = dL/dloss_t               (dprc_head_errors)
+ *   dh = E W,  dW = E^T h,  every sample's squared norm of h_i^T E_i             (dprc_head_backward)
+ *   grad = sum_i c_i h_i^T E_i                                                   (dprc_head_clip_accumulate)
+ * for the same lse and g.  A token with a negative target has no loss: loss_t = 0 and E_t = 0, and neither
+ * h_t nor g_t (NaN, say) reaches any output but lse_t.  A target of V or more makes loss_t and lse_t NaN, and
+ * with that lse every gradient of the token.  Products are summed in fp32, exponentials taken in fp32; E is
+ * rounded to the head's dtype once (as the gradient of stored logits is), then enters the products.
+ *
+ * The last four go through the vocabulary in pieces of `piece` columns, of which E is held in the workspace:
+ * a positive multiple of DPRC_HEAD_BLOCK, or 0 for as many as E of 1 GiB holds (at least one block).  dh, dW
+ * and grad do not depend on it beyond the rounding of their fp32 sums.
+ *
+ * Estimates: for the norms the head counts as ceil(V / DPRC_HEAD_BLOCK) layers of DPRC_HEAD_BLOCK outputs each,
+ * with probes of their own (layer ids layer_id, layer_id + 1, ...): their gradients are disjoint columns of
+ * the head's, so that the squared norms add up, and the estimate is that of dprc_norm_hutch for these
+ * layers.
+ *
+ *   h       [B,T,d] token rows (stride ldh), W [V,d] rows (stride ldw), both of `dtype`; any alignment of
+ *           the element.  bf16 rows of W on 16-byte boundaries with d a multiple of 8 are faster.
+ *   target  [B*T] int64.  loss, lse, g: [B*T] fp32.
+ *   dh      [B,T,d] token rows of `dtype`, may be NULL; dW [V,d] rows of `dtype`, may be NULL.  Neither may
+ *           overlap an input.
+ *   norms   may be NULL: k, probe, seed, side, n2 and accumulate as in dprc_norm_hutch.
+ *   c       [B] fp32.  grad [d,V] fp32, row stride ldg, (=|+=) by accumulate: the layout of
+ *           dprc_clip_accumulate.
+ *   E       (dprc_head_errors) [B,T,nv] token rows of `dtype`, stride lde: the columns v0 .. v0 + nv of E.
+ * B <= 65535, B*T <= 2^31, d and V <= 2^30, d*V <= 2^40. */
+#define DPRC_HEAD_BLOCK 8192
+typedef struct {
+  const void* h;
+  const void* W;
+  const int64_t* target;
+  int64_t B, T, d, V;     /* all >= 1 */
+  int64_t ldh, ldw;
+  dprc_dtype dtype;
+  int64_t piece;
+} dprc_head;
+typedef struct {
+  int32_t k;
+  dprc_probe probe;
+  uint64_t seed;
+  dprc_side side;
+  uint32_t layer_id;
+  float* n2;              /* [B] */
+  int32_t accumulate;
+} dprc_head_norms;
+size_t dprc_head_loss_workspace(const dprc_head* H);
+dprc_status dprc_head_loss(const dprc_head* H, float* loss, float* lse, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+size_t dprc_head_errors_workspace(const dprc_head* H);
+dprc_status dprc_head_errors(const dprc_head* H, const float* lse, const float* g, int64_t v0, int64_t nv,
+                             void* E, int64_t lde, void* ws, size_t ws_bytes, hipStream_t stream);
+/* dh, dW: whether they are wanted; norms: its k, probe and side. */
+size_t dprc_head_backward_workspace(const dprc_head* H, int32_t dh, int32_t dW, const dprc_head_norms* norms);
+dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float* g, void* dh, int64_t lddh,
+                               void* dW, int64_t lddw, const dprc_head_norms* norms, void* ws, size_t ws_bytes,
+                               hipStream_t stream);
+size_t dprc_head_clip_accumulate_workspace(const dprc_head* H);
+dprc_status dprc_head_clip_accumulate(const dprc_head* H, const float* lse, const float* g, const float* c,
+                                      float* grad, int64_t ldg, int32_t accumulate, void* ws, size_t ws_bytes,
+                                      hipStream_t stream);
+
+/* ---- rotary positions -----------------------------------------------------------------
+ * The pairs (a, b) of the first 2 r features of every head, turned by the angle position * freqs[j], j < r:
+ *   a' = scale (a cos - b sin),  b' = scale (b cos + a sin);   inverse != 0: -sin for sin.
+ * Pair j is the features (j, r + j), or (2 j, 2 j + 1) with interleaved != 0; features from 2 r on are copied.
+ * The inverse call is the transpose: applied to a gradient it is the backward pass.
+ *   freqs   [r] fp64, radians a position (scaled for long contexts or not, as the caller likes), device.
+ *   pos     [B*T] int64 positions, device; NULL: start + t.  The angle is formed and reduced in fp64.
+ *   x       `count` (1 to 4) tensors [B,T,H,D], elements of x dtype at x + b*xb + t*xt + h*xh + feature, to y
+ *           likewise (ydtype).  y may be x (with its dtype and strides); otherwise outputs overlap neither
+ *           inputs nor each other.
+ * B*T <= 2^31, 1 <= 2 r <= D <= 2^20, r <= 4096, at most 2^16 heads in all. */
+typedef struct {
+  int64_t B, T;
+  int32_t D, r;
+  const double* freqs;
+  const int64_t* pos;
+  int64_t start;
+  float scale;
+  int32_t interleaved, inverse;
+  dprc_dtype xdtype, ydtype;
+} dprc_rope;
+typedef struct {
+  const void* x;
+  void* y;
+  int64_t H, xb, xt, xh, yb, yt, yh;
+} dprc_heads;
+dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t count, hipStream_t stream);
+
+/* ---- the joint norm of many tensors, and clipping ---------------------------------------
+ * dprc_grad_norm: norm[0] = sqrt(sum over the tensors of x^2).  dprc_grad_clip: out = c x for every tensor, c =
+ * min(1, max_norm / norm), and norm[0] (norm may be NULL).  Of a private gradient with its noise this is
+ * post-processing, which costs no privacy.  Squares are summed in fp64 in a fixed order; a norm that is not
+ * finite gives c = 0: zeros, as dprc_clip_scale does for such a sample.  Each tensor is rows x cols
+ * elements of its own dtype, rows ldx apart, to out (row stride ldo, may be x with ldo = ldx; NULL in
+ * dprc_grad_norm); outputs overlap nothing else.  A tensor may be empty (rows or cols 0).  The array is HOST
+ * memory, read during the call.  max_norm > 0 and finite; rows and cols <= 2^40.  Workspace:
+ * dprc_grad_norm_workspace() bytes. */
+typedef struct {
+  const void* x;
+  void* out;
+  int64_t rows, cols, ldx, ldo;
+  dprc_dtype dtype;
+} dprc_tensor;
+size_t dprc_grad_norm_workspace(const dprc_tensor* tensors, int32_t count);
+dprc_status dprc_grad_norm(const dprc_tensor* tensors, int32_t count, float* norm, void* ws, size_t ws_bytes,
+                           hipStream_t stream);
+dprc_status dprc_grad_clip(const dprc_tensor* tensors, int32_t count, float max_norm, float* norm, void* ws,
+                           size_t ws_bytes, hipStream_t stream);
+
 /* ---- Envelope CDF of the Hutchinson estimate (privacy accounting) ------------------
  * Proposition on the extremal envelope and the appendix algorithms cdf-grid and
  * binary-search-xplus.  dprc_envelope_middle evaluates MiddleRegionCDF at nx
@@ -451,7 +566,15 @@ typedef enum {
   DPRC_KERNEL_LAYERNORM = 25,         /* dropout, residual sum and norm          */
   DPRC_KERNEL_LAYERNORM_BACKWARD = 26,
   DPRC_KERNEL_VECTOR_NORMS = 27,      /* squared norms of per-sample vectors     */
-  DPRC_KERNEL_VECTOR_SUMS = 28        /* clipped sums of per-sample vectors      */
+  DPRC_KERNEL_VECTOR_SUMS = 28,       /* clipped sums of per-sample vectors      */
+  DPRC_KERNEL_HEAD_SUMS = 29,         /* head: logit tiles' maxima and sums      */
+  DPRC_KERNEL_HEAD_JOIN = 30,         /* head: losses and log-sum-exps           */
+  DPRC_KERNEL_HEAD_ERRORS = 31,       /* head: E of a piece of the vocabulary    */
+  DPRC_KERNEL_HEAD_BACK = 32,         /* head: E W                               */
+  DPRC_KERNEL_HEAD_ROWS = 33,         /* head: rows laid out, sums rounded       */
+  DPRC_KERNEL_ROTARY = 34,
+  DPRC_KERNEL_GRAD_SQUARES = 35,      /* joint norm of many tensors              */
+  DPRC_KERNEL_GRAD_SCALE = 36         /* their clipping                          */
 } dprc_kernel_kind;
 dprc_status dprc_trace_launches(hipEvent_t* events, int32_t* kinds, int32_t capacity,
                                 int32_t* count);

@@ -1759,3 +1759,461 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
 }
 
 }  // extern "C"
+
+// ---- output head, rotary positions, joint norm ---------------------------------------------------
+namespace {
+
+constexpr int64_t kHeadPieceBytes = (int64_t)1 << 30;
+constexpr int64_t kHeadPieceMax = (int64_t)1 << 21;   // columns: offsets within a tile of E stay below 2^31
+constexpr int32_t kHeadBlocks = 32;                   // of a dprc_norm_hutch call
+
+dprc_status check_head(const dprc_head* H) {
+  if (!H || !H->h || !H->W || !H->target || H->B < 1 || H->T < 1 || H->d < 1 || H->V < 1 || H->ldh < H->d ||
+      H->ldw < H->d || !dtype_ok(H->dtype) || H->piece < 0 || H->piece % DPRC_HEAD_BLOCK)
+    return DPRC_ERROR_INVALID_VALUE;
+  const size_t e = elem_bytes(H->dtype);
+  if (H->B > 65535 || H->T > (1LL << 30) || H->B * H->T > (1LL << 31) || H->d > (1LL << 30) || H->V > (1LL << 30) ||
+      H->d * H->V > (1LL << 40) || !aligned(H->h, e) || !aligned(H->W, e) || !aligned(H->target, 8))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  return DPRC_SUCCESS;
+}
+
+// rows that the head's kernels read in 16-byte pieces, offsets within a tile of them below 2^31
+bool head_vec(const dprc_head& H, const void* p, int64_t ld) {
+  return H.dtype == DPRC_F32 || (rows16(p, ld) && H.d % 8 == 0 && ld < (1LL << 22));
+}
+
+struct HeadBufs {
+  int64_t N, piece, lde, ldc;          // tokens; columns of a piece; row strides of E and of h's copy
+  int32_t S;                           // splits of dh
+  void* rows;                          // h laid out [N][ldc]
+  void* E;                             // [N][lde]
+  float* planes;                       // [S][N][d]
+  float* dW;                           // [piece][d], bf16 heads
+  float* one;
+  void* acc;                           // accumulation's and estimates' workspaces
+  size_t acc_bytes;
+  void* hutch;
+  size_t hutch_bytes;
+};
+
+int64_t head_piece(const dprc_head& H) {
+  const int64_t row = H.B * H.T * (int64_t)elem_bytes(H.dtype) * DPRC_HEAD_BLOCK;
+  const int64_t piece = H.piece ? H.piece : std::max<int64_t>(1, kHeadPieceBytes / row) * DPRC_HEAD_BLOCK;
+  return std::min({piece, H.V, kHeadPieceMax});
+}
+
+HeadRows head_rows(const dprc_head& H, const HeadBufs& b) { return HeadRows{b.rows, b.ldc, b.N, H.d}; }
+
+// The layer of the head's columns v0 .. v0 + nv, of which E holds a piece from its own column c0 on.
+dprc_layer head_layer(const dprc_head& H, const HeadBufs& b, int64_t c0, int64_t nv, uint32_t id) {
+  const char* E = static_cast<const char*>(b.E) + c0 * (int64_t)elem_bytes(H.dtype);
+  return dprc_layer{b.rows, E, H.B, H.T, H.d, nv, b.ldc, b.lde, H.dtype, id};
+}
+
+// dW as the accumulation forms it: E^T h over all tokens as one sample.
+dprc_layer head_weight_layer(const dprc_head& H, const HeadBufs& b, int64_t nv) {
+  return dprc_layer{b.E, b.rows, 1, b.N, nv, H.d, b.lde, b.ldc, H.dtype, 0};
+}
+
+// The blocks of columns v0 .. v0 + nv, up to kHeadBlocks at a time: f(layers, count, first column) for each group.
+template <class F>
+dprc_status head_blocks(const dprc_head& H, const HeadBufs& b, int64_t v0, int64_t nv, uint32_t id, F&& f) {
+  dprc_layer L[kHeadBlocks];
+  for (int64_t c = 0; c < nv;) {
+    const int64_t first = c;
+    int32_t n = 0;
+    for (; n < kHeadBlocks && c < nv; ++n, c += DPRC_HEAD_BLOCK)
+      L[n] = head_layer(H, b, c, std::min<int64_t>(DPRC_HEAD_BLOCK, nv - c), id + (uint32_t)((v0 + c) / DPRC_HEAD_BLOCK));
+    const dprc_status s = f(L, n, first);
+    if (s != DPRC_SUCCESS) return s;
+  }
+  return DPRC_SUCCESS;
+}
+
+size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_head_norms* norms, void* ws, HeadBufs& b) {
+  const size_t e = elem_bytes(H.dtype);
+  Arena ar(ws);
+  b = HeadBufs{};
+  b.N = H.B * H.T;
+  b.piece = head_piece(H);
+  b.lde = round_up(b.piece, 64);
+  b.ldc = round_up(H.d, 8);
+  b.rows = ar.take<char>((size_t)(b.N * b.ldc) * e);
+  b.E = ar.take<char>((size_t)(b.N * b.lde) * e);
+  // buffers of a shape to ask for sizes with: only their alignment counts
+  HeadBufs probe = b;
+  probe.rows = probe.E = reinterpret_cast<void*>((uintptr_t)kAlign);
+  if (dh) {
+    b.S = head_back_plan(b.N, H.d, b.piece, H.dtype == DPRC_BF16, 0).S;
+    b.planes = ar.take<float>((size_t)b.S * b.N * H.d);
+  }
+  const int64_t rest = H.V % b.piece;
+  if (dW) {
+    b.one = ar.take<float>(1);
+    if (H.dtype == DPRC_BF16) b.dW = ar.take<float>((size_t)b.piece * H.d);
+  }
+  for (const int64_t nv : {b.piece, rest}) {
+    if (nv == 0) continue;
+    if (dW) {
+      const dprc_layer L = head_weight_layer(H, probe, nv);
+      b.acc_bytes = std::max(b.acc_bytes, dprc_clip_accumulate_workspace(&L));
+    }
+    if (clip) {
+      const dprc_layer L = head_layer(H, probe, 0, nv, 0);
+      b.acc_bytes = std::max(b.acc_bytes, dprc_clip_accumulate_workspace(&L));
+    }
+    if (norms)
+      head_blocks(H, probe, 0, nv, 0, [&](const dprc_layer* L, int32_t n, int64_t) {
+        b.hutch_bytes = std::max(b.hutch_bytes, dprc_norm_hutch_workspace(L, n, norms->k, norms->probe, norms->side));
+        return DPRC_SUCCESS;
+      });
+  }
+  b.acc = ar.take<char>(b.acc_bytes);
+  b.hutch = ar.take<char>(b.hutch_bytes);
+  return ar.off;
+}
+
+HeadArgs head_args(const dprc_head& H, const HeadRows& h, int64_t v0, int64_t nv) {
+  HeadArgs a{};
+  const char* W = static_cast<const char*>(H.W) + v0 * H.ldw * (int64_t)elem_bytes(H.dtype);
+  a.W = HeadRows{W, H.ldw, nv, H.d};
+  a.h = h;
+  a.N = H.B * H.T; a.nv = nv; a.v0 = v0;
+  a.bf16 = H.dtype == DPRC_BF16;
+  a.vec_w = head_vec(H, H.W, H.ldw);
+  a.target = H.target;
+  return a;
+}
+
+// h's rows laid out for the gradients, then f(v0, nv) for every piece with its E formed.
+template <class F>
+dprc_status head_pieces(const dprc_head& H, const HeadBufs& b, const float* lse, const float* g, hipStream_t stream, F&& f) {
+  const HeadRows h{H.h, H.ldh, b.N, H.d};
+  hipError_t e = traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+    return launch_head_rows(h, H.dtype == DPRC_BF16, H.target, b.rows, b.ldc, stream); });
+  if (e != hipSuccess) return DPRC_ERROR_HIP;
+  for (int64_t v0 = 0; v0 < H.V; v0 += b.piece) {
+    const int64_t nv = std::min(b.piece, H.V - v0);
+    HeadArgs a = head_args(H, head_rows(H, b), v0, nv);
+    a.lse = lse; a.g = g;
+    a.E = b.E; a.lde = b.lde; a.width = round_up(nv, 8);
+    if (traced(DPRC_KERNEL_HEAD_ERRORS, stream, [&] { return launch_head_errors(a, stream); }) != hipSuccess)
+      return DPRC_ERROR_HIP;
+    const dprc_status s = f(v0, nv);
+    if (s != DPRC_SUCCESS) return s;
+  }
+  return DPRC_SUCCESS;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dprc_head_loss_workspace(const dprc_head* H) {
+  if (check_head(H) != DPRC_SUCCESS) return 0;
+  Arena ar(nullptr);
+  if (!head_vec(*H, H->h, H->ldh)) ar.take<char>((size_t)(H->B * H->T * round_up(H->d, 8)) * 2);
+  ar.take<float2>((size_t)ceil_div(H->V, head_tile_rows(H->dtype == DPRC_BF16)) * H->B * H->T);
+  return ar.off;
+}
+
+dprc_status dprc_head_loss(const dprc_head* H, float* loss, float* lse, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dprc_status st = check_head(H);
+  if (st == DPRC_ERROR_INVALID_VALUE || !loss || !lse || loss == lse) return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(loss, 4) || !aligned(lse, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  if (ws_bytes < dprc_head_loss_workspace(H)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
+  Arena ar(ws);
+  HeadRows h{H->h, H->ldh, H->B * H->T, H->d};
+  if (!head_vec(*H, H->h, H->ldh)) {
+    const int64_t ld = round_up(H->d, 8);
+    uint16_t* rows = ar.take<uint16_t>((size_t)(h.rows * ld));
+    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_rows(h, 1, nullptr, rows, ld, stream); }) != hipSuccess)
+      return DPRC_ERROR_HIP;
+    h.p = rows;
+    h.ld = ld;
+  }
+  HeadArgs a = head_args(*H, h, 0, H->V);
+  a.part = ar.take<float2>((size_t)ceil_div(H->V, head_tile_rows(a.bf16)) * a.N);
+  if (traced(DPRC_KERNEL_HEAD_SUMS, stream, [&] { return launch_head_sums(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
+  return hip_status(traced(DPRC_KERNEL_HEAD_JOIN, stream, [&] { return launch_head_join(a, loss, lse, stream); }));
+}
+
+size_t dprc_head_errors_workspace(const dprc_head* H) {
+  if (check_head(H) != DPRC_SUCCESS || head_vec(*H, H->h, H->ldh)) return 0;
+  return (size_t)round_up(H->B * H->T * round_up(H->d, 8) * 2, kAlign);
+}
+
+dprc_status dprc_head_errors(const dprc_head* H, const float* lse, const float* g, int64_t v0, int64_t nv, void* E,
+                             int64_t lde, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dprc_status st = check_head(H);
+  if (st == DPRC_ERROR_INVALID_VALUE || !lse || !g || !E || v0 < 0 || nv < 1 || v0 > H->V - nv || lde < nv)
+    return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(E, elem_bytes(H->dtype))) return DPRC_ERROR_NOT_SUPPORTED;
+  const size_t need = dprc_head_errors_workspace(H);
+  if (ws_bytes < need) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (need && (!ws || !aligned(ws, kAlign))) return DPRC_ERROR_INVALID_VALUE;
+  HeadRows h{H->h, H->ldh, H->B * H->T, H->d};
+  if (need) {
+    const int64_t ld = round_up(H->d, 8);
+    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_rows(h, 1, nullptr, ws, ld, stream); }) != hipSuccess)
+      return DPRC_ERROR_HIP;
+    h.p = ws;
+    h.ld = ld;
+  }
+  HeadArgs a = head_args(*H, h, v0, nv);
+  a.lse = lse; a.g = g;
+  a.E = E; a.lde = lde; a.width = nv;
+  return hip_status(traced(DPRC_KERNEL_HEAD_ERRORS, stream, [&] { return launch_head_errors(a, stream); }));
+}
+
+static dprc_status check_head_norms(const dprc_head_norms* n) {
+  if (!n) return DPRC_SUCCESS;
+  if (n->k < 1 || n->k > 256 || !n->n2) return DPRC_ERROR_INVALID_VALUE;
+  if (n->probe != DPRC_PROBE_RADEMACHER && n->probe != DPRC_PROBE_HADAMARD && n->probe != DPRC_PROBE_GAUSSIAN)
+    return DPRC_ERROR_INVALID_VALUE;
+  if (n->side != DPRC_SIDE_OUT && n->side != DPRC_SIDE_IN && n->side != DPRC_SIDE_AUTO) return DPRC_ERROR_INVALID_VALUE;
+  if ((n->probe == DPRC_PROBE_GAUSSIAN && n->k > kMaxGaussK) || !aligned(n->n2, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  return DPRC_SUCCESS;
+}
+
+size_t dprc_head_backward_workspace(const dprc_head* H, int32_t dh, int32_t dW, const dprc_head_norms* norms) {
+  if (check_head(H) != DPRC_SUCCESS) return 0;
+  HeadBufs b;
+  return head_layout(*H, dh, dW, false, norms, nullptr, b);
+}
+
+dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float* g, void* dh, int64_t lddh, void* dW,
+                               int64_t lddw, const dprc_head_norms* norms, void* ws, size_t ws_bytes,
+                               hipStream_t stream) {
+  dprc_status st = check_head(H);
+  if (st == DPRC_ERROR_INVALID_VALUE || !lse || !g || (!dh && !dW && !norms) || (dh && lddh < H->d) ||
+      (dW && lddw < H->d) || (dh && (dh == H->h || dh == H->W || dh == dW)) || (dW && (dW == H->h || dW == H->W)))
+    return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS || (st = check_head_norms(norms)) != DPRC_SUCCESS) return st;
+  const size_t e = elem_bytes(H->dtype);
+  if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(dh, e) || !aligned(dW, e)) return DPRC_ERROR_NOT_SUPPORTED;
+  HeadBufs b;
+  if (ws_bytes < head_layout(*H, dh, dW, false, norms, nullptr, b)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
+  head_layout(*H, dh, dW, false, norms, ws, b);
+  const int bf16 = H->dtype == DPRC_BF16;
+  if (dW && traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_one(b.one, stream); }) != hipSuccess)
+    return DPRC_ERROR_HIP;
+  st = head_pieces(*H, b, lse, g, stream, [&](int64_t v0, int64_t nv) -> dprc_status {
+    dprc_status s;
+    if (norms) {
+      s = head_blocks(*H, b, v0, nv, norms->layer_id, [&](const dprc_layer* L, int32_t n, int64_t c) {
+        return dprc_norm_hutch(L, n, norms->k, norms->probe, norms->seed, norms->side, norms->n2, nullptr,
+                               norms->accumulate || v0 + c > 0, b.hutch, b.hutch_bytes, stream);
+      });
+      if (s != DPRC_SUCCESS) return s;
+    }
+    if (dh) {
+      const HeadBackPlan plan = head_back_plan(b.N, H->d, nv, bf16, b.S);
+      HeadBackArgs a{};
+      a.E = HeadRows{b.E, b.lde, b.N, bf16 ? round_up(nv, 8) : nv};   // (columns behind nv are zeros, and meet none of W's rows)
+      a.W = head_args(*H, head_rows(*H, b), v0, nv).W;
+      a.N = b.N; a.d = H->d;
+      a.per_split = plan.per_split; a.S = plan.S;
+      a.bf16 = bf16; a.vec_w = head_vec(*H, H->W, H->ldw);
+      a.add = v0 > 0;
+      a.planes = b.planes;
+      if (traced(DPRC_KERNEL_HEAD_BACK, stream, [&] { return launch_head_back(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
+    }
+    if (dW) {
+      const dprc_layer L = head_weight_layer(*H, b, nv);
+      char* out = static_cast<char*>(dW) + v0 * lddw * (int64_t)e;
+      s = dprc_clip_accumulate(&L, b.one, bf16 ? b.dW : reinterpret_cast<float*>(out), bf16 ? H->d : lddw, 0, b.acc, b.acc_bytes, stream);
+      if (s != DPRC_SUCCESS) return s;
+      if (bf16 && traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+            return launch_head_round(b.dW, 1, nv, H->d, 1, out, lddw, stream); }) != hipSuccess)
+        return DPRC_ERROR_HIP;
+    }
+    return DPRC_SUCCESS;
+  });
+  if (st != DPRC_SUCCESS || !dh) return st;
+  return hip_status(traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+    return launch_head_round(b.planes, b.S, b.N, H->d, bf16, dh, lddh, stream); }));
+}
+
+size_t dprc_head_clip_accumulate_workspace(const dprc_head* H) {
+  if (check_head(H) != DPRC_SUCCESS) return 0;
+  HeadBufs b;
+  return head_layout(*H, false, false, true, nullptr, nullptr, b);
+}
+
+dprc_status dprc_head_clip_accumulate(const dprc_head* H, const float* lse, const float* g, const float* c, float* grad,
+                                      int64_t ldg, int32_t accumulate, void* ws, size_t ws_bytes, hipStream_t stream) {
+  const dprc_status st = check_head(H);
+  if (st == DPRC_ERROR_INVALID_VALUE || !lse || !g || !c || !grad || ldg < H->V) return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(c, 4) || !aligned(grad, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  HeadBufs b;
+  if (ws_bytes < head_layout(*H, false, false, true, nullptr, nullptr, b)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
+  head_layout(*H, false, false, true, nullptr, ws, b);
+  return head_pieces(*H, b, lse, g, stream, [&](int64_t v0, int64_t nv) {
+    const dprc_layer L = head_layer(*H, b, 0, nv, 0);
+    return dprc_clip_accumulate(&L, c, grad + v0, ldg, accumulate, b.acc, b.acc_bytes, stream);
+  });
+}
+
+dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t count, hipStream_t stream) {
+  if (!R || !heads || count < 1 || R->B < 1 || R->T < 1 || R->r < 1 || (int64_t)2 * R->r > R->D || !R->freqs ||
+      !dtype_ok(R->xdtype) || !dtype_ok(R->ydtype) || !std::isfinite(R->scale))
+    return DPRC_ERROR_INVALID_VALUE;
+  const int64_t most = 1LL << 31;
+  if (count > kRotaryTensors || R->B > most || R->T > most || R->B * R->T > most || R->D > (1 << 20) || R->r > 4096 ||
+      !aligned(R->freqs, 8) || !aligned(R->pos, 8))
+    return DPRC_ERROR_NOT_SUPPORTED;
+  RotaryArgs a{};
+  a.B = R->B; a.T = R->T; a.D = R->D; a.r = R->r; a.count = count;
+  a.xbf16 = R->xdtype == DPRC_BF16; a.ybf16 = R->ydtype == DPRC_BF16;
+  a.interleaved = R->interleaved; a.inverse = R->inverse; a.scale = R->scale;
+  a.start = R->start; a.pos = R->pos; a.freqs = R->freqs;
+  int64_t total = 0;
+  for (int32_t i = 0; i < count; ++i) {
+    const dprc_heads& h = heads[i];
+    if (!h.x || !h.y || h.H < 1) return DPRC_ERROR_INVALID_VALUE;
+    if (h.x == h.y && (a.xbf16 != a.ybf16 || (R->B > 1 && h.xb != h.yb) || (R->T > 1 && h.xt != h.yt) ||
+                       (h.H > 1 && h.xh != h.yh)))
+      return DPRC_ERROR_INVALID_VALUE;
+    if (h.H > (1 << 16) || !aligned(h.x, elem_bytes(R->xdtype)) || !aligned(h.y, elem_bytes(R->ydtype)))
+      return DPRC_ERROR_NOT_SUPPORTED;
+    a.x[i] = RotaryTensor{h.x, h.y, h.xb, h.xt, h.xh, h.yb, h.yt, h.yh, (int32_t)h.H};
+    total += h.H;
+  }
+  if (total > (1 << 16)) return DPRC_ERROR_NOT_SUPPORTED;
+  a.heads = (int32_t)total;
+  return hip_status(traced(DPRC_KERNEL_ROTARY, stream, [&] { return launch_rotary(a, stream); }));
+}
+
+}  // extern "C"
+
+namespace {
+
+constexpr int64_t kGradBlocks = 2048;       // workgroups, and parts of the sum, of a call
+
+dprc_status check_tensors(const dprc_tensor* t, int32_t count, bool out) {
+  if (count < 0 || (count > 0 && !t)) return DPRC_ERROR_INVALID_VALUE;
+  for (int32_t i = 0; i < count; ++i) {
+    if (t[i].rows < 0 || t[i].cols < 0 || !dtype_ok(t[i].dtype)) return DPRC_ERROR_INVALID_VALUE;
+    if (t[i].rows == 0 || t[i].cols == 0) continue;
+    if (!t[i].x || (out && !t[i].out) || (t[i].rows > 1 && (t[i].ldx < t[i].cols || (out && t[i].ldo < t[i].cols))) ||
+        (out && t[i].x == t[i].out && t[i].rows > 1 && t[i].ldx != t[i].ldo))
+      return DPRC_ERROR_INVALID_VALUE;
+  }
+  for (int32_t i = 0; i < count; ++i) {
+    const size_t e = elem_bytes(t[i].dtype);
+    if (t[i].rows > (1LL << 40) || t[i].cols > (1LL << 40) ||
+        (t[i].rows && t[i].cols && (!aligned(t[i].x, e) || (out && !aligned(t[i].out, e)))))
+      return DPRC_ERROR_NOT_SUPPORTED;
+  }
+  return DPRC_SUCCESS;
+}
+
+// Calls f(args) for every launch over the tensors, in order; args.parts is that of the call.
+template <class F>
+dprc_status grad_launches(const dprc_tensor* t, int32_t count, GradArgs& a, F&& f) {
+  int64_t filled = 0;
+  for (int32_t i = 0; i < count; ++i) filled += t[i].rows > 0 && t[i].cols > 0;
+  const int64_t launches = ceil_div(filled, kGradTensors);
+  int32_t part0 = 0;
+  for (int32_t i = 0; i < count;) {
+    a.count = 0;
+    a.chunks = 0;
+    for (; i < count && a.count < kGradTensors; ++i) {
+      if (t[i].rows == 0 || t[i].cols == 0) continue;
+      GradTensor& g = a.t[a.count++];
+      g.x = t[i].x; g.out = t[i].out;
+      g.rows = t[i].rows; g.cols = t[i].cols; g.ldx = t[i].ldx; g.ldo = t[i].ldo;
+      g.bf16 = t[i].dtype == DPRC_BF16;
+      if (g.rows > 1 && g.ldx == g.cols && (!g.out || g.ldo == g.cols)) {   // one long row
+        g.cols *= g.rows;
+        g.rows = 1;
+      }
+      g.chunk0 = a.chunks;
+      a.chunks += g.cols >= kGradChunk ? g.rows * ceil_div(g.cols, kGradChunk) : ceil_div(g.rows, kGradChunk / g.cols);
+    }
+    if (a.count == 0) break;
+    a.blocks = (int32_t)std::min<int64_t>(a.chunks, std::max<int64_t>(64, kGradBlocks / launches));
+    a.part0 = part0;
+    part0 += a.blocks;
+    const dprc_status s = f(a);
+    if (s != DPRC_SUCCESS) return s;
+  }
+  return DPRC_SUCCESS;
+}
+
+int32_t grad_parts(const dprc_tensor* t, int32_t count) {
+  GradArgs a{};
+  int32_t parts = 0;
+  grad_launches(t, count, a, [&](const GradArgs& g) {
+    parts += g.blocks;
+    return DPRC_SUCCESS;
+  });
+  return parts;
+}
+
+dprc_status grad_squares(const dprc_tensor* t, int32_t count, GradArgs& a, hipStream_t stream) {
+  return grad_launches(t, count, a, [&](const GradArgs& g) {
+    return hip_status(traced(DPRC_KERNEL_GRAD_SQUARES, stream, [&] { return launch_grad_squares(g, stream); })); });
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t dprc_grad_norm_workspace(const dprc_tensor* tensors, int32_t count) {
+  if (check_tensors(tensors, count, false) != DPRC_SUCCESS) return 0;
+  return (size_t)round_up(std::max<int64_t>(1, grad_parts(tensors, count)) * (int64_t)sizeof(double), kAlign);
+}
+
+dprc_status dprc_grad_norm(const dprc_tensor* tensors, int32_t count, float* norm, void* ws, size_t ws_bytes,
+                           hipStream_t stream) {
+  const dprc_status st = check_tensors(tensors, count, false);
+  if (st == DPRC_ERROR_INVALID_VALUE || !norm) return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(norm, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  if (ws_bytes < dprc_grad_norm_workspace(tensors, count)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
+  GradArgs a{};
+  a.part = static_cast<double*>(ws);
+  a.parts = grad_parts(tensors, count);
+  a.norm = norm;
+  const dprc_status s = grad_squares(tensors, count, a, stream);
+  if (s != DPRC_SUCCESS) return s;
+  return hip_status(traced(DPRC_KERNEL_GRAD_SQUARES, stream, [&] { return launch_grad_norm(a, stream); }));
+}
+
+dprc_status dprc_grad_clip(const dprc_tensor* tensors, int32_t count, float max_norm, float* norm, void* ws,
+                           size_t ws_bytes, hipStream_t stream) {
+  const dprc_status st = check_tensors(tensors, count, true);
+  if (st == DPRC_ERROR_INVALID_VALUE || !(max_norm > 0.f) || std::isinf(max_norm)) return DPRC_ERROR_INVALID_VALUE;
+  if (st != DPRC_SUCCESS) return st;
+  if (!aligned(norm, 4)) return DPRC_ERROR_NOT_SUPPORTED;
+  if (ws_bytes < dprc_grad_norm_workspace(tensors, count)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
+  if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
+  GradArgs a{};
+  a.part = static_cast<double*>(ws);
+  a.parts = grad_parts(tensors, count);
+  a.max_norm = (double)max_norm;
+  dprc_status s = grad_squares(tensors, count, a, stream);
+  if (s != DPRC_SUCCESS) return s;
+  if (a.parts == 0) {                                 // nothing but the norm, 0
+    a.norm = norm;
+    return norm ? hip_status(traced(DPRC_KERNEL_GRAD_SQUARES, stream, [&] { return launch_grad_norm(a, stream); })) : DPRC_SUCCESS;
+  }
+  a.norm = norm;
+  return grad_launches(tensors, count, a, [&](GradArgs& g) {
+    const dprc_status e = hip_status(traced(DPRC_KERNEL_GRAD_SCALE, stream, [&] { return launch_grad_scale(g, stream); }));
+    g.norm = nullptr;
+    return e;
+  });
+}
+
+}  // extern "C"

@@ -455,6 +455,93 @@ int vector_sum_splits(int64_t B, int64_t n);
 hipError_t launch_vector_norms(const VectorArgs& a, hipStream_t st);
 hipError_t launch_vector_sums(const VectorArgs& a, hipStream_t st);
 
+// Rows of an operand (see k_head.hip).
+struct HeadRows {
+  const void* p;
+  int64_t ld, rows, width;
+};
+
+// The logits of N tokens over the nv vocabulary rows from v0 on, and what is made of them (see dprc_head).
+struct HeadArgs {
+  HeadRows W;              // the rows from v0 on: [nv][d]
+  HeadRows h;              // [N][d], for bf16 in 16-byte pieces
+  int64_t N, nv, v0;
+  int32_t bf16, vec_w;
+  const int64_t* target;   // [N]
+  float2* part;            // forward: [tiles][N] maximum and sum
+  const float* lse;        // errors: [N]
+  const float* g;          // errors: [N]
+  void* E;                 // errors: [N][lde], columns v0 .. v0 + width
+  int64_t lde, width;      // width >= nv: the columns past nv are zeros
+};
+int head_tile_rows(int bf16);         // vocabulary rows of a tile
+hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st);
+hipError_t launch_head_errors(const HeadArgs& a, hipStream_t st);
+hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st);   // nv = V, v0 = 0
+
+// planes[S][N][d] (=|+=) the splits' sums of E W over a piece of the vocabulary.
+struct HeadBackArgs {
+  HeadRows E, W;           // [N][nv], [nv][d]
+  int64_t N, d, per_split;
+  int32_t S, bf16, vec_w, add;
+  float* planes;
+};
+struct HeadBackPlan {
+  int64_t per_split;
+  int32_t S;
+};
+// most > 0: at most so many splits
+HeadBackPlan head_back_plan(int64_t N, int64_t d, int64_t nv, int bf16, int32_t most);
+hipError_t launch_head_back(const HeadBackArgs& a, hipStream_t st);
+hipError_t launch_head_rows(const HeadRows& X, int bf16, const int64_t* target, void* out, int64_t ldo, hipStream_t st);
+hipError_t launch_head_round(const float* planes, int S, int64_t rows, int64_t cols, int bf16, void* out, int64_t ldo,
+                             hipStream_t st);
+hipError_t launch_head_one(float* one, hipStream_t st);
+
+// Rotary positions of up to kRotaryTensors tensors [B][T][H][D] (see dprc_rotary).
+constexpr int kRotaryTensors = 4;
+struct RotaryTensor {
+  const void* x;
+  void* y;
+  int64_t xb, xt, xh, yb, yt, yh;    // strides of samples, tokens and heads
+  int32_t H;
+};
+struct RotaryArgs {
+  int64_t B, T;
+  int32_t D, r, heads;               // heads: of all tensors
+  int32_t count, per_block;          // per_block: tokens of a workgroup (set by the launcher)
+  int32_t xbf16, ybf16, interleaved, inverse;
+  float scale;
+  int64_t start;
+  const int64_t* pos;                // [B][T], may be null
+  const double* freqs;               // [r]
+  RotaryTensor x[kRotaryTensors];
+};
+hipError_t launch_rotary(RotaryArgs a, hipStream_t st);
+
+// The joint norm of many tensors and their clipping (see dprc_grad_clip).  A tensor is rows of cols
+// elements; its chunks of about kGradChunk elements are numbered from chunk0 on.
+constexpr int64_t kGradChunk = 16384;
+constexpr int kGradTensors = 48;     // of a launch: 2.8 KB of kernel arguments
+struct GradTensor {
+  const void* x;
+  void* out;
+  int64_t rows, cols, ldx, ldo, chunk0;
+  int32_t bf16;
+};
+struct GradArgs {
+  int32_t count, blocks;
+  int64_t chunks;
+  double* part;                      // [parts], this launch's from part0 on
+  int32_t part0, parts;
+  double max_norm;
+  float* norm;                       // may be null
+  GradTensor t[kGradTensors];
+};
+hipError_t launch_grad_squares(const GradArgs& a, hipStream_t st);
+hipError_t launch_grad_norm(const GradArgs& a, hipStream_t st);
+hipError_t launch_grad_scale(const GradArgs& a, hipStream_t st);
+
 // Gaussian probe columns, column j at [j*ld .. j*ld + ld) (rows >= m zero);
 // any of hi/lo (both or neither) and f32 may be null.
 hipError_t launch_gauss_probe(uint32_t key0, uint32_t key1, uint32_t layer, int64_t m, int32_t k, int64_t ld,

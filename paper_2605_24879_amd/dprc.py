@@ -8,6 +8,7 @@ current stream.  A missing library or a non-zero dprc_status raises
 RuntimeError; there is no fallback.
 """
 
+import array
 import ctypes
 import os
 
@@ -22,6 +23,7 @@ SIDE_OUT, SIDE_IN, SIDE_AUTO = 0, 1, 2
 PROBE_RADEMACHER, PROBE_HADAMARD, PROBE_GAUSSIAN = 0, 1, 2
 STREAM_PROBE, STREAM_SKETCH, STREAM_NOISE, STREAM_GAUSS_PROBE, STREAM_DROPOUT = 0, 1, 2, 3, 4
 LAYERNORM, RMSNORM = 0, 1
+HEAD_BLOCK = 8192
 
 EXPORTS = ["dprc_norm_hutch_workspace", "dprc_norm_hutch", "dprc_norm_hutch_clip", "dprc_norm_hutch_clip_static", "dprc_norm_hutchpp_workspace",
            "dprc_norm_hutchpp", "dprc_clip_scale", "dprc_clip_accumulate_workspace",
@@ -30,7 +32,10 @@ EXPORTS = ["dprc_norm_hutch_workspace", "dprc_norm_hutch", "dprc_norm_hutch_clip
            "dprc_pld_step", "dprc_pld_fold", "dprc_pld_delta", "dprc_status_string",
            "dprc_version", "dprc_trace_launches", "dprc_dropout", "dprc_layernorm",
            "dprc_layernorm_backward_workspace", "dprc_layernorm_backward", "dprc_norm_vectors_workspace",
-           "dprc_norm_vectors", "dprc_clip_accumulate_vectors_workspace", "dprc_clip_accumulate_vectors"]
+           "dprc_norm_vectors", "dprc_clip_accumulate_vectors_workspace", "dprc_clip_accumulate_vectors",
+           "dprc_head_loss_workspace", "dprc_head_loss", "dprc_head_errors_workspace", "dprc_head_errors",
+           "dprc_head_backward_workspace", "dprc_head_backward", "dprc_head_clip_accumulate_workspace",
+           "dprc_head_clip_accumulate", "dprc_rotary", "dprc_grad_norm_workspace", "dprc_grad_norm", "dprc_grad_clip"]
 
 
 class Layer(ctypes.Structure):
@@ -53,6 +58,27 @@ class LN(ctypes.Structure):
                 ("dtype", ctypes.c_int), ("wdtype", ctypes.c_int), ("kind", ctypes.c_int), ("eps", ctypes.c_float),
                 ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p),
                 ("p", ctypes.c_float), ("site_id", ctypes.c_uint32), ("seed", ctypes.c_uint64)]
+
+
+class HeadDesc(ctypes.Structure):
+    """Mirror of dprc_head."""
+    _fields_ = [("h", ctypes.c_void_p), ("W", ctypes.c_void_p), ("target", ctypes.c_void_p),
+                ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("d", ctypes.c_int64), ("V", ctypes.c_int64),
+                ("ldh", ctypes.c_int64), ("ldw", ctypes.c_int64), ("dtype", ctypes.c_int), ("piece", ctypes.c_int64)]
+
+
+class HeadNorms(ctypes.Structure):
+    """Mirror of dprc_head_norms."""
+    _fields_ = [("k", ctypes.c_int32), ("probe", ctypes.c_int), ("seed", ctypes.c_uint64), ("side", ctypes.c_int),
+                ("layer_id", ctypes.c_uint32), ("n2", ctypes.c_void_p), ("accumulate", ctypes.c_int32)]
+
+
+class Rope(ctypes.Structure):
+    """Mirror of dprc_rope."""
+    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("D", ctypes.c_int32), ("r", ctypes.c_int32),
+                ("freqs", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("start", ctypes.c_int64),
+                ("scale", ctypes.c_float), ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
+                ("xdtype", ctypes.c_int), ("ydtype", ctypes.c_int)]
 
 
 _lib = None
@@ -104,6 +130,18 @@ def lib():
             "dprc_norm_vectors": (ctypes.c_int, [P, I64, I64, I64, P, I32, P, SZ, P]),
             "dprc_clip_accumulate_vectors_workspace": (SZ, [I64, I64]),
             "dprc_clip_accumulate_vectors": (ctypes.c_int, [P, I64, P, I64, I64, P, I32, P, SZ, P]),
+            "dprc_head_loss_workspace": (SZ, [P]),
+            "dprc_head_loss": (ctypes.c_int, [P, P, P, P, SZ, P]),
+            "dprc_head_errors_workspace": (SZ, [P]),
+            "dprc_head_errors": (ctypes.c_int, [P, P, P, I64, I64, P, I64, P, SZ, P]),
+            "dprc_head_backward_workspace": (SZ, [P, I32, I32, P]),
+            "dprc_head_backward": (ctypes.c_int, [P, P, P, P, I64, P, I64, P, P, SZ, P]),
+            "dprc_head_clip_accumulate_workspace": (SZ, [P]),
+            "dprc_head_clip_accumulate": (ctypes.c_int, [P, P, P, P, P, I64, I32, P, SZ, P]),
+            "dprc_rotary": (ctypes.c_int, [P, P, I32, P]),
+            "dprc_grad_norm_workspace": (SZ, [P, I32]),
+            "dprc_grad_norm": (ctypes.c_int, [P, I32, P, P, SZ, P]),
+            "dprc_grad_clip": (ctypes.c_int, [P, I32, F, P, P, SZ, P]),
             "dprc_status_string": (ctypes.c_char_p, [ctypes.c_int]),
             "dprc_version": (ctypes.c_char_p, []),
             "dprc_trace_launches": (ctypes.c_int, [P, P, I32, P]),
@@ -637,6 +675,237 @@ def dprc_clip_accumulate_vectors(G, c, grad=None, accumulate=False, ws=None):
     return grad
 
 
+def _head(h, W, target, piece):
+    """dprc_head of hidden states h [B, T, d], weight W [V, d] and targets [B, T]."""
+    ldh = _token_rows(h, "h")
+    B, T, d = h.shape
+    dev = h.get_device()
+    if W.dim() != 2 or W.shape[1] != d or W.dtype != h.dtype or W.get_device() != dev or (d > 1 and W.stride(1) != 1):
+        raise ValueError(f"W must be [V, {d}] {h.dtype} with contiguous rows on {h.device}, not {list(W.shape)} "
+                         f"{W.dtype} on {W.device}")
+    if target.shape != (B, T) or target.dtype != torch.int64 or target.get_device() != dev or not target.is_contiguous():
+        raise ValueError(f"target must be contiguous int64 [{B}, {T}] on {h.device}")
+    V = W.shape[0]
+    return HeadDesc(h.data_ptr(), W.data_ptr(), target.data_ptr(), B, T, d, V, ldh, W.stride(0) if V > 1 else d,
+                    _dtype_code(h), piece)
+
+
+def _tokens(x, name, H, dev):
+    """The pointer of contiguous fp32 values [B, T]."""
+    if x.shape != (H.B, H.T):
+        raise ValueError(f"{name} must be [{H.B}, {H.T}]")
+    return _vector(x, name, H.B * H.T, dev)
+
+
+def _new_tokens(h):
+    return torch.empty(h.shape[:2], dtype=torch.float32, device=h.device)
+
+
+def dprc_head_loss(h, W, target, loss=None, lse=None, ws=None):
+    """Cross entropy of the logits h W^T against target [B, T] (int64; negative: none), without storing the logits:
+    returns (loss, lse), [B, T] fp32.  h [B, T, d] token rows, W [V, d]."""
+    H = _head(h, W, target, 0)
+    dev = h.get_device()
+    loss = _new_tokens(h) if loss is None else loss
+    lse = _new_tokens(h) if lse is None else lse
+    need = lib().dprc_head_loss_workspace(ctypes.byref(H))
+    ws = _workspace(need, h.device, ws)
+    _check(lib().dprc_head_loss(ctypes.byref(H), _tokens(loss, "loss", H, dev), _tokens(lse, "lse", H, dev),
+                                ws.data_ptr(), need, _stream(h.device)))
+    return loss, lse
+
+
+def dprc_head_errors(h, W, target, lse, g, v0=0, nv=None, E=None, ws=None):
+    """E [B, T, nv]: the columns v0 .. v0 + nv (all by default) of the gradient of the logits, g (softmax - onehot)."""
+    H = _head(h, W, target, 0)
+    dev = h.get_device()
+    nv = W.shape[0] - v0 if nv is None else nv
+    if E is None:
+        E = torch.empty(H.B, H.T, nv, dtype=h.dtype, device=h.device)
+    elif E.shape != (H.B, H.T, nv) or E.dtype != h.dtype or E.get_device() != dev:
+        raise ValueError(f"E must be {[H.B, H.T, nv]} {h.dtype} on {h.device}")
+    lde = _token_rows(E, "E")
+    need = lib().dprc_head_errors_workspace(ctypes.byref(H))
+    ws = _workspace(need, h.device, ws) if need else None
+    _check(lib().dprc_head_errors(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev), v0, nv,
+                                  E.data_ptr(), lde, _ptr(ws), need, _stream(h.device)))
+    return E
+
+
+def dprc_head_backward(h, W, target, lse, g, hidden_grad=True, weight_grad=True, dh=None, dW=None, k=0, seed=0,
+                       layer_id=0, side=SIDE_OUT, probe=PROBE_RADEMACHER, n2=None, accumulate=False, piece=0, ws=None):
+    """Gradients of dprc_head_loss from g = dL/dloss [B, T] and lse: returns (dh, dW), None where not wanted.
+
+    With k > 0 returns (dh, dW, n2): n2 [B] (=|+=) the estimates of every sample's squared norm of its own weight
+    gradient, with the arguments of dprc_norm_hutch; the head counts as ceil(V / HEAD_BLOCK) layers, from
+    layer_id on.  piece: columns of the vocabulary held at a time (a multiple of HEAD_BLOCK)."""
+    H = _head(h, W, target, piece)
+    dev = h.get_device()
+    lddh = lddw = H.d
+    if dh is not None:
+        lddh = _token_rows(dh, "dh", h)
+    elif hidden_grad:
+        dh = h.new_empty(h.shape)
+    if dW is not None:
+        if dW.shape != W.shape or dW.dtype != W.dtype or dW.get_device() != dev or (H.d > 1 and dW.stride(1) != 1):
+            raise ValueError(f"dW must be {list(W.shape)} {W.dtype} with contiguous rows on {W.device}")
+        lddw = dW.stride(0) if H.V > 1 else H.d
+    elif weight_grad:
+        dW = W.new_empty(W.shape)
+    norms = None
+    if k != 0:
+        if n2 is None:
+            n2 = _new_n2(H.B, h.device, accumulate)
+        norms = ctypes.byref(HeadNorms(k, probe, seed, side, layer_id, _vector(n2, "n2", H.B, dev), int(bool(accumulate))))
+    need = lib().dprc_head_backward_workspace(ctypes.byref(H), dh is not None, dW is not None, norms)
+    ws = _workspace(need, h.device, ws)
+    _check(lib().dprc_head_backward(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev), _ptr(dh), lddh,
+                                    _ptr(dW), lddw, norms, ws.data_ptr(), need, _stream(h.device)))
+    return (dh, dW) if k == 0 else (dh, dW, n2)
+
+
+def dprc_head_clip_accumulate(h, W, target, lse, g, c, grad=None, accumulate=False, piece=0, ws=None):
+    """The head's clipped gradient: grad [d, V] (fp32) (=|+=) sum_i c_i h_i^T E_i, E as in dprc_head_errors."""
+    H = _head(h, W, target, piece)
+    dev = h.get_device()
+    if grad is None:
+        grad = (torch.zeros if accumulate else torch.empty)(H.d, H.V, dtype=torch.float32, device=h.device)
+    elif (grad.shape != (H.d, H.V) or grad.dtype != torch.float32 or grad.get_device() != dev or
+          (H.V > 1 and grad.stride(1) != 1)):
+        raise ValueError(f"grad must be fp32 [{H.d}, {H.V}] with contiguous rows on {h.device}")
+    need = lib().dprc_head_clip_accumulate_workspace(ctypes.byref(H))
+    ws = _workspace(need, h.device, ws)
+    _check(lib().dprc_head_clip_accumulate(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev),
+                                           _vector(c, "c", H.B, dev), grad.data_ptr(), grad.stride(0) if H.d > 1 else H.V,
+                                           int(bool(accumulate)), ws.data_ptr(), need, _stream(h.device)))
+    return grad
+
+
+def _apart(x):
+    """Whether no two elements of x share an address."""
+    span = 1
+    for s, n in sorted((s, n) for s, n in zip(x.stride(), x.shape) if n > 1):
+        if s < span:
+            return False
+        span = s * n
+    return True
+
+
+def dprc_rotary(x, freqs, pos=None, start=0, scale=1.0, interleaved=False, inverse=False, heads_first=False, out=None,
+                out_dtype=None):
+    """The first 2 len(freqs) features of every head of x [B, T, H, D] turned by position * freqs (fp64 radians).
+
+    x may be a list of up to four tensors (q and k) of one type; the result is a list then.  Positions are pos
+    [B, T] (int64), or start + t.  inverse turns back: the same call on a gradient is the backward pass.  A result
+    that is not given in out (x itself, too) is in the memory order [B, T, H, D], or [B, H, T, D] with
+    heads_first; its shape is x's."""
+    xs = x if isinstance(x, (list, tuple)) else [x]
+    outs = [None] * len(xs) if out is None else list(out) if isinstance(out, (list, tuple)) else [out]
+    if not xs or len(outs) != len(xs):
+        raise ValueError("one result per tensor")
+    B, T, _, D = xs[0].shape if xs[0].dim() == 4 else (0, 0, 0, 0)
+    dtype, dev, index = xs[0].dtype, xs[0].device, xs[0].get_device()
+    ydtype = dtype if out_dtype is None else out_dtype
+    if outs[0] is not None:
+        ydtype = outs[0].dtype
+    desc = array.array("q")
+    for j, t in enumerate(xs):
+        if t.dim() != 4 or t.shape[0] != B or t.shape[1] != T or t.shape[3] != D or t.dtype != dtype or t.get_device() != index:
+            raise ValueError(f"every tensor must be [{B}, {T}, heads, {D}] {dtype} on {dev}")
+        H = t.shape[2]
+        y = outs[j]
+        if y is None:
+            if heads_first:
+                y = torch.empty((B, H, T, D), dtype=ydtype, device=dev).transpose(1, 2)
+            else:
+                y = torch.empty((B, T, H, D), dtype=ydtype, device=dev)
+            outs[j] = y
+        elif y.shape != t.shape or y.dtype != ydtype or y.get_device() != index or not _apart(y):
+            raise ValueError(f"out must be {list(t.shape)} {ydtype} on {dev}, no element twice")
+        (xb, xt, xh, xd), (yb, yt, yh, yd) = t.stride(), y.stride()
+        if (xd != 1 or yd != 1) and D > 1:
+            raise ValueError("a head's features must be contiguous")
+        desc.extend((t.data_ptr(), y.data_ptr(), H, xb, xt, xh, yb, yt, yh))
+    if len({y.data_ptr() for y in outs}) < len(outs):
+        raise ValueError("a result is listed twice")
+    if freqs.dim() != 1 or freqs.dtype != torch.float64:
+        raise ValueError("freqs must be fp64 [r]")
+    if pos is not None and pos.shape != (B, T):
+        raise ValueError(f"pos must be [{B}, {T}]")
+    R = Rope(B, T, D, freqs.numel(), _vector(freqs, "freqs", freqs.numel(), index, torch.float64),
+             _vector(pos, "pos", B * T, index, torch.int64), start, scale, bool(interleaved), bool(inverse),
+             _dtype_code(xs[0]), _dtype_code(outs[0]))
+    _check(lib().dprc_rotary(ctypes.byref(R), desc.buffer_info()[0], len(xs), _stream(dev)))
+    return outs if isinstance(x, (list, tuple)) else outs[0]
+
+
+def _tensor_rows(t, name):
+    """(rows, cols, row stride) of a contiguous tensor, or of a matrix with contiguous rows."""
+    if t.is_contiguous():
+        return 1, t.numel(), t.numel()
+    if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
+        return t.shape[0], t.shape[1], t.stride(0)
+    raise ValueError(f"{name} must be contiguous, or a matrix with contiguous rows of their own")
+
+
+def _tensors(tensors, outs):
+    """dprc_tensor array of the tensors (as 64-bit words), their number and device."""
+    words = array.array("q")
+    dev = index = None
+    for j, t in enumerate(tensors):
+        if dev is None:
+            dev, index = t.device, t.get_device()
+        rows, cols, ldx = _tensor_rows(t, "a tensor")
+        y, ldo = None, ldx
+        if outs is not None:
+            y = outs[j]
+            if y is not t:
+                if y.shape != t.shape or y.dtype != t.dtype or y.get_device() != index:
+                    raise ValueError("every result must have its tensor's shape, dtype and device")
+                r, c, ldo = _tensor_rows(y, "a result")
+                if r != rows:                  # one of them is contiguous
+                    rows, cols = t.shape
+                    ldx, ldo = ldx if ldx != t.numel() else cols, ldo if ldo != t.numel() else cols
+            y = y.data_ptr()
+        if t.get_device() != index:
+            raise ValueError("the tensors must be on one GPU")
+        words.extend((t.data_ptr(), y or 0, rows, cols, ldx, ldo, _dtype_code(t)))
+    return words, dev
+
+
+def _grad_norm_args(tensors, outs, norm, ws):
+    words, dev = _tensors(tensors, outs)
+    if dev is None:
+        raise ValueError("no tensors")
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    at, n = words.buffer_info()[0], len(words) // 7
+    stream = _stream(dev)
+    need = lib().dprc_grad_norm_workspace(at, n)
+    return words, at, n, norm, _vector(norm, "norm", 1, tensors[0].get_device()), _workspace(need, dev, ws), need, stream
+
+
+def dprc_grad_norm(tensors, norm=None, ws=None):
+    """The joint 2-norm of a list of tensors (bf16 or fp32, any shapes): returns norm [1] fp32."""
+    words, at, n, norm, out, ws, need, stream = _grad_norm_args(tensors, None, norm, ws)
+    _check(lib().dprc_grad_norm(at, n, out, ws.data_ptr(), need, stream))
+    return norm
+
+
+def dprc_grad_clip(tensors, max_norm, outs=None, norm=None, ws=None):
+    """Every tensor times min(1, max_norm / the joint norm), into outs (by default the tensors themselves): returns
+    (outs, norm [1]).  A norm that is not finite gives zeros."""
+    outs = list(tensors) if outs is None else list(outs)
+    if len(outs) != len(tensors):
+        raise ValueError("one result per tensor")
+    places = [y.data_ptr() for y in outs if y.numel()]
+    if len(set(places)) < len(places):
+        raise ValueError("a result is listed twice")
+    words, at, n, norm, out, ws, need, stream = _grad_norm_args(tensors, outs, norm, ws)
+    _check(lib().dprc_grad_clip(at, n, max_norm, out, ws.data_ptr(), need, stream))
+    return outs, norm
+
+
 def dprc_version():
     return lib().dprc_version().decode()
 
@@ -646,7 +915,9 @@ KERNEL_NAMES = {1: "project", 2: "token_reduce", 3: "qr", 4: "hutchpp_final", 5:
                 11: "token_reduce_f32", 12: "sample_sq", 13: "accumulate_f32",
                 14: "token_splits", 15: "sample_sum", 16: "qr_combine", 17: "qr_expand", 18: "hutchpp_sum",
                 19: "probe_gauss", 20: "adamw", 21: "envelope", 22: "chi2_cdf", 23: "pld", 24: "dropout",
-                25: "layernorm", 26: "layernorm_backward", 27: "vector_norms", 28: "vector_sums"}
+                25: "layernorm", 26: "layernorm_backward", 27: "vector_norms", 28: "vector_sums", 29: "head_sums",
+                30: "head_join", 31: "head_errors", 32: "head_back", 33: "head_rows", 34: "rotary", 35: "grad_squares",
+                36: "grad_scale"}
 
 
 def dprc_trace_launches(events_ptr, kinds_ptr, capacity, count_ptr):

@@ -1,0 +1,303 @@
+"""The output head's cross entropy and its gradients against the 64-bit oracle.
+
+Tolerances, with u = 2^-24 and r = 2^-8 for bf16 heads (0 for fp32):
+
+* a logit is a chain of at most d fp32 sums of exact (bf16) or once rounded products: off by (d + 1) u times the
+  sum of its terms' magnitudes; delta_t is the largest of a token;
+* exp(l - c) is taken as 2^(l log2 e - c log2 e): the product with log2 e, the two roundings of the
+  difference and of log2 e itself are off by 4 u (|l| + |c|) at most in the exponent, 2^x by 4 u of itself,
+  and what lies below the smallest normal number may become zero: 2^-126 for p and for E each;
+* lse: the sum of V positive terms in chains of at most 160 + V / 128 roundings, the logarithm and its
+  sum with the maximum 4 u of their magnitudes: delta + 4 u (|top| + max|l|) + (170 + V / 128) u + 4 u |lse|;
+* loss: that, delta again for the target's logit, and u of the difference's terms;
+* E: |g| p times what the exponent is off by, 8 u |E| for the products (of the target's entry: 4 u |g| more for
+  the difference), and r |E|;
+* dh, dW: E's own error through the product, chains of at most V (N) sums and 64 planes: (V + 64) u times the
+  terms' magnitudes, and r of the result.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import estimators as est
+from oracle import head as O
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+R = {"bf16": 2.0 ** -8, "f32": 0.0}
+f64 = est.as_f64
+
+
+@pytest.fixture(scope="module")
+def D():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2605_24879_amd import dprc
+    dprc.lib()
+    return dprc
+
+
+def make(B, T, d, V, dtype, seed=0, pad=0, wpad=0, scale=1.0, ignored="some"):
+    """h, W, target, g; what lies between the rows is NaN, and so are the rows without a target."""
+    gen = torch.Generator().manual_seed(seed)
+    W = torch.full((V, d + wpad), float("nan"))
+    W[:, :d] = torch.randn(V, d, generator=gen) * (scale / d ** 0.5)
+    W = W.to(DT[dtype]).cuda()[:, :d]
+    target = torch.randint(0, V, (B, T), generator=gen)
+    h = torch.full((B, T, d + pad), float("nan"))
+    h[..., :d] = torch.randn(B, T, d, generator=gen) + 4.0 * torch.rand(B, T, 1, generator=gen) * W.cpu()[target].float()
+    if ignored == "some":
+        target[torch.rand(B, T, generator=gen) < 0.2] = -100
+    elif ignored == "all":
+        target[:] = -1
+    g = torch.randn(B, T, generator=gen) / T
+    return h.to(DT[dtype]).cuda()[..., :d], W, target.cuda(), g.cuda()
+
+
+def spoil(h, target, g):
+    """NaN and infinity where nothing has a loss."""
+    h, g = h.clone(), g.clone()
+    h[target < 0] = float("nan")
+    g[target < 0] = float("inf")
+    return h, g
+
+
+def delta(h, W):
+    return (h.shape[-1] + 1) * U * (np.abs(h) @ np.abs(W).T).max(-1)
+
+
+def exponent(h, W, lse):
+    return delta(h, W) + 4 * U * (np.abs(h @ W.T).max(-1) + np.abs(lse))
+
+
+def within(got, ref, tol, name=""):
+    got = f64(got)
+    bad = ~(np.abs(got - ref) <= tol)
+    assert not bad.any(), (name, int(bad.sum()), got[bad][:4], ref[bad][:4], np.broadcast_to(tol, ref.shape)[bad][:4])
+
+
+SHAPES = [(1, 1, 1, 1), (1, 1, 8, 2), (2, 3, 5, 7), (1, 1, 64, 300), (2, 37, 72, 257), (3, 50, 136, 1009), (64, 1, 96, 1500),
+          (65, 1, 200, 513), (1, 300, 129, 777), (2, 130, 320, 2050), (1, 257, 1030, 260)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,d,V", SHAPES)
+def test_loss(D, B, T, d, V, dtype):
+    h, W, target, _ = make(B, T, d, V, dtype, seed=V)
+    loss, lse = D.dprc_head_loss(h, W, target)
+    hn, Wn, tn = f64(h), f64(W), target.cpu().numpy()
+    rl, rz = O.loss(hn, Wn, tn)
+    big = np.abs(hn @ Wn.T).max(-1)
+    tz = delta(hn, Wn) + 8 * U * big + (170 + V / 128) * U + 4 * U * np.abs(rz)
+    within(lse, rz, tz, "lse")
+    within(loss, rl, np.where(tn < 0, 0.0, tz + delta(hn, Wn) + 2 * U * (np.abs(rz) + big)), "loss")
+
+
+def check_backward(D, h, W, target, g, dtype, **kw):
+    lse = D.dprc_head_loss(h, W, target)[1]
+    hn, Wn, tn, zn, gn = f64(h), f64(W), target.cpu().numpy(), f64(lse), f64(g)
+    E = O.errors(hn, Wn, tn, zn, gn)
+    kept = (tn >= 0)[..., None]
+    p = np.where(kept, np.exp(hn @ Wn.T - zn[..., None]), 0.0)
+    ga = np.where(kept, np.abs(gn)[..., None], 0.0)
+    tE = ga * p * (exponent(hn, Wn, zn)[..., None] + 8 * U) + 8 * U * np.abs(E) + R[dtype] * np.abs(E) + (1 + ga) * 2.0 ** -126
+    np.put_along_axis(tE, np.maximum(tn, 0)[..., None], np.take_along_axis(tE + 4 * U * ga, np.maximum(tn, 0)[..., None], -1), -1)
+    tE = np.where(kept, tE, 0.0)
+    hs, gs = spoil(h, target, g)
+    within(D.dprc_head_errors(hs, W, target, lse, gs), E, tE, "E")
+    dh, dW = D.dprc_head_backward(hs, W, target, lse, gs, **kw)
+    V, N = W.shape[0], h.shape[0] * h.shape[1]
+    ref = E @ Wn
+    within(dh, ref, tE @ np.abs(Wn) + (V + 64) * U * (np.abs(E) + tE) @ np.abs(Wn) + R[dtype] * 1.01 * np.abs(ref)
+           + R[dtype] * tE @ np.abs(Wn), "dh")
+    Ef, tf, hf = E.reshape(N, V), tE.reshape(N, V), np.where(kept, hn, 0.0).reshape(N, -1)
+    ref = Ef.T @ hf
+    own = tf.T @ np.abs(hf)
+    within(dW, ref, own * (1 + R[dtype]) + (N + 64) * U * (np.abs(Ef) + tf).T @ np.abs(hf) + R[dtype] * 1.01 * np.abs(ref), "dW")
+    return lse, E
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,d,V", SHAPES)
+def test_backward(D, B, T, d, V, dtype):
+    h, W, target, g = make(B, T, d, V, dtype, seed=V + 1)
+    check_backward(D, h, W, target, g, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("pad,wpad,d", [(3, 0, 128), (8, 8, 128), (0, 5, 64), (1, 1, 131), (0, 0, 131), (4, 4, 132)])
+def test_strides(D, pad, wpad, d, dtype):
+    h, W, target, g = make(2, 90, d, 600, dtype, seed=pad, pad=pad, wpad=wpad)
+    check_backward(D, h, W, target, g, dtype)
+    base = D.dprc_head_loss(h.contiguous(), W.contiguous(), target)
+    got = D.dprc_head_loss(h, W, target)
+    for x, y in zip(base, got):
+        torch.testing.assert_close(x, y, rtol=1e-6, atol=1e-6, equal_nan=True)
+    # results into rows of their own, what lies between them left alone
+    out = torch.full((2, 90, d + 5), 7.0, dtype=h.dtype, device="cuda")
+    wide = torch.full((600, d + 3), 7.0, dtype=h.dtype, device="cuda")
+    dh, dW = D.dprc_head_backward(h, W, target, base[1], g, dh=out[..., :d], dW=wide[:, :d])
+    r = D.dprc_head_backward(h, W, target, base[1], g)
+    assert torch.equal(dh, r[0]) and torch.equal(dW, r[1])
+    assert (out[..., d:] == 7).all() and (wide[:, d:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V,piece", [(20000, 8192), (16384, 8192), (16400, 16384), (8193, 8192), (17001, 0)])
+def test_pieces(D, V, piece, dtype):
+    h, W, target, g = make(2, 35, 48, V, dtype, seed=V)
+    check_backward(D, h, W, target, g, dtype, piece=piece)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_logits(D, dtype):
+    """Probabilities of 1 and of 0: logits of hundreds."""
+    h, W, target, g = make(2, 70, 64, 500, dtype, seed=5, scale=300.0)
+    check_backward(D, h, W, target, g, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_no_targets_at_all(D, dtype):
+    h, W, target, g = make(2, 70, 64, 500, dtype, seed=5, ignored="all")
+    loss, lse = D.dprc_head_loss(h, W, target)
+    assert (loss == 0).all() and lse.isfinite().all()
+    hs, gs = spoil(h, target, g)
+    dh, dW, n2 = D.dprc_head_backward(hs, W, target, lse, gs, k=4)
+    assert not dh.any() and not dW.any() and not n2.any()
+    assert not D.dprc_head_clip_accumulate(hs, W, target, lse, gs, torch.ones(2, device="cuda")).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_targets_past_the_vocabulary_and_infinite_logits(D, dtype):
+    h, W, target, g = make(2, 70, 64, 500, dtype, seed=6, ignored="none")
+    clean = D.dprc_head_loss(h, W, target)
+    target[0, 3], target[1, 5] = 500, 2 ** 40
+    loss, lse = D.dprc_head_loss(h, W, target)
+    bad = torch.zeros_like(target, dtype=torch.bool)
+    bad[0, 3] = bad[1, 5] = True
+    assert torch.equal(loss.isnan(), bad) and torch.equal(lse.isnan(), bad)
+    assert torch.equal(loss[~bad], clean[0][~bad])
+    dh, _ = D.dprc_head_backward(h, W, target, lse, g)
+    assert torch.equal(dh.isnan().all(-1), bad) and torch.equal(dh.isnan().any(-1), bad)
+    # a row of the vocabulary at -infinity takes no part (all features of h positive)
+    hp, Wi = h.abs(), W.clone()
+    Wi[17] = float("-inf")
+    some = torch.where(target == 17, 18, target).clamp(max=499)
+    keep = torch.arange(500, device="cuda") != 17
+    l1, z1 = D.dprc_head_loss(hp, Wi, some)
+    l0, z0 = D.dprc_head_loss(hp, W[keep].contiguous(), some - (some > 17).long())
+    torch.testing.assert_close(z1, z0, rtol=1e-5, atol=1e-5)
+    torch.testing.assert_close(l1, l0, rtol=1e-5, atol=1e-5)
+    assert (D.dprc_head_errors(hp, Wi, some, z1, g)[..., 17] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("side", [0, 1, 2])
+@pytest.mark.parametrize("probe,k", [(0, 16), (2, 8), (0, 33)])
+def test_private(D, dtype, side, probe, k):
+    """The estimates are those of the head's blocks as layers, the clipped gradient theirs side by side."""
+    B, T, d, V = 3, 40, 72, 20001
+    h, W, target, g = make(B, T, d, V, dtype, seed=side)
+    lse = D.dprc_head_loss(h, W, target)[1]
+    E = D.dprc_head_errors(h, W, target, lse, g)
+    hs, gs = spoil(h, target, g)
+    start = torch.rand(B, device="cuda")
+    for piece in (8192, 16384, 0):
+        dh, dW, n2 = D.dprc_head_backward(hs, W, target, lse, gs, hidden_grad=False, weight_grad=False, k=k, seed=11,
+                                          layer_id=7, side=side, probe=probe, piece=piece)
+        assert dh is None and dW is None
+        ref = 0
+        for b, v0 in enumerate(range(0, V, D.HEAD_BLOCK)):
+            Ab = torch.where((target >= 0)[..., None], h, torch.zeros_like(h)).contiguous()
+            ref = ref + D.dprc_norm_hutch([(Ab, E[..., v0:v0 + D.HEAD_BLOCK].contiguous(), 7 + b)], k, 11, side=side,
+                                          probe=probe).double()
+        np.testing.assert_allclose(f64(n2), f64(ref), rtol=1e-5)
+        more = start.clone()
+        D.dprc_head_backward(hs, W, target, lse, gs, k=k, seed=11, layer_id=7, side=side, probe=probe, piece=piece, n2=more,
+                             accumulate=True)
+        np.testing.assert_allclose(f64(more), f64(start) + f64(n2), rtol=1e-5)
+        c = torch.tensor([0.5, 0.0, 1.0], device="cuda")
+        grad = D.dprc_head_clip_accumulate(hs, W, target, lse, gs, c, piece=piece)
+        En, hn, cn = f64(E), np.where((target >= 0).cpu().numpy()[..., None], f64(h), 0.0), f64(c)
+        rg = est.clip_accumulate(hn, En, cn)
+        mag = est.clip_accumulate(np.abs(hn), np.abs(En), cn)
+        within(grad, rg, (B * T + 8) * U * mag, "grad")       # chains of B T sums, a rescaling for every sample
+        wide = torch.full((d, V + 3), 2.0, device="cuda")
+        D.dprc_head_clip_accumulate(hs, W, target, lse, gs, c, grad=wide[:, :V], accumulate=True, piece=piece)
+        within(wide[:, :V], rg + 2.0, (B * T + 8) * U * mag + U * (np.abs(rg) + 2.0), "grad")
+        assert (wide[:, V:] == 2).all()
+
+
+def test_errors_of_columns(D):
+    h, W, target, g = make(2, 40, 64, 3001, "bf16", seed=9)
+    lse = D.dprc_head_loss(h, W, target)[1]
+    E = D.dprc_head_errors(h, W, target, lse, g)
+    buf = torch.full((2, 40, 1007), 5.0, dtype=torch.bfloat16, device="cuda")
+    for v0, nv in ((0, 1), (3000, 1), (1234, 1001), (256, 512)):
+        buf[:] = 5.0
+        out = D.dprc_head_errors(h, W, target, lse, g, v0=v0, nv=nv, E=buf[..., 1:1 + nv])
+        assert torch.equal(out, E[..., v0:v0 + nv])
+        assert (buf[..., 0] == 5).all() and (buf[..., 1 + nv:] == 5).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_gradient_is_that_of_differences(D, dtype):
+    """sum g loss along a direction of h and of W against dh and dW (fp32 inputs; bf16 through its own loss)."""
+    h, W, target, g = make(2, 20, 40, 300, dtype, seed=3)
+    lse = D.dprc_head_loss(h, W, target)[1]
+    dh, dW = D.dprc_head_backward(h, W, target, lse, g)
+    hn, Wn, tn, gn = f64(h), f64(W), target.cpu().numpy(), f64(g)
+    rng = np.random.default_rng(0)
+    uh, uw, eps = rng.standard_normal(hn.shape), rng.standard_normal(Wn.shape), 1e-5
+    f = lambda a: (gn * O.loss(hn + a * uh, Wn + a * uw, tn)[0]).sum()
+    slope = (f(eps) - f(-eps)) / (2 * eps)
+    terms = np.abs(f64(dh) * uh).sum() + np.abs(f64(dW) * uw).sum()
+    # the difference's own error is of order eps^2; the gradients' that of the other tests
+    assert abs((f64(dh) * uh).sum() + (f64(dW) * uw).sum() - slope) <= (2 * R[dtype] + 1e-5) * terms
+
+
+def test_repeats_and_streams(D):
+    """Two calls at once, on streams of their own with workspaces of their own, give what one gives."""
+    h, W, target, g = make(2, 300, 128, 9000, "bf16", seed=4)
+    lse = D.dprc_head_loss(h, W, target)[1]
+    ref = D.dprc_head_backward(h, W, target, lse, g, k=8, seed=1)
+    s = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    out = []
+    for st in s:
+        with torch.cuda.stream(st):
+            l, z = D.dprc_head_loss(h, W, target)
+            out.append((z, *D.dprc_head_backward(h, W, target, z, g, k=8, seed=1)))
+    torch.cuda.synchronize()
+    for z, *rest in out:
+        assert torch.equal(z, lse) and all(torch.equal(a, b) for a, b in zip(rest, ref))
+
+
+def test_captured(D):
+    h, W, target, g = make(2, 100, 128, 9000, "bf16", seed=8)
+    static = dict(h=h.clone(), g=g.clone(), target=target.clone())
+    c = torch.tensor([0.5, 1.0], device="cuda")
+
+    def step():
+        loss, lse = D.dprc_head_loss(static["h"], W, static["target"])
+        dh, dW, n2 = D.dprc_head_backward(static["h"], W, static["target"], lse, static["g"], k=8, seed=1)
+        return loss, lse, dh, dW, n2, D.dprc_head_clip_accumulate(static["h"], W, static["target"], lse, static["g"], c)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step()
+    for seed in (8, 21, 22):
+        h2, _, t2, g2 = make(2, 100, 128, 9000, "bf16", seed=seed)
+        for k, v in dict(h=h2, g=g2, target=t2).items():
+            static[k].copy_(v)
+        graph.replay()
+        got = [o.clone() for o in outs]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, step()))
