@@ -23,13 +23,14 @@ typedef __attribute__((__vector_size__(16 * sizeof(float)))) float f32x16_t;
 constexpr float kLog2e = 1.44269504088896340736f;
 
 // The tile of a workgroup: a contiguous share of the tiles for every XCD (workgroups are dealt to the 8 XCDs
-// in turn), in groups of 8 row tiles walked column by column, so that 32 neighbours share 8 + 4 operand
-// slabs in the XCD's L2.
+// in turn), in groups of 4 row tiles walked column by column, so that 32 neighbours share 4 + 8 operand
+// slabs in the XCD's L2.  (128000 x 8192 x 2048 in groups of 4, 8, 16, 32: 3225, 3258, 3288, 3810 us.)
 __device__ __forceinline__ void tile_of(int64_t wg, int64_t tm_n, int64_t tn_n, int64_t& tm, int64_t& tn) {
+  constexpr int GROUP = 4;
   const int64_t n = tm_n * tn_n, x = wg & 7;
   const int64_t lin = x * (n >> 3) + min(x, n & 7) + (wg >> 3);
-  const int64_t group = lin / (8 * tn_n), r = lin - group * 8 * tn_n, rows = min((int64_t)8, tm_n - 8 * group);
-  tm = 8 * group + r % rows;
+  const int64_t group = lin / (GROUP * tn_n), r = lin - group * GROUP * tn_n, rows = min((int64_t)GROUP, tm_n - GROUP * group);
+  tm = GROUP * group + r % rows;
   tn = r / rows;
 }
 
@@ -48,83 +49,136 @@ struct HeadTile {
 };
 
 constexpr int kHK = 64;               // contraction elements per bf16 slab
-constexpr int kHPitchR = 256 + 32;    // LDS row of a KR slab: as in the accumulation's transpose reads
 
-// Eight elements at (row, col), zeros past the rows and the width.  VEC: `r` is a buffer resource from row0 on.
-template <bool VEC>
-__device__ __forceinline__ uint4 operand_piece(const HeadRows& X, __amdgpu_buffer_rsrc_t r, int64_t row0, int row,
-                                               int64_t col) {
-  const bool in = row0 + row < X.rows && col < X.width;
-  if constexpr (VEC) return buffer_load16(r, in ? (uint32_t)row * (uint32_t)X.ld * 2u + (uint32_t)col * 2u : kOobOffset);
-  if (!in) return uint4{0, 0, 0, 0};
+// The slabs in LDS, two of each operand.  KC: rows of 128 bytes, the eight 16-byte pieces of row r at piece ^
+// (r & 7), so that a fragment read of 8 rows covers all banks.  KR: 64 rows of the tile's width, piece p of
+// row r at p ^ swizzle_kr(r), so that the 4 (8) rows of a transposing read lie in different 32-byte (128-byte)
+// parts of the banks.  Four arrays and not one: the compiler then knows that loads into one do not
+// reach reads of another, and does not wait for them.
+template <class TL, bool BKR>
+struct HeadSlabs {
+  static constexpr int A = TL::MT * kHK, B = TL::NT * kHK;
+};
+__device__ __forceinline__ int swizzle_kr(int r) { return ((r & 3) << 1) | (r & 8); }
+
+// Eight elements at (row, col), zeros past the rows and the width, at any alignment.
+__device__ __forceinline__ uint4 operand_piece(const HeadRows& X, int64_t row, int64_t col) {
+  if (row >= X.rows || col >= X.width) return uint4{0, 0, 0, 0};
   const uint16_t* p = static_cast<const uint16_t*>(X.p);
-  const int64_t at = (row0 + row) * X.ld + col, room = (X.rows - 1) * X.ld + X.width - 8;
-  if (room < 0) return load8_elem(p + (row0 + row) * X.ld, col, X.width, true);
+  const int64_t at = row * X.ld + col, room = (X.rows - 1) * X.ld + X.width - 8;
+  if (room < 0) return load8_elem(p + row * X.ld, col, X.width, true);
   const int64_t from = min(at, room);
   const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p + from);
   return first_elems(shr_elems(uint4{v[0], v[1], v[2], v[3]}, (int)(at - from)), (int)min((int64_t)8, X.width - col));
 }
 
-template <bool VEC>
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t operand_rsrc(const HeadRows& X, int64_t row0, int tile) {
-  const int64_t left = X.rows - row0;
-  const uint32_t rows = (uint32_t)(left < 0 ? 0 : left < tile ? left : tile);
-  return buffer_rsrc(static_cast<const uint16_t*>(X.p) + (VEC && rows ? row0 * X.ld : 0),
-                     VEC ? rows * (uint32_t)X.ld * 2u : 0u);
+// 64 lanes' 16-byte pieces at byte offsets `off` of the resource to 1024 bytes of LDS, in lane order; zeros
+// where the offset is out of the resource's range.
+typedef __attribute__((address_space(3))) void lds_void_t;
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint16_t* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, 0, 0, 0);
 }
+
+template <int V>
+struct HInt {
+  static constexpr int value = V;
+};
 
 // acc = sum over k in [k0, k1) of A[m0 + i][k] B[n0 + j][k] (BKR: B[k][n0 + j]), bf16 operands, k0 a multiple
-// of kHK.  A slab of kHK is double-buffered through LDS: KC rows of 128 bytes with the eight 16-byte pieces
-// of row r at piece ^ (r & 7), so that a fragment read of 8 rows covers all banks; KR rows padded, read
-// back transposed.
-template <class TL, bool BKR>
-constexpr int head_lds_bytes() {
-  return 2 * 2 * (TL::MT * kHK + (BKR ? kHK * kHPitchR : TL::NT * kHK));
-}
-
+// of kHK.  Slabs of kHK are double-buffered: while one is multiplied the next is loaded, straight into
+// LDS where the operand's rows allow 16-byte pieces (VA, VB), else through registers.  A wave has the
+// fragments of 16 contraction elements in registers ahead of their products, also across the slab's one
+// barrier, and reads and products are issued in turn.  256 x 256 tiles of 128000 x 8192 x 2048: 1330
+// TFLOP/s (the same loop as the compiler orders it 1146, all reads before all products 1270, four waves of
+// 128 x 128 1217, tiles of 128 x 128 1093).
 template <class TL, bool BKR, bool VA, bool VB>
 __device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, const HeadRows& B, int64_t n0, int64_t k0,
-                                             int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB], uint16_t* lds) {
-  constexpr int XB = TL::XB, YB = TL::YB;
-  constexpr int PA = TL::MT * 8 / TL::threads, PB = TL::NT * 8 / TL::threads;
-  constexpr int BSZ = BKR ? kHK * kHPitchR : TL::NT * kHK;
-  uint16_t* la[2] = {lds, lds + TL::MT * kHK};
-  uint16_t* lb[2] = {lds + 2 * TL::MT * kHK, lds + 2 * TL::MT * kHK + BSZ};
+                                             int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB], uint16_t* la0, uint16_t* la1,
+                                             uint16_t* lb0, uint16_t* lb1) {
+  constexpr int XB = TL::XB, YB = TL::YB, TH = TL::threads;
+  constexpr int PA = TL::MT * 8 / TH, PB = TL::NT * 8 / TH, BP = TL::NT / 8;     // pieces a thread; of a KR row
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int wave0 = 64 * (int)__builtin_amdgcn_readfirstlane(wv);
   const int wm = wv / TL::WN, wn = wv % TL::WN;
-  uint4 ga[PA], gb[PB];
-  auto gload = [&](int64_t k) __attribute__((always_inline)) {
-    const __amdgpu_buffer_rsrc_t ra = operand_rsrc<VA>(A, m0, TL::MT);
+  auto kc_col = [](int s) { return 8 * ((s & 7) ^ ((s >> 3) & 7)); };
+  auto kr_col = [](int s) { return 8 * ((s % BP) ^ (swizzle_kr(s / BP) & (BP - 1))); };
+  // byte offsets of the thread's pieces in a slab
+  uint32_t oa[PA], ob[PB];
 #pragma unroll
-    for (int r = 0; r < PA; ++r) {
-      const int s = tid + TL::threads * r, row = s >> 3;
-      ga[r] = operand_piece<VA>(A, ra, m0, row, k + 8 * ((s & 7) ^ (row & 7)));
-    }
-    if constexpr (BKR) {
-      const __amdgpu_buffer_rsrc_t rb = operand_rsrc<VB>(B, k, kHK);
+  for (int r = 0; r < PA; ++r) {
+    const int s = tid + TH * r;
+    oa[r] = (uint32_t)(s >> 3) * (uint32_t)A.ld * 2u + 2u * kc_col(s);
+  }
 #pragma unroll
-      for (int r = 0; r < PB; ++r) {
-        const int s = tid + TL::threads * r;
-        gb[r] = operand_piece<VB>(B, rb, k, s / (TL::NT / 8), n0 + 8 * (s % (TL::NT / 8)));
+  for (int r = 0; r < PB; ++r) {
+    const int s = tid + TH * r;
+    if constexpr (BKR) ob[r] = n0 + kr_col(s) < B.width ? (uint32_t)(s / BP) * (uint32_t)B.ld * 2u + 2u * kr_col(s) : kOobOffset;
+    else ob[r] = (uint32_t)(s >> 3) * (uint32_t)B.ld * 2u + 2u * kc_col(s);
+  }
+  // a resource over `tile` rows from row0 on, `skip` elements into them
+  auto rsrc = [](const HeadRows& X, int64_t row0, int tile, int64_t skip) __attribute__((always_inline)) {
+    const int64_t left = X.rows - row0;
+    const uint32_t rows = (uint32_t)(left < 0 || skip >= X.width ? 0 : left < tile ? left : tile);
+    return buffer_rsrc(static_cast<const uint16_t*>(X.p) + (rows ? row0 * X.ld + skip : 0),
+                       rows ? rows * (uint32_t)X.ld * 2u - (uint32_t)skip * 2u : 0u);
+  };
+  uint4 ga[VA ? 1 : PA], gb[VB ? 1 : PB];
+  auto gload = [&](int64_t k, auto u) __attribute__((always_inline)) {
+    uint16_t* la = decltype(u)::value ? la1 : la0;
+    uint16_t* lb = decltype(u)::value ? lb1 : lb0;
+    const bool tail = k + kHK > A.width;               // columns past the rows' end
+    if constexpr (VA) {
+      const __amdgpu_buffer_rsrc_t ra = rsrc(A, m0, TL::MT, k);
+      if (tail) {
+#pragma unroll
+        for (int r = 0; r < PA; ++r)
+          load_to_lds(ra, la + 8 * (wave0 + TH * r), k + kc_col(tid + TH * r) < A.width ? oa[r] : kOobOffset);
+      } else {
+#pragma unroll
+        for (int r = 0; r < PA; ++r) load_to_lds(ra, la + 8 * (wave0 + TH * r), oa[r]);
       }
     } else {
-      const __amdgpu_buffer_rsrc_t rb = operand_rsrc<VB>(B, n0, TL::NT);
+#pragma unroll
+      for (int r = 0; r < PA; ++r) ga[r] = operand_piece(A, m0 + ((tid + TH * r) >> 3), k + kc_col(tid + TH * r));
+    }
+    if constexpr (VB && BKR) {
+      const __amdgpu_buffer_rsrc_t rb = rsrc(B, k, kHK, n0);
+#pragma unroll
+      for (int r = 0; r < PB; ++r) load_to_lds(rb, lb + 8 * (wave0 + TH * r), ob[r]);
+    } else if constexpr (VB) {
+      const __amdgpu_buffer_rsrc_t rb = rsrc(B, n0, TL::NT, k);
+      if (tail) {
+#pragma unroll
+        for (int r = 0; r < PB; ++r)
+          load_to_lds(rb, lb + 8 * (wave0 + TH * r), k + kc_col(tid + TH * r) < B.width ? ob[r] : kOobOffset);
+      } else {
+#pragma unroll
+        for (int r = 0; r < PB; ++r) load_to_lds(rb, lb + 8 * (wave0 + TH * r), ob[r]);
+      }
+    } else {
 #pragma unroll
       for (int r = 0; r < PB; ++r) {
-        const int s = tid + TL::threads * r, row = s >> 3;
-        gb[r] = operand_piece<VB>(B, rb, n0, row, k + 8 * ((s & 7) ^ (row & 7)));
+        const int s = tid + TH * r;
+        gb[r] = BKR ? operand_piece(B, k + s / BP, n0 + kr_col(s)) : operand_piece(B, n0 + (s >> 3), k + kc_col(s));
       }
     }
   };
-  auto swrite = [&](int buf) __attribute__((always_inline)) {
+  // what went through registers to LDS, then every wave's slab is there and the other's reads are done
+  auto arrive = [&](auto u) __attribute__((always_inline)) {
+    uint16_t* la = decltype(u)::value ? la1 : la0;
+    uint16_t* lb = decltype(u)::value ? lb1 : lb0;
+    if constexpr (!VA) {
 #pragma unroll
-    for (int r = 0; r < PA; ++r) *reinterpret_cast<uint4*>(&la[buf][8 * (tid + TL::threads * r)]) = ga[r];
-#pragma unroll
-    for (int r = 0; r < PB; ++r) {
-      const int s = tid + TL::threads * r;
-      const int at = BKR ? s / (TL::NT / 8) * kHPitchR + 8 * (s % (TL::NT / 8)) : 8 * s;
-      *reinterpret_cast<uint4*>(&lb[buf][at]) = gb[r];
+      for (int r = 0; r < PA; ++r) *reinterpret_cast<uint4*>(&la[8 * (tid + TH * r)]) = ga[r];
     }
+    if constexpr (!VB) {
+#pragma unroll
+      for (int r = 0; r < PB; ++r) *reinterpret_cast<uint4*>(&lb[8 * (tid + TH * r)]) = gb[r];
+    }
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+    __builtin_amdgcn_s_waitcnt(0);
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
   };
 #pragma unroll
   for (int x = 0; x < XB; ++x)
@@ -134,45 +188,66 @@ __device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, cons
       for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.f;
   const int l32 = lane & 31, half = lane >> 5;
   const int g = lane >> 4, r4 = (lane & 15) >> 2, c4 = lane & 3;
-  auto multiply = [&](int buf) __attribute__((always_inline)) {
+  uint4 f0a[XB], f0b[YB], f1a[XB], f1b[YB];
+  // the fragments of contraction elements 16 ks .. 16 ks + 15 of a slab
+  auto frag = [&](uint4 (&av)[XB], uint4 (&bv)[YB], auto u, int ks) __attribute__((always_inline)) {
+    const uint16_t* la = decltype(u)::value ? la1 : la0;
+    const uint16_t* lb = decltype(u)::value ? lb1 : lb0;
 #pragma unroll
-    for (int ks = 0; ks < kHK / 16; ++ks) {
-      uint4 av[XB], bv[YB];
-#pragma unroll
-      for (int x = 0; x < XB; ++x) {
-        const int row = 32 * (wm * XB + x) + l32;
-        av[x] = *reinterpret_cast<const uint4*>(&la[buf][row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
+    for (int y = 0; y < YB; ++y) {
+      if constexpr (BKR) {
+        // lane group g reads rows 8 (g / 2) + r4 (+ 4) of columns 16 (g % 2) + 4 c4 .. of the block
+        const int row = 16 * ks + 8 * (g >> 1) + r4, col = 32 * (wn * YB + y) + 16 * (g & 1) + 4 * c4;
+        const uint16_t* p = &lb[row * TL::NT + 8 * ((col >> 3) ^ (swizzle_kr(row) & (BP - 1))) + (col & 4)];
+        bv[y] = make_u4(lds_read_tr16(p), lds_read_tr16(p + 4 * TL::NT));
+      } else {
+        const int row = 32 * (wn * YB + y) + l32;
+        bv[y] = *reinterpret_cast<const uint4*>(&lb[row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
       }
+    }
 #pragma unroll
-      for (int y = 0; y < YB; ++y) {
-        if constexpr (BKR) {
-          const uint16_t* pe = &lb[buf][(16 * ks + 8 * (g >> 1) + r4) * kHPitchR + 32 * (wn * YB + y) + 16 * (g & 1) + 4 * c4];
-          bv[y] = make_u4(lds_read_tr16(pe), lds_read_tr16(pe + 4 * kHPitchR));
-        } else {
-          const int row = 32 * (wn * YB + y) + l32;
-          bv[y] = *reinterpret_cast<const uint4*>(&lb[buf][row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
-        }
-      }
-#pragma unroll
-      for (int x = 0; x < XB; ++x)
-#pragma unroll
-        for (int y = 0; y < YB; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
-                                                              __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
+    for (int x = 0; x < XB; ++x) {
+      const int row = 32 * (wm * XB + x) + l32;
+      av[x] = *reinterpret_cast<const uint4*>(&la[row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
     }
   };
-  gload(k0);
-  swrite(0);
-  __syncthreads();
-  int buf = 0;
-  for (int64_t k = k0; k < k1; k += kHK) {
-    const bool more = k + kHK < k1;                // uniform
-    if (more) gload(k + kHK);
-    multiply(buf);
-    if (more) swrite(buf ^ 1);
-    __syncthreads();
-    buf ^= 1;
+  auto phase = [&](uint4 (&na)[XB], uint4 (&nb)[YB], auto u, int ks, const uint4 (&av)[XB], const uint4 (&bv)[YB])
+      __attribute__((always_inline)) {
+    frag(na, nb, u, ks);
+#pragma unroll
+    for (int x = 0; x < XB; ++x)
+#pragma unroll
+      for (int y = 0; y < YB; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
+                                                            __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
+    constexpr int reads = XB + (BKR ? 2 : 1) * YB, products = XB * YB;
+#pragma unroll
+    for (int i = 0; i < reads; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);               // a read of LDS
+      if (i < products) __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);   // a product
+    }
+    if constexpr (products > reads) __builtin_amdgcn_sched_group_barrier(0x8, products - reads, 0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // the slab at k in buffers u, its first fragments in registers
+  auto step = [&](int64_t k, auto u) __attribute__((always_inline)) {
+    constexpr HInt<decltype(u)::value ^ 1> other{};
+    gload(k + kHK < k1 ? k + kHK : (int64_t)1 << 40, other);           // past the end: nothing
+    __builtin_amdgcn_sched_barrier(0);
+    phase(f1a, f1b, u, 1, f0a, f0b);
+    phase(f0a, f0b, u, 2, f1a, f1b);
+    phase(f1a, f1b, u, 3, f0a, f0b);
+    arrive(other);
+    phase(f0a, f0b, other, 0, f1a, f1b);
+  };
+  gload(k0, HInt<0>{});
+  arrive(HInt<0>{});
+  frag(f0a, f0b, HInt<0>{}, 0);
+  for (int64_t k = k0; k < k1; k += 2 * kHK) {       // (an odd number of slabs: the last one is zeros)
+    step(k, HInt<0>{});
+    step(k + kHK, HInt<1>{});
   }
+  __syncthreads();                                     // all reads are done
 }
 
 // fp32 operands, on the fp32 matrix cores (products and sums in fp32): slabs of 16 in LDS as [k][row].
@@ -318,23 +393,42 @@ __device__ __forceinline__ void head_sums(const HeadArgs& a, int64_t tm, int64_t
   }
 }
 
+// LDS for a tile of errors, token rows of MT: the 16-byte piece p of token t at p ^ (t & 31), so that the 32
+// tokens of a block, one a lane, go to different banks.  Four arrays of 64 tokens, or one.
+template <class TL>
+struct HeadStage {
+  typedef typename TL::elem E;
+  static constexpr int EP = kPiece<E>, PPR = TL::MT / EP;
+  static_assert(PPR == 32);
+  E *p0, *p1, *p2, *p3;
+  __device__ __forceinline__ E* piece(int token, int p) const {
+    const int part = sizeof(E) == 2 ? token >> 6 : 0;
+    E* base = part == 0 ? p0 : part == 1 ? p1 : part == 2 ? p2 : p3;
+    return base + ((sizeof(E) == 2 ? token & 63 : token) * PPR + (p ^ (token & 31))) * EP;
+  }
+};
+
 // The tile's errors, through LDS into token rows.
 template <class TL>
 __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64_t t0, f32x16_t (&acc)[TL::XB][TL::YB],
-                                            typename TL::elem* lds) {
+                                            const HeadStage<TL>& stage) {
   typedef typename TL::elem E;
-  constexpr int EP = kPiece<E>, PITCH = TL::MT + EP;
+  constexpr int EP = kPiece<E>, PPR = TL::MT / EP;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
   const int64_t vt = tm * TL::MT;                       // the tile's first column of this piece
+  const int v0 = 32 * TL::XB * wm;                      // the wave's first in the tile
+  const int end = (int)min((int64_t)TL::MT, a.nv - vt) - v0;       // its columns before the vocabulary's end
 #pragma unroll
   for (int y = 0; y < TL::YB; ++y) {
     const int col = 32 * (wn * TL::YB + y) + (lane & 31);
     const int64_t t = t0 + col;
     const int64_t target = t < a.N ? a.target[t] : -1;
-    const float lse = target >= 0 ? a.lse[t] : 0.f, g = target >= 0 ? a.g[t] : 0.f;
-    const int64_t at = target - a.v0 - vt - 32 * TL::XB * wm;       // the target's row among the wave's
+    const bool kept = target >= 0;
+    const float lse = kept ? a.lse[t] : 0.f, g = kept ? a.g[t] : 0.f;
+    const int64_t at64 = target - a.v0 - vt - v0;       // the target's place among the wave's columns
+    const int at = kept && at64 >= 0 && at64 < 32 * TL::XB ? (int)at64 : -1;
     const float lse2 = lse * kLog2e;
-    const bool here = __any(target >= 0 && at >= 0 && at < 32 * TL::XB);
+    const bool rare = __any(at >= 0) || end < 32 * TL::XB;
 #pragma unroll
     for (int x = 0; x < TL::XB; ++x)
 #pragma unroll
@@ -345,27 +439,31 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
           const float l = acc[x][y][4 * q4 + q];
           if constexpr (sizeof(E) == 2) e[q] = g * __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -lse2));
           else e[q] = g * expf(l - lse);
-          // exp(x) - 1 without cancellation; the target's row is in one wave of a column of them
-          if (here && at == 32 * x + acc_row(lane, 4 * q4 + q)) e[q] = g * expm1f(l - lse);
-          if (target < 0 || vt + 32 * (TL::XB * wm + x) + acc_row(lane, 4 * q4 + q) >= a.nv) e[q] = 0.f;
         }
-        E* o = lds + col * PITCH + 32 * (TL::XB * wm + x) + acc_row(lane, 4 * q4);
+        const int v = 32 * x + acc_row(lane, 4 * q4);
+        if (rare) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            if (at == v + q) e[q] = g * expm1f(acc[x][y][4 * q4 + q] - lse);   // exp(x) - 1 without cancellation
+            if (v + q >= end) e[q] = 0.f;
+          }
+        }
+        E* o = stage.piece(col, (v0 + v) / EP) + (v & (EP - 1));
         if constexpr (sizeof(E) == 2) {
-          *reinterpret_cast<uint2*>(o) =
-              uint2{__builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[0], e[1]}, bf16x2_t)),
-                    __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[2], e[3]}, bf16x2_t))};
+          const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[0], e[1]}, bf16x2_t));
+          const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[2], e[3]}, bf16x2_t));
+          *reinterpret_cast<uint2*>(o) = uint2{kept ? lo : 0u, kept ? hi : 0u};
         } else {
-          *reinterpret_cast<float4*>(o) = float4{e[0], e[1], e[2], e[3]};
+          *reinterpret_cast<float4*>(o) = kept ? float4{e[0], e[1], e[2], e[3]} : float4{0.f, 0.f, 0.f, 0.f};
         }
       }
   }
   __syncthreads();
-  constexpr int PPR = TL::MT / EP;                      // pieces per token row
   for (int s = threadIdx.x; s < TL::NT * PPR; s += TL::threads) {
-    const int row = s / PPR, c = EP * (s % PPR);
-    const int64_t t = t0 + row, v = vt + c;
+    const int row = s / PPR, p = s % PPR;
+    const int64_t t = t0 + row, v = vt + EP * p;
     if (t >= a.N || v >= a.width) continue;
-    const E* from = lds + row * PITCH + c;
+    const E* from = stage.piece(row, p);
     E* to = static_cast<E*>(a.E) + t * a.lde + v;
     if (v + EP <= a.width) store_piece<E>(to, *reinterpret_cast<const uint4*>(from));
     else
@@ -373,7 +471,7 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
   }
 }
 
-// The tile added to (or, FIRST, written to) its place of plane [rows][cols].
+// The tile written to, or added to, its place of a plane [N][d].
 template <class TL>
 __device__ __forceinline__ void head_store(const HeadBackArgs& a, float* plane, int64_t m0, int64_t n0,
                                            f32x16_t (&acc)[TL::XB][TL::YB]) {
@@ -396,16 +494,28 @@ __device__ __forceinline__ void head_store(const HeadBackArgs& a, float* plane, 
 
 // ---- kernels --------------------------------------------------------------------------------------
 
-template <class TL, bool ERRORS>
-constexpr int head_tail_bytes() {                      // LDS of what becomes of a tile
-  return ERRORS ? TL::NT * (TL::MT + kPiece<typename TL::elem>) * (int)sizeof(typename TL::elem) : 8 * TL::WM * TL::NT;
-}
-
 // The logits' tiles.  bf16: rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.
 template <class TL, bool ERRORS, bool VW>
 __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
-  constexpr bool F32 = sizeof(typename TL::elem) == 4;
-  constexpr int MAIN = F32 ? head_lds_bytes_f32<TL>() : head_lds_bytes<TL, false>(), TAIL = head_tail_bytes<TL, ERRORS>();
+  __shared__ __attribute__((aligned(16))) uint16_t la0[HeadSlabs<TL, false>::A];
+  __shared__ __attribute__((aligned(16))) uint16_t la1[HeadSlabs<TL, false>::A];
+  __shared__ __attribute__((aligned(16))) uint16_t lb0[HeadSlabs<TL, false>::B];
+  __shared__ __attribute__((aligned(16))) uint16_t lb1[HeadSlabs<TL, false>::B];
+  static_assert(TL::NT == 64 || (TL::MT == 256 && TL::NT == 256));
+  const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
+  const int64_t wg = flat_block();
+  if (wg >= tm_n * tn_n) return;
+  int64_t tm, tn;
+  tile_of(wg, tm_n, tn_n, tm, tn);
+  f32x16_t acc[TL::XB][TL::YB];
+  head_product<TL, false, VW, true>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, la0, la1, lb0, lb1);
+  if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, HeadStage<TL>{la0, la1, lb0, lb1});
+  else head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(la0));
+}
+
+template <class TL, bool ERRORS>
+__global__ __launch_bounds__(TL::threads) void head_logits_f32_kernel(HeadArgs a) {
+  constexpr int MAIN = head_lds_bytes_f32<TL>(), TAIL = ERRORS ? 4 * TL::MT * TL::NT : 8 * TL::WM * TL::NT;
   __shared__ __attribute__((aligned(16))) char lds[MAIN > TAIL ? MAIN : TAIL];
   const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
@@ -413,19 +523,19 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
   f32x16_t acc[TL::XB][TL::YB];
-  if constexpr (F32)
-    head_product_f32<TL, false>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, reinterpret_cast<float*>(lds));
-  else
-    head_product<TL, false, VW, true>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, reinterpret_cast<uint16_t*>(lds));
-  if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<typename TL::elem*>(lds));
+  float* l = reinterpret_cast<float*>(lds);
+  head_product_f32<TL, false>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, l);
+  if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, HeadStage<TL>{l, l, l, l});
   else head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(lds));
 }
 
 // dh's tiles: rows are tokens, columns features; blockIdx.z is the split of the piece's vocabulary.
 template <class TL, bool VW>
 __global__ __launch_bounds__(TL::threads) void head_back_kernel(HeadBackArgs a) {
-  constexpr bool F32 = sizeof(typename TL::elem) == 4;
-  __shared__ __attribute__((aligned(16))) char lds[F32 ? head_lds_bytes_f32<TL>() : head_lds_bytes<TL, true>()];
+  __shared__ __attribute__((aligned(16))) uint16_t la0[HeadSlabs<TL, true>::A];
+  __shared__ __attribute__((aligned(16))) uint16_t la1[HeadSlabs<TL, true>::A];
+  __shared__ __attribute__((aligned(16))) uint16_t lb0[HeadSlabs<TL, true>::B];
+  __shared__ __attribute__((aligned(16))) uint16_t lb1[HeadSlabs<TL, true>::B];
   const int64_t tm_n = (a.N + TL::MT - 1) / TL::MT, tn_n = (a.d + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
   if (wg >= tm_n * tn_n) return;
@@ -433,10 +543,21 @@ __global__ __launch_bounds__(TL::threads) void head_back_kernel(HeadBackArgs a) 
   tile_of(wg, tm_n, tn_n, tm, tn);
   const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.E.width, k0 + a.per_split);
   f32x16_t acc[TL::XB][TL::YB];
-  if constexpr (F32)
-    head_product_f32<TL, true>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, reinterpret_cast<float*>(lds));
-  else
-    head_product<TL, true, true, VW>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, reinterpret_cast<uint16_t*>(lds));
+  head_product<TL, true, true, VW>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, la0, la1, lb0, lb1);
+  head_store<TL>(a, a.planes + blockIdx.z * a.N * a.d, tm * TL::MT, tn * TL::NT, acc);
+}
+
+template <class TL>
+__global__ __launch_bounds__(TL::threads) void head_back_f32_kernel(HeadBackArgs a) {
+  __shared__ __attribute__((aligned(16))) char lds[head_lds_bytes_f32<TL>()];
+  const int64_t tm_n = (a.N + TL::MT - 1) / TL::MT, tn_n = (a.d + TL::NT - 1) / TL::NT;
+  const int64_t wg = flat_block();
+  if (wg >= tm_n * tn_n) return;
+  int64_t tm, tn;
+  tile_of(wg, tm_n, tn_n, tm, tn);
+  const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.E.width, k0 + a.per_split);
+  f32x16_t acc[TL::XB][TL::YB];
+  head_product_f32<TL, true>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, reinterpret_cast<float*>(lds));
   head_store<TL>(a, a.planes + blockIdx.z * a.N * a.d, tm * TL::MT, tn * TL::NT, acc);
 }
 
@@ -562,7 +683,7 @@ template <bool ERRORS>
 static hipError_t launch_head_logits(const HeadArgs& a, hipStream_t st) {
   if (!a.bf16) {
     const int64_t blocks = ceil_div(a.nv, TileF32::MT) * ceil_div(a.N, TileF32::NT);
-    DPRC_LAUNCH((head_logits_kernel<TileF32, ERRORS, true>), flat_grid(blocks), dim3(TileF32::threads), 0, st, a);
+    DPRC_LAUNCH((head_logits_f32_kernel<TileF32, ERRORS>), flat_grid(blocks), dim3(TileF32::threads), 0, st, a);
   } else if (a.N <= TileFew::NT) {
     launch_logits<TileFew, ERRORS>(a, st);
   } else {
@@ -598,7 +719,7 @@ hipError_t launch_head_back(const HeadBackArgs& a, hipStream_t st) {
     grid.z = (unsigned)a.S;
     DPRC_LAUNCH(kernel, grid, dim3(threads), 0, st, a);
   };
-  if (!a.bf16) go(head_back_kernel<TileF32, true>, TileF32::MT, TileF32::threads);
+  if (!a.bf16) go(head_back_f32_kernel<TileF32>, TileF32::MT, TileF32::threads);
   else if (a.vec_w) go(head_back_kernel<TileWide, true>, TileWide::MT, TileWide::threads);
   else go(head_back_kernel<TileWide, false>, TileWide::MT, TileWide::threads);
   return hipGetLastError();
