@@ -17,8 +17,12 @@ With ``junctions`` the norms, the residual sums before them and a dropout of rat
 (``norm``: "rms" or "layer"), which ``norms()`` lists for private training, and a
 dropout of the same rate inside the MLP as ``junction.Dropout`` (``dropouts()``).
 
+With ``rotary`` the rotary positions run as ``paper_2605_24879_amd.rotary.Rotary``, which turns q and k in one call;
+with ``head`` the output layer and its cross entropy as ``paper_2605_24879_amd.head.Head``: the model called with targets
+then gives per-token losses and stores no logits, and ``head`` is what private training takes.
+
 ``linears()`` lists the projections in model order (per block q, k, v, o,
-gate, up, down; then lm_head), which keeps the shared-input layers adjacent.
+gate, up, down; then lm_head, unless it runs as ``head``), which keeps the shared-input layers adjacent.
 """
 
 import itertools
@@ -57,7 +61,7 @@ def _rope(x, cos, sin):
 
 
 class Block(nn.Module):
-    def __init__(self, hidden, mlp, heads, kv_heads, make_norm=RMSNorm, make_drop=nn.Identity):
+    def __init__(self, hidden, mlp, heads, kv_heads, make_norm=RMSNorm, make_drop=nn.Identity, rotary=None):
         super().__init__()
         hd = hidden // heads
         self.heads, self.kv_heads, self.hd = heads, kv_heads, hd
@@ -71,13 +75,17 @@ class Block(nn.Module):
         self.up = nn.Linear(hidden, mlp, bias=False)
         self.down = nn.Linear(mlp, hidden, bias=False)
         self.act_drop = make_drop()
+        self.rotary = rotary                   # None: _rope
 
     def attend(self, h, cos, sin, mask):
         B, T, _ = h.shape
-        q = self.q(h).view(B, T, self.heads, self.hd).transpose(1, 2).float()
-        k = self.k(h).view(B, T, self.kv_heads, self.hd).transpose(1, 2).float()
+        q = self.q(h).view(B, T, self.heads, self.hd)
+        k = self.k(h).view(B, T, self.kv_heads, self.hd)
         v = self.v(h).view(B, T, self.kv_heads, self.hd).transpose(1, 2).float()
-        q, k = _rope(q, cos, sin), _rope(k, cos, sin)
+        if self.rotary is not None:
+            q, k = (x.transpose(1, 2) for x in self.rotary(q, k, heads_first=True, out_dtype=torch.float32))
+        else:
+            q, k = (_rope(x.transpose(1, 2).float(), cos, sin) for x in (q, k))
         rep = self.heads // self.kv_heads
         k = k.repeat_interleave(rep, dim=1)
         v = v.repeat_interleave(rep, dim=1).contiguous()
@@ -106,7 +114,7 @@ class JunctionBlock(Block):
 
 class LlamaShaped(nn.Module):
     def __init__(self, layers=16, hidden=2048, mlp=8192, heads=32, kv_heads=8, vocab=128256,
-                 rope_base=500000.0, junctions=False, norm="rms", dropout=0.0):
+                 rope_base=500000.0, junctions=False, norm="rms", dropout=0.0, rotary=False, head=False):
         super().__init__()
         self.embed = nn.Embedding(vocab, hidden)
         self.junctions = bool(junctions)
@@ -118,9 +126,19 @@ class LlamaShaped(nn.Module):
             make_drop = lambda: Dropout(dropout, site_id=next(sites))
         elif norm != "rms" or dropout:
             raise ValueError("layer norm and dropout come with junctions")
-        self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm, make_drop) for _ in range(layers)])
+        rot = None
+        if rotary:
+            from paper_2605_24879_amd.rotary import Rotary
+            with torch.device("cpu"):           # frequencies are values, whatever device the model is laid out on
+                rot = Rotary(hidden // heads, base=rope_base)
+        self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm, make_drop, rot) for _ in range(layers)])
         self.norm = make_norm(hidden)
         self.lm_head = nn.Linear(hidden, vocab, bias=False)
+        head_of = None
+        if head:
+            from paper_2605_24879_amd.head import Head
+            head_of = Head(self.lm_head)
+        self.__dict__["head"] = head_of         # not a submodule: the weight keeps its one name
         self.rope_base = rope_base
         self.hd = hidden // heads
 
@@ -128,7 +146,7 @@ class LlamaShaped(nn.Module):
         out = []
         for b in self.blocks:
             out += [b.q, b.k, b.v, b.o, b.gate, b.up, b.down]
-        return out + [self.lm_head]
+        return out if self.head is not None else out + [self.lm_head]
 
     def norms(self):
         return [m for b in self.blocks for m in (b.norm1, b.norm2)] + [self.norm]
@@ -136,7 +154,10 @@ class LlamaShaped(nn.Module):
     def dropouts(self):
         return [b.act_drop for b in self.blocks] if self.junctions else []
 
-    def forward(self, tokens):
+    def forward(self, tokens, targets=None):
+        """Logits [B, T, vocab], or with targets [B, T] (and the model's ``head``) the tokens' losses [B, T]."""
+        if targets is not None and self.head is None:
+            raise ValueError("losses come with head=True")
         B, T = tokens.shape
         cos, sin = _rope_tables(T, self.hd, self.rope_base, tokens.device)
         mask = torch.full((T, T), float("-inf"), device=tokens.device).triu(1)
@@ -145,10 +166,12 @@ class LlamaShaped(nn.Module):
             branch, x = x, None
             for b in self.blocks:
                 branch, x = b(branch, x, cos, sin, mask)
-            return self.lm_head(self.norm(branch, x)[0])
-        for b in self.blocks:
-            x = b(x, cos, sin, mask)
-        return self.lm_head(self.norm(x))
+            y = self.norm(branch, x)[0]
+        else:
+            for b in self.blocks:
+                x = b(x, cos, sin, mask)
+            y = self.norm(x)
+        return self.lm_head(y) if targets is None else self.head(y, targets)
 
 
 def build(seed=0, device="cuda", dtype=torch.bfloat16, **sizes):
