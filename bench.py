@@ -56,6 +56,8 @@ def parse():
                     help="replay a captured HIP graph per step instead of launching from the host")
     ap.add_argument("--junctions", action="store_true",
                     help="llama_step: residual sums and norms as fused junctions whose weights are trained too")
+    ap.add_argument("--head", action="store_true",
+                    help="llama_step: the output layer and its loss as a head that stores no logits, rotary positions by the library")
     ap.add_argument("--copy-calibration", type=float, default=0.0, metavar="BYTES",
                     help="only run 5 device copies of BYTES bytes (calibrates FETCH_SIZE / WRITE_SIZE counters)")
     return ap.parse_args()
@@ -582,12 +584,14 @@ def run_llama_step(args, torch, D):
     B, T, k, C, sigma = cfg["B"], cfg["T"], cfg["k"], cfg["C"], cfg["sigma"]
     steps, warmup = min(args.steps, 10), max(1, min(args.warmup, 3))
     print(f"[bench] workload=llama_step B={B} T={T}: building the model", file=sys.stderr, flush=True)
-    model = llama.build(seed=0, device="cuda", junctions=args.junctions)
+    model = llama.build(seed=0, device="cuda", junctions=args.junctions, head=args.head, rotary=args.head)
     tok = llama.tokens(B, T, llama.LLAMA_3_2_1B["vocab"], device="cuda")
     drv = dpsgd.DPSGDRC(model.linears(), C=C, sigma=sigma, k=k, lr=cfg["lr"],
-                        norms=model.norms() if args.junctions else ())
+                        norms=model.norms() if args.junctions else (), head=model.head)
     loss_fn = lambda: llama.per_sample_loss(model(tok[:, :-1]), tok[:, 1:])
-    layer_shapes = [(lin.in_features, lin.out_features) for lin in drv.linears]
+    if args.head:
+        loss_fn = lambda: model(tok[:, :-1], tok[:, 1:]).mean(dim=1)
+    layer_shapes = [(lin.in_features, lin.out_features) for lin in drv.linears + ([model.lm_head] if args.head else [])]
     Ev = lambda: torch.cuda.Event(enable_timing=True)
 
     def private_step(ev=None):
@@ -611,6 +615,7 @@ def run_llama_step(args, torch, D):
     for _ in range(warmup):
         private_step()
     torch.cuda.synchronize()
+    torch.cuda.reset_peak_memory_stats()
     print(f"[bench] llama_step: warm, timing {steps} steps", file=sys.stderr, flush=True)
     stage = [0.0] * 4
     t0, t1 = Ev(), Ev()
@@ -647,7 +652,8 @@ def run_llama_step(args, torch, D):
     extra = {"stages_ms": {"forward_and_capture": round(stage[0], 3), "norms_and_clip": round(stage[1], 3),
                            "clipped_gemm": round(stage[2], 3), "noise_and_adamw_fused": round(stage[3], 3)},
              "library_kernels": kernels}
-    if not args.no_extra and not args.junctions:
+    extra["peak_GB"] = round(torch.cuda.max_memory_allocated() / 1e9, 2)
+    if not args.no_extra and not args.junctions and not args.head:
         extra.update(llama_context_steps(torch, D, dpsgd, drv, loss_fn, model, B, T, k, C, sigma, steps))
     rec = {"metric": "DP-SGD-RC training-step tokens/s, Llama-3.2-1B-shaped stack",
            "value": round(B * T / (ms_per_step * 1e-3), 1), "unit": "tokens/s", "n_gpus": 1,
