@@ -574,7 +574,8 @@ typedef enum {
   DPRC_KERNEL_HEAD_ROWS = 33,         /* head: rows laid out, sums rounded       */
   DPRC_KERNEL_ROTARY = 34,
   DPRC_KERNEL_GRAD_SQUARES = 35,      /* joint norm of many tensors              */
-  DPRC_KERNEL_GRAD_SCALE = 36         /* their clipping                          */
+  DPRC_KERNEL_GRAD_SCALE = 36,        /* their clipping                          */
+  DPRC_KERNEL_HEAD_WEIGHT = 37        /* head: E^T h                             */
 } dprc_kernel_kind;
 dprc_status dprc_trace_launches(hipEvent_t* events, int32_t* kinds, int32_t capacity,
                                 int32_t* count);

@@ -1780,17 +1780,17 @@ dprc_status check_head(const dprc_head* H) {
 
 // rows that the head's kernels read in 16-byte pieces, offsets within a tile of them below 2^31
 bool head_vec(const dprc_head& H, const void* p, int64_t ld) {
-  return H.dtype == DPRC_F32 || (rows16(p, ld) && H.d % 8 == 0 && ld < (1LL << 22));
+  const int64_t piece = 16 / (int64_t)elem_bytes(H.dtype);
+  return aligned(p, 16) && ld % piece == 0 && H.d % piece == 0 && ld < (1LL << 21);
 }
 
 struct HeadBufs {
   int64_t N, piece, lde, ldc;          // tokens; columns of a piece; row strides of E and of h's copy
-  int32_t S;                           // splits of dh
   void* rows;                          // h laid out [N][ldc]
   void* E;                             // [N][lde]
-  float* planes;                       // [S][N][d]
-  float* dW;                           // [piece][d], bf16 heads
-  float* one;
+  HeadMulPlan dh;
+  float* dh_planes;                    // [S][N][d]; null: one piece, one split
+  float* dW_planes;                    // [S][columns of a piece][d] where a piece's plan has several splits
   void* acc;                           // accumulation's and estimates' workspaces
   size_t acc_bytes;
   void* hutch;
@@ -1809,11 +1809,6 @@ HeadRows head_rows(const dprc_head& H, const HeadBufs& b) { return HeadRows{b.ro
 dprc_layer head_layer(const dprc_head& H, const HeadBufs& b, int64_t c0, int64_t nv, uint32_t id) {
   const char* E = static_cast<const char*>(b.E) + c0 * (int64_t)elem_bytes(H.dtype);
   return dprc_layer{b.rows, E, H.B, H.T, H.d, nv, b.ldc, b.lde, H.dtype, id};
-}
-
-// dW as the accumulation forms it: E^T h over all tokens as one sample.
-dprc_layer head_weight_layer(const dprc_head& H, const HeadBufs& b, int64_t nv) {
-  return dprc_layer{b.E, b.rows, 1, b.N, nv, H.d, b.lde, b.ldc, H.dtype, 0};
 }
 
 // The blocks of columns v0 .. v0 + nv, up to kHeadBlocks at a time: f(layers, count, first column) for each group.
@@ -1844,20 +1839,18 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
   // buffers of a shape to ask for sizes with: only their alignment counts
   HeadBufs probe = b;
   probe.rows = probe.E = reinterpret_cast<void*>((uintptr_t)kAlign);
+  const int bf16 = H.dtype == DPRC_BF16;
   if (dh) {
-    b.S = head_back_plan(b.N, H.d, b.piece, H.dtype == DPRC_BF16, 0).S;
-    b.planes = ar.take<float>((size_t)b.S * b.N * H.d);
+    b.dh = head_mul_plan(b.N, H.d, b.piece, bf16);
+    if (b.dh.S > 1 || b.piece < H.V) b.dh_planes = ar.take<float>((size_t)b.dh.S * b.N * H.d);
   }
   const int64_t rest = H.V % b.piece;
-  if (dW) {
-    b.one = ar.take<float>(1);
-    if (H.dtype == DPRC_BF16) b.dW = ar.take<float>((size_t)b.piece * H.d);
-  }
+  int64_t dW_floats = 0;
   for (const int64_t nv : {b.piece, rest}) {
     if (nv == 0) continue;
     if (dW) {
-      const dprc_layer L = head_weight_layer(H, probe, nv);
-      b.acc_bytes = std::max(b.acc_bytes, dprc_clip_accumulate_workspace(&L));
+      const int32_t S = head_mul_plan(nv, H.d, b.N, bf16).S;
+      if (S > 1) dW_floats = std::max(dW_floats, S * nv * H.d);
     }
     if (clip) {
       const dprc_layer L = head_layer(H, probe, 0, nv, 0);
@@ -1869,6 +1862,7 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
         return DPRC_SUCCESS;
       });
   }
+  if (dW_floats) b.dW_planes = ar.take<float>((size_t)dW_floats);
   b.acc = ar.take<char>(b.acc_bytes);
   b.hutch = ar.take<char>(b.hutch_bytes);
   return ar.off;
@@ -1913,8 +1907,8 @@ extern "C" {
 size_t dprc_head_loss_workspace(const dprc_head* H) {
   if (check_head(H) != DPRC_SUCCESS) return 0;
   Arena ar(nullptr);
-  if (!head_vec(*H, H->h, H->ldh)) ar.take<char>((size_t)(H->B * H->T * round_up(H->d, 8)) * 2);
-  ar.take<float2>((size_t)ceil_div(H->V, head_tile_rows(H->dtype == DPRC_BF16)) * H->B * H->T);
+  if (!head_vec(*H, H->h, H->ldh)) ar.take<char>((size_t)(H->B * H->T * round_up(H->d, 8)) * elem_bytes(H->dtype));
+  ar.take<float2>((size_t)head_sum_tiles(H->B * H->T, H->V, H->dtype == DPRC_BF16) * H->B * H->T);
   return ar.off;
 }
 
@@ -1929,21 +1923,22 @@ dprc_status dprc_head_loss(const dprc_head* H, float* loss, float* lse, void* ws
   HeadRows h{H->h, H->ldh, H->B * H->T, H->d};
   if (!head_vec(*H, H->h, H->ldh)) {
     const int64_t ld = round_up(H->d, 8);
-    uint16_t* rows = ar.take<uint16_t>((size_t)(h.rows * ld));
-    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_rows(h, 1, nullptr, rows, ld, stream); }) != hipSuccess)
+    char* rows = ar.take<char>((size_t)(h.rows * ld) * elem_bytes(H->dtype));
+    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+          return launch_head_rows(h, H->dtype == DPRC_BF16, nullptr, rows, ld, stream); }) != hipSuccess)
       return DPRC_ERROR_HIP;
     h.p = rows;
     h.ld = ld;
   }
   HeadArgs a = head_args(*H, h, 0, H->V);
-  a.part = ar.take<float2>((size_t)ceil_div(H->V, head_tile_rows(a.bf16)) * a.N);
+  a.part = ar.take<float2>((size_t)head_sum_tiles(a.N, a.nv, a.bf16) * a.N);
   if (traced(DPRC_KERNEL_HEAD_SUMS, stream, [&] { return launch_head_sums(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
   return hip_status(traced(DPRC_KERNEL_HEAD_JOIN, stream, [&] { return launch_head_join(a, loss, lse, stream); }));
 }
 
 size_t dprc_head_errors_workspace(const dprc_head* H) {
   if (check_head(H) != DPRC_SUCCESS || head_vec(*H, H->h, H->ldh)) return 0;
-  return (size_t)round_up(H->B * H->T * round_up(H->d, 8) * 2, kAlign);
+  return (size_t)round_up(H->B * H->T * round_up(H->d, 8) * (int64_t)elem_bytes(H->dtype), kAlign);
 }
 
 dprc_status dprc_head_errors(const dprc_head* H, const float* lse, const float* g, int64_t v0, int64_t nv, void* E,
@@ -1959,7 +1954,8 @@ dprc_status dprc_head_errors(const dprc_head* H, const float* lse, const float* 
   HeadRows h{H->h, H->ldh, H->B * H->T, H->d};
   if (need) {
     const int64_t ld = round_up(H->d, 8);
-    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_rows(h, 1, nullptr, ws, ld, stream); }) != hipSuccess)
+    if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+          return launch_head_rows(h, H->dtype == DPRC_BF16, nullptr, ws, ld, stream); }) != hipSuccess)
       return DPRC_ERROR_HIP;
     h.p = ws;
     h.ld = ld;
@@ -2001,8 +1997,15 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
   if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
   head_layout(*H, dh, dW, false, norms, ws, b);
   const int bf16 = H->dtype == DPRC_BF16;
-  if (dW && traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_one(b.one, stream); }) != hipSuccess)
-    return DPRC_ERROR_HIP;
+  // a product's sums in planes, or with one split of all of them in the result; then the planes rounded
+  auto multiply = [&](HeadMulArgs& a, const HeadMulPlan& plan, int kind) -> dprc_status {
+    a.per_split = plan.per_split; a.S = plan.S; a.small = plan.small; a.bf16 = bf16;
+    return hip_status(traced(kind, stream, [&] { return launch_head_mul(a, stream); }));
+  };
+  auto round = [&](const float* planes, int S, int64_t rows, void* out, int64_t ld) {
+    return hip_status(traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
+      return launch_head_round(planes, S, rows, H->d, bf16, out, ld, stream); }));
+  };
   st = head_pieces(*H, b, lse, g, stream, [&](int64_t v0, int64_t nv) -> dprc_status {
     dprc_status s;
     if (norms) {
@@ -2012,32 +2015,34 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
       });
       if (s != DPRC_SUCCESS) return s;
     }
-    if (dh) {
-      const HeadBackPlan plan = head_back_plan(b.N, H->d, nv, bf16, b.S);
-      HeadBackArgs a{};
-      a.E = HeadRows{b.E, b.lde, b.N, bf16 ? round_up(nv, 8) : nv};   // (columns behind nv are zeros, and meet none of W's rows)
-      a.W = head_args(*H, head_rows(*H, b), v0, nv).W;
-      a.N = b.N; a.d = H->d;
-      a.per_split = plan.per_split; a.S = plan.S;
-      a.bf16 = bf16; a.vec_w = head_vec(*H, H->W, H->ldw);
+    if (dh) {                                          // (E's columns behind nv are zeros, and meet none of W's rows)
+      HeadMulArgs a{};
+      a.A = HeadRows{b.E, b.lde, b.N, round_up(nv, 8)};
+      a.B = head_args(*H, head_rows(*H, b), v0, nv).W;
+      a.rows = b.N; a.cols = H->d; a.K = nv;
+      a.vec_b = head_vec(*H, H->W, H->ldw);
       a.add = v0 > 0;
-      a.planes = b.planes;
-      if (traced(DPRC_KERNEL_HEAD_BACK, stream, [&] { return launch_head_back(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
+      a.planes = b.dh_planes;
+      if (!b.dh_planes) { a.out = dh; a.ldo = lddh; }
+      if ((s = multiply(a, v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16), DPRC_KERNEL_HEAD_BACK)) != DPRC_SUCCESS) return s;
     }
     if (dW) {
-      const dprc_layer L = head_weight_layer(*H, b, nv);
+      const HeadMulPlan plan = head_mul_plan(nv, H->d, b.N, bf16);
       char* out = static_cast<char*>(dW) + v0 * lddw * (int64_t)e;
-      s = dprc_clip_accumulate(&L, b.one, bf16 ? b.dW : reinterpret_cast<float*>(out), bf16 ? H->d : lddw, 0, b.acc, b.acc_bytes, stream);
-      if (s != DPRC_SUCCESS) return s;
-      if (bf16 && traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
-            return launch_head_round(b.dW, 1, nv, H->d, 1, out, lddw, stream); }) != hipSuccess)
-        return DPRC_ERROR_HIP;
+      HeadMulArgs a{};
+      a.A = HeadRows{b.E, b.lde, b.N, nv};
+      a.B = head_rows(*H, b);
+      a.rows = nv; a.cols = H->d; a.K = b.N;
+      a.akr = 1; a.vec_b = 1;
+      a.planes = b.dW_planes;
+      if (plan.S == 1) { a.out = out; a.ldo = lddw; }
+      if ((s = multiply(a, plan, DPRC_KERNEL_HEAD_WEIGHT)) != DPRC_SUCCESS) return s;
+      if (plan.S > 1 && (s = round(b.dW_planes, plan.S, nv, out, lddw)) != DPRC_SUCCESS) return s;
     }
     return DPRC_SUCCESS;
   });
-  if (st != DPRC_SUCCESS || !dh) return st;
-  return hip_status(traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
-    return launch_head_round(b.planes, b.S, b.N, H->d, bf16, dh, lddh, stream); }));
+  if (st != DPRC_SUCCESS || !b.dh_planes) return st;
+  return round(b.dh_planes, b.dh.S, b.N, dh, lddh);
 }
 
 size_t dprc_head_clip_accumulate_workspace(const dprc_head* H) {

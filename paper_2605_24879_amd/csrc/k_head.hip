@@ -37,46 +37,51 @@ __device__ __forceinline__ void tile_of(int64_t wg, int64_t tm_n, int64_t tn_n, 
 // ---- products of tiles ----------------------------------------------------------------------------
 // Accumulators as the 32 x 32 MFMAs hold them: WM x WN waves of XB x YB blocks; lane l of block (x, y) has
 // rows 8 (q / 4) + 4 (l / 32) + q % 4, q < 16, of column l % 32.
-//
-// An operand is `rows` rows of `width` elements, ld apart.  KC: its rows are the tile's rows (columns), the
-// contraction runs along them.  KR: the contraction runs over its rows, the tile's columns along them.
 
 template <class E, int WM_, int WN_, int XB_, int YB_>
 struct HeadTile {
   typedef E elem;
   static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_;
   static constexpr int MT = 32 * XB * WM, NT = 32 * YB * WN, threads = 64 * WM * WN;
+  static constexpr int EP = kPiece<E>;                  // elements of a 16-byte piece
+  static constexpr int slab = 8 * EP;                   // contraction elements of a slab: 64 bf16, 32 fp32
 };
 
-constexpr int kHK = 64;               // contraction elements per bf16 slab
+// An operand is `rows` rows of `width` elements, ld apart.  KC: its rows are the tile's rows (columns), the
+// contraction runs along them.  KR: the contraction runs over its rows, the tile's rows (columns) along them.
+// A slab of it in LDS is 128 bytes for every row (column) of the tile.  KC: rows of 128 bytes, piece p of row r
+// at p ^ (r & 7), so that a fragment read of 8 rows covers all banks.  KR, bf16: rows of the tile's width,
+// piece p of row r at p ^ swizzle_kr(r), so that the 4 (8) rows of a transposing read lie in different
+// 32-byte (128-byte) parts of the banks; fp32 fragments are read along the rows and need none.
+template <class E>
+__device__ __forceinline__ int swizzle_kr(int r, int pieces) {
+  return sizeof(E) == 2 ? (((r & 3) << 1) | (r & 8)) & (pieces - 1) : 0;
+}
 
-// The slabs in LDS, two of each operand.  KC: rows of 128 bytes, the eight 16-byte pieces of row r at piece ^
-// (r & 7), so that a fragment read of 8 rows covers all banks.  KR: 64 rows of the tile's width, piece p of
-// row r at p ^ swizzle_kr(r), so that the 4 (8) rows of a transposing read lie in different 32-byte (128-byte)
-// parts of the banks.  Four arrays and not one: the compiler then knows that loads into one do not
-// reach reads of another, and does not wait for them.
-template <class TL, bool BKR>
-struct HeadSlabs {
-  static constexpr int A = TL::MT * kHK, B = TL::NT * kHK;
-};
-__device__ __forceinline__ int swizzle_kr(int r) { return ((r & 3) << 1) | (r & 8); }
-
-// Eight elements at (row, col), zeros past the rows and the width, at any alignment.
+// A piece at (row, col), zeros past the rows and the width, at any alignment of the element.
+template <class E>
 __device__ __forceinline__ uint4 operand_piece(const HeadRows& X, int64_t row, int64_t col) {
   if (row >= X.rows || col >= X.width) return uint4{0, 0, 0, 0};
-  const uint16_t* p = static_cast<const uint16_t*>(X.p);
-  const int64_t at = row * X.ld + col, room = (X.rows - 1) * X.ld + X.width - 8;
-  if (room < 0) return load8_elem(p + row * X.ld, col, X.width, true);
-  const int64_t from = min(at, room);
-  const u32x4_any v = *reinterpret_cast<const u32x4_any*>(p + from);
-  return first_elems(shr_elems(uint4{v[0], v[1], v[2], v[3]}, (int)(at - from)), (int)min((int64_t)8, X.width - col));
+  const E* p = static_cast<const E*>(X.p) + row * X.ld;
+  if constexpr (sizeof(E) == 2) {
+    const int64_t at = row * X.ld + col, room = (X.rows - 1) * X.ld + X.width - 8;
+    if (room < 0) return load8_elem(p, col, X.width, true);
+    const int64_t from = min(at, room);
+    const u32x4_any v = *reinterpret_cast<const u32x4_any*>(static_cast<const E*>(X.p) + from);
+    return first_elems(shr_elems(uint4{v[0], v[1], v[2], v[3]}, (int)(at - from)), (int)min((int64_t)8, X.width - col));
+  } else {
+    if (col + 4 <= X.width) return load_piece<E>(p + col);
+    return uint4{__float_as_uint(p[col]), col + 1 < X.width ? __float_as_uint(p[col + 1]) : 0u,
+                 col + 2 < X.width ? __float_as_uint(p[col + 2]) : 0u, 0u};
+  }
 }
 
 // 64 lanes' 16-byte pieces at byte offsets `off` of the resource to 1024 bytes of LDS, in lane order; zeros
-// where the offset is out of the resource's range.
+// where the offset is out of the resource's range.  NT: for an operand that is streamed once.
 typedef __attribute__((address_space(3))) void lds_void_t;
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint16_t* lds, uint32_t off) {
-  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, 0, 0, 0);
+template <bool NT>
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, void* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, 0, 0, NT ? kCachePolicyNT : 0);
 }
 
 template <int V>
@@ -84,97 +89,116 @@ struct HInt {
   static constexpr int value = V;
 };
 
-// acc = sum over k in [k0, k1) of A[m0 + i][k] B[n0 + j][k] (BKR: B[k][n0 + j]), bf16 operands, k0 a multiple
-// of kHK.  Slabs of kHK are double-buffered: while one is multiplied the next is loaded, straight into
-// LDS where the operand's rows allow 16-byte pieces (VA, VB), else through registers.  A wave has the
-// fragments of 16 contraction elements in registers ahead of their products, also across the slab's one
-// barrier, and reads and products are issued in turn.  256 x 256 tiles of 128000 x 8192 x 2048: 1330
-// TFLOP/s (the same loop as the compiler orders it 1146, all reads before all products 1270, four waves of
-// 128 x 128 1217, tiles of 128 x 128 1093).
-template <class TL, bool BKR, bool VA, bool VB>
-__device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, const HeadRows& B, int64_t n0, int64_t k0,
-                                             int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB], uint16_t* la0, uint16_t* la1,
-                                             uint16_t* lb0, uint16_t* lb1) {
-  constexpr int XB = TL::XB, YB = TL::YB, TH = TL::threads;
-  constexpr int PA = TL::MT * 8 / TH, PB = TL::NT * 8 / TH, BP = TL::NT / 8;     // pieces a thread; of a KR row
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int wave0 = 64 * (int)__builtin_amdgcn_readfirstlane(wv);
-  const int wm = wv / TL::WN, wn = wv % TL::WN;
-  auto kc_col = [](int s) { return 8 * ((s & 7) ^ ((s >> 3) & 7)); };
-  auto kr_col = [](int s) { return 8 * ((s % BP) ^ (swizzle_kr(s / BP) & (BP - 1))); };
-  // byte offsets of the thread's pieces in a slab
-  uint32_t oa[PA], ob[PB];
+// One operand's slabs of a tile of T rows (columns) from t0 on: loads, straight into LDS where its rows allow
+// 16-byte pieces (VEC), else through registers.
+template <class TL, int T, bool KR, bool VEC, bool NT>
+struct HeadOperand {
+  typedef typename TL::elem E;
+  static constexpr int EP = TL::EP, P = T * 8 / TL::threads, RP = T / EP;    // pieces of a thread; of a KR row
+  static_assert(T * 8 % TL::threads == 0);
+  const HeadRows& X;
+  int64_t t0;
+  int wave0;                           // the wave's first thread
+  uint32_t off[VEC ? P : 1];           // byte offsets of the thread's pieces in a slab
+  uint4 reg[VEC ? 1 : P];
+
+  static __device__ __forceinline__ int kc_col(int s) { return EP * ((s & 7) ^ ((s >> 3) & 7)); }
+  static __device__ __forceinline__ int kr_col(int s) { return EP * ((s % RP) ^ swizzle_kr<E>(s / RP, RP)); }
+
+  __device__ __forceinline__ HeadOperand(const HeadRows& X_, int64_t t) : X(X_), t0(t) {
+    wave0 = 64 * (int)__builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if constexpr (VEC) {
 #pragma unroll
-  for (int r = 0; r < PA; ++r) {
-    const int s = tid + TH * r;
-    oa[r] = (uint32_t)(s >> 3) * (uint32_t)A.ld * 2u + 2u * kc_col(s);
+      for (int r = 0; r < P; ++r) {
+        const int s = threadIdx.x + TL::threads * r;
+        const int row = KR ? s / RP : s >> 3, col = KR ? kr_col(s) : kc_col(s);
+        off[r] = KR && t0 + col >= X.width ? kOobOffset : ((uint32_t)row * (uint32_t)X.ld + (uint32_t)col) * (uint32_t)sizeof(E);
+      }
+    }
   }
-#pragma unroll
-  for (int r = 0; r < PB; ++r) {
-    const int s = tid + TH * r;
-    if constexpr (BKR) ob[r] = n0 + kr_col(s) < B.width ? (uint32_t)(s / BP) * (uint32_t)B.ld * 2u + 2u * kr_col(s) : kOobOffset;
-    else ob[r] = (uint32_t)(s >> 3) * (uint32_t)B.ld * 2u + 2u * kc_col(s);
-  }
-  // a resource over `tile` rows from row0 on, `skip` elements into them
-  auto rsrc = [](const HeadRows& X, int64_t row0, int tile, int64_t skip) __attribute__((always_inline)) {
+  // a resource over `n` rows from row0 on, `skip` elements into them
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(int64_t row0, int n, int64_t skip) const {
     const int64_t left = X.rows - row0;
-    const uint32_t rows = (uint32_t)(left < 0 || skip >= X.width ? 0 : left < tile ? left : tile);
-    return buffer_rsrc(static_cast<const uint16_t*>(X.p) + (rows ? row0 * X.ld + skip : 0),
-                       rows ? rows * (uint32_t)X.ld * 2u - (uint32_t)skip * 2u : 0u);
-  };
-  uint4 ga[VA ? 1 : PA], gb[VB ? 1 : PB];
+    const uint32_t rows = (uint32_t)(left < 0 || skip >= X.width ? 0 : left < n ? left : n);
+    return buffer_rsrc(static_cast<const E*>(X.p) + (rows ? row0 * X.ld + skip : 0),
+                       rows ? (rows * (uint32_t)X.ld - (uint32_t)skip) * (uint32_t)sizeof(E) : 0u);
+  }
+  // the slab at k on its way to LDS
+  __device__ __forceinline__ void load(int64_t k, E* lds) {
+    if constexpr (VEC && KR) {
+      const __amdgpu_buffer_rsrc_t r0 = rsrc(k, TL::slab, t0);
+#pragma unroll
+      for (int r = 0; r < P; ++r) load_to_lds<NT>(r0, lds + EP * (wave0 + TL::threads * r), off[r]);
+    } else if constexpr (VEC) {
+      const __amdgpu_buffer_rsrc_t r0 = rsrc(t0, T, k);
+      if (k + TL::slab > X.width) {                      // columns past the rows' end
+#pragma unroll
+        for (int r = 0; r < P; ++r)
+          load_to_lds<NT>(r0, lds + EP * (wave0 + TL::threads * r),
+                          k + kc_col(threadIdx.x + TL::threads * r) < X.width ? off[r] : kOobOffset);
+      } else {
+#pragma unroll
+        for (int r = 0; r < P; ++r) load_to_lds<NT>(r0, lds + EP * (wave0 + TL::threads * r), off[r]);
+      }
+    } else {
+#pragma unroll
+      for (int r = 0; r < P; ++r) {
+        const int s = threadIdx.x + TL::threads * r;
+        reg[r] = KR ? operand_piece<E>(X, k + s / RP, t0 + kr_col(s)) : operand_piece<E>(X, t0 + (s >> 3), k + kc_col(s));
+      }
+    }
+  }
+  __device__ __forceinline__ void arrive(E* lds) const {
+    if constexpr (!VEC) {
+#pragma unroll
+      for (int r = 0; r < P; ++r) *reinterpret_cast<uint4*>(lds + EP * (threadIdx.x + TL::threads * r)) = reg[r];
+    }
+  }
+  // The fragment of the 32 rows (columns) from b on, for contraction elements 2 EP ks .. of the slab: the
+  // lane's row b + l % 32, its EP elements from 2 EP ks + EP (l / 32) on.  (fp32: four MFMAs of K = 2 take the
+  // elements i and EP + i of these.)
+  static constexpr int reads = !KR ? 1 : sizeof(E) == 2 ? 2 : 4;
+  static __device__ __forceinline__ uint4 frag(const E* lds, int b, int ks, int lane) {
+    const int l32 = lane & 31, half = lane >> 5;
+    if constexpr (!KR) {
+      const int row = b + l32;
+      return *reinterpret_cast<const uint4*>(&lds[row * TL::slab + EP * ((2 * ks + half) ^ (row & 7))]);
+    } else if constexpr (sizeof(E) == 2) {
+      // lane group g reads rows 8 (g / 2) + r4 (+ 4) of columns 16 (g % 2) + 4 c4 .. of the block
+      const int g = lane >> 4, r4 = (lane & 15) >> 2, c4 = lane & 3;
+      const int row = 16 * ks + 8 * (g >> 1) + r4, col = b + 16 * (g & 1) + 4 * c4;
+      const E* p = &lds[row * T + EP * ((col >> 3) ^ swizzle_kr<E>(row, RP)) + (col & 4)];
+      return make_u4(lds_read_tr16(p), lds_read_tr16(p + 4 * T));
+    } else {
+      const E* p = &lds[(8 * ks + 4 * half) * T + b + l32];
+      return uint4{__float_as_uint(p[0]), __float_as_uint(p[T]), __float_as_uint(p[2 * T]), __float_as_uint(p[3 * T])};
+    }
+  }
+};
+
+// acc = sum over k in [k0, k1) of A[i][k] B[j][k], i and j the tile's rows and columns; k0 a multiple of the
+// slab.  fp32 products and sums (bf16 products are exact).  Slabs are double-buffered: while one is
+// multiplied the next is loaded.  A wave has the next fragments in registers ahead of their products, also
+// across the slab's one barrier, and reads and products are issued in turn.  Four LDS arrays and not one: the
+// compiler then knows that loads into one do not reach reads of another, and does not wait for them.
+// bf16, 256 x 256 tiles of 128000 x 8192 x 2048: 1330 TFLOP/s (the same loop as the compiler orders it 1146, all
+// reads before all products 1270, four waves of 128 x 128 1217, tiles of 128 x 128 1093).
+template <class TL, class OA, class OB>
+__device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB],
+                                             typename TL::elem* la0, typename TL::elem* la1, typename TL::elem* lb0,
+                                             typename TL::elem* lb1) {
+  typedef typename TL::elem E;
+  constexpr int XB = TL::XB, YB = TL::YB;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int wm = wv / TL::WN, wn = wv % TL::WN;
   auto gload = [&](int64_t k, auto u) __attribute__((always_inline)) {
-    uint16_t* la = decltype(u)::value ? la1 : la0;
-    uint16_t* lb = decltype(u)::value ? lb1 : lb0;
-    const bool tail = k + kHK > A.width;               // columns past the rows' end
-    if constexpr (VA) {
-      const __amdgpu_buffer_rsrc_t ra = rsrc(A, m0, TL::MT, k);
-      if (tail) {
-#pragma unroll
-        for (int r = 0; r < PA; ++r)
-          load_to_lds(ra, la + 8 * (wave0 + TH * r), k + kc_col(tid + TH * r) < A.width ? oa[r] : kOobOffset);
-      } else {
-#pragma unroll
-        for (int r = 0; r < PA; ++r) load_to_lds(ra, la + 8 * (wave0 + TH * r), oa[r]);
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < PA; ++r) ga[r] = operand_piece(A, m0 + ((tid + TH * r) >> 3), k + kc_col(tid + TH * r));
-    }
-    if constexpr (VB && BKR) {
-      const __amdgpu_buffer_rsrc_t rb = rsrc(B, k, kHK, n0);
-#pragma unroll
-      for (int r = 0; r < PB; ++r) load_to_lds(rb, lb + 8 * (wave0 + TH * r), ob[r]);
-    } else if constexpr (VB) {
-      const __amdgpu_buffer_rsrc_t rb = rsrc(B, n0, TL::NT, k);
-      if (tail) {
-#pragma unroll
-        for (int r = 0; r < PB; ++r)
-          load_to_lds(rb, lb + 8 * (wave0 + TH * r), k + kc_col(tid + TH * r) < B.width ? ob[r] : kOobOffset);
-      } else {
-#pragma unroll
-        for (int r = 0; r < PB; ++r) load_to_lds(rb, lb + 8 * (wave0 + TH * r), ob[r]);
-      }
-    } else {
-#pragma unroll
-      for (int r = 0; r < PB; ++r) {
-        const int s = tid + TH * r;
-        gb[r] = BKR ? operand_piece(B, k + s / BP, n0 + kr_col(s)) : operand_piece(B, n0 + (s >> 3), k + kc_col(s));
-      }
-    }
+    A.load(k, decltype(u)::value ? la1 : la0);
+    B.load(k, decltype(u)::value ? lb1 : lb0);
   };
   // what went through registers to LDS, then every wave's slab is there and the other's reads are done
   auto arrive = [&](auto u) __attribute__((always_inline)) {
-    uint16_t* la = decltype(u)::value ? la1 : la0;
-    uint16_t* lb = decltype(u)::value ? lb1 : lb0;
-    if constexpr (!VA) {
-#pragma unroll
-      for (int r = 0; r < PA; ++r) *reinterpret_cast<uint4*>(&la[8 * (tid + TH * r)]) = ga[r];
-    }
-    if constexpr (!VB) {
-#pragma unroll
-      for (int r = 0; r < PB; ++r) *reinterpret_cast<uint4*>(&lb[8 * (tid + TH * r)]) = gb[r];
-    }
+    A.arrive(decltype(u)::value ? la1 : la0);
+    B.arrive(decltype(u)::value ? lb1 : lb0);
     __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
     __builtin_amdgcn_s_waitcnt(0);
     __builtin_amdgcn_s_barrier();
@@ -186,41 +210,38 @@ __device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, cons
     for (int y = 0; y < YB; ++y)
 #pragma unroll
       for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.f;
-  const int l32 = lane & 31, half = lane >> 5;
-  const int g = lane >> 4, r4 = (lane & 15) >> 2, c4 = lane & 3;
   uint4 f0a[XB], f0b[YB], f1a[XB], f1b[YB];
-  // the fragments of contraction elements 16 ks .. 16 ks + 15 of a slab
   auto frag = [&](uint4 (&av)[XB], uint4 (&bv)[YB], auto u, int ks) __attribute__((always_inline)) {
-    const uint16_t* la = decltype(u)::value ? la1 : la0;
-    const uint16_t* lb = decltype(u)::value ? lb1 : lb0;
+    const E* la = decltype(u)::value ? la1 : la0;
+    const E* lb = decltype(u)::value ? lb1 : lb0;
 #pragma unroll
-    for (int y = 0; y < YB; ++y) {
-      if constexpr (BKR) {
-        // lane group g reads rows 8 (g / 2) + r4 (+ 4) of columns 16 (g % 2) + 4 c4 .. of the block
-        const int row = 16 * ks + 8 * (g >> 1) + r4, col = 32 * (wn * YB + y) + 16 * (g & 1) + 4 * c4;
-        const uint16_t* p = &lb[row * TL::NT + 8 * ((col >> 3) ^ (swizzle_kr(row) & (BP - 1))) + (col & 4)];
-        bv[y] = make_u4(lds_read_tr16(p), lds_read_tr16(p + 4 * TL::NT));
-      } else {
-        const int row = 32 * (wn * YB + y) + l32;
-        bv[y] = *reinterpret_cast<const uint4*>(&lb[row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
-      }
-    }
+    for (int y = 0; y < YB; ++y) bv[y] = OB::frag(lb, 32 * (wn * YB + y), ks, lane);
 #pragma unroll
-    for (int x = 0; x < XB; ++x) {
-      const int row = 32 * (wm * XB + x) + l32;
-      av[x] = *reinterpret_cast<const uint4*>(&la[row * kHK + 8 * ((2 * ks + half) ^ (row & 7))]);
-    }
+    for (int x = 0; x < XB; ++x) av[x] = OA::frag(la, 32 * (wm * XB + x), ks, lane);
   };
   auto phase = [&](uint4 (&na)[XB], uint4 (&nb)[YB], auto u, int ks, const uint4 (&av)[XB], const uint4 (&bv)[YB])
       __attribute__((always_inline)) {
     frag(na, nb, u, ks);
+    if constexpr (sizeof(E) == 2) {
 #pragma unroll
-    for (int x = 0; x < XB; ++x)
+      for (int x = 0; x < XB; ++x)
 #pragma unroll
-      for (int y = 0; y < YB; ++y)
-        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
-                                                            __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
-    constexpr int reads = XB + (BKR ? 2 : 1) * YB, products = XB * YB;
+        for (int y = 0; y < YB; ++y)
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
+                                                              __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int x = 0; x < XB; ++x)
+#pragma unroll
+          for (int y = 0; y < YB; ++y) {
+            const float a = __uint_as_float(i == 0 ? av[x].x : i == 1 ? av[x].y : i == 2 ? av[x].z : av[x].w);
+            const float b = __uint_as_float(i == 0 ? bv[y].x : i == 1 ? bv[y].y : i == 2 ? bv[y].z : bv[y].w);
+            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, acc[x][y], 0, 0, 0);
+          }
+    }
+    constexpr int reads = XB * OA::reads + YB * OB::reads, products = XB * YB * (sizeof(E) == 2 ? 1 : 4);
 #pragma unroll
     for (int i = 0; i < reads; ++i) {
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);               // a read of LDS
@@ -232,7 +253,7 @@ __device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, cons
   // the slab at k in buffers u, its first fragments in registers
   auto step = [&](int64_t k, auto u) __attribute__((always_inline)) {
     constexpr HInt<decltype(u)::value ^ 1> other{};
-    gload(k + kHK < k1 ? k + kHK : (int64_t)1 << 40, other);           // past the end: nothing
+    gload(k + TL::slab < k1 ? k + TL::slab : (int64_t)1 << 40, other);     // past the end: zeros
     __builtin_amdgcn_sched_barrier(0);
     phase(f1a, f1b, u, 1, f0a, f0b);
     phase(f0a, f0b, u, 2, f1a, f1b);
@@ -243,101 +264,11 @@ __device__ __forceinline__ void head_product(const HeadRows& A, int64_t m0, cons
   gload(k0, HInt<0>{});
   arrive(HInt<0>{});
   frag(f0a, f0b, HInt<0>{}, 0);
-  for (int64_t k = k0; k < k1; k += 2 * kHK) {       // (an odd number of slabs: the last one is zeros)
+  for (int64_t k = k0; k < k1; k += 2 * TL::slab) {  // (an odd number of slabs: the last one is zeros)
     step(k, HInt<0>{});
-    step(k + kHK, HInt<1>{});
+    step(k + TL::slab, HInt<1>{});
   }
   __syncthreads();                                     // all reads are done
-}
-
-// fp32 operands, on the fp32 matrix cores (products and sums in fp32): slabs of 16 in LDS as [k][row].
-constexpr int kHKf = 16;
-
-__device__ __forceinline__ float4 operand_piece_f32(const HeadRows& X, int64_t row, int64_t col) {
-  float4 v{0.f, 0.f, 0.f, 0.f};
-  if (row >= X.rows || col >= X.width) return v;
-  const float* p = static_cast<const float*>(X.p) + row * X.ld + col;
-  if (col + 4 <= X.width) {
-    const uint4 d = load_piece<float>(p);
-    return __builtin_bit_cast(float4, d);
-  }
-  v.x = p[0];
-  if (col + 1 < X.width) v.y = p[1];
-  if (col + 2 < X.width) v.z = p[2];
-  return v;
-}
-
-template <class TL>
-constexpr int head_lds_bytes_f32() {
-  return 2 * 4 * kHKf * (TL::MT + 4 + TL::NT + 4);
-}
-
-template <class TL, bool BKR>
-__device__ __forceinline__ void head_product_f32(const HeadRows& A, int64_t m0, const HeadRows& B, int64_t n0, int64_t k0,
-                                                 int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB], float* lds) {
-  constexpr int XB = TL::XB, YB = TL::YB, LA = TL::MT + 4, LB = TL::NT + 4;
-  constexpr int PA = TL::MT * kHKf / 4 / TL::threads, PB = TL::NT * kHKf / 4 / TL::threads;
-  float* la[2] = {lds, lds + kHKf * LA};
-  float* lb[2] = {lds + 2 * kHKf * LA, lds + 2 * kHKf * LA + kHKf * LB};
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int wm = wv / TL::WN, wn = wv % TL::WN, l32 = lane & 31, half = lane >> 5;
-  float4 ga[PA], gb[PB];
-  auto gload = [&](int64_t k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int r = 0; r < PA; ++r) {
-      const int s = tid + TL::threads * r;
-      ga[r] = operand_piece_f32(A, m0 + (s >> 2), k + 4 * (s & 3));
-    }
-#pragma unroll
-    for (int r = 0; r < PB; ++r) {
-      const int s = tid + TL::threads * r;
-      gb[r] = BKR ? operand_piece_f32(B, k + s / (TL::NT / 4), n0 + 4 * (s % (TL::NT / 4)))
-                  : operand_piece_f32(B, n0 + (s >> 2), k + 4 * (s & 3));
-    }
-  };
-  auto swrite = [&](int buf) __attribute__((always_inline)) {
-    auto across = [&](float* l, int ld, int s, const float4& v) __attribute__((always_inline)) {
-      float* o = l + 4 * (s & 3) * ld + (s >> 2);
-      o[0] = v.x; o[ld] = v.y; o[2 * ld] = v.z; o[3 * ld] = v.w;
-    };
-#pragma unroll
-    for (int r = 0; r < PA; ++r) across(la[buf], LA, tid + TL::threads * r, ga[r]);
-#pragma unroll
-    for (int r = 0; r < PB; ++r) {
-      const int s = tid + TL::threads * r;
-      if constexpr (BKR) *reinterpret_cast<float4*>(&lb[buf][s / (TL::NT / 4) * LB + 4 * (s % (TL::NT / 4))]) = gb[r];
-      else across(lb[buf], LB, s, gb[r]);
-    }
-  };
-#pragma unroll
-  for (int x = 0; x < XB; ++x)
-#pragma unroll
-    for (int y = 0; y < YB; ++y)
-#pragma unroll
-      for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.f;
-  gload(k0);
-  swrite(0);
-  __syncthreads();
-  int buf = 0;
-  for (int64_t k = k0; k < k1; k += kHKf) {
-    const bool more = k + kHKf < k1;
-    if (more) gload(k + kHKf);
-#pragma unroll
-    for (int ks = 0; ks < kHKf / 2; ++ks) {
-      float av[XB], bv[YB];
-#pragma unroll
-      for (int x = 0; x < XB; ++x) av[x] = la[buf][(2 * ks + half) * LA + 32 * (wm * XB + x) + l32];
-#pragma unroll
-      for (int y = 0; y < YB; ++y) bv[y] = lb[buf][(2 * ks + half) * LB + 32 * (wn * YB + y) + l32];
-#pragma unroll
-      for (int x = 0; x < XB; ++x)
-#pragma unroll
-        for (int y = 0; y < YB; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(av[x], bv[y], acc[x][y], 0, 0, 0);
-    }
-    if (more) swrite(buf ^ 1);
-    __syncthreads();
-    buf ^= 1;
-  }
 }
 
 // ---- what becomes of a tile -----------------------------------------------------------------------
@@ -393,18 +324,19 @@ __device__ __forceinline__ void head_sums(const HeadArgs& a, int64_t tm, int64_t
   }
 }
 
-// LDS for a tile of errors, token rows of MT: the 16-byte piece p of token t at p ^ (t & 31), so that the 32
-// tokens of a block, one a lane, go to different banks.  Four arrays of 64 tokens, or one.
+// LDS for a tile, stored transposed: rows of MT elements for its columns, the 16-byte piece p of row t at
+// p ^ (t & 31), so that the columns of a block, one a lane, go to different banks.  The four arrays of a
+// product's slabs in turn, 128 bytes for every row of the tile each.
 template <class TL>
 struct HeadStage {
   typedef typename TL::elem E;
-  static constexpr int EP = kPiece<E>, PPR = TL::MT / EP;
-  static_assert(PPR == 32);
+  static constexpr int EP = TL::EP, PPR = TL::MT / EP, TPA = 128 / (int)sizeof(E);   // pieces of a row; rows of an array
+  static_assert(TL::NT <= 2 * TPA || TL::MT == TL::NT);
   E *p0, *p1, *p2, *p3;
-  __device__ __forceinline__ E* piece(int token, int p) const {
-    const int part = sizeof(E) == 2 ? token >> 6 : 0;
+  __device__ __forceinline__ E* piece(int t, int p) const {
+    const int part = t / TPA;
     E* base = part == 0 ? p0 : part == 1 ? p1 : part == 2 ? p2 : p3;
-    return base + ((sizeof(E) == 2 ? token & 63 : token) * PPR + (p ^ (token & 31))) * EP;
+    return base + ((t % TPA) * PPR + (p ^ (t & (PPR < 32 ? PPR - 1 : 31)))) * EP;
   }
 };
 
@@ -471,131 +403,114 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
   }
 }
 
-// The tile written to, or added to, its place of a plane [N][d].
+// The tile written to, or added to, its place of a plane [rows][cols], or rounded into the result's rows.
 template <class TL>
-__device__ __forceinline__ void head_store(const HeadBackArgs& a, float* plane, int64_t m0, int64_t n0,
+__device__ __forceinline__ void head_store(const HeadMulArgs& a, int split, int64_t m0, int64_t n0,
                                            f32x16_t (&acc)[TL::XB][TL::YB]) {
+  typedef typename TL::elem E;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  float* plane = a.planes + split * a.rows * a.cols;
 #pragma unroll
   for (int x = 0; x < TL::XB; ++x)
 #pragma unroll
     for (int y = 0; y < TL::YB; ++y) {
       const int64_t col = n0 + 32 * (wn * TL::YB + y) + (lane & 31);
-      if (col >= a.d) continue;
+      if (col >= a.cols) continue;
 #pragma unroll
       for (int q = 0; q < 16; ++q) {
         const int64_t row = m0 + 32 * (wm * TL::XB + x) + acc_row(lane, q);
-        if (row >= a.N) continue;
-        float* o = plane + row * a.d + col;
-        *o = a.add ? *o + acc[x][y][q] : acc[x][y][q];
+        if (row >= a.rows) continue;
+        const float v = acc[x][y][q];
+        if (a.out) {
+          E* o = static_cast<E*>(a.out) + row * a.ldo + col;
+          if constexpr (sizeof(E) == 2) *o = __builtin_bit_cast(uint16_t, (__bf16)v);
+          else *o = v;
+        } else {
+          float* o = plane + row * a.cols + col;
+          *o = a.add ? *o + v : v;
+        }
       }
     }
 }
 
 // ---- kernels --------------------------------------------------------------------------------------
 
-// The logits' tiles.  bf16: rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.
-template <class TL, bool ERRORS, bool VW>
+#define DPRC_HEAD_SLABS(TL)                                                                     \
+  __shared__ __attribute__((aligned(16))) typename TL::elem la0[TL::MT * TL::slab];             \
+  __shared__ __attribute__((aligned(16))) typename TL::elem la1[TL::MT * TL::slab];             \
+  __shared__ __attribute__((aligned(16))) typename TL::elem lb0[TL::NT * TL::slab];             \
+  __shared__ __attribute__((aligned(16))) typename TL::elem lb1[TL::NT * TL::slab]
+
+// The logits' tiles.  Rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.  STREAM: W is
+// read once, past the caches.
+template <class TL, bool ERRORS, bool VW, bool STREAM>
 __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
-  __shared__ __attribute__((aligned(16))) uint16_t la0[HeadSlabs<TL, false>::A];
-  __shared__ __attribute__((aligned(16))) uint16_t la1[HeadSlabs<TL, false>::A];
-  __shared__ __attribute__((aligned(16))) uint16_t lb0[HeadSlabs<TL, false>::B];
-  __shared__ __attribute__((aligned(16))) uint16_t lb1[HeadSlabs<TL, false>::B];
-  static_assert(TL::NT == 64 || (TL::MT == 256 && TL::NT == 256));
+  DPRC_HEAD_SLABS(TL);
   const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
   if (wg >= tm_n * tn_n) return;
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
   f32x16_t acc[TL::XB][TL::YB];
-  head_product<TL, false, VW, true>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, la0, la1, lb0, lb1);
+  head_product<TL>(HeadOperand<TL, TL::MT, false, VW, STREAM>(a.W, tm * TL::MT),
+                   HeadOperand<TL, TL::NT, false, true, false>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
   if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, HeadStage<TL>{la0, la1, lb0, lb1});
   else head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(la0));
 }
 
-template <class TL, bool ERRORS>
-__global__ __launch_bounds__(TL::threads) void head_logits_f32_kernel(HeadArgs a) {
-  constexpr int MAIN = head_lds_bytes_f32<TL>(), TAIL = ERRORS ? 4 * TL::MT * TL::NT : 8 * TL::WM * TL::NT;
-  __shared__ __attribute__((aligned(16))) char lds[MAIN > TAIL ? MAIN : TAIL];
-  const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
+// Tiles of A B, blockIdx.z the split of the contraction.  B's rows are the contraction's; so are A's with AKR.
+template <class TL, bool AKR, bool VB>
+__global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
+  DPRC_HEAD_SLABS(TL);
+  const int64_t tm_n = (a.rows + TL::MT - 1) / TL::MT, tn_n = (a.cols + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
   if (wg >= tm_n * tn_n) return;
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
+  const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.K, k0 + a.per_split);
   f32x16_t acc[TL::XB][TL::YB];
-  float* l = reinterpret_cast<float*>(lds);
-  head_product_f32<TL, false>(a.W, tm * TL::MT, a.h, tn * TL::NT, 0, a.W.width, acc, l);
-  if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, HeadStage<TL>{l, l, l, l});
-  else head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(lds));
+  head_product<TL>(HeadOperand<TL, TL::MT, AKR, true, false>(a.A, tm * TL::MT),
+                   HeadOperand<TL, TL::NT, true, VB, false>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
+  head_store<TL>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, acc);
 }
 
-// dh's tiles: rows are tokens, columns features; blockIdx.z is the split of the piece's vocabulary.
-template <class TL, bool VW>
-__global__ __launch_bounds__(TL::threads) void head_back_kernel(HeadBackArgs a) {
-  __shared__ __attribute__((aligned(16))) uint16_t la0[HeadSlabs<TL, true>::A];
-  __shared__ __attribute__((aligned(16))) uint16_t la1[HeadSlabs<TL, true>::A];
-  __shared__ __attribute__((aligned(16))) uint16_t lb0[HeadSlabs<TL, true>::B];
-  __shared__ __attribute__((aligned(16))) uint16_t lb1[HeadSlabs<TL, true>::B];
-  const int64_t tm_n = (a.N + TL::MT - 1) / TL::MT, tn_n = (a.d + TL::NT - 1) / TL::NT;
-  const int64_t wg = flat_block();
-  if (wg >= tm_n * tn_n) return;
-  int64_t tm, tn;
-  tile_of(wg, tm_n, tn_n, tm, tn);
-  const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.E.width, k0 + a.per_split);
-  f32x16_t acc[TL::XB][TL::YB];
-  head_product<TL, true, true, VW>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, la0, la1, lb0, lb1);
-  head_store<TL>(a, a.planes + blockIdx.z * a.N * a.d, tm * TL::MT, tn * TL::NT, acc);
-}
-
-template <class TL>
-__global__ __launch_bounds__(TL::threads) void head_back_f32_kernel(HeadBackArgs a) {
-  __shared__ __attribute__((aligned(16))) char lds[head_lds_bytes_f32<TL>()];
-  const int64_t tm_n = (a.N + TL::MT - 1) / TL::MT, tn_n = (a.d + TL::NT - 1) / TL::NT;
-  const int64_t wg = flat_block();
-  if (wg >= tm_n * tn_n) return;
-  int64_t tm, tn;
-  tile_of(wg, tm_n, tn_n, tm, tn);
-  const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.E.width, k0 + a.per_split);
-  f32x16_t acc[TL::XB][TL::YB];
-  head_product_f32<TL, true>(a.E, tm * TL::MT, a.W, tn * TL::NT, k0, k1, acc, reinterpret_cast<float*>(lds));
-  head_store<TL>(a, a.planes + blockIdx.z * a.N * a.d, tm * TL::MT, tn * TL::NT, acc);
-}
-
-// Joins the tiles' maxima and sums in a fixed order and takes the target's logit, summed in fp32.  16 tokens
-// per workgroup: 64 groups of 16 lanes go through the tiles, then a wave per token multiplies h_t and
-// W_y(t).  A target past the vocabulary makes both outputs NaN.
-template <class E>
+// Joins the tiles' maxima and sums in a fixed order and takes the target's logit, summed in fp32.  TPB tokens per
+// workgroup: 64 / TPB groups of TPB lanes of every wave go through the tiles and are joined, then the waves; a
+// wave per token multiplies h_t and W_y(t).  A target past the vocabulary makes both outputs NaN.
+template <class E, int TPB>
 __global__ __launch_bounds__(1024) void head_join_kernel(HeadArgs a, int64_t tiles, float* loss, float* lse) {
-  __shared__ float2 buf[64][16];
-  __shared__ float out[16];
-  const int64_t t0 = (int64_t)flat_block() * 16;
+  __shared__ float2 buf[16][TPB];
+  const int64_t t0 = (int64_t)flat_block() * TPB;
   if (t0 >= a.N) return;
-  const int j = threadIdx.x & 15, grp = threadIdx.x >> 4, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int j = threadIdx.x % TPB, grp = threadIdx.x / TPB, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int64_t t = t0 + wv, y = wv < TPB && t < a.N ? a.target[t] : -1;
   float2 v{-1e38f, 0.f};
   if (t0 + j < a.N)
-    for (int64_t s = grp; s < tiles; s += 64) v = join(v, a.part[s * a.N + t0 + j]);
-  buf[grp][j] = v;
+    for (int64_t s = grp; s < tiles; s += 1024 / TPB) v = join(v, a.part[s * a.N + t0 + j]);
+#pragma unroll
+  for (int off = TPB; off < 64; off *= 2) v = join(v, float2{__shfl_xor(v.x, off, 64), __shfl_xor(v.y, off, 64)});
+  if (lane < TPB) buf[wv][lane] = v;
   __syncthreads();
-  if (threadIdx.x < 16) {
-    for (int k = 1; k < 64; ++k) v = join(v, buf[k][j]);
-    out[j] = v.x + logf(v.y);
-  }
-  __syncthreads();
-  const int64_t t = t0 + wv;
-  if (t >= a.N) return;
-  const int64_t y = a.target[t];
+  if (wv >= TPB || t >= a.N) return;
+  v = buf[lane & 15][wv];
+#pragma unroll
+  for (int off = 1; off < 16; off *= 2) v = join(v, float2{__shfl_xor(v.x, off, 64), __shfl_xor(v.y, off, 64)});
   float dot = 0.f;
   if (y >= 0 && y < a.W.rows) {
-    const E* h = static_cast<const E*>(a.h.p) + t * a.h.ld;
-    const E* w = static_cast<const E*>(a.W.p) + y * a.W.ld;
-    for (int64_t c = lane; c < a.W.width; c += 64) {
-      if constexpr (sizeof(E) == 2) dot = fmaf(bf16_to_f32(h[c]), bf16_to_f32(w[c]), dot);
-      else dot = fmaf(h[c], w[c], dot);
+    const HeadRows h{static_cast<const E*>(a.h.p) + t * a.h.ld, a.h.ld, 1, a.W.width};
+    const HeadRows w{static_cast<const E*>(a.W.p) + y * a.W.ld, a.W.ld, 1, a.W.width};
+    constexpr int EP = kPiece<E>;
+    for (int64_t c = EP * lane; c < a.W.width; c += EP * 64) {
+      float u[EP], v[EP];
+      unpack<E>(operand_piece<E>(h, 0, c), u);
+      unpack<E>(operand_piece<E>(w, 0, c), v);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) dot = fmaf(u[j], v[j], dot);
     }
   }
   dot = wave_sum(dot);
   if (lane > 0) return;
-  const float z = y >= a.W.rows ? NAN : out[wv], l = z - dot;
+  const float z = y >= a.W.rows ? NAN : v.x + logf(v.y), l = z - dot;
   lse[t] = z;
   loss[t] = y < 0 ? 0.f : l < 0.f ? 0.f : l;           // a probability is at most 1
 }
@@ -662,66 +577,113 @@ __global__ __launch_bounds__(256) void head_round_kernel(const float* planes, in
   }
 }
 
-__global__ void head_one_kernel(float* one) { *one = 1.f; }
-
 // ---- launches -------------------------------------------------------------------------------------
 
 typedef HeadTile<uint16_t, 2, 4, 4, 2> TileWide;       // 256 x 256, eight waves of 128 x 64
 typedef HeadTile<uint16_t, 8, 1, 1, 2> TileFew;        // 256 x 64, eight waves of 32 x 64: up to 64 tokens
+typedef HeadTile<uint16_t, 2, 2, 1, 1> TileSmall;      // 64 x 64, four waves of 32 x 32
 typedef HeadTile<float, 2, 2, 2, 2> TileF32;           // 128 x 128, four waves of 64 x 64
+typedef HeadTile<float, 2, 2, 1, 1> TileSmallF32;      // 64 x 64
 
-int head_tile_rows(int bf16) { return bf16 ? TileWide::MT : TileF32::MT; }
+// Whether tiles of `side` x `side` leave most of the 256 CUs without one, so that small ones are faster.
+static bool few_tiles(int64_t m, int64_t n, int64_t side) { return ceil_div(m, side) * ceil_div(n, side) < 96; }
+static bool logits_small(const HeadArgs& a) { return few_tiles(a.nv, a.N, a.bf16 ? 256 : 128); }
 
-template <class TL, bool ERRORS>
+template <class TL, bool ERRORS, bool STREAM>
 static void launch_logits(const HeadArgs& a, hipStream_t st) {
   const int64_t blocks = ceil_div(a.nv, TL::MT) * ceil_div(a.N, TL::NT);
-  if (a.vec_w) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, true>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
-  else DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
+  if (a.vec_w) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, true, STREAM>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
+  else DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false, STREAM>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
 }
 
 template <bool ERRORS>
 static hipError_t launch_head_logits(const HeadArgs& a, hipStream_t st) {
-  if (!a.bf16) {
-    const int64_t blocks = ceil_div(a.nv, TileF32::MT) * ceil_div(a.N, TileF32::NT);
-    DPRC_LAUNCH((head_logits_f32_kernel<TileF32, ERRORS>), flat_grid(blocks), dim3(TileF32::threads), 0, st, a);
+  if (logits_small(a)) {
+    if (a.bf16) launch_logits<TileSmall, ERRORS, false>(a, st);
+    else launch_logits<TileSmallF32, ERRORS, false>(a, st);
+  } else if (!a.bf16) {
+    launch_logits<TileF32, ERRORS, false>(a, st);
   } else if (a.N <= TileFew::NT) {
-    launch_logits<TileFew, ERRORS>(a, st);
+    launch_logits<TileFew, ERRORS, true>(a, st);
   } else {
-    launch_logits<TileWide, ERRORS>(a, st);
+    launch_logits<TileWide, ERRORS, false>(a, st);
   }
   return hipGetLastError();
+}
+
+// vocabulary rows of a tile of the sums
+static int64_t sums_tile(const HeadArgs& a) { return logits_small(a) ? 64 : a.bf16 ? 256 : 128; }
+int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16) {
+  HeadArgs a{};
+  a.N = N;
+  a.nv = nv;
+  a.bf16 = bf16;
+  return ceil_div(nv, sums_tile(a));
 }
 
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st) { return launch_head_logits<false>(a, st); }
 hipError_t launch_head_errors(const HeadArgs& a, hipStream_t st) { return launch_head_logits<true>(a, st); }
 
 hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st) {
-  const int64_t tiles = ceil_div(a.nv, head_tile_rows(a.bf16)), blocks = ceil_div(a.N, 16);
-  if (a.bf16) DPRC_LAUNCH(head_join_kernel<uint16_t>, flat_grid(blocks), dim3(1024), 0, st, a, tiles, loss, lse);
-  else DPRC_LAUNCH(head_join_kernel<float>, flat_grid(blocks), dim3(1024), 0, st, a, tiles, loss, lse);
+  const int64_t tiles = head_sum_tiles(a.N, a.nv, a.bf16);
+  auto go = [&](auto kernel, int tpb) { DPRC_LAUNCH(kernel, flat_grid(ceil_div(a.N, tpb)), dim3(1024), 0, st, a, tiles, loss, lse); };
+  if (a.N <= 1024) {
+    if (a.bf16) go(head_join_kernel<uint16_t, 4>, 4);
+    else go(head_join_kernel<float, 4>, 4);
+  } else {
+    if (a.bf16) go(head_join_kernel<uint16_t, 16>, 16);
+    else go(head_join_kernel<float, 16>, 16);
+  }
   return hipGetLastError();
 }
 
-HeadBackPlan head_back_plan(int64_t N, int64_t d, int64_t nv, int bf16, int32_t most) {
-  const int64_t tile = bf16 ? 256 : 128, slab = bf16 ? kHK : kHKf;
-  const int64_t tiles = ceil_div(N, tile) * ceil_div(d, tile), slabs = ceil_div(nv, slab);
-  int64_t want = tiles >= 256 ? 1 : std::min<int64_t>(ceil_div(256, tiles), std::max<int64_t>(1, slabs / 16));
-  if (most > 0) want = std::min<int64_t>(want, most);
-  HeadBackPlan p;
+static bool mul_small(int64_t rows, int64_t cols, int64_t K, int bf16) {
+  return few_tiles(rows, cols, bf16 ? 256 : 128) && K < 8192;
+}
+
+static HeadMulPlan split_plan(int64_t K, int64_t want, int small, int bf16) {
+  const int64_t slab = bf16 ? TileWide::slab : TileF32::slab, slabs = ceil_div(K, slab);
+  HeadMulPlan p;
+  p.small = small;
   p.per_split = ceil_div(slabs, want) * slab;
   p.S = (int32_t)ceil_div(slabs * slab, p.per_split);
   return p;
 }
 
-hipError_t launch_head_back(const HeadBackArgs& a, hipStream_t st) {
-  auto go = [&](auto kernel, int tile, int threads) {
-    dim3 grid = flat_grid(ceil_div(a.N, tile) * ceil_div(a.d, tile));
+HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16) {
+  const int small = mul_small(rows, cols, K, bf16);
+  const int64_t tile = small ? 64 : bf16 ? 256 : 128, tiles = ceil_div(rows, tile) * ceil_div(cols, tile);
+  const int64_t slabs = ceil_div(K, bf16 ? TileWide::slab : TileF32::slab);
+  const int64_t want = tiles >= 256 ? 1 : std::min<int64_t>(ceil_div(256, tiles), std::max<int64_t>(1, slabs / (small ? 4 : 16)));
+  return split_plan(K, want, small, bf16);
+}
+
+HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16) { return split_plan(K, p.S, p.small, bf16); }
+
+template <bool AKR>
+static void launch_mul(const HeadMulArgs& a, hipStream_t st) {
+  auto go = [&](auto kernel, auto tile) {
+    typedef decltype(tile) TL;
+    dim3 grid = flat_grid(ceil_div(a.rows, TL::MT) * ceil_div(a.cols, TL::NT));
     grid.z = (unsigned)a.S;
-    DPRC_LAUNCH(kernel, grid, dim3(threads), 0, st, a);
+    DPRC_LAUNCH(kernel, grid, dim3(TL::threads), 0, st, a);
   };
-  if (!a.bf16) go(head_back_f32_kernel<TileF32>, TileF32::MT, TileF32::threads);
-  else if (a.vec_w) go(head_back_kernel<TileWide, true>, TileWide::MT, TileWide::threads);
-  else go(head_back_kernel<TileWide, false>, TileWide::MT, TileWide::threads);
+  auto rows = [&](auto tile) {
+    typedef decltype(tile) TL;
+    if constexpr (AKR) go(head_mul_kernel<TL, true, true>, tile);      // h's copy
+    else if (a.vec_b) go(head_mul_kernel<TL, false, true>, tile);
+    else go(head_mul_kernel<TL, false, false>, tile);
+  };
+  const bool small = a.small;
+  if (a.bf16 && small) rows(TileSmall{});
+  else if (a.bf16) rows(TileWide{});
+  else if (small) rows(TileSmallF32{});
+  else rows(TileF32{});
+}
+
+hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st) {
+  if (a.akr) launch_mul<true>(a, st);
+  else launch_mul<false>(a, st);
   return hipGetLastError();
 }
 
@@ -737,11 +699,6 @@ hipError_t launch_head_round(const float* planes, int S, int64_t rows, int64_t c
   const int64_t blocks = ceil_div(rows * ceil_div(cols, 4), 256);
   if (bf16) DPRC_LAUNCH(head_round_kernel<uint16_t>, flat_grid(blocks), dim3(256), 0, st, planes, S, rows, cols, (uint16_t*)out, ldo);
   else DPRC_LAUNCH(head_round_kernel<float>, flat_grid(blocks), dim3(256), 0, st, planes, S, rows, cols, (float*)out, ldo);
-  return hipGetLastError();
-}
-
-hipError_t launch_head_one(float* one, hipStream_t st) {
-  DPRC_LAUNCH(head_one_kernel, dim3(1), dim3(1), 0, st, one);
   return hipGetLastError();
 }
 

@@ -474,29 +474,32 @@ struct HeadArgs {
   void* E;                 // errors: [N][lde], columns v0 .. v0 + width
   int64_t lde, width;      // width >= nv: the columns past nv are zeros
 };
-int head_tile_rows(int bf16);         // vocabulary rows of a tile
+int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16);
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_errors(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st);   // nv = V, v0 = 0
 
-// planes[S][N][d] (=|+=) the splits' sums of E W over a piece of the vocabulary.
-struct HeadBackArgs {
-  HeadRows E, W;           // [N][nv], [nv][d]
-  int64_t N, d, per_split;
-  int32_t S, bf16, vec_w, add;
+// A B with rows of B along the result's: E W (akr = 0: A [rows][K]) or E^T h (akr = 1: A [K][rows]).  The sums of S splits
+// of K to planes[S][rows][cols] (=|+=), or with S = 1 rounded to out.
+struct HeadMulArgs {
+  HeadRows A, B;           // A in 16-byte pieces
+  int64_t rows, cols, K, per_split;
+  int32_t S, bf16, vec_b, akr, small, add;
   float* planes;
+  void* out;               // null: planes
+  int64_t ldo;
 };
-struct HeadBackPlan {
+struct HeadMulPlan {
   int64_t per_split;
-  int32_t S;
+  int32_t S, small;
 };
-// most > 0: at most so many splits
-HeadBackPlan head_back_plan(int64_t N, int64_t d, int64_t nv, int bf16, int32_t most);
-hipError_t launch_head_back(const HeadBackArgs& a, hipStream_t st);
+HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16);
+// of a shorter contraction: the same tiles, at most as many splits
+HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16);
+hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st);
 hipError_t launch_head_rows(const HeadRows& X, int bf16, const int64_t* target, void* out, int64_t ldo, hipStream_t st);
 hipError_t launch_head_round(const float* planes, int S, int64_t rows, int64_t cols, int bf16, void* out, int64_t ldo,
                              hipStream_t st);
-hipError_t launch_head_one(float* one, hipStream_t st);
 
 // Rotary positions of up to kRotaryTensors tensors [B][T][H][D] (see dprc_rotary).
 constexpr int kRotaryTensors = 4;

@@ -917,7 +917,7 @@ KERNEL_NAMES = {1: "project", 2: "token_reduce", 3: "qr", 4: "hutchpp_final", 5:
                 19: "probe_gauss", 20: "adamw", 21: "envelope", 22: "chi2_cdf", 23: "pld", 24: "dropout",
                 25: "layernorm", 26: "layernorm_backward", 27: "vector_norms", 28: "vector_sums", 29: "head_sums",
                 30: "head_join", 31: "head_errors", 32: "head_back", 33: "head_rows", 34: "rotary", 35: "grad_squares",
-                36: "grad_scale"}
+                36: "grad_scale", 37: "head_weight"}
 
 
 def dprc_trace_launches(events_ptr, kinds_ptr, capacity, count_ptr):
