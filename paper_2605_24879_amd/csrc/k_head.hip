@@ -340,27 +340,44 @@ struct HeadStage {
   }
 };
 
+// What the errors of a lane's tokens are formed with, one token in each of the wave's column blocks.  Loaded
+// before the product, whose time hides the loads', and looked at after it.
+template <class TL>
+struct HeadTokens {
+  int64_t target[TL::YB];
+  float lse[TL::YB], g[TL::YB];
+  __device__ __forceinline__ HeadTokens(const HeadArgs& a, int64_t t0) {
+    const int wn = (threadIdx.x >> 6) % TL::WN;
+#pragma unroll
+    for (int y = 0; y < TL::YB; ++y) {                  // (past the last token: the last one's, not stored)
+      const int64_t t = min(a.N - 1, t0 + 32 * (wn * TL::YB + y) + (threadIdx.x & 31));
+      target[y] = a.target[t];
+      lse[y] = a.lse[t];
+      g[y] = a.g[t];
+    }
+  }
+};
+
 // The tile's errors, through LDS into token rows.
 template <class TL>
-__device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64_t t0, f32x16_t (&acc)[TL::XB][TL::YB],
-                                            const HeadStage<TL>& stage) {
+__device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64_t t0, const HeadTokens<TL>& tok,
+                                            f32x16_t (&acc)[TL::XB][TL::YB], const HeadStage<TL>& stage) {
   typedef typename TL::elem E;
-  constexpr int EP = kPiece<E>, PPR = TL::MT / EP;
+  constexpr int EP = TL::EP, PPR = TL::MT / EP;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
   const int64_t vt = tm * TL::MT;                       // the tile's first column of this piece
   const int v0 = 32 * TL::XB * wm;                      // the wave's first in the tile
-  const int end = (int)min((int64_t)TL::MT, a.nv - vt) - v0;       // its columns before the vocabulary's end
+  const int end = (int)min((int64_t)TL::MT, a.nv - vt); // the tile's columns before the vocabulary's end
 #pragma unroll
   for (int y = 0; y < TL::YB; ++y) {
     const int col = 32 * (wn * TL::YB + y) + (lane & 31);
-    const int64_t t = t0 + col;
-    const int64_t target = t < a.N ? a.target[t] : -1;
-    const bool kept = target >= 0;
-    const float lse = kept ? a.lse[t] : 0.f, g = kept ? a.g[t] : 0.f;
-    const int64_t at64 = target - a.v0 - vt - v0;       // the target's place among the wave's columns
-    const int at = kept && at64 >= 0 && at64 < 32 * TL::XB ? (int)at64 : -1;
-    const float lse2 = lse * kLog2e;
-    const bool rare = __any(at >= 0) || end < 32 * TL::XB;
+    const bool kept = tok.target[y] >= 0;
+    const float g = tok.g[y], lse = tok.lse[y], lse2 = lse * kLog2e;
+    // the target's or the vocabulary's end among the wave's rows: few waves
+    const int64_t row = tok.target[y] - a.v0 - vt - v0;
+    const int at = kept && row >= 0 && row < 32 * TL::XB ? (int)row : -1;
+    const bool rare = __any(at >= 0) || end < v0 + 32 * TL::XB;
+    float own = 0.f;                                    // the target's logit
 #pragma unroll
     for (int x = 0; x < TL::XB; ++x)
 #pragma unroll
@@ -372,15 +389,15 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
           if constexpr (sizeof(E) == 2) e[q] = g * __builtin_amdgcn_exp2f(fmaf(l, kLog2e, -lse2));
           else e[q] = g * expf(l - lse);
         }
-        const int v = 32 * x + acc_row(lane, 4 * q4);
+        const int v = v0 + 32 * x + acc_row(lane, 4 * q4);
         if (rare) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            if (at == v + q) e[q] = g * expm1f(acc[x][y][4 * q4 + q] - lse);   // exp(x) - 1 without cancellation
-            if (v + q >= end) e[q] = 0.f;
+            own = at == v - v0 + q ? acc[x][y][4 * q4 + q] : own;
+            e[q] = v + q >= end ? 0.f : e[q];
           }
         }
-        E* o = stage.piece(col, (v0 + v) / EP) + (v & (EP - 1));
+        E* o = stage.piece(col, v / EP) + (v & (EP - 1));
         if constexpr (sizeof(E) == 2) {
           const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[0], e[1]}, bf16x2_t));
           const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{e[2], e[3]}, bf16x2_t));
@@ -389,17 +406,39 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
           *reinterpret_cast<float4*>(o) = kept ? float4{e[0], e[1], e[2], e[3]} : float4{0.f, 0.f, 0.f, 0.f};
         }
       }
+    if (at >= 0 && ((at >> 2) & 1) == (lane >> 5)) {     // exp(x) - 1 without cancellation
+      const float e = g * expm1f(own - lse);
+      E* o = stage.piece(col, (v0 + at) / EP) + (at & (EP - 1));
+      if constexpr (sizeof(E) == 2) *o = __builtin_bit_cast(uint16_t, (__bf16)e);
+      else *o = e;
+    }
   }
   __syncthreads();
-  for (int s = threadIdx.x; s < TL::NT * PPR; s += TL::threads) {
-    const int row = s / PPR, p = s % PPR;
-    const int64_t t = t0 + row, v = vt + EP * p;
-    if (t >= a.N || v >= a.width) continue;
-    const E* from = stage.piece(row, p);
-    E* to = static_cast<E*>(a.E) + t * a.lde + v;
-    if (v + EP <= a.width) store_piece<E>(to, *reinterpret_cast<const uint4*>(from));
-    else
-      for (int j = 0; v + j < a.width; ++j) to[j] = from[j];
+  // a thread stores one piece of every ROWS-th token, R of them read before the first is stored
+  constexpr int ROWS = TL::threads / PPR, R = TL::NT / ROWS < 8 ? TL::NT / ROWS : 8;
+  static_assert(TL::threads % PPR == 0 && TL::NT % (ROWS * R) == 0);
+  const int p = threadIdx.x % PPR, row0 = threadIdx.x / PPR;
+  const int64_t v = vt + EP * p, room = a.width - v;
+  if (room <= 0) return;
+  const int rows = (int)min((int64_t)TL::NT, a.N - t0);
+  E* to = static_cast<E*>(a.E) + (t0 + row0) * a.lde + v;
+  for (int row = row0; row < rows; row += ROWS * R) {
+    uint4 w[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) w[r] = *reinterpret_cast<const uint4*>(stage.piece(row + ROWS * r, p));
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      if (row + ROWS * r < rows) {
+        if (room >= EP) {
+          if (a.stream) store_piece<E, true>(to, w[r]);
+          else store_piece<E>(to, w[r]);
+        } else {
+          const E* from = stage.piece(row + ROWS * r, p);
+          for (int j = 0; j < room; ++j) to[j] = from[j];
+        }
+      }
+      to += ROWS * a.lde;
+    }
   }
 }
 
@@ -452,10 +491,18 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
   f32x16_t acc[TL::XB][TL::YB];
-  head_product<TL>(HeadOperand<TL, TL::MT, false, VW, STREAM>(a.W, tm * TL::MT),
-                   HeadOperand<TL, TL::NT, false, true, false>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
-  if constexpr (ERRORS) head_errors<TL>(a, tm, tn * TL::NT, acc, HeadStage<TL>{la0, la1, lb0, lb1});
-  else head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(la0));
+  auto product = [&] {
+    head_product<TL>(HeadOperand<TL, TL::MT, false, VW, STREAM>(a.W, tm * TL::MT),
+                     HeadOperand<TL, TL::NT, false, true, false>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
+  };
+  if constexpr (ERRORS) {
+    const HeadTokens<TL> tok(a, tn * TL::NT);
+    product();
+    head_errors<TL>(a, tm, tn * TL::NT, tok, acc, HeadStage<TL>{la0, la1, lb0, lb1});
+  } else {
+    product();
+    head_sums<TL>(a, tm, tn * TL::NT, acc, reinterpret_cast<float2*>(la0));
+  }
 }
 
 // Tiles of A B, blockIdx.z the split of the contraction.  B's rows are the contraction's; so are A's with AKR.
@@ -622,7 +669,12 @@ int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16) {
 }
 
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st) { return launch_head_logits<false>(a, st); }
-hipError_t launch_head_errors(const HeadArgs& a, hipStream_t st) { return launch_head_logits<true>(a, st); }
+// E past the caches where it is larger than they are: 8192 x 65536 x 2048 1924 and 1898 us, 4096 x 50176 x 1024 504 and 472
+// (without storing E at all 1780 and 418: every CU stores its tile at about the same time).
+hipError_t launch_head_errors(HeadArgs a, hipStream_t st) {
+  a.stream = a.N * a.width * (a.bf16 ? 2 : 4) > kStreamRowsBytes;
+  return launch_head_logits<true>(a, st);
+}
 
 hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st) {
   const int64_t tiles = head_sum_tiles(a.N, a.nv, a.bf16);

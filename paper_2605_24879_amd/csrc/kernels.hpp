@@ -473,10 +473,11 @@ struct HeadArgs {
   const float* g;          // errors: [N]
   void* E;                 // errors: [N][lde], columns v0 .. v0 + width
   int64_t lde, width;      // width >= nv: the columns past nv are zeros
+  int32_t stream;          // errors: past the caches (set by the launcher)
 };
 int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16);
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st);
-hipError_t launch_head_errors(const HeadArgs& a, hipStream_t st);
+hipError_t launch_head_errors(HeadArgs a, hipStream_t st);
 hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st);   // nv = V, v0 = 0
 
 // A B with rows of B along the result's: E W (akr = 0: A [rows][K]) or E^T h (akr = 1: A [K][rows]).  The sums of S splits
