@@ -1999,7 +1999,7 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
   const int bf16 = H->dtype == DPRC_BF16;
   // a product's sums in planes, or with one split of all of them in the result; then the planes rounded
   auto multiply = [&](HeadMulArgs& a, const HeadMulPlan& plan, int kind) -> dprc_status {
-    a.per_split = plan.per_split; a.S = plan.S; a.small = plan.small; a.bf16 = bf16;
+    a.per_split = plan.per_split; a.S = plan.S; a.side = plan.side; a.bf16 = bf16;
     return hip_status(traced(kind, stream, [&] { return launch_head_mul(a, stream); }));
   };
   auto round = [&](const float* planes, int S, int64_t rows, void* out, int64_t ld) {

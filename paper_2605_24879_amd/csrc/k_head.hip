@@ -77,7 +77,7 @@ __device__ __forceinline__ uint4 operand_piece(const HeadRows& X, int64_t row, i
 }
 
 // 64 lanes' 16-byte pieces at byte offsets `off` of the resource to 1024 bytes of LDS, in lane order; zeros
-// where the offset is out of the resource's range.  NT: for an operand that is streamed once.
+// where the offset is out of the resource's range.
 typedef __attribute__((address_space(3))) void lds_void_t;
 template <bool NT>
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, void* lds, uint32_t off) {
@@ -91,7 +91,8 @@ struct HInt {
 
 // One operand's slabs of a tile of T rows (columns) from t0 on: loads, straight into LDS where its rows allow
 // 16-byte pieces (VEC), else through registers.
-template <class TL, int T, bool KR, bool VEC, bool NT>
+// NT: past the caches.
+template <class TL, int T, bool KR, bool VEC, bool NT = false>
 struct HeadOperand {
   typedef typename TL::elem E;
   static constexpr int EP = TL::EP, P = T * 8 / TL::threads, RP = T / EP;    // pieces of a thread; of a KR row
@@ -176,6 +177,30 @@ struct HeadOperand {
   }
 };
 
+// acc += the products of a wave's fragments
+template <class E, int XB, int YB>
+__device__ __forceinline__ void head_mfma(const uint4 (&av)[XB], const uint4 (&bv)[YB], f32x16_t (&acc)[XB][YB]) {
+  if constexpr (sizeof(E) == 2) {
+#pragma unroll
+    for (int x = 0; x < XB; ++x)
+#pragma unroll
+      for (int y = 0; y < YB; ++y)
+        acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
+                                                            __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int x = 0; x < XB; ++x)
+#pragma unroll
+        for (int y = 0; y < YB; ++y) {
+          const float a = __uint_as_float(i == 0 ? av[x].x : i == 1 ? av[x].y : i == 2 ? av[x].z : av[x].w);
+          const float b = __uint_as_float(i == 0 ? bv[y].x : i == 1 ? bv[y].y : i == 2 ? bv[y].z : bv[y].w);
+          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, acc[x][y], 0, 0, 0);
+        }
+  }
+}
+
 // acc = sum over k in [k0, k1) of A[i][k] B[j][k], i and j the tile's rows and columns; k0 a multiple of the
 // slab.  fp32 products and sums (bf16 products are exact).  Slabs are double-buffered: while one is
 // multiplied the next is loaded.  A wave has the next fragments in registers ahead of their products, also
@@ -222,25 +247,7 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
   auto phase = [&](uint4 (&na)[XB], uint4 (&nb)[YB], auto u, int ks, const uint4 (&av)[XB], const uint4 (&bv)[YB])
       __attribute__((always_inline)) {
     frag(na, nb, u, ks);
-    if constexpr (sizeof(E) == 2) {
-#pragma unroll
-      for (int x = 0; x < XB; ++x)
-#pragma unroll
-        for (int y = 0; y < YB; ++y)
-          acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, av[x]),
-                                                              __builtin_bit_cast(bf16x8_t, bv[y]), acc[x][y], 0, 0, 0);
-    } else {
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int x = 0; x < XB; ++x)
-#pragma unroll
-          for (int y = 0; y < YB; ++y) {
-            const float a = __uint_as_float(i == 0 ? av[x].x : i == 1 ? av[x].y : i == 2 ? av[x].z : av[x].w);
-            const float b = __uint_as_float(i == 0 ? bv[y].x : i == 1 ? bv[y].y : i == 2 ? bv[y].z : bv[y].w);
-            acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, b, acc[x][y], 0, 0, 0);
-          }
-    }
+    head_mfma<E, XB, YB>(av, bv, acc);
     constexpr int reads = XB * OA::reads + YB * OB::reads, products = XB * YB * (sizeof(E) == 2 ? 1 : 4);
 #pragma unroll
     for (int i = 0; i < reads; ++i) {
@@ -331,7 +338,7 @@ template <class TL>
 struct HeadStage {
   typedef typename TL::elem E;
   static constexpr int EP = TL::EP, PPR = TL::MT / EP, TPA = 128 / (int)sizeof(E);   // pieces of a row; rows of an array
-  static_assert(TL::NT <= 2 * TPA || TL::MT == TL::NT);
+  static_assert(TL::NT <= 2 * TPA || TL::MT == TL::NT, "the arrays' sizes");
   E *p0, *p1, *p2, *p3;
   __device__ __forceinline__ E* piece(int t, int p) const {
     const int part = t / TPA;
@@ -480,9 +487,8 @@ __device__ __forceinline__ void head_store(const HeadMulArgs& a, int split, int6
   __shared__ __attribute__((aligned(16))) typename TL::elem lb0[TL::NT * TL::slab];             \
   __shared__ __attribute__((aligned(16))) typename TL::elem lb1[TL::NT * TL::slab]
 
-// The logits' tiles.  Rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.  STREAM: W is
-// read once, past the caches.
-template <class TL, bool ERRORS, bool VW, bool STREAM>
+// The logits' tiles.  Rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.
+template <class TL, bool ERRORS, bool VW>
 __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   DPRC_HEAD_SLABS(TL);
   const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
@@ -491,9 +497,10 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
   f32x16_t acc[TL::XB][TL::YB];
+  constexpr bool STREAM = TL::NT < TL::MT;              // few tokens: every row of W is read once
   auto product = [&] {
     head_product<TL>(HeadOperand<TL, TL::MT, false, VW, STREAM>(a.W, tm * TL::MT),
-                     HeadOperand<TL, TL::NT, false, true, false>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
+                     HeadOperand<TL, TL::NT, false, true>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
   };
   if constexpr (ERRORS) {
     const HeadTokens<TL> tok(a, tn * TL::NT);
@@ -516,8 +523,8 @@ __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
   tile_of(wg, tm_n, tn_n, tm, tn);
   const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.K, k0 + a.per_split);
   f32x16_t acc[TL::XB][TL::YB];
-  head_product<TL>(HeadOperand<TL, TL::MT, AKR, true, false>(a.A, tm * TL::MT),
-                   HeadOperand<TL, TL::NT, true, VB, false>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
+  head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
+                   HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
   head_store<TL>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, acc);
 }
 
@@ -627,45 +634,57 @@ __global__ __launch_bounds__(256) void head_round_kernel(const float* planes, in
 // ---- launches -------------------------------------------------------------------------------------
 
 typedef HeadTile<uint16_t, 2, 4, 4, 2> TileWide;       // 256 x 256, eight waves of 128 x 64
-typedef HeadTile<uint16_t, 8, 1, 1, 2> TileFew;        // 256 x 64, eight waves of 32 x 64: up to 64 tokens
+typedef HeadTile<uint16_t, 2, 2, 2, 2> TileMid;        // 128 x 128, four waves of 64 x 64
 typedef HeadTile<uint16_t, 2, 2, 1, 1> TileSmall;      // 64 x 64, four waves of 32 x 32
-typedef HeadTile<float, 2, 2, 2, 2> TileF32;           // 128 x 128, four waves of 64 x 64
-typedef HeadTile<float, 2, 2, 1, 1> TileSmallF32;      // 64 x 64
+typedef HeadTile<float, 2, 2, 2, 2> TileMidF32;
+typedef HeadTile<float, 2, 2, 1, 1> TileSmallF32;
+typedef HeadTile<uint16_t, 8, 1, 1, 2> TileFew;        // 256 x 64, eight waves of 32 x 64
+typedef HeadTile<float, 4, 1, 2, 1> TileFewF32;        // 256 x 32, four waves of 64 x 32
 
-// Whether tiles of `side` x `side` leave most of the 256 CUs without one, so that small ones are faster.
-static bool few_tiles(int64_t m, int64_t n, int64_t side) { return ceil_div(m, side) * ceil_div(n, side) < 96; }
-static bool logits_small(const HeadArgs& a) { return few_tiles(a.nv, a.N, a.bf16 ? 256 : 128); }
+// The side of the tiles of an m x n result: the largest that leaves no CU without a tile, else small ones.
+static int tile_side(int64_t m, int64_t n, int bf16) {
+  if (bf16 && ceil_div(m, 256) * ceil_div(n, 256) >= 192) return 256;
+  return ceil_div(m, 128) * ceil_div(n, 128) >= 192 ? 128 : 64;
+}
 
-template <class TL, bool ERRORS, bool STREAM>
-static void launch_logits(const HeadArgs& a, hipStream_t st) {
-  const int64_t blocks = ceil_div(a.nv, TL::MT) * ceil_div(a.N, TL::NT);
-  if (a.vec_w) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, true, STREAM>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
-  else DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false, STREAM>), flat_grid(blocks), dim3(TL::threads), 0, st, a);
+// Up to 64 tokens (32 in fp32) of a large vocabulary: tiles of all tokens and 256 rows of W, which bounds the call and
+// is read past the caches.  64 tokens of 128256 x 2048 bf16 114 us (525 MB); with three and four slabs of loads under
+// way and one such workgroup a CU 115, with every wave reading rows of its own into registers 313.
+static bool few_tokens(int64_t N, int64_t nv, int bf16) { return N <= (bf16 ? 64 : 32) && nv >= 64 * 256; }
+
+static int logits_side(int64_t N, int64_t nv, int bf16) {
+  if (few_tokens(N, nv, bf16)) return 0;
+  // one column of tiles: narrow ones, of which two share a CU
+  const int side = tile_side(nv, N, bf16);
+  return bf16 ? (N <= 128 ? std::min(side, 128) : side) : (N <= 64 ? 64 : side);
 }
 
 template <bool ERRORS>
 static hipError_t launch_head_logits(const HeadArgs& a, hipStream_t st) {
-  if (logits_small(a)) {
-    if (a.bf16) launch_logits<TileSmall, ERRORS, false>(a, st);
-    else launch_logits<TileSmallF32, ERRORS, false>(a, st);
-  } else if (!a.bf16) {
-    launch_logits<TileF32, ERRORS, false>(a, st);
-  } else if (a.N <= TileFew::NT) {
-    launch_logits<TileFew, ERRORS, true>(a, st);
+  auto tiles = [&](auto tile) {
+    typedef decltype(tile) TL;
+    const dim3 grid = flat_grid(ceil_div(a.nv, TL::MT) * ceil_div(a.N, TL::NT));
+    if (a.vec_w) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, true>), grid, dim3(TL::threads), 0, st, a);
+    else DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false>), grid, dim3(TL::threads), 0, st, a);
+  };
+  const int side = logits_side(a.N, a.nv, a.bf16);
+  if (a.bf16) {
+    if (side == 0) tiles(TileFew{});
+    else if (side == 256) tiles(TileWide{});
+    else if (side == 128) tiles(TileMid{});
+    else tiles(TileSmall{});
   } else {
-    launch_logits<TileWide, ERRORS, false>(a, st);
+    if (side == 0) tiles(TileFewF32{});
+    else if (side == 128) tiles(TileMidF32{});
+    else tiles(TileSmallF32{});
   }
   return hipGetLastError();
 }
 
-// vocabulary rows of a tile of the sums
-static int64_t sums_tile(const HeadArgs& a) { return logits_small(a) ? 64 : a.bf16 ? 256 : 128; }
+// tiles of the vocabulary that the sums leave
 int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16) {
-  HeadArgs a{};
-  a.N = N;
-  a.nv = nv;
-  a.bf16 = bf16;
-  return ceil_div(nv, sums_tile(a));
+  const int side = logits_side(N, nv, bf16);
+  return ceil_div(nv, side == 0 ? 256 : side);
 }
 
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st) { return launch_head_logits<false>(a, st); }
@@ -689,28 +708,27 @@ hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStrea
   return hipGetLastError();
 }
 
-static bool mul_small(int64_t rows, int64_t cols, int64_t K, int bf16) {
-  return few_tiles(rows, cols, bf16 ? 256 : 128) && K < 8192;
-}
-
-static HeadMulPlan split_plan(int64_t K, int64_t want, int small, int bf16) {
-  const int64_t slab = bf16 ? TileWide::slab : TileF32::slab, slabs = ceil_div(K, slab);
+static HeadMulPlan split_plan(int64_t K, int64_t want, int side, int bf16) {
+  const int64_t slab = bf16 ? TileWide::slab : TileMidF32::slab, slabs = ceil_div(K, slab);
   HeadMulPlan p;
-  p.small = small;
+  p.side = side;
   p.per_split = ceil_div(slabs, want) * slab;
   p.S = (int32_t)ceil_div(slabs * slab, p.per_split);
   return p;
 }
 
+// Long contractions are split among large tiles, short ones take smaller tiles.
 HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16) {
-  const int small = mul_small(rows, cols, K, bf16);
-  const int64_t tile = small ? 64 : bf16 ? 256 : 128, tiles = ceil_div(rows, tile) * ceil_div(cols, tile);
-  const int64_t slabs = ceil_div(K, bf16 ? TileWide::slab : TileF32::slab);
-  const int64_t want = tiles >= 256 ? 1 : std::min<int64_t>(ceil_div(256, tiles), std::max<int64_t>(1, slabs / (small ? 4 : 16)));
-  return split_plan(K, want, small, bf16);
+  const int64_t slabs = ceil_div(K, bf16 ? TileWide::slab : TileMidF32::slab);
+  int side = tile_side(rows, cols, bf16);
+  const int most = bf16 ? 256 : 128;
+  if (ceil_div(rows, most) * ceil_div(cols, most) * (slabs / 16) >= 192) side = most;
+  const int64_t tiles = ceil_div(rows, side) * ceil_div(cols, side);
+  const int64_t want = tiles >= 192 ? 1 : std::min<int64_t>(ceil_div(256, tiles), std::max<int64_t>(1, slabs / (side == 64 ? 4 : 16)));
+  return split_plan(K, want, side, bf16);
 }
 
-HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16) { return split_plan(K, p.S, p.small, bf16); }
+HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16) { return split_plan(K, p.S, p.side, bf16); }
 
 template <bool AKR>
 static void launch_mul(const HeadMulArgs& a, hipStream_t st) {
@@ -726,11 +744,11 @@ static void launch_mul(const HeadMulArgs& a, hipStream_t st) {
     else if (a.vec_b) go(head_mul_kernel<TL, false, true>, tile);
     else go(head_mul_kernel<TL, false, false>, tile);
   };
-  const bool small = a.small;
-  if (a.bf16 && small) rows(TileSmall{});
-  else if (a.bf16) rows(TileWide{});
-  else if (small) rows(TileSmallF32{});
-  else rows(TileF32{});
+  if (a.bf16 && a.side == 256) rows(TileWide{});
+  else if (a.bf16 && a.side == 128) rows(TileMid{});
+  else if (a.bf16) rows(TileSmall{});
+  else if (a.side == 128) rows(TileMidF32{});
+  else rows(TileSmallF32{});
 }
 
 hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st) {

@@ -485,14 +485,14 @@ hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStrea
 struct HeadMulArgs {
   HeadRows A, B;           // A in 16-byte pieces
   int64_t rows, cols, K, per_split;
-  int32_t S, bf16, vec_b, akr, small, add;
+  int32_t S, side, bf16, vec_b, akr, add;   // side: of the tiles
   float* planes;
   void* out;               // null: planes
   int64_t ldo;
 };
 struct HeadMulPlan {
   int64_t per_split;
-  int32_t S, small;
+  int32_t S, side;
 };
 HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16);
 // of a shorter contraction: the same tiles, at most as many splits
