@@ -1764,6 +1764,13 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
 namespace {
 
 constexpr int64_t kHeadPieceBytes = (int64_t)1 << 30;
+// Rows of W that do not start on 16-byte boundaries are laid out so, a piece at a time, for as many tokens as make up
+// for it, counted once for every product that reads them.  20001 x 1027 bf16, us with and without: loss of 128,
+// 256, 512, 2042 tokens 45, 49, 66, 130 and 42, 61, 107, 196; gradients of 64, 256, 2042 115, 137, 428 and 132, 206,
+// 625.  fp32: loss of 512, 2042 tokens 240, 711 and 232, 722; gradients of 256, 512, 2042 467, 767, 2704 and 466, 798,
+// 2945.
+constexpr int64_t kHeadCopyTokens[2] = {1024, 192};   // fp32, bf16
+constexpr int64_t kHeadCopyBytes = (int64_t)1 << 28;  // of a piece of W, in the forward pass
 constexpr int64_t kHeadPieceMax = (int64_t)1 << 21;   // columns: offsets within a tile of E stay below 2^31
 constexpr int32_t kHeadBlocks = 32;                   // of a dprc_norm_hutch call
 
@@ -1784,9 +1791,14 @@ bool head_vec(const dprc_head& H, const void* p, int64_t ld) {
   return aligned(p, 16) && ld % piece == 0 && H.d % piece == 0 && ld < (1LL << 21);
 }
 
+bool head_copies_w(const dprc_head& H, int products) {
+  return !head_vec(H, H.W, H.ldw) && H.B * H.T * products >= kHeadCopyTokens[H.dtype == DPRC_BF16];
+}
+
 struct HeadBufs {
   int64_t N, piece, lde, ldc;          // tokens; columns of a piece; row strides of E and of h's copy
   void* rows;                          // h laid out [N][ldc]
+  void* W;                             // a piece of W laid out [piece][ldc]; null: W itself
   void* E;                             // [N][lde]
   HeadMulPlan dh;
   float* dh_planes;                    // [S][N][d]; null: one piece, one split
@@ -1836,6 +1848,7 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
   b.ldc = round_up(H.d, 8);
   b.rows = ar.take<char>((size_t)(b.N * b.ldc) * e);
   b.E = ar.take<char>((size_t)(b.N * b.lde) * e);
+  if (head_copies_w(H, dh ? 2 : 1)) b.W = ar.take<char>((size_t)(b.piece * b.ldc) * e);
   // buffers of a shape to ask for sizes with: only their alignment counts
   HeadBufs probe = b;
   probe.rows = probe.E = reinterpret_cast<void*>((uintptr_t)kAlign);
@@ -1880,7 +1893,19 @@ HeadArgs head_args(const dprc_head& H, const HeadRows& h, int64_t v0, int64_t nv
   return a;
 }
 
-// h's rows laid out for the gradients, then f(v0, nv) for every piece with its E formed.
+// The rows of W in `a` laid out in 16-byte pieces in `copy`, with zeros behind them (null: left where they are).
+dprc_status head_lay_w(HeadArgs& a, void* copy, hipStream_t stream) {
+  if (!copy) return DPRC_SUCCESS;
+  const int64_t ld = round_up(a.W.width, 8);
+  if (traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] { return launch_head_rows(a.W, a.bf16, nullptr, copy, ld, stream); }) != hipSuccess)
+    return DPRC_ERROR_HIP;
+  a.W.p = copy;
+  a.W.ld = ld;
+  a.vec_w = 1;
+  return DPRC_SUCCESS;
+}
+
+// h's rows laid out for the gradients, then f(the call that formed E) for every piece.
 template <class F>
 dprc_status head_pieces(const dprc_head& H, const HeadBufs& b, const float* lse, const float* g, hipStream_t stream, F&& f) {
   const HeadRows h{H.h, H.ldh, b.N, H.d};
@@ -1892,12 +1917,28 @@ dprc_status head_pieces(const dprc_head& H, const HeadBufs& b, const float* lse,
     HeadArgs a = head_args(H, head_rows(H, b), v0, nv);
     a.lse = lse; a.g = g;
     a.E = b.E; a.lde = b.lde; a.width = round_up(nv, 8);
+    dprc_status s = head_lay_w(a, b.W, stream);
+    if (s != DPRC_SUCCESS) return s;
     if (traced(DPRC_KERNEL_HEAD_ERRORS, stream, [&] { return launch_head_errors(a, stream); }) != hipSuccess)
       return DPRC_ERROR_HIP;
-    const dprc_status s = f(v0, nv);
-    if (s != DPRC_SUCCESS) return s;
+    if ((s = f(a)) != DPRC_SUCCESS) return s;
   }
   return DPRC_SUCCESS;
+}
+
+// Columns of a piece of the forward pass: all of them, or where W is laid out a piece at a time whole tiles of it.
+int64_t head_loss_piece(const dprc_head& H) {
+  if (!head_copies_w(H, 1)) return H.V;
+  return std::min(H.V, std::max<int64_t>(256, kHeadCopyBytes / (round_up(H.d, 8) * (int64_t)elem_bytes(H.dtype)) / 256 * 256));
+}
+
+// tiles of all pieces' sums, the same for every whole piece
+int64_t head_loss_tiles(const dprc_head& H) {
+  const int64_t N = H.B * H.T, piece = head_loss_piece(H);
+  const int bf16 = H.dtype == DPRC_BF16;
+  int64_t tiles = H.V / piece * head_sum_tiles(N, piece, bf16);
+  if (H.V % piece) tiles += head_sum_tiles(N, H.V % piece, bf16);
+  return tiles;
 }
 
 }  // namespace
@@ -1908,7 +1949,8 @@ size_t dprc_head_loss_workspace(const dprc_head* H) {
   if (check_head(H) != DPRC_SUCCESS) return 0;
   Arena ar(nullptr);
   if (!head_vec(*H, H->h, H->ldh)) ar.take<char>((size_t)(H->B * H->T * round_up(H->d, 8)) * elem_bytes(H->dtype));
-  ar.take<float2>((size_t)head_sum_tiles(H->B * H->T, H->V, H->dtype == DPRC_BF16) * H->B * H->T);
+  if (head_copies_w(*H, 1)) ar.take<char>((size_t)(head_loss_piece(*H) * round_up(H->d, 8)) * elem_bytes(H->dtype));
+  ar.take<float2>((size_t)head_loss_tiles(*H) * H->B * H->T);
   return ar.off;
 }
 
@@ -1930,10 +1972,20 @@ dprc_status dprc_head_loss(const dprc_head* H, float* loss, float* lse, void* ws
     h.p = rows;
     h.ld = ld;
   }
-  HeadArgs a = head_args(*H, h, 0, H->V);
-  a.part = ar.take<float2>((size_t)head_sum_tiles(a.N, a.nv, a.bf16) * a.N);
-  if (traced(DPRC_KERNEL_HEAD_SUMS, stream, [&] { return launch_head_sums(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
-  return hip_status(traced(DPRC_KERNEL_HEAD_JOIN, stream, [&] { return launch_head_join(a, loss, lse, stream); }));
+  const int64_t piece = head_loss_piece(*H), tiles = head_loss_tiles(*H);
+  void* copy = head_copies_w(*H, 1) ? ar.take<char>((size_t)(piece * round_up(H->d, 8)) * elem_bytes(H->dtype)) : nullptr;
+  float2* part = ar.take<float2>((size_t)tiles * h.rows);
+  HeadArgs all = head_args(*H, h, 0, H->V);
+  all.part = part;
+  for (int64_t v0 = 0; v0 < H->V; v0 += piece) {
+    HeadArgs a = head_args(*H, h, v0, std::min(piece, H->V - v0));
+    a.part = part;
+    const dprc_status s = head_lay_w(a, copy, stream);
+    if (s != DPRC_SUCCESS) return s;
+    if (traced(DPRC_KERNEL_HEAD_SUMS, stream, [&] { return launch_head_sums(a, stream); }) != hipSuccess) return DPRC_ERROR_HIP;
+    part += head_sum_tiles(a.N, a.nv, a.bf16) * a.N;
+  }
+  return hip_status(traced(DPRC_KERNEL_HEAD_JOIN, stream, [&] { return launch_head_join(all, tiles, loss, lse, stream); }));
 }
 
 size_t dprc_head_errors_workspace(const dprc_head* H) {
@@ -2006,7 +2058,8 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
     return hip_status(traced(DPRC_KERNEL_HEAD_ROWS, stream, [&] {
       return launch_head_round(planes, S, rows, H->d, bf16, out, ld, stream); }));
   };
-  st = head_pieces(*H, b, lse, g, stream, [&](int64_t v0, int64_t nv) -> dprc_status {
+  st = head_pieces(*H, b, lse, g, stream, [&](const HeadArgs& formed) -> dprc_status {
+    const int64_t v0 = formed.v0, nv = formed.nv;
     dprc_status s;
     if (norms) {
       s = head_blocks(*H, b, v0, nv, norms->layer_id, [&](const dprc_layer* L, int32_t n, int64_t c) {
@@ -2018,9 +2071,9 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
     if (dh) {                                          // (E's columns behind nv are zeros, and meet none of W's rows)
       HeadMulArgs a{};
       a.A = HeadRows{b.E, b.lde, b.N, round_up(nv, 8)};
-      a.B = head_args(*H, head_rows(*H, b), v0, nv).W;
+      a.B = formed.W;
       a.rows = b.N; a.cols = H->d; a.K = nv;
-      a.vec_b = head_vec(*H, H->W, H->ldw);
+      a.vec_b = formed.vec_w;
       a.add = v0 > 0;
       a.planes = b.dh_planes;
       if (!b.dh_planes) { a.out = dh; a.ldo = lddh; }
@@ -2061,9 +2114,9 @@ dprc_status dprc_head_clip_accumulate(const dprc_head* H, const float* lse, cons
   if (ws_bytes < head_layout(*H, false, false, true, nullptr, nullptr, b)) return DPRC_ERROR_WORKSPACE_TOO_SMALL;
   if (!ws || !aligned(ws, kAlign)) return DPRC_ERROR_INVALID_VALUE;
   head_layout(*H, false, false, true, nullptr, ws, b);
-  return head_pieces(*H, b, lse, g, stream, [&](int64_t v0, int64_t nv) {
-    const dprc_layer L = head_layer(*H, b, 0, nv, 0);
-    return dprc_clip_accumulate(&L, c, grad + v0, ldg, accumulate, b.acc, b.acc_bytes, stream);
+  return head_pieces(*H, b, lse, g, stream, [&](const HeadArgs& formed) {
+    const dprc_layer L = head_layer(*H, b, 0, formed.nv, 0);
+    return dprc_clip_accumulate(&L, c, grad + formed.v0, ldg, accumulate, b.acc, b.acc_bytes, stream);
   });
 }
 

@@ -695,8 +695,7 @@ hipError_t launch_head_errors(HeadArgs a, hipStream_t st) {
   return launch_head_logits<true>(a, st);
 }
 
-hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st) {
-  const int64_t tiles = head_sum_tiles(a.N, a.nv, a.bf16);
+hipError_t launch_head_join(const HeadArgs& a, int64_t tiles, float* loss, float* lse, hipStream_t st) {
   auto go = [&](auto kernel, int tpb) { DPRC_LAUNCH(kernel, flat_grid(ceil_div(a.N, tpb)), dim3(1024), 0, st, a, tiles, loss, lse); };
   if (a.N <= 1024) {
     if (a.bf16) go(head_join_kernel<uint16_t, 4>, 4);

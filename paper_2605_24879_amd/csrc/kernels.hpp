@@ -478,7 +478,8 @@ struct HeadArgs {
 int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16);
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st);
 hipError_t launch_head_errors(HeadArgs a, hipStream_t st);
-hipError_t launch_head_join(const HeadArgs& a, float* loss, float* lse, hipStream_t st);   // nv = V, v0 = 0
+// tiles: of all the calls that wrote part; nv = V, v0 = 0
+hipError_t launch_head_join(const HeadArgs& a, int64_t tiles, float* loss, float* lse, hipStream_t st);
 
 // A B with rows of B along the result's: E W (akr = 0: A [rows][K]) or E^T h (akr = 1: A [K][rows]).  The sums of S splits
 // of K to planes[S][rows][cols] (=|+=), or with S = 1 rounded to out.

@@ -153,6 +153,23 @@ def test_pieces(D, V, piece, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_weights_laid_out_in_pieces(D, dtype):
+    """Rows of W off the 16-byte boundaries and enough tokens for a copy of them: as with aligned rows."""
+    T, V, d = 1100, 9000, 131
+    h, W, target, g = make(1, T, d, V, dtype, seed=12, wpad=3)
+    check_backward(D, h, W, target, g, dtype, piece=8192)
+    hz, Wz = (torch.nn.functional.pad(x, (0, 5)) for x in (h, W))
+    for a, b in zip(D.dprc_head_loss(h, W, target), D.dprc_head_loss(hz, Wz, target)):
+        torch.testing.assert_close(a, b, rtol=1e-6, atol=1e-6)
+    # more than a piece of the forward pass: 2^28 bytes of W
+    d, V = 4093, 37000 if dtype == "bf16" else 17000
+    h, W, target, g = make(1, 1024, d, V, dtype, seed=13)
+    hz, Wz = (torch.nn.functional.pad(x, (0, 3)) for x in (h, W))
+    for a, b in zip(D.dprc_head_loss(h, W, target), D.dprc_head_loss(hz, Wz, target)):
+        torch.testing.assert_close(a, b, rtol=1e-6, atol=1e-6)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_large_logits(D, dtype):
     """Probabilities of 1 and of 0: logits of hundreds."""
     h, W, target, g = make(2, 70, 64, 500, dtype, seed=5, scale=300.0)
