@@ -1798,6 +1798,7 @@ bool head_copies_w(const dprc_head& H, int products) {
 struct HeadBufs {
   int64_t N, piece, lde, ldc;          // tokens; columns of a piece; row strides of E and of h's copy
   void* rows;                          // h laid out [N][ldc]
+  float* lo;                           // [N], for dh and dW of bf16 heads
   void* W;                             // a piece of W laid out [piece][ldc]; null: W itself
   void* E;                             // [N][lde]
   HeadMulPlan dh;
@@ -1848,6 +1849,7 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
   b.ldc = round_up(H.d, 8);
   b.rows = ar.take<char>((size_t)(b.N * b.ldc) * e);
   b.E = ar.take<char>((size_t)(b.N * b.lde) * e);
+  if (H.dtype == DPRC_BF16 && (dh || dW)) b.lo = ar.take<float>((size_t)b.N);
   if (head_copies_w(H, dh ? 2 : 1)) b.W = ar.take<char>((size_t)(b.piece * b.ldc) * e);
   // buffers of a shape to ask for sizes with: only their alignment counts
   HeadBufs probe = b;
@@ -1917,6 +1919,7 @@ dprc_status head_pieces(const dprc_head& H, const HeadBufs& b, const float* lse,
     HeadArgs a = head_args(H, head_rows(H, b), v0, nv);
     a.lse = lse; a.g = g;
     a.E = b.E; a.lde = b.lde; a.width = round_up(nv, 8);
+    a.lo = b.lo;
     dprc_status s = head_lay_w(a, b.W, stream);
     if (s != DPRC_SUCCESS) return s;
     if (traced(DPRC_KERNEL_HEAD_ERRORS, stream, [&] { return launch_head_errors(a, stream); }) != hipSuccess)
@@ -2050,7 +2053,8 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
   head_layout(*H, dh, dW, false, norms, ws, b);
   const int bf16 = H->dtype == DPRC_BF16;
   // a product's sums in planes, or with one split of all of them in the result; then the planes rounded
-  auto multiply = [&](HeadMulArgs& a, const HeadMulPlan& plan, int kind) -> dprc_status {
+  auto multiply = [&](HeadMulArgs& a, const HeadMulPlan& plan, int64_t v0, int kind) -> dprc_status {
+    a.lo = b.lo; a.target = H->target; a.v0 = v0;
     a.per_split = plan.per_split; a.S = plan.S; a.side = plan.side; a.bf16 = bf16;
     return hip_status(traced(kind, stream, [&] { return launch_head_mul(a, stream); }));
   };
@@ -2077,7 +2081,7 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
       a.add = v0 > 0;
       a.planes = b.dh_planes;
       if (!b.dh_planes) { a.out = dh; a.ldo = lddh; }
-      if ((s = multiply(a, v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16), DPRC_KERNEL_HEAD_BACK)) != DPRC_SUCCESS) return s;
+      if ((s = multiply(a, v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16), v0, DPRC_KERNEL_HEAD_BACK)) != DPRC_SUCCESS) return s;
     }
     if (dW) {
       const HeadMulPlan plan = head_mul_plan(nv, H->d, b.N, bf16);
@@ -2089,7 +2093,7 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
       a.akr = 1; a.vec_b = 1;
       a.planes = b.dW_planes;
       if (plan.S == 1) { a.out = out; a.ldo = lddw; }
-      if ((s = multiply(a, plan, DPRC_KERNEL_HEAD_WEIGHT)) != DPRC_SUCCESS) return s;
+      if ((s = multiply(a, plan, v0, DPRC_KERNEL_HEAD_WEIGHT)) != DPRC_SUCCESS) return s;
       if (plan.S > 1 && (s = round(b.dW_planes, plan.S, nv, out, lddw)) != DPRC_SUCCESS) return s;
     }
     return DPRC_SUCCESS;

@@ -416,8 +416,12 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
     if (at >= 0 && ((at >> 2) & 1) == (lane >> 5)) {     // exp(x) - 1 without cancellation
       const float e = g * expm1f(own - lse);
       E* o = stage.piece(col, (v0 + at) / EP) + (at & (EP - 1));
-      if constexpr (sizeof(E) == 2) *o = __builtin_bit_cast(uint16_t, (__bf16)e);
-      else *o = e;
+      if constexpr (sizeof(E) == 2) {
+        *o = __builtin_bit_cast(uint16_t, (__bf16)e);
+        if (a.lo && t0 + col < a.N) a.lo[t0 + col] = e - (float)(__bf16)e;
+      } else {
+        *o = e;
+      }
     }
   }
   __syncthreads();
@@ -445,6 +449,108 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
         }
       }
       to += ROWS * a.lde;
+    }
+  }
+}
+
+// ---- the target's entries to 16 bits ---------------------------------------------------------------
+// E_t,y(t) = g_t (p - 1) is by far the largest entry of most rows, and tokens of one sample share g: its rounding
+// to bf16 would be an error of up to 2^-9 of dh_t, and of a row of dW alike, in one direction for whole samples (an
+// error of 0.0022 to 0.0028 of all of dh and dW where the results' own rounding is 0.0017).  What it loses, lo_t, joins
+// the products as slabs of their own, formed in LDS:
+//   dh:  64 tokens of the tile at a time, A their diagonal of lo_t, B the rows W_y(t);
+//   dW:  up to 64 tokens whose target is among the tile's rows, in their order, A one lo_t in every row, B the
+//        rows h_t.
+template <class TL, bool AKR>
+__device__ __forceinline__ void head_targets(const HeadMulArgs& a, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
+                                             f32x16_t (&acc)[TL::XB][TL::YB], uint16_t* la0, uint16_t* la1, uint16_t* lb0) {
+  constexpr int TH = TL::threads, NW = TH / 64, PA = TL::MT * 8 / TH, PB = TL::NT * 8 / TH, RP = TL::NT / 8;
+  typedef HeadOperand<TL, TL::MT, AKR, true> OA;
+  typedef HeadOperand<TL, TL::NT, true, true> OB;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  // A's slab: the k-th entry, zero where there is none, at row `row` of the tile; B's: row(k) of the operand
+  auto slab = [&](auto row_of, bool in, int row, float lo) __attribute__((always_inline)) {
+#pragma unroll
+    for (int r = 0; r < PA; ++r) *reinterpret_cast<uint4*>(&la0[8 * (tid + TH * r)]) = uint4{0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < PB; ++r) {
+      const int s = tid + TH * r;
+      const int64_t from = row_of(s / RP);
+      *reinterpret_cast<uint4*>(&lb0[8 * s]) = from < 0 ? uint4{0, 0, 0, 0} : operand_piece<uint16_t>(a.B, from, n0 + OB::kr_col(s));
+    }
+    __syncthreads();
+    if (in) {                                           // (at most the first 64 threads)
+      const int at = AKR ? tid * TL::MT + 8 * ((row >> 3) ^ swizzle_kr<uint16_t>(tid, TL::MT / 8)) + (row & 7)
+                         : row * TL::slab + 8 * ((tid >> 3) ^ (row & 7)) + (tid & 7);
+      la0[at] = __builtin_bit_cast(uint16_t, (__bf16)lo);
+    }
+    __syncthreads();
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) {
+      uint4 av[TL::XB], bv[TL::YB];
+#pragma unroll
+      for (int y = 0; y < TL::YB; ++y) bv[y] = OB::frag(lb0, 32 * (wn * TL::YB + y), ks, lane);
+#pragma unroll
+      for (int x = 0; x < TL::XB; ++x) av[x] = OA::frag(la0, 32 * (wm * TL::XB + x), ks, lane);
+      head_mfma<uint16_t, TL::XB, TL::YB>(av, bv, acc);
+    }
+    __syncthreads();
+  };
+  if constexpr (!AKR) {
+    auto place = [&](int64_t t) __attribute__((always_inline)) {   // the target's row of B, or -1
+      const int64_t y = t < a.rows ? a.target[t] - a.v0 : -1;
+      return y < a.B.rows ? y : (int64_t)-1;
+    };
+    for (int j = 0; j < TL::MT && m0 + j < a.rows; j += 64) {
+      const int64_t t = m0 + j + tid;
+      const bool in = tid < 64 && place(t) >= 0;
+      slab([&](int k) __attribute__((always_inline)) { return place(m0 + j + k); }, in, j + tid, in ? a.lo[t] : 0.f);
+    }
+  } else {
+    constexpr int R = 4;                                // targets a thread looks at in a round
+    int* list = reinterpret_cast<int*>(la1);            // tokens, and their rows of the tile
+    uint8_t* rows = reinterpret_cast<uint8_t*>(list + R * TH + 64);
+    int* counts = reinterpret_cast<int*>(rows + R * TH + 64);
+    static_assert(5 * (R * TH + 64) + 4 * R * NW <= 128 * TL::MT && TL::MT <= 256);
+    int n = 0;
+    for (int64_t base = k0; base < k1; base += R * TH) {
+      int64_t row[R];
+      uint64_t mask[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        const int64_t t = base + r * TH + tid;
+        row[r] = t < k1 ? a.target[t] - a.v0 - m0 : -1;
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        mask[r] = __ballot(row[r] >= 0 && row[r] < TL::MT && m0 + row[r] < a.rows);
+        if (lane == 0) counts[r * NW + wv] = __popcll(mask[r]);
+      }
+      __syncthreads();
+      int before[R], total = n;
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        for (int w = 0; w < NW; ++w) {
+          if (w == wv) before[r] = total;
+          total += counts[r * NW + w];
+        }
+#pragma unroll
+      for (int r = 0; r < R; ++r)
+        if (mask[r] >> lane & 1) {
+          const int at = before[r] + __popcll(mask[r] & (((uint64_t)1 << lane) - 1));
+          list[at] = (int)(base + r * TH + tid);
+          rows[at] = (uint8_t)row[r];
+        }
+      __syncthreads();
+      n = total;
+      if (n < 64 && base + R * TH < k1) continue;       // (the same for all threads)
+      for (int g = 0; g < n; g += 64) {
+        const bool in = tid < 64 && g + tid < n;
+        const int own = in ? list[g + tid] : 0;
+        slab([&](int k) __attribute__((always_inline)) { return g + k < n ? (int64_t)list[g + k] : (int64_t)-1; }, in,
+             in ? rows[g + tid] : 0, in ? a.lo[own] : 0.f);
+      }
+      n = 0;
     }
   }
 }
@@ -525,6 +631,8 @@ __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
   f32x16_t acc[TL::XB][TL::YB];
   head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
                    HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
+  if constexpr (sizeof(typename TL::elem) == 2)
+    if (AKR || k0 == 0) head_targets<TL, AKR>(a, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
   head_store<TL>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, acc);
 }
 

@@ -474,6 +474,7 @@ struct HeadArgs {
   void* E;                 // errors: [N][lde], columns v0 .. v0 + width
   int64_t lde, width;      // width >= nv: the columns past nv are zeros
   int32_t stream;          // errors: past the caches (set by the launcher)
+  float* lo;               // errors, bf16: [N] what the rounding of the target's entry lost (may be null)
 };
 int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16);
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st);
@@ -490,6 +491,9 @@ struct HeadMulArgs {
   float* planes;
   void* out;               // null: planes
   int64_t ldo;
+  const float* lo;         // bf16: [tokens] what the target's entries of E lack
+  const int64_t* target;   // bf16: [tokens]
+  int64_t v0;              // the piece's first column
 };
 struct HeadMulPlan {
   int64_t per_split;

@@ -152,6 +152,32 @@ def test_pieces(D, V, piece, dtype):
     check_backward(D, h, W, target, g, dtype, piece=piece)
 
 
+@pytest.mark.parametrize("B,T,d,V,wpad,piece", [(1, 1, 64, 300, 0, 0), (2, 77, 72, 1000, 0, 0), (2, 77, 72, 1000, 3, 0),
+                                                (1, 700, 264, 20000, 0, 8192), (1, 300, 136, 9000, 0, 0), (4, 600, 520, 600, 0, 0)])
+def test_the_targets_entry_enters_to_16_bits(D, B, T, d, V, wpad, piece):
+    """bf16: of the target's entry of E no more is lost than 2^-17 (the second half of its split is rounded to bf16: 2^-8 of
+    at most 2^-8 of it, halved), where the others are off by r: with one g for all tokens whose rounding is the worst
+    there is, dh and dW are off by the rounding of the result and the others' share."""
+    h, W, target, _ = make(B, T, d, V, "bf16", seed=V, wpad=wpad)
+    target[0, T // 2:] = int(target[0, 0])                  # one target many times over
+    g = torch.full((B, T), 1.0 + 2.0 ** -8, device="cuda")
+    lse = D.dprc_head_loss(h, W, target)[1]
+    hn, Wn, tn, zn = f64(h), f64(W), target.cpu().numpy(), f64(lse)
+    E = O.errors(hn, Wn, tn, zn, f64(g))
+    kept = (tn >= 0)[..., None]
+    tE = R["bf16"] * np.abs(E)
+    at = np.maximum(tn, 0)[..., None]
+    np.put_along_axis(tE, at, 2.0 ** -17 * np.take_along_axis(np.abs(E), at, -1), -1)
+    tE = np.where(kept, tE + 2 * np.where(kept, np.exp(hn @ Wn.T - zn[..., None]), 0) * (exponent(hn, Wn, zn)[..., None] + 8 * U)
+                  + 16 * U * np.abs(E), 0.0)
+    dh, dW = D.dprc_head_backward(h, W, target, lse, g, piece=piece)
+    ref = E @ Wn
+    within(dh, ref, (1 + R["bf16"]) * tE @ np.abs(Wn) + (V + 64) * U * np.abs(E) @ np.abs(Wn) + R["bf16"] * np.abs(ref), "dh")
+    Ef, tf, hf = E.reshape(B * T, V), tE.reshape(B * T, V), np.where(kept, hn, 0.0).reshape(B * T, d)
+    ref = Ef.T @ hf
+    within(dW, ref, (1 + R["bf16"]) * tf.T @ np.abs(hf) + (B * T + 64) * U * np.abs(Ef).T @ np.abs(hf) + R["bf16"] * np.abs(ref), "dW")
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_weights_laid_out_in_pieces(D, dtype):
     """Rows of W off the 16-byte boundaries and enough tokens for a copy of them: as with aligned rows."""
