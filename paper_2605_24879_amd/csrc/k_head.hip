@@ -461,8 +461,8 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
 //   dh:  64 tokens of the tile at a time, A their diagonal of lo_t, B the rows W_y(t);
 //   dW:  up to 64 tokens whose target is among the tile's rows, in their order, A one lo_t in every row, B the
 //        rows h_t.
-template <class TL, bool AKR>
-__device__ __forceinline__ void head_targets(const HeadMulArgs& a, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
+template <class TL, bool AKR, bool VB>
+__device__ __forceinline__ void head_targets(const HeadMulArgs& a, int split, int64_t m0, int64_t n0, int64_t k0, int64_t k1,
                                              f32x16_t (&acc)[TL::XB][TL::YB], uint16_t* la0, uint16_t* la1, uint16_t* lb0) {
   constexpr int TH = TL::threads, NW = TH / 64, PA = TL::MT * 8 / TH, PB = TL::NT * 8 / TH, RP = TL::NT / 8;
   typedef HeadOperand<TL, TL::MT, AKR, true> OA;
@@ -470,14 +470,20 @@ __device__ __forceinline__ void head_targets(const HeadMulArgs& a, int64_t m0, i
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
   // A's slab: the k-th entry, zero where there is none, at row `row` of the tile; B's: row(k) of the operand
   auto slab = [&](auto row_of, bool in, int row, float lo) __attribute__((always_inline)) {
+    uint4 v[PB];
+    bool there[PB];
+#pragma unroll
+    for (int r = 0; r < PB; ++r) {                      // all loads first: whole pieces (VB) need no condition
+      const int s = tid + TH * r;
+      const int64_t from = row_of(s / RP), col = n0 + OB::kr_col(s);
+      there[r] = from >= 0 && col < a.B.width;
+      if constexpr (VB) v[r] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(a.B.p) + (there[r] ? from * a.B.ld + col : 0));
+      else v[r] = there[r] ? operand_piece<uint16_t>(a.B, from, col) : uint4{0, 0, 0, 0};
+    }
 #pragma unroll
     for (int r = 0; r < PA; ++r) *reinterpret_cast<uint4*>(&la0[8 * (tid + TH * r)]) = uint4{0, 0, 0, 0};
 #pragma unroll
-    for (int r = 0; r < PB; ++r) {
-      const int s = tid + TH * r;
-      const int64_t from = row_of(s / RP);
-      *reinterpret_cast<uint4*>(&lb0[8 * s]) = from < 0 ? uint4{0, 0, 0, 0} : operand_piece<uint16_t>(a.B, from, n0 + OB::kr_col(s));
-    }
+    for (int r = 0; r < PB; ++r) *reinterpret_cast<uint4*>(&lb0[8 * (tid + TH * r)]) = select4(there[r], v[r], uint4{0, 0, 0, 0});
     __syncthreads();
     if (in) {                                           // (at most the first 64 threads)
       const int at = AKR ? tid * TL::MT + 8 * ((row >> 3) ^ swizzle_kr<uint16_t>(tid, TL::MT / 8)) + (row & 7)
@@ -498,10 +504,10 @@ __device__ __forceinline__ void head_targets(const HeadMulArgs& a, int64_t m0, i
   };
   if constexpr (!AKR) {
     auto place = [&](int64_t t) __attribute__((always_inline)) {   // the target's row of B, or -1
-      const int64_t y = t < a.rows ? a.target[t] - a.v0 : -1;
-      return y < a.B.rows ? y : (int64_t)-1;
+      const int64_t y = a.target[min(t, a.rows - 1)] - a.v0;
+      return t < a.rows && y < a.B.rows ? y : (int64_t)-1;
     };
-    for (int j = 0; j < TL::MT && m0 + j < a.rows; j += 64) {
+    for (int j = 64 * split; j < TL::MT && m0 + j < a.rows; j += 64 * a.S) {   // dealt to the splits
       const int64_t t = m0 + j + tid;
       const bool in = tid < 64 && place(t) >= 0;
       slab([&](int k) __attribute__((always_inline)) { return place(m0 + j + k); }, in, j + tid, in ? a.lo[t] : 0.f);
@@ -632,7 +638,7 @@ __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
   head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
                    HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
   if constexpr (sizeof(typename TL::elem) == 2)
-    if (AKR || k0 == 0) head_targets<TL, AKR>(a, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
+    head_targets<TL, AKR, VB>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
   head_store<TL>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, acc);
 }
 
