@@ -432,7 +432,7 @@ dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t cou
  * finite gives c = 0: zeros, as dprc_clip_scale does for such a sample.  Each tensor is rows x cols
  * elements of its own dtype, rows ldx apart, to out (row stride ldo, may be x with ldo = ldx; NULL in
  * dprc_grad_norm); outputs overlap nothing else.  A tensor may be empty (rows or cols 0).  The array is HOST
- * memory, read during the call.  max_norm > 0 and finite; rows and cols <= 2^40.  Workspace:
+ * memory, read during the call.  max_norm > 0 and finite; rows, cols and rows * cols <= 2^40.  Workspace:
  * dprc_grad_norm_workspace() bytes. */
 typedef struct {
   const void* x;

@@ -2158,7 +2158,16 @@ dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t cou
 
 namespace {
 
-constexpr int64_t kGradBlocks = 2048;       // workgroups, and parts of the sum, of a call
+constexpr int64_t kGradBlocks = 1024;       // workgroups, and parts of the sum, of a call
+constexpr int64_t kGradSmall = 1 << 14;     // elements that one workgroup clips (79047 take 19 us so, 13 in two launches)
+constexpr int64_t kGradStream = (int64_t)300 << 20;   // bytes of tensors from which on they go past the caches
+constexpr int64_t kGradKeep = 3000;         // chunks at a launch's end that do not (188 MiB of fp32: 243 million values 500 us; 0, 1000, 2048: 514, 514, 505)
+
+int64_t grad_bytes(const dprc_tensor* t, int32_t count) {
+  int64_t n = 0;
+  for (int32_t i = 0; i < count; ++i) n += t[i].rows * t[i].cols * (int64_t)elem_bytes(t[i].dtype);
+  return n;
+}
 
 dprc_status check_tensors(const dprc_tensor* t, int32_t count, bool out) {
   if (count < 0 || (count > 0 && !t)) return DPRC_ERROR_INVALID_VALUE;
@@ -2171,6 +2180,7 @@ dprc_status check_tensors(const dprc_tensor* t, int32_t count, bool out) {
   }
   for (int32_t i = 0; i < count; ++i) {
     const size_t e = elem_bytes(t[i].dtype);
+    if (t[i].cols > 0 && t[i].rows > (1LL << 40) / t[i].cols) return DPRC_ERROR_NOT_SUPPORTED;
     if (t[i].rows > (1LL << 40) || t[i].cols > (1LL << 40) ||
         (t[i].rows && t[i].cols && (!aligned(t[i].x, e) || (out && !aligned(t[i].out, e)))))
       return DPRC_ERROR_NOT_SUPPORTED;
@@ -2184,6 +2194,7 @@ dprc_status grad_launches(const dprc_tensor* t, int32_t count, GradArgs& a, F&& 
   int64_t filled = 0;
   for (int32_t i = 0; i < count; ++i) filled += t[i].rows > 0 && t[i].cols > 0;
   const int64_t launches = ceil_div(filled, kGradTensors);
+  const bool past = grad_bytes(t, count) > kGradStream;
   int32_t part0 = 0;
   for (int32_t i = 0; i < count;) {
     a.count = 0;
@@ -2203,6 +2214,7 @@ dprc_status grad_launches(const dprc_tensor* t, int32_t count, GradArgs& a, F&& 
     }
     if (a.count == 0) break;
     a.blocks = (int32_t)std::min<int64_t>(a.chunks, std::max<int64_t>(64, kGradBlocks / launches));
+    a.keep = past ? std::max<int64_t>(1, a.chunks - kGradKeep) : 0;
     a.part0 = part0;
     part0 += a.blocks;
     const dprc_status s = f(a);
@@ -2264,7 +2276,17 @@ dprc_status dprc_grad_clip(const dprc_tensor* tensors, int32_t count, float max_
   a.part = static_cast<double*>(ws);
   a.parts = grad_parts(tensors, count);
   a.max_norm = (double)max_norm;
-  dprc_status s = grad_squares(tensors, count, a, stream);
+  int64_t elements = 0, launches = 0;
+  dprc_status s = grad_launches(tensors, count, a, [&](const GradArgs& g) {
+    for (int32_t i = 0; i < g.count; ++i) elements += g.t[i].rows * g.t[i].cols;
+    ++launches;
+    return DPRC_SUCCESS;
+  });
+  if (launches == 1 && elements <= kGradSmall) {
+    a.norm = norm;
+    return hip_status(traced(DPRC_KERNEL_GRAD_SCALE, stream, [&] { return launch_grad_small(a, stream); }));
+  }
+  s = grad_squares(tensors, count, a, stream);
   if (s != DPRC_SUCCESS) return s;
   if (a.parts == 0) {                                 // nothing but the norm, 0
     a.norm = norm;

@@ -35,15 +35,28 @@ __device__ __forceinline__ GradChunk grad_chunk(const GradArgs& a, int64_t c) {
   return k;
 }
 
+// Threads of a row of n columns: all of the workgroup, or a power of two of them with a piece each.
 template <class E>
-__device__ __forceinline__ double row_squares(const E* row, int64_t n, double t) {
-  constexpr int EP = kPiece<E>;
-  constexpr int U = 4;
-  int64_t c = EP * threadIdx.x;
-  for (; c + (U - 1) * EP * 256 + EP <= n; c += U * EP * 256) {
+__device__ __forceinline__ int grad_tpr(int64_t n, int threads) {
+  int tpr = 1;
+  while (tpr < threads && tpr * kPiece<E> < n) tpr *= 2;
+  return tpr;
+}
+
+__device__ __forceinline__ double get64(uint16_t x) { return (double)bf16_to_f32(x); }
+__device__ __forceinline__ double get64(float x) { return (double)x; }
+
+constexpr int kGradUnroll = 4;      // pieces loaded before the first is worked on
+
+template <class E, bool NT>
+__device__ __forceinline__ double row_squares(const E* row, int64_t n, int lane, int tpr, double t) {
+  constexpr int EP = kPiece<E>, U = kGradUnroll;
+  const int64_t step = (int64_t)EP * tpr;
+  int64_t c = (int64_t)EP * lane;
+  for (; c + (U - 1) * step + EP <= n; c += U * step) {
     uint4 v[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) v[u] = load_piece<E>(row + c + u * EP * 256);
+    for (int u = 0; u < U; ++u) v[u] = load_piece<E, NT>(row + c + u * step);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       float x[EP];
@@ -52,43 +65,49 @@ __device__ __forceinline__ double row_squares(const E* row, int64_t n, double t)
       for (int j = 0; j < EP; ++j) t = fma((double)x[j], (double)x[j], t);
     }
   }
-  for (; c < n; c += EP * 256) {
+  for (; c < n; c += step) {
     if (c + EP <= n) {
       float x[EP];
       unpack<E>(load_piece<E>(row + c), x);
 #pragma unroll
       for (int j = 0; j < EP; ++j) t = fma((double)x[j], (double)x[j], t);
     } else {
-      for (int64_t j = c; j < n; ++j) {
-        const double x = sizeof(E) == 2 ? (double)bf16_to_f32((uint32_t)row[j]) : (double)row[j];
-        t = fma(x, x, t);
-      }
+      for (int64_t j = c; j < n; ++j) t = fma(get64(row[j]), get64(row[j]), t);
     }
   }
   return t;
 }
 
+template <class E, bool NT>
+__device__ __forceinline__ double chunk_squares(const GradTensor& g, const GradChunk& k, int threads, double t) {
+  const int tpr = grad_tpr<E>(k.cols, threads), lane = threadIdx.x & (tpr - 1);
+  for (int64_t r = threadIdx.x / tpr; r < k.rows; r += threads / tpr)
+    t = row_squares<E, NT>((const E*)g.x + (k.row + r) * g.ldx + k.col, k.cols, lane, tpr, t);
+  return t;
+}
+
+template <int WAVES>
 __device__ __forceinline__ double block_sum(double t) {
-  __shared__ double buf[4];
+  __shared__ double buf[WAVES];
   t = wave_sum(t);
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = t;
   __syncthreads();
-  t = buf[0] + buf[1] + buf[2] + buf[3];
+  t = 0.0;
+  for (int w = 0; w < WAVES; ++w) t += buf[w];
   __syncthreads();
   return t;
 }
 
+// Chunks before a.keep are read past the caches, which then hold the last ones when the scaling begins.
 __global__ __launch_bounds__(256) void grad_squares_kernel(GradArgs a) {
   double t = 0.0;
   for (int64_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
     const GradChunk k = grad_chunk(a, c);
     const GradTensor& g = a.t[k.tensor];
-    for (int64_t r = k.row; r < k.row + k.rows; ++r) {
-      if (g.bf16) t = row_squares<uint16_t>((const uint16_t*)g.x + r * g.ldx + k.col, k.cols, t);
-      else t = row_squares<float>((const float*)g.x + r * g.ldx + k.col, k.cols, t);
-    }
+    if (c < a.keep) t = g.bf16 ? chunk_squares<uint16_t, true>(g, k, 256, t) : chunk_squares<float, true>(g, k, 256, t);
+    else t = g.bf16 ? chunk_squares<uint16_t, false>(g, k, 256, t) : chunk_squares<float, false>(g, k, 256, t);
   }
-  t = block_sum(t);
+  t = block_sum<4>(t);
   if (threadIdx.x == 0) a.part[a.part0 + blockIdx.x] = t;
 }
 
@@ -96,7 +115,7 @@ __global__ __launch_bounds__(256) void grad_squares_kernel(GradArgs a) {
 __device__ __forceinline__ double grad_total(const GradArgs& a) {
   double t = 0.0;
   for (int k = threadIdx.x; k < a.parts; k += 256) t += a.part[k];
-  return block_sum(t);
+  return block_sum<4>(t);
 }
 
 __global__ __launch_bounds__(256) void grad_norm_kernel(GradArgs a) {
@@ -104,40 +123,105 @@ __global__ __launch_bounds__(256) void grad_norm_kernel(GradArgs a) {
   if (threadIdx.x == 0) *a.norm = (float)sqrt(t);
 }
 
-// c x to out, the factor and the product in fp64 (a factor of fp32 could be subnormal where x is large).
-// Nothing is read where c = 0 (a norm that is not finite), so that no NaN survives.
-template <class E>
-__device__ __forceinline__ void scale_row(const E* x, E* out, int64_t n, double c) {
-  constexpr int EP = kPiece<E>;
-  for (int64_t k = EP * threadIdx.x; k < n; k += EP * 256) {
-    if (k + EP <= n) {
-      float v[EP] = {};
-      if (c != 0.0) unpack<E>(load_piece<E>(x + k), v);
+// min(1, max_norm / norm), 0 for a norm that is not finite
+__device__ __forceinline__ double grad_factor(const GradArgs& a, double norm) {
+  return !(norm <= 1.7976931348623157e308) ? 0.0 : norm <= a.max_norm ? 1.0 : a.max_norm / norm;
+}
+
+// c x to out in fp32, or with WIDE in fp64: for a factor that fp32 holds in fewer bits, or not at all.
+template <class E, bool NT, bool WIDE>
+__device__ __forceinline__ void scale_row(const E* x, E* out, int64_t n, int lane, int tpr, double c) {
+  constexpr int EP = kPiece<E>, U = kGradUnroll;
+  const int64_t step = (int64_t)EP * tpr;
+  const float cf = (float)c;
+  auto times = [&](float v) __attribute__((always_inline)) { return WIDE ? (float)((double)v * c) : v * cf; };
+  int64_t k = (int64_t)EP * lane;
+  for (; k + (U - 1) * step + EP <= n; k += U * step) {
+    uint4 v[U];
 #pragma unroll
-      for (int j = 0; j < EP; ++j) v[j] = (float)((double)v[j] * c);
-      store_piece<E>(out + k, pack<E>(v));
+    for (int u = 0; u < U; ++u) v[u] = load_piece<E, NT>(x + k + u * step);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      float y[EP];
+      unpack<E>(v[u], y);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) y[j] = times(y[j]);
+      store_piece<E, NT>(out + k + u * step, pack<E>(y));
+    }
+  }
+  for (; k < n; k += step) {
+    if (k + EP <= n) {
+      float y[EP];
+      unpack<E>(load_piece<E>(x + k), y);
+#pragma unroll
+      for (int j = 0; j < EP; ++j) y[j] = times(y[j]);
+      store_piece<E>(out + k, pack<E>(y));
     } else {
       for (int64_t j = k; j < n; ++j) {
-        if constexpr (sizeof(E) == 2)
-          out[j] = c != 0.0 ? __builtin_bit_cast(uint16_t, (__bf16)(float)((double)bf16_to_f32(x[j]) * c)) : 0;
-        else out[j] = c != 0.0 ? (float)((double)x[j] * c) : 0.f;
+        const float y = times((float)get64(x[j]));
+        if constexpr (sizeof(E) == 2) out[j] = __builtin_bit_cast(uint16_t, (__bf16)y);
+        else out[j] = y;
       }
     }
   }
 }
 
+// Zeros for c = 0 (a norm that is not finite): nothing is read, so that no NaN survives.
+template <class E>
+__device__ __forceinline__ void zero_row(E* out, int64_t n, int lane, int tpr) {
+  constexpr int EP = kPiece<E>;
+  for (int64_t k = (int64_t)EP * lane; k < n; k += (int64_t)EP * tpr) {
+    if (k + EP <= n) store_piece<E>(out + k, uint4{0, 0, 0, 0});
+    else
+      for (int64_t j = k; j < n; ++j) out[j] = (E)0;
+  }
+}
+
+template <class E, bool NT>
+__device__ __forceinline__ void chunk_scale(const GradTensor& g, const GradChunk& k, int threads, double c) {
+  if (c == 1.0 && g.out == g.x) return;                  // its values already
+  const int tpr = grad_tpr<E>(k.cols, threads), lane = threadIdx.x & (tpr - 1);
+  for (int64_t r = threadIdx.x / tpr; r < k.rows; r += threads / tpr) {
+    const E* x = (const E*)g.x + (k.row + r) * g.ldx + k.col;
+    E* out = (E*)g.out + (k.row + r) * g.ldo + k.col;
+    if (c == 0.0) zero_row<E>(out, k.cols, lane, tpr);
+    else if (c < 0x1p-100) scale_row<E, NT, true>(x, out, k.cols, lane, tpr, c);
+    else scale_row<E, NT, false>(x, out, k.cols, lane, tpr, c);
+  }
+}
+
+// From the last chunk on: what the squares read last is still in the caches.
 __global__ __launch_bounds__(256) void grad_scale_kernel(GradArgs a) {
-  const double norm = sqrt(grad_total(a));
+  const double norm = sqrt(grad_total(a)), c = grad_factor(a, norm);
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;
-  const double c = !(norm <= 1.7976931348623157e308) ? 0.0 : norm <= a.max_norm ? 1.0 : a.max_norm / norm;
-  for (int64_t q = blockIdx.x; q < a.chunks; q += gridDim.x) {
+  for (int64_t q = a.chunks - 1 - blockIdx.x; q >= 0; q -= gridDim.x) {
     const GradChunk k = grad_chunk(a, q);
     const GradTensor& g = a.t[k.tensor];
-    if (c == 1.0 && g.out == g.x) continue;              // its values already
-    for (int64_t r = k.row; r < k.row + k.rows; ++r) {
-      if (g.bf16) scale_row<uint16_t>((const uint16_t*)g.x + r * g.ldx + k.col, (uint16_t*)g.out + r * g.ldo + k.col, k.cols, c);
-      else scale_row<float>((const float*)g.x + r * g.ldx + k.col, (float*)g.out + r * g.ldo + k.col, k.cols, c);
+    if (a.keep > 0) {
+      if (g.bf16) chunk_scale<uint16_t, true>(g, k, 256, c);
+      else chunk_scale<float, true>(g, k, 256, c);
+    } else {
+      if (g.bf16) chunk_scale<uint16_t, false>(g, k, 256, c);
+      else chunk_scale<float, false>(g, k, 256, c);
     }
+  }
+}
+
+// Few elements in all: one workgroup does both.
+__global__ __launch_bounds__(1024) void grad_small_kernel(GradArgs a) {
+  double t = 0.0;
+  for (int i = 0; i < a.count; ++i) {
+    const GradTensor& g = a.t[i];
+    const GradChunk k{i, 0, g.rows, 0, g.cols};
+    t = g.bf16 ? chunk_squares<uint16_t, false>(g, k, 1024, t) : chunk_squares<float, false>(g, k, 1024, t);
+  }
+  const double norm = sqrt(block_sum<16>(t)), c = grad_factor(a, norm);
+  if (a.norm && threadIdx.x == 0) *a.norm = (float)norm;
+  for (int i = 0; i < a.count; ++i) {
+    const GradTensor& g = a.t[i];
+    const GradChunk k{i, 0, g.rows, 0, g.cols};
+    if (g.bf16) chunk_scale<uint16_t, false>(g, k, 1024, c);
+    else chunk_scale<float, false>(g, k, 1024, c);
   }
 }
 
@@ -151,6 +235,10 @@ hipError_t launch_grad_norm(const GradArgs& a, hipStream_t st) {
 }
 hipError_t launch_grad_scale(const GradArgs& a, hipStream_t st) {
   DPRC_LAUNCH(grad_scale_kernel, dim3((unsigned)a.blocks), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+hipError_t launch_grad_small(const GradArgs& a, hipStream_t st) {
+  DPRC_LAUNCH(grad_small_kernel, dim3(1), dim3(1024), 0, st, a);
   return hipGetLastError();
 }
 

@@ -543,6 +543,7 @@ struct GradArgs {
   int64_t chunks;
   double* part;                      // [parts], this launch's from part0 on
   int32_t part0, parts;
+  int64_t keep;                      // the first chunk that is kept in the caches; 0: all are
   double max_norm;
   float* norm;                       // may be null
   GradTensor t[kGradTensors];
@@ -550,6 +551,7 @@ struct GradArgs {
 hipError_t launch_grad_squares(const GradArgs& a, hipStream_t st);
 hipError_t launch_grad_norm(const GradArgs& a, hipStream_t st);
 hipError_t launch_grad_scale(const GradArgs& a, hipStream_t st);
+hipError_t launch_grad_small(const GradArgs& a, hipStream_t st);   // all tensors of a call: squares and scale
 
 // Gaussian probe columns, column j at [j*ld .. j*ld + ld) (rows >= m zero);
 // any of hi/lo (both or neither) and f32 may be null.

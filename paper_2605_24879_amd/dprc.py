@@ -11,6 +11,7 @@ RuntimeError; there is no fallback.
 import array
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -60,25 +61,12 @@ class LN(ctypes.Structure):
                 ("p", ctypes.c_float), ("site_id", ctypes.c_uint32), ("seed", ctypes.c_uint64)]
 
 
-class HeadDesc(ctypes.Structure):
-    """Mirror of dprc_head."""
-    _fields_ = [("h", ctypes.c_void_p), ("W", ctypes.c_void_p), ("target", ctypes.c_void_p),
-                ("B", ctypes.c_int64), ("T", ctypes.c_int64), ("d", ctypes.c_int64), ("V", ctypes.c_int64),
-                ("ldh", ctypes.c_int64), ("ldw", ctypes.c_int64), ("dtype", ctypes.c_int), ("piece", ctypes.c_int64)]
-
-
-class HeadNorms(ctypes.Structure):
-    """Mirror of dprc_head_norms."""
-    _fields_ = [("k", ctypes.c_int32), ("probe", ctypes.c_int), ("seed", ctypes.c_uint64), ("side", ctypes.c_int),
-                ("layer_id", ctypes.c_uint32), ("n2", ctypes.c_void_p), ("accumulate", ctypes.c_int32)]
-
-
-class Rope(ctypes.Structure):
-    """Mirror of dprc_rope."""
-    _fields_ = [("B", ctypes.c_int64), ("T", ctypes.c_int64), ("D", ctypes.c_int32), ("r", ctypes.c_int32),
-                ("freqs", ctypes.c_void_p), ("pos", ctypes.c_void_p), ("start", ctypes.c_int64),
-                ("scale", ctypes.c_float), ("interleaved", ctypes.c_int32), ("inverse", ctypes.c_int32),
-                ("xdtype", ctypes.c_int), ("ydtype", ctypes.c_int)]
+# dprc_head, dprc_head_norms, dprc_rope and dprc_tensor as they lie in memory (packing them takes a fifth of
+# building a ctypes structure)
+HEAD = struct.Struct("=9qi4xq")          # h, W, target, B, T, d, V, ldh, ldw, dtype, piece
+HEAD_NORMS = struct.Struct("=iiQiIqi4x")  # k, probe, seed, side, layer_id, n2, accumulate
+ROPE = struct.Struct("=qqiiqqqfiiii4x")  # B, T, D, r, freqs, pos, start, scale, interleaved, inverse, xdtype, ydtype
+TENSOR = struct.Struct("=6qi4x")         # x, out, rows, cols, ldx, ldo, dtype
 
 
 _lib = None
@@ -676,7 +664,7 @@ def dprc_clip_accumulate_vectors(G, c, grad=None, accumulate=False, ws=None):
 
 
 def _head(h, W, target, piece):
-    """dprc_head of hidden states h [B, T, d], weight W [V, d] and targets [B, T]."""
+    """dprc_head of hidden states h [B, T, d], weight W [V, d] and targets [B, T]; and (B, T, d, V)."""
     ldh = _token_rows(h, "h")
     B, T, d = h.shape
     dev = h.get_device()
@@ -686,49 +674,45 @@ def _head(h, W, target, piece):
     if target.shape != (B, T) or target.dtype != torch.int64 or target.get_device() != dev or not target.is_contiguous():
         raise ValueError(f"target must be contiguous int64 [{B}, {T}] on {h.device}")
     V = W.shape[0]
-    return HeadDesc(h.data_ptr(), W.data_ptr(), target.data_ptr(), B, T, d, V, ldh, W.stride(0) if V > 1 else d,
-                    _dtype_code(h), piece)
+    return HEAD.pack(h.data_ptr(), W.data_ptr(), target.data_ptr(), B, T, d, V, ldh, W.stride(0) if V > 1 else d,
+                     _dtype_code(h), piece), (B, T, d, V)
 
 
-def _tokens(x, name, H, dev):
-    """The pointer of contiguous fp32 values [B, T]."""
-    if x.shape != (H.B, H.T):
-        raise ValueError(f"{name} must be [{H.B}, {H.T}]")
-    return _vector(x, name, H.B * H.T, dev)
-
-
-def _new_tokens(h):
-    return torch.empty(h.shape[:2], dtype=torch.float32, device=h.device)
+def _tokens(x, name, like):
+    """The pointer of contiguous fp32 values [B, T] beside target `like`."""
+    if (x.shape != like.shape or x.dtype != torch.float32 or x.get_device() != like.get_device() or
+            not x.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous fp32 {list(like.shape)} on {like.device}")
+    return x.data_ptr()
 
 
 def dprc_head_loss(h, W, target, loss=None, lse=None, ws=None):
     """Cross entropy of the logits h W^T against target [B, T] (int64; negative: none), without storing the logits:
     returns (loss, lse), [B, T] fp32.  h [B, T, d] token rows, W [V, d]."""
-    H = _head(h, W, target, 0)
-    dev = h.get_device()
-    loss = _new_tokens(h) if loss is None else loss
-    lse = _new_tokens(h) if lse is None else lse
-    need = lib().dprc_head_loss_workspace(ctypes.byref(H))
-    ws = _workspace(need, h.device, ws)
-    _check(lib().dprc_head_loss(ctypes.byref(H), _tokens(loss, "loss", H, dev), _tokens(lse, "lse", H, dev),
-                                ws.data_ptr(), need, _stream(h.device)))
+    H, (B, T, _, _) = _head(h, W, target, 0)
+    dev = h.device
+    loss = torch.empty((B, T), dtype=torch.float32, device=dev) if loss is None else loss
+    lse = torch.empty((B, T), dtype=torch.float32, device=dev) if lse is None else lse
+    need = lib().dprc_head_loss_workspace(H)
+    ws = _workspace(need, dev, ws)
+    _check(lib().dprc_head_loss(H, _tokens(loss, "loss", target), _tokens(lse, "lse", target), ws.data_ptr(), need,
+                                _stream(dev)))
     return loss, lse
 
 
 def dprc_head_errors(h, W, target, lse, g, v0=0, nv=None, E=None, ws=None):
     """E [B, T, nv]: the columns v0 .. v0 + nv (all by default) of the gradient of the logits, g (softmax - onehot)."""
-    H = _head(h, W, target, 0)
-    dev = h.get_device()
-    nv = W.shape[0] - v0 if nv is None else nv
+    H, (B, T, _, V) = _head(h, W, target, 0)
+    nv = V - v0 if nv is None else nv
     if E is None:
-        E = torch.empty(H.B, H.T, nv, dtype=h.dtype, device=h.device)
-    elif E.shape != (H.B, H.T, nv) or E.dtype != h.dtype or E.get_device() != dev:
-        raise ValueError(f"E must be {[H.B, H.T, nv]} {h.dtype} on {h.device}")
+        E = torch.empty(B, T, nv, dtype=h.dtype, device=h.device)
+    elif E.shape != (B, T, nv) or E.dtype != h.dtype or E.get_device() != h.get_device():
+        raise ValueError(f"E must be {[B, T, nv]} {h.dtype} on {h.device}")
     lde = _token_rows(E, "E")
-    need = lib().dprc_head_errors_workspace(ctypes.byref(H))
+    need = lib().dprc_head_errors_workspace(H)
     ws = _workspace(need, h.device, ws) if need else None
-    _check(lib().dprc_head_errors(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev), v0, nv,
-                                  E.data_ptr(), lde, _ptr(ws), need, _stream(h.device)))
+    _check(lib().dprc_head_errors(H, _tokens(lse, "lse", target), _tokens(g, "g", target), v0, nv, E.data_ptr(), lde,
+                                  _ptr(ws), need, _stream(h.device)))
     return E
 
 
@@ -739,45 +723,44 @@ def dprc_head_backward(h, W, target, lse, g, hidden_grad=True, weight_grad=True,
     With k > 0 returns (dh, dW, n2): n2 [B] (=|+=) the estimates of every sample's squared norm of its own weight
     gradient, with the arguments of dprc_norm_hutch; the head counts as ceil(V / HEAD_BLOCK) layers, from
     layer_id on.  piece: columns of the vocabulary held at a time (a multiple of HEAD_BLOCK)."""
-    H = _head(h, W, target, piece)
-    dev = h.get_device()
-    lddh = lddw = H.d
+    H, (B, T, d, V) = _head(h, W, target, piece)
+    lddh = lddw = d
     if dh is not None:
         lddh = _token_rows(dh, "dh", h)
     elif hidden_grad:
-        dh = h.new_empty(h.shape)
+        dh = h.new_empty((B, T, d))
     if dW is not None:
-        if dW.shape != W.shape or dW.dtype != W.dtype or dW.get_device() != dev or (H.d > 1 and dW.stride(1) != 1):
+        if dW.shape != W.shape or dW.dtype != W.dtype or dW.get_device() != W.get_device() or (d > 1 and dW.stride(1) != 1):
             raise ValueError(f"dW must be {list(W.shape)} {W.dtype} with contiguous rows on {W.device}")
-        lddw = dW.stride(0) if H.V > 1 else H.d
+        lddw = dW.stride(0) if V > 1 else d
     elif weight_grad:
-        dW = W.new_empty(W.shape)
+        dW = W.new_empty((V, d))
     norms = None
     if k != 0:
         if n2 is None:
-            n2 = _new_n2(H.B, h.device, accumulate)
-        norms = ctypes.byref(HeadNorms(k, probe, seed, side, layer_id, _vector(n2, "n2", H.B, dev), int(bool(accumulate))))
-    need = lib().dprc_head_backward_workspace(ctypes.byref(H), dh is not None, dW is not None, norms)
+            n2 = _new_n2(B, h.device, accumulate)
+        norms = HEAD_NORMS.pack(k, probe, seed, side, layer_id, _vector(n2, "n2", B, h.get_device()), bool(accumulate))
+    need = lib().dprc_head_backward_workspace(H, dh is not None, dW is not None, norms)
     ws = _workspace(need, h.device, ws)
-    _check(lib().dprc_head_backward(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev), _ptr(dh), lddh,
-                                    _ptr(dW), lddw, norms, ws.data_ptr(), need, _stream(h.device)))
+    _check(lib().dprc_head_backward(H, _tokens(lse, "lse", target), _tokens(g, "g", target), _ptr(dh), lddh, _ptr(dW), lddw,
+                                    norms, ws.data_ptr(), need, _stream(h.device)))
     return (dh, dW) if k == 0 else (dh, dW, n2)
 
 
 def dprc_head_clip_accumulate(h, W, target, lse, g, c, grad=None, accumulate=False, piece=0, ws=None):
     """The head's clipped gradient: grad [d, V] (fp32) (=|+=) sum_i c_i h_i^T E_i, E as in dprc_head_errors."""
-    H = _head(h, W, target, piece)
+    H, (B, _, d, V) = _head(h, W, target, piece)
     dev = h.get_device()
     if grad is None:
-        grad = (torch.zeros if accumulate else torch.empty)(H.d, H.V, dtype=torch.float32, device=h.device)
-    elif (grad.shape != (H.d, H.V) or grad.dtype != torch.float32 or grad.get_device() != dev or
-          (H.V > 1 and grad.stride(1) != 1)):
-        raise ValueError(f"grad must be fp32 [{H.d}, {H.V}] with contiguous rows on {h.device}")
-    need = lib().dprc_head_clip_accumulate_workspace(ctypes.byref(H))
+        grad = (torch.zeros if accumulate else torch.empty)(d, V, dtype=torch.float32, device=h.device)
+    elif (grad.shape != (d, V) or grad.dtype != torch.float32 or grad.get_device() != dev or
+          (V > 1 and grad.stride(1) != 1)):
+        raise ValueError(f"grad must be fp32 [{d}, {V}] with contiguous rows on {h.device}")
+    need = lib().dprc_head_clip_accumulate_workspace(H)
     ws = _workspace(need, h.device, ws)
-    _check(lib().dprc_head_clip_accumulate(ctypes.byref(H), _tokens(lse, "lse", H, dev), _tokens(g, "g", H, dev),
-                                           _vector(c, "c", H.B, dev), grad.data_ptr(), grad.stride(0) if H.d > 1 else H.V,
-                                           int(bool(accumulate)), ws.data_ptr(), need, _stream(h.device)))
+    _check(lib().dprc_head_clip_accumulate(H, _tokens(lse, "lse", target), _tokens(g, "g", target), _vector(c, "c", B, dev),
+                                           grad.data_ptr(), grad.stride(0) if d > 1 else V, bool(accumulate),
+                                           ws.data_ptr(), need, _stream(h.device)))
     return grad
 
 
@@ -799,110 +782,121 @@ def dprc_rotary(x, freqs, pos=None, start=0, scale=1.0, interleaved=False, inver
     [B, T] (int64), or start + t.  inverse turns back: the same call on a gradient is the backward pass.  A result
     that is not given in out (x itself, too) is in the memory order [B, T, H, D], or [B, H, T, D] with
     heads_first; its shape is x's."""
-    xs = x if isinstance(x, (list, tuple)) else [x]
+    several = isinstance(x, (list, tuple))
+    xs = x if several else (x,)
     outs = [None] * len(xs) if out is None else list(out) if isinstance(out, (list, tuple)) else [out]
     if not xs or len(outs) != len(xs):
         raise ValueError("one result per tensor")
-    B, T, _, D = xs[0].shape if xs[0].dim() == 4 else (0, 0, 0, 0)
-    dtype, dev, index = xs[0].dtype, xs[0].device, xs[0].get_device()
-    ydtype = dtype if out_dtype is None else out_dtype
-    if outs[0] is not None:
-        ydtype = outs[0].dtype
-    desc = array.array("q")
+    x0 = xs[0]
+    B, T, _, D = x0.shape if x0.dim() == 4 else (0, 0, 0, 0)
+    dtype, dev, index = x0.dtype, x0.device, x0.get_device()
+    ydtype = outs[0].dtype if outs[0] is not None else dtype if out_dtype is None else out_dtype
+    words, places = [], set()
     for j, t in enumerate(xs):
-        if t.dim() != 4 or t.shape[0] != B or t.shape[1] != T or t.shape[3] != D or t.dtype != dtype or t.get_device() != index:
+        shape = t.shape
+        if len(shape) != 4 or shape[0] != B or shape[1] != T or shape[3] != D or t.dtype != dtype or t.get_device() != index:
             raise ValueError(f"every tensor must be [{B}, {T}, heads, {D}] {dtype} on {dev}")
-        H = t.shape[2]
+        H = shape[2]
+        xb, xt, xh, xd = t.stride()
         y = outs[j]
         if y is None:
-            if heads_first:
-                y = torch.empty((B, H, T, D), dtype=ydtype, device=dev).transpose(1, 2)
-            else:
-                y = torch.empty((B, T, H, D), dtype=ydtype, device=dev)
-            outs[j] = y
-        elif y.shape != t.shape or y.dtype != ydtype or y.get_device() != index or not _apart(y):
-            raise ValueError(f"out must be {list(t.shape)} {ydtype} on {dev}, no element twice")
-        (xb, xt, xh, xd), (yb, yt, yh, yd) = t.stride(), y.stride()
+            y = torch.empty((B, H, T, D) if heads_first else (B, T, H, D), dtype=ydtype, device=dev)
+            yb, yt, yh, yd = (H * T * D, D, T * D, 1) if heads_first else (T * H * D, H * D, D, 1)
+            outs[j] = y.transpose(1, 2) if heads_first else y
+        else:
+            if y.shape != shape or y.dtype != ydtype or y.get_device() != index or not _apart(y):
+                raise ValueError(f"out must be {list(shape)} {ydtype} on {dev}, no element twice")
+            yb, yt, yh, yd = y.stride()
         if (xd != 1 or yd != 1) and D > 1:
             raise ValueError("a head's features must be contiguous")
-        desc.extend((t.data_ptr(), y.data_ptr(), H, xb, xt, xh, yb, yt, yh))
-    if len({y.data_ptr() for y in outs}) < len(outs):
+        place = y.data_ptr()
+        places.add(place)
+        words += (t.data_ptr(), place, H, xb, xt, xh, yb, yt, yh)
+    if len(places) < len(outs):
         raise ValueError("a result is listed twice")
     if freqs.dim() != 1 or freqs.dtype != torch.float64:
         raise ValueError("freqs must be fp64 [r]")
     if pos is not None and pos.shape != (B, T):
         raise ValueError(f"pos must be [{B}, {T}]")
-    R = Rope(B, T, D, freqs.numel(), _vector(freqs, "freqs", freqs.numel(), index, torch.float64),
-             _vector(pos, "pos", B * T, index, torch.int64), start, scale, bool(interleaved), bool(inverse),
-             _dtype_code(xs[0]), _dtype_code(outs[0]))
-    _check(lib().dprc_rotary(ctypes.byref(R), desc.buffer_info()[0], len(xs), _stream(dev)))
-    return outs if isinstance(x, (list, tuple)) else outs[0]
+    r = freqs.numel()
+    R = ROPE.pack(B, T, D, r, _vector(freqs, "freqs", r, index, torch.float64),
+                  0 if pos is None else _vector(pos, "pos", B * T, index, torch.int64), start, scale, bool(interleaved),
+                  bool(inverse), _dtype_code(x0), _dtype_code(outs[0]))
+    heads = array.array("q", words)
+    _check(lib().dprc_rotary(R, heads.buffer_info()[0], len(xs), _stream(dev)))
+    return outs if several else outs[0]
 
 
 def _tensor_rows(t, name):
     """(rows, cols, row stride) of a contiguous tensor, or of a matrix with contiguous rows."""
     if t.is_contiguous():
-        return 1, t.numel(), t.numel()
+        n = t.numel()
+        return 1, n, n
     if t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and t.stride(0) >= t.shape[1]:
         return t.shape[0], t.shape[1], t.stride(0)
     raise ValueError(f"{name} must be contiguous, or a matrix with contiguous rows of their own")
 
 
+_DTYPE_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
 def _tensors(tensors, outs):
-    """dprc_tensor array of the tensors (as 64-bit words), their number and device."""
-    words = array.array("q")
-    dev = index = None
+    """dprc_tensor array of the tensors (as bytes) with their results, if any."""
+    if not tensors:
+        raise ValueError("no tensors")
+    index, parts, places, pack = tensors[0].get_device(), [], set(), TENSOR.pack
     for j, t in enumerate(tensors):
-        if dev is None:
-            dev, index = t.device, t.get_device()
+        code = _DTYPE_CODES.get(t.dtype)
+        if code is None:
+            raise TypeError(f"unsupported dtype {t.dtype}; use bfloat16 or float32")
+        if t.get_device() != index:
+            raise ValueError("the tensors must be on one GPU")
         rows, cols, ldx = _tensor_rows(t, "a tensor")
-        y, ldo = None, ldx
+        place, ldo = 0, ldx
         if outs is not None:
             y = outs[j]
+            place = y.data_ptr()
             if y is not t:
                 if y.shape != t.shape or y.dtype != t.dtype or y.get_device() != index:
                     raise ValueError("every result must have its tensor's shape, dtype and device")
-                r, c, ldo = _tensor_rows(y, "a result")
+                r, _, ldo = _tensor_rows(y, "a result")
                 if r != rows:                  # one of them is contiguous
+                    n = rows * cols
                     rows, cols = t.shape
-                    ldx, ldo = ldx if ldx != t.numel() else cols, ldo if ldo != t.numel() else cols
-            y = y.data_ptr()
-        if t.get_device() != index:
-            raise ValueError("the tensors must be on one GPU")
-        words.extend((t.data_ptr(), y or 0, rows, cols, ldx, ldo, _dtype_code(t)))
-    return words, dev
-
-
-def _grad_norm_args(tensors, outs, norm, ws):
-    words, dev = _tensors(tensors, outs)
-    if dev is None:
-        raise ValueError("no tensors")
-    if norm is None:
-        norm = torch.empty(1, dtype=torch.float32, device=dev)
-    at, n = words.buffer_info()[0], len(words) // 7
-    stream = _stream(dev)
-    need = lib().dprc_grad_norm_workspace(at, n)
-    return words, at, n, norm, _vector(norm, "norm", 1, tensors[0].get_device()), _workspace(need, dev, ws), need, stream
+                    ldx, ldo = ldx if ldx != n else cols, ldo if ldo != n else cols
+            if place in places and t.numel():
+                raise ValueError("a result is listed twice")
+            places.add(place)
+        parts.append(pack(t.data_ptr(), place, rows, cols, ldx, ldo, code))
+    return b"".join(parts)
 
 
 def dprc_grad_norm(tensors, norm=None, ws=None):
     """The joint 2-norm of a list of tensors (bf16 or fp32, any shapes): returns norm [1] fp32."""
-    words, at, n, norm, out, ws, need, stream = _grad_norm_args(tensors, None, norm, ws)
-    _check(lib().dprc_grad_norm(at, n, out, ws.data_ptr(), need, stream))
+    words, n = _tensors(tensors, None), len(tensors)
+    dev = tensors[0].device
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    need = lib().dprc_grad_norm_workspace(words, n)
+    ws = _workspace(need, dev, ws)
+    _check(lib().dprc_grad_norm(words, n, _vector(norm, "norm", 1, tensors[0].get_device()), ws.data_ptr(), need, _stream(dev)))
     return norm
 
 
 def dprc_grad_clip(tensors, max_norm, outs=None, norm=None, ws=None):
     """Every tensor times min(1, max_norm / the joint norm), into outs (by default the tensors themselves): returns
     (outs, norm [1]).  A norm that is not finite gives zeros."""
-    outs = list(tensors) if outs is None else list(outs)
+    outs = list(tensors if outs is None else outs)
     if len(outs) != len(tensors):
         raise ValueError("one result per tensor")
-    places = [y.data_ptr() for y in outs if y.numel()]
-    if len(set(places)) < len(places):
-        raise ValueError("a result is listed twice")
-    words, at, n, norm, out, ws, need, stream = _grad_norm_args(tensors, outs, norm, ws)
-    _check(lib().dprc_grad_clip(at, n, max_norm, out, ws.data_ptr(), need, stream))
+    words, n = _tensors(tensors, outs), len(outs)
+    dev = outs[0].device
+    if norm is None:
+        norm = torch.empty(1, dtype=torch.float32, device=dev)
+    need = lib().dprc_grad_norm_workspace(words, n)
+    ws = _workspace(need, dev, ws)
+    _check(lib().dprc_grad_clip(words, n, max_norm, _vector(norm, "norm", 1, outs[0].get_device()), ws.data_ptr(), need,
+                                _stream(dev)))
     return outs, norm
 
 

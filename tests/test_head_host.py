@@ -21,13 +21,13 @@ PTR = 0x100000
 def head(**kw):
     f = dict(h=PTR, W=2 * PTR, target=3 * PTR, B=2, T=8, d=64, V=300, ldh=64, ldw=64, dtype=dprc.BF16, piece=0)
     f.update(kw)
-    return ctypes.byref(dprc.HeadDesc(*f.values()))
+    return dprc.HEAD.pack(*f.values())
 
 
 def norms(**kw):
     f = dict(k=4, probe=0, seed=0, side=0, layer_id=0, n2=9 * PTR, accumulate=0)
     f.update(kw)
-    return ctypes.byref(dprc.HeadNorms(*f.values()))
+    return dprc.HEAD_NORMS.pack(*f.values())
 
 
 BIG = 1 << 50
@@ -99,7 +99,7 @@ def test_head_workspace_is_bounded():
     """No more than about 1 GiB of E however large the vocabulary, and what `piece` says."""
     L = dprc.lib()
     H = lambda **kw: head(**dict(dict(B=8, T=4096, d=2048, ldh=2048, ldw=2048, V=128256), **kw))
-    rows, planes = 8 * 4096 * 2048 * 2, 8 * 4096 * 2048 * 4
+    rows, planes = 8 * 4096 * (2048 * 2 + 4), 8 * 4096 * 2048 * 4
     assert L.dprc_head_backward_workspace(H(), 1, 0, None) <= (1 << 30) + rows + planes + 1024
     assert L.dprc_head_backward_workspace(H(piece=8192), 1, 0, None) <= (1 << 29) + rows + planes + 1024
     assert L.dprc_head_loss_workspace(H()) <= 8 * 4096 * 8 * 502
@@ -108,7 +108,7 @@ def test_head_workspace_is_bounded():
 def rope(**kw):
     f = dict(B=2, T=8, D=64, r=32, freqs=PTR, pos=0, start=0, scale=1.0, interleaved=0, inverse=0, xdtype=1, ydtype=1)
     f.update(kw)
-    return ctypes.byref(dprc.Rope(*f.values()))
+    return dprc.ROPE.pack(*f.values())
 
 
 def heads(x=2 * PTR, y=3 * PTR, H=4, xb=2048, xt=256, xh=64, yb=2048, yt=256, yh=64):
@@ -141,7 +141,7 @@ def test_rotary_refusals():
 def tensors(*ts):
     f = dict(x=PTR, out=2 * PTR, rows=3, cols=5, ldx=5, ldo=5, dtype=1)
     ts = [dict(f, **t) for t in ts]
-    return (ctypes.c_int64 * max(1, 7 * len(ts)))(*[w for t in ts for w in t.values()]), len(ts)
+    return b"".join(dprc.TENSOR.pack(*t.values()) for t in ts), len(ts)
 
 
 @built
@@ -228,8 +228,8 @@ def test_binding_refuses_mismatched_tensors(calls):
     wide = torch.zeros(4, 9)[:, :5]
     dprc.dprc_grad_clip([a, wide], 1.0, outs=[wide, a])
     assert calls[-1][0] == "dprc_grad_clip" and calls[-1][1][1] == 2
-    words, _ = dprc._tensors([a, wide, a], [wide, a, torch.zeros(4, 5)])      # rows, columns, row strides
-    assert [list(words)[7 * j + 2:7 * j + 6] for j in range(3)] == [[4, 5, 5, 9], [4, 5, 9, 5], [1, 20, 20, 20]]
+    words = dprc._tensors([a, wide, a], [wide, a, torch.zeros(4, 5)])         # rows, columns, row strides
+    assert [t[2:6] for t in dprc.TENSOR.iter_unpack(words)] == [(4, 5, 5, 9), (4, 5, 9, 5), (1, 20, 20, 20)]
 
 
 def test_oracle_against_torch():
