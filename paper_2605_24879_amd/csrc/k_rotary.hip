@@ -7,6 +7,9 @@
 // tokens: their cosines and sines are made once for all heads of all tensors and kept in LDS.
 // The angle is reduced to a fraction of a turn in 64 bits (in 32 a position of 10^6 would lose 0.06 of a
 // radian); sine and cosine of the fraction are taken in 32.
+// A thread takes eight pairs at a time, two 16-byte loads of bfloat16; the r mod 8 pairs left at the end of a head go as
+// 4, 2 and 1 (one at a time: 138 us for 16+4 heads of 96 with r 13 and 2^16 tokens, so 112).  32 + 8 heads of 64
+// bfloat16 features, 2^15 tokens: 72 us, 4.6 TB/s; with non-temporal loads and stores 77.  A step of 64 tokens: 3.6 us.
 #include <algorithm>
 #include "device.hpp"
 #include "kernels.hpp"
@@ -14,22 +17,59 @@
 
 namespace dprc {
 
+// Eight features at any alignment of the element
 template <class E>
-__device__ __forceinline__ void load8(const E* p, float (&x)[8]) {
+__device__ __forceinline__ void load8(const E* p, float* x) {
 #pragma unroll
   for (int k = 0; k < 8; k += kPiece<E>) unpack<E>(load_piece<E>(p + k), x + k);
 }
 template <class E>
-__device__ __forceinline__ void store8(E* p, const float (&x)[8]) {
+__device__ __forceinline__ void store8(E* p, const float* x) {
 #pragma unroll
   for (int k = 0; k < 8; k += kPiece<E>) store_piece<E>(p + k, pack<E>(x + k));
 }
-__device__ __forceinline__ float get1(const uint16_t* p) { return bf16_to_f32(*p); }
-__device__ __forceinline__ float get1(const float* p) { return *p; }
-__device__ __forceinline__ void put1(uint16_t* p, float x) {
-  *p = __builtin_bit_cast(uint16_t, (__bf16)x);
+
+// The first n < 8 of them, as 4, 2 and 1; element i of what is loaded is in x[i] for the first four, then from x[4] on
+// for the two and in x[6].
+__device__ __forceinline__ void load_some(const uint16_t* p, int n, float* x) {
+  if (n & 4) {
+    const u32x2_any2 v = *reinterpret_cast<const u32x2_any2*>(p);
+    x[0] = __uint_as_float(v[0] << 16); x[1] = __uint_as_float(v[0] & 0xFFFF0000u);
+    x[2] = __uint_as_float(v[1] << 16); x[3] = __uint_as_float(v[1] & 0xFFFF0000u);
+  }
+  if (n & 2) {
+    const uint32_t v = *reinterpret_cast<const u32_any2*>(p + (n & 4));
+    x[4] = __uint_as_float(v << 16);
+    x[5] = __uint_as_float(v & 0xFFFF0000u);
+  }
+  if (n & 1) x[6] = bf16_to_f32(p[n & 6]);
 }
-__device__ __forceinline__ void put1(float* p, float x) { *p = x; }
+__device__ __forceinline__ void load_some(const float* p, int n, float* x) {
+  if (n & 4) unpack<float>(load_piece<float>(p), x);
+  if (n & 2) {
+    x[4] = p[n & 4];
+    x[5] = p[(n & 4) + 1];
+  }
+  if (n & 1) x[6] = p[n & 6];
+}
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2_t{a, b}, bf16x2_t));
+}
+__device__ __forceinline__ void store_some(uint16_t* p, int n, const float* x) {
+  if (n & 4) store_part(p, uint2{pack2(x[0], x[1]), pack2(x[2], x[3])});
+  if (n & 2) store_part(p + (n & 4), pack2(x[4], x[5]));
+  if (n & 1) p[n & 6] = (uint16_t)pack2(x[6], 0.f);
+}
+__device__ __forceinline__ void store_some(float* p, int n, const float* x) {
+  if (n & 4) store_piece<float>(p, pack<float>(x));
+  if (n & 2) {
+    p[n & 4] = x[4];
+    p[(n & 4) + 1] = x[5];
+  }
+  if (n & 1) p[n & 6] = x[6];
+}
+// where x[i] of these lies
+__device__ __forceinline__ int some_at(int i, int n) { return i < 4 ? i : i < 6 ? (n & 4) + i - 4 : n & 6; }
 
 __device__ __forceinline__ void turn(float2 cs, float& a, float& b) {
   const float c = a * cs.x - b * cs.y;
@@ -37,47 +77,63 @@ __device__ __forceinline__ void turn(float2 cs, float& a, float& b) {
   a = c;
 }
 
-// Eight pairs from pair j on (or the r - j left), or eight features behind the pairs.
+// Eight pairs from pair 8 * unit on (or the r - j left), or eight features behind the pairs.
 template <class X, class Y, bool INTERLEAVED>
 __device__ __forceinline__ void rotary_unit(const X* x, Y* y, const float2* cs, int unit, int units, int r, int D) {
+  float u[8] = {}, v[8] = {};
   if (unit >= units) {
     const int c = 2 * r + 8 * (unit - units);
     if (c + 8 <= D) {
-      float v[8];
       load8<X>(x + c, v);
       store8<Y>(y + c, v);
     } else {
-      for (int k = c; k < D; ++k) put1(y + k, get1(x + k));
+      load_some(x + c, D - c, v);
+      store_some(y + c, D - c, v);
     }
     return;
   }
-  const int j = 8 * unit;
-  if (j + 8 > r) {
-    for (int k = j; k < r; ++k) {
-      const int ia = INTERLEAVED ? 2 * k : k, ib = INTERLEAVED ? 2 * k + 1 : r + k;
-      float a = get1(x + ia), b = get1(x + ib);
-      turn(cs[k], a, b);
-      put1(y + ia, a);
-      put1(y + ib, b);
-    }
-    return;
-  }
-  float u[8], v[8];
-  const int iu = INTERLEAVED ? 2 * j : j, iv = INTERLEAVED ? 2 * j + 8 : r + j;
-  load8<X>(x + iu, u);
-  load8<X>(x + iv, v);
+  const int j = 8 * unit, left = r - j;
+  if (left >= 8) {
+    const int iu = INTERLEAVED ? 2 * j : j, iv = INTERLEAVED ? 2 * j + 8 : r + j;
+    load8<X>(x + iu, u);
+    load8<X>(x + iv, v);
 #pragma unroll
-  for (int k = 0; k < 8; ++k) {
-    if constexpr (INTERLEAVED) {
-      if (k < 4) turn(cs[j + k], u[2 * k], u[2 * k + 1]);
-      else turn(cs[j + k], v[2 * k - 8], v[2 * k - 7]);
-    } else {
-      turn(cs[j + k], u[k], v[k]);
+    for (int k = 0; k < 8; ++k) {
+      if constexpr (INTERLEAVED) {
+        if (k < 4) turn(cs[j + k], u[2 * k], u[2 * k + 1]);
+        else turn(cs[j + k], v[2 * k - 8], v[2 * k - 7]);
+      } else {
+        turn(cs[j + k], u[k], v[k]);
+      }
     }
+    store8<Y>(y + iu, u);
+    store8<Y>(y + iv, v);
+  } else if constexpr (INTERLEAVED) {                  // 4 pairs as 8 features, the others as 4 and 2
+    const int rest = 2 * (left & 3), at = 2 * (r - (left & 3));
+    if (left & 4) load8<X>(x + 2 * j, u);
+    load_some(x + at, rest, v);
+    if (left & 4) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) turn(cs[j + k], u[2 * k], u[2 * k + 1]);
+      store8<Y>(y + 2 * j, u);
+    }
+    if (rest & 4) {
+      turn(cs[at / 2], v[0], v[1]);
+      turn(cs[at / 2 + 1], v[2], v[3]);
+    }
+    if (rest & 2) turn(cs[r - 1], v[4], v[5]);
+    store_some(y + at, rest, v);
+  } else {
+    load_some(x + j, left, u);
+    load_some(x + r + j, left, v);
+#pragma unroll
+    for (int k = 0; k < 7; ++k) turn(cs[min(j + some_at(k, left), r - 1)], u[k], v[k]);
+    store_some(y + j, left, u);
+    store_some(y + r + j, left, v);
   }
-  store8<Y>(y + iu, u);
-  store8<Y>(y + iv, v);
 }
+
+constexpr int kRotaryItems = 1280;   // units of a workgroup, where there are tokens for 512 such (2560: 5 to 15% slower; 640: within 4%)
 
 template <class X, class Y, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
@@ -113,7 +169,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
 
 hipError_t launch_rotary(RotaryArgs a, hipStream_t st) {
   const int64_t tokens = a.B * a.T, items = (int64_t)a.heads * ((a.r + 7) / 8 + (a.D - 2 * a.r + 7) / 8);
-  int64_t per = std::max<int64_t>(1, 1280 / items);
+  int64_t per = std::max<int64_t>(1, kRotaryItems / items);
   per = std::min<int64_t>({per, std::max<int64_t>(1, tokens / 512), 4096 / a.r});
   a.per_block = (int32_t)std::max<int64_t>(1, per);
   const dim3 grid = flat_grid(ceil_div(tokens, a.per_block));
