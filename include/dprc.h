@@ -340,8 +340,10 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
  *   grad = sum_i c_i h_i^T E_i                                                   (dprc_head_clip_accumulate)
  * for the same lse and g.  A token with a negative target has no loss: loss_t = 0 and E_t = 0, and neither
  * h_t nor g_t (NaN, say) reaches any output but lse_t.  A target of V or more makes loss_t and lse_t NaN, and
- * with that lse every gradient of the token.  Products are summed in fp32, exponentials taken in fp32; E is
- * rounded to the head's dtype once (as the gradient of stored logits is), then enters the products.
+ * with that lse every gradient of the token.  Products are summed in fp32, exponentials taken in fp32 (logits of
+ * 1e38 or more give infinities or NaN); E is rounded to the head's dtype once (as the gradient of stored logits is),
+ * then enters the products.  In dh and dW of bf16 heads the target's entry of E, by far the largest of its row, enters
+ * as two bf16 numbers: the rounded one and what its rounding lost.
  *
  * The last four go through the vocabulary in pieces of `piece` columns, of which E is held in the workspace:
  * a positive multiple of DPRC_HEAD_BLOCK, or 0 for as many as E of 1 GiB holds (at least one block).  dh, dW
@@ -361,7 +363,7 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
  *   c       [B] fp32.  grad [d,V] fp32, row stride ldg, (=|+=) by accumulate: the layout of
  *           dprc_clip_accumulate.
  *   E       (dprc_head_errors) [B,T,nv] token rows of `dtype`, stride lde: the columns v0 .. v0 + nv of E.
- * B <= 65535, B*T <= 2^31, d and V <= 2^30, d*V <= 2^40. */
+ * B <= 65535, B*T <= 2^31, d <= 2^20, V <= 2^30, d*V and d*B*T <= 2^40, B*T*V <= 2^44. */
 #define DPRC_HEAD_BLOCK 8192
 typedef struct {
   const void* h;
@@ -407,7 +409,7 @@ dprc_status dprc_head_clip_accumulate(const dprc_head* H, const float* lse, cons
  *   x       `count` (1 to 4) tensors [B,T,H,D], elements of x dtype at x + b*xb + t*xt + h*xh + feature, to y
  *           likewise (ydtype).  y may be x (with its dtype and strides); otherwise outputs overlap neither
  *           inputs nor each other.
- * B*T <= 2^31, 1 <= 2 r <= D <= 2^20, r <= 4096, at most 2^16 heads in all. */
+ * B*T <= 2^31, 1 <= 2 r <= D <= 2^20, r <= 4096, at most 2^16 heads and 2^30 features of a token in all. */
 typedef struct {
   int64_t B, T;
   int32_t D, r;

@@ -1779,8 +1779,9 @@ dprc_status check_head(const dprc_head* H) {
       H->ldw < H->d || !dtype_ok(H->dtype) || H->piece < 0 || H->piece % DPRC_HEAD_BLOCK)
     return DPRC_ERROR_INVALID_VALUE;
   const size_t e = elem_bytes(H->dtype);
-  if (H->B > 65535 || H->T > (1LL << 30) || H->B * H->T > (1LL << 31) || H->d > (1LL << 30) || H->V > (1LL << 30) ||
-      H->d * H->V > (1LL << 40) || !aligned(H->h, e) || !aligned(H->W, e) || !aligned(H->target, 8))
+  // (offsets within a tile's rows and the numbers of tiles stay below 2^31)
+  if (H->B > 65535 || H->T > (1LL << 30) || H->B * H->T > (1LL << 31) || H->d > (1LL << 20) || H->V > (1LL << 30) ||
+      H->d * H->V > (1LL << 40) || H->B * H->T > (1LL << 40) / H->d || H->B * H->T > (1LL << 44) / H->V || !aligned(H->h, e) || !aligned(H->W, e) || !aligned(H->target, 8))
     return DPRC_ERROR_NOT_SUPPORTED;
   return DPRC_SUCCESS;
 }
@@ -1999,7 +2000,8 @@ size_t dprc_head_errors_workspace(const dprc_head* H) {
 dprc_status dprc_head_errors(const dprc_head* H, const float* lse, const float* g, int64_t v0, int64_t nv, void* E,
                              int64_t lde, void* ws, size_t ws_bytes, hipStream_t stream) {
   const dprc_status st = check_head(H);
-  if (st == DPRC_ERROR_INVALID_VALUE || !lse || !g || !E || v0 < 0 || nv < 1 || v0 > H->V - nv || lde < nv)
+  if (st == DPRC_ERROR_INVALID_VALUE || !lse || !g || !E || E == H->h || E == H->W || v0 < 0 || nv < 1 || v0 > H->V - nv ||
+      lde < nv)
     return DPRC_ERROR_INVALID_VALUE;
   if (st != DPRC_SUCCESS) return st;
   if (!aligned(lse, 4) || !aligned(g, 4) || !aligned(E, elem_bytes(H->dtype))) return DPRC_ERROR_NOT_SUPPORTED;
@@ -2144,12 +2146,14 @@ dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t cou
     if (h.x == h.y && (a.xbf16 != a.ybf16 || (R->B > 1 && h.xb != h.yb) || (R->T > 1 && h.xt != h.yt) ||
                        (h.H > 1 && h.xh != h.yh)))
       return DPRC_ERROR_INVALID_VALUE;
+    for (int32_t j = 0; j < count; ++j)
+      if (j != i && (h.y == heads[j].x || h.y == heads[j].y)) return DPRC_ERROR_INVALID_VALUE;
     if (h.H > (1 << 16) || !aligned(h.x, elem_bytes(R->xdtype)) || !aligned(h.y, elem_bytes(R->ydtype)))
       return DPRC_ERROR_NOT_SUPPORTED;
     a.x[i] = RotaryTensor{h.x, h.y, h.xb, h.xt, h.xh, h.yb, h.yt, h.yh, (int32_t)h.H};
     total += h.H;
   }
-  if (total > (1 << 16)) return DPRC_ERROR_NOT_SUPPORTED;
+  if (total > (1 << 16) || total * R->D > (1LL << 30)) return DPRC_ERROR_NOT_SUPPORTED;
   a.heads = (int32_t)total;
   return hip_status(traced(DPRC_KERNEL_ROTARY, stream, [&] { return launch_rotary(a, stream); }));
 }

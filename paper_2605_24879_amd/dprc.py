@@ -739,7 +739,7 @@ def dprc_head_backward(h, W, target, lse, g, hidden_grad=True, weight_grad=True,
     if k != 0:
         if n2 is None:
             n2 = _new_n2(B, h.device, accumulate)
-        norms = HEAD_NORMS.pack(k, probe, seed, side, layer_id, _vector(n2, "n2", B, h.get_device()), bool(accumulate))
+        norms = HEAD_NORMS.pack(k, probe, seed & 0xFFFFFFFFFFFFFFFF, side, layer_id & 0xFFFFFFFF, _vector(n2, "n2", B, h.get_device()), bool(accumulate))
     need = lib().dprc_head_backward_workspace(H, dh is not None, dW is not None, norms)
     ws = _workspace(need, h.device, ws)
     _check(lib().dprc_head_backward(H, _tokens(lse, "lse", target), _tokens(g, "g", target), _ptr(dh), lddh, _ptr(dW), lddw,
@@ -845,6 +845,7 @@ def _tensors(tensors, outs):
     if not tensors:
         raise ValueError("no tensors")
     index, parts, places, pack = tensors[0].get_device(), [], set(), TENSOR.pack
+    sources = None
     for j, t in enumerate(tensors):
         code = _DTYPE_CODES.get(t.dtype)
         if code is None:
@@ -857,6 +858,9 @@ def _tensors(tensors, outs):
             y = outs[j]
             place = y.data_ptr()
             if y is not t:
+                sources = {x.data_ptr() for x in tensors} if sources is None else sources
+                if place in sources and place != t.data_ptr() and t.numel():
+                    raise ValueError("a result lies where another tensor does")
                 if y.shape != t.shape or y.dtype != t.dtype or y.get_device() != index:
                     raise ValueError("every result must have its tensor's shape, dtype and device")
                 r, _, ldo = _tensor_rows(y, "a result")

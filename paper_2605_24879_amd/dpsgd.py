@@ -64,10 +64,11 @@ def step_seed(seed, step):
 
 
 class HeadPart:
-    """The trained head's part of a capture: what its gradients are formed from, and the estimates n2 under key."""
+    """The trained head's part of a capture: what its gradients are formed from with the weights of `state`, and the
+    estimates n2 under key."""
 
-    def __init__(self, h, target, lse, g, key, n2):
-        self.h, self.target, self.lse, self.g, self.key, self.n2 = h, target, lse, g, key, n2
+    def __init__(self, h, target, lse, g, key, n2, state):
+        self.h, self.target, self.lse, self.g, self.key, self.n2, self.state = h, target, lse, g, key, n2, state
 
 
 class Pairs(list):
@@ -114,6 +115,7 @@ class DPSGDRC:
             lin.weight.requires_grad_(True)
         self.norms, self.dropouts = list(norms), list(dropouts)
         self._gather_vectors()
+        self._head = None
         self.head, self.max_norm = head, None if max_norm is None else float(max_norm)
         if self.max_norm is not None and not 0.0 < self.max_norm < float("inf"):
             raise ValueError("max_norm must be positive and finite")
@@ -191,6 +193,10 @@ class DPSGDRC:
         """How the head's norms are estimated: its blocks are numbered behind the linear layers."""
         return dict(k=self.k, seed=key, layer_id=len(self.linears), side=self.side, probe=self.probe)
 
+    def _head_state(self):
+        """What changes with the head's weight, by this step's updates or otherwise."""
+        return self.steps, self.head.linear.weight._version
+
     def _take_head(self, key):
         """What the head's backward call does during a capture: the estimates on the way to dh."""
         self._head = None
@@ -200,7 +206,8 @@ class DPSGDRC:
                 raise RuntimeError("the trained head ran twice in one step")
             dh, _, n2 = D.dprc_head_backward(h, weight, target, lse, g, hidden_grad=want_h, weight_grad=False,
                                              **self._head_args(key))
-            self._head = HeadPart(h.detach(), target, lse, g, key, n2)
+            # (a copy of the targets: a caller may fill its buffer anew before the head is read again)
+            self._head = HeadPart(h.detach(), target.clone(), lse, g, key, n2, self._head_state())
             return dh
         return take
 
@@ -241,7 +248,7 @@ class DPSGDRC:
                 m.sink = None
             if self.head is not None:
                 self.head.sink = None
-        part, self._head = (self._head, None) if self.head is not None else (None, None)
+            part, self._head = self._head, None
         E = E[:len(self._S)]
         if any(e is None for e in E) or (self.norms and (self._G is None or len(self._filled) < len(self.norms))):
             raise RuntimeError("a trained layer or norm has no part in the loss")
@@ -274,6 +281,8 @@ class DPSGDRC:
         part = getattr(pairs, "head", None)
         if part is None:
             raise ValueError("pairs must be what capture returned, the head's part with the layers'")
+        if part.state != self._head_state():
+            raise RuntimeError("the head's weight has changed since the capture: its gradients are formed from it again")
         batches = [A.shape[0] for (A, _, _) in pairs] + ([pairs.vectors.shape[0]] if self.norms else [])
         if any(B != part.h.shape[0] for B in batches):
             raise ValueError(f"the head's batch of {part.h.shape[0]} samples is not the layers'")

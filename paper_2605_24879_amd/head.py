@@ -36,7 +36,10 @@ class _HeadFn(torch.autograd.Function):
 
 class Head(nn.Module):
     """Per-token losses [B, T] (fp32) of hidden states [B, T, d] against target ids [B, T] (int64): cross entropy over
-    the outputs of ``linear``.  A negative target has no loss.  ``linear`` stays the owner of the weight."""
+    the outputs of ``linear``.  A negative target has no loss.  ``linear`` stays the owner of the weight.
+
+    In a captured pass take gradients with torch.autograd.grad: torch ends the process where ``backward`` is captured while
+    an eager graph of the same leaves lives."""
 
     def __init__(self, linear):
         super().__init__()

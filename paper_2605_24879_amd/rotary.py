@@ -94,7 +94,8 @@ class Rotary(nn.Module):
     def on(self, device):
         """The frequencies on a device."""
         if device not in self._on:
-            self._on[device] = self.freqs.to(device)
+            with torch.inference_mode(False):   # they may be saved for a backward pass later on
+                self._on[device] = self.freqs.to(device)
         return self._on[device]
 
     def forward(self, *xs, pos=None, start=0, heads_first=False, out_dtype=None):

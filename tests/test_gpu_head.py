@@ -319,6 +319,31 @@ def test_repeats_and_streams(D):
         assert torch.equal(z, lse) and all(torch.equal(a, b) for a, b in zip(rest, ref))
 
 
+@pytest.mark.parametrize("odd", [0, 1])
+def test_strides_past_32_bits(D, odd):
+    """Rows so far apart that offsets pass 2^32 bytes: what rows side by side give."""
+    B, T, d, V = 2, 75, 64, 4500
+    h, W, target, g = make(B, T, d, V, "bf16", seed=4)
+    far = lambda rows, ld: torch.empty(rows * ld, dtype=torch.bfloat16, device="cuda").view(rows, ld)[:, :d]
+    ld = (1 << 19) + 8 + odd
+    ref_W = far(V, 72 + odd)                              # the same path: whole pieces, or rows off their boundaries
+    ref_W.copy_(W)
+    far_W, far_h = far(V, ld), far(B * T, 1 << 24).unflatten(0, (B, T))
+    far_W.copy_(W)
+    far_h.copy_(h)
+    assert far_W.stride(0) * V * 2 > 1 << 32 and far_h.stride(1) * B * T * 2 > 1 << 32
+    loss, lse = D.dprc_head_loss(h, ref_W, target)
+    for got, want in zip(D.dprc_head_loss(far_h, far_W, target), (loss, lse)):
+        assert torch.equal(got, want)
+    want = D.dprc_head_backward(h, ref_W, target, lse, g, k=4, seed=1)
+    dW, dh = far(V, ld), far(B * T, 1 << 24).unflatten(0, (B, T))
+    for got, w in zip(D.dprc_head_backward(far_h, far_W, target, lse, g, k=4, seed=1, dh=dh, dW=dW), want):
+        assert torch.equal(got, w)
+    E = far(B * T, 1 << 24).unflatten(0, (B, T))
+    assert torch.equal(D.dprc_head_errors(far_h, far_W, target, lse, g, v0=4400, nv=d, E=E),
+                       D.dprc_head_errors(h, ref_W, target, lse, g, v0=4400, nv=d))
+
+
 def test_captured(D):
     h, W, target, g = make(2, 100, 128, 9000, "bf16", seed=8)
     static = dict(h=h.clone(), g=g.clone(), target=target.clone())

@@ -179,6 +179,15 @@ def test_they_train_together(mods):
     drv.remove_hooks()
 
 
+def test_rotary_first_called_for_inference(mods):
+    rot = mods[3].Rotary(8)
+    x = torch.randn(2, 3, 4, 8, device="cuda", requires_grad=True)
+    with torch.inference_mode():
+        y = rot(x)
+    g, = torch.autograd.grad(rot(x).sum(), x)            # the frequencies are saved for this
+    assert torch.equal(rot(x.detach()), y) and g.isfinite().all()
+
+
 def test_a_captured_pass(mods):
     """Losses and gradients of the model in a graph, replayed on other tokens."""
     model = _model(head=True, rotary=True)

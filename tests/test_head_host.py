@@ -56,12 +56,14 @@ def test_head_descriptions(call):
                 dict(dtype=2), dict(piece=-8192), dict(piece=100)):
         assert call(head(**bad)) == INVALID, bad
     assert call(None) == INVALID
-    wide = dict(d=64, ldh=64, ldw=64)
+    wide = dict(d=64, ldh=4096, ldw=4096)
     for bad in (dict(h=PTR + 1), dict(W=PTR + 1), dict(target=PTR + 4), dict(B=65536), dict(T=(1 << 30) + 1), dict(T=1 << 30, B=4),
-                dict(V=(1 << 30) + 1), dict(dtype=dprc.F32, h=PTR + 2)):
+                dict(V=(1 << 30) + 1), dict(dtype=dprc.F32, h=PTR + 2), dict(T=1 << 29, V=1 << 15), dict(T=1 << 29, d=1 << 12)):
         kw = dict(wide, **bad)
         if call is clip:
             assert call(head(**kw), ldg=1 << 31) == UNSUPPORTED, bad
+        elif call is back:
+            assert call(head(**kw), lddh=4096, lddw=4096) == UNSUPPORTED, bad
         else:
             assert call(head(**kw)) == UNSUPPORTED, bad
     assert call(head(d=1 << 21, ldh=1 << 21, ldw=1 << 21, V=1 << 20), **(
@@ -78,6 +80,7 @@ def test_head_arguments():
     assert errors(H, lse=0) == errors(H, g=0) == errors(H, E=0) == errors(H, v0=-1) == errors(H, nv=0) == INVALID
     assert errors(H, v0=291) == errors(H, nv=301, lde=301) == errors(H, lde=9) == INVALID
     assert errors(head(ldh=65), ws=0) == INVALID and errors(head(ldh=65), n=8) == SMALL
+    assert errors(H, E=PTR) == errors(H, E=2 * PTR) == INVALID
     assert errors(H, E=6 * PTR + 1) == UNSUPPORTED
     assert back(H, lse=0) == back(H, g=0) == back(H, dh=0, dW=0) == back(H, lddh=63) == back(H, lddw=63) == INVALID
     assert back(H, dh=PTR) == back(H, dW=2 * PTR) == back(H, dW=6 * PTR) == back(H, ws=0) == INVALID
@@ -135,7 +138,10 @@ def test_rotary_refusals():
     assert rotary(rope(ydtype=0), heads(y=2 * PTR)) == INVALID
     for bad in (dict(x=PTR + 1), dict(y=PTR + 1), dict(H=(1 << 16) + 1)):
         assert rotary(rope(), heads(**bad)) == UNSUPPORTED, bad
-    assert rotary(rope(), heads(H=1 << 16), heads(H=1)) == UNSUPPORTED
+    assert rotary(rope(), heads(H=1 << 16), heads(x=4 * PTR, y=5 * PTR, H=1)) == UNSUPPORTED
+    assert rotary(rope(D=1 << 15, r=16), heads(H=1 << 15), heads(x=4 * PTR, y=5 * PTR, H=1)) == UNSUPPORTED
+    # a result over another tensor, or over another result
+    assert rotary(rope(), ok, heads(x=4 * PTR, y=2 * PTR)) == rotary(rope(), ok, heads(x=4 * PTR, y=3 * PTR)) == INVALID
 
 
 def tensors(*ts):
@@ -226,9 +232,12 @@ def test_binding_refuses_mismatched_tensors(calls):
             dprc.dprc_grad_clip(ts, 1.0, **kw)
     assert not calls
     wide = torch.zeros(4, 9)[:, :5]
-    dprc.dprc_grad_clip([a, wide], 1.0, outs=[wide, a])
+    with pytest.raises(ValueError, match="another"):
+        dprc.dprc_grad_clip([a, wide], 1.0, outs=[wide, a])
+    assert not calls
+    dprc.dprc_grad_clip([a, wide], 1.0, outs=[torch.zeros(4, 9)[:, :5], torch.zeros(4, 5)])
     assert calls[-1][0] == "dprc_grad_clip" and calls[-1][1][1] == 2
-    words = dprc._tensors([a, wide, a], [wide, a, torch.zeros(4, 5)])         # rows, columns, row strides
+    words = dprc._tensors([a, wide, a], [torch.zeros(4, 9)[:, :5], torch.zeros(4, 5), torch.zeros(4, 5)])   # rows, columns, row strides
     assert [t[2:6] for t in dprc.TENSOR.iter_unpack(words)] == [(4, 5, 5, 9), (4, 5, 9, 5), (1, 20, 20, 20)]
 
 

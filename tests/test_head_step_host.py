@@ -150,6 +150,10 @@ def test_capture_has_the_heads_part():
             drv.estimate(bad, 7)
         with pytest.raises(ValueError):
             drv.clipped_sums(bad, c)
+    with torch.no_grad():
+        model.lm_head.weight.mul_(1.0)                      # the head's gradients are formed from it again
+    with pytest.raises(RuntimeError, match="changed"):
+        drv.clipped_sums(pairs, c)
     drv.remove_hooks()
 
 
@@ -160,6 +164,22 @@ def test_the_head_alone_is_trained():
     rows = [torch.autograd.grad(loss_of(model, tok[i:i + 1])()[0], model.lm_head.weight)[0] for i in range(3)]
     assert np.allclose(n2.numpy(), [(f64(g) ** 2).sum() for g in rows], rtol=1e-4)
     assert len(grads) == 1 and torch.allclose(grads[0], sum(ci * g.t() for ci, g in zip(c, rows)), rtol=1e-3, atol=1e-6)
+    # targets in a buffer that is filled anew before the clipped sums, and a capture that fails half-way
+    x, y = model.norm(model.embed(tok[:, :-1])).detach(), tok[:, 1:].contiguous()
+    pairs = drv.capture(lambda: model.head(x, y).mean(1))[1]
+    want = drv.clipped_sums(pairs, c)[0]
+    y.zero_()
+    assert torch.equal(drv.clipped_sums(pairs, c)[0], want)
+
+    def fails():
+        torch.autograd.grad(model.head(x, y).sum(), model.lm_head.weight, allow_unused=True)
+        raise KeyError
+    with pytest.raises(KeyError):
+        drv.capture(fails)
+    assert drv._head is None and model.head.sink is None
+    drv.update(drv.clipped_sums(pairs, c), 3, 0)
+    with pytest.raises(RuntimeError, match="changed"):
+        drv.estimate(pairs, 0)
 
 
 def test_what_the_step_refuses():
@@ -251,3 +271,7 @@ def test_rotary_module():
     assert torch.equal(rot(q.detach(), pos=pos), a.detach()) and not rot(q.detach()).requires_grad
     with pytest.raises(ValueError):
         rot(torch.zeros(1, 1, 1, 6))
+    first = rotary.Rotary(8)
+    with torch.inference_mode():                            # then trained
+        first(torch.zeros(1, 1, 1, 8, dtype=torch.float64))
+    torch.autograd.grad(first(q).sum(), q)
