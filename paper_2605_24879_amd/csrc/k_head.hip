@@ -49,13 +49,14 @@ struct HeadTile {
 
 // An operand is `rows` rows of `width` elements, ld apart.  KC: its rows are the tile's rows (columns), the
 // contraction runs along them.  KR: the contraction runs over its rows, the tile's rows (columns) along them.
-// A slab of it in LDS is 128 bytes for every row (column) of the tile.  KC: rows of 128 bytes, piece p of row r
-// at p ^ (r & 7), so that a fragment read of 8 rows covers all banks.  KR, bf16: rows of the tile's width,
-// piece p of row r at p ^ swizzle_kr(r), so that the 4 (8) rows of a transposing read lie in different
-// 32-byte (128-byte) parts of the banks; fp32 fragments are read along the rows and need none.
+// A slab of it in LDS is 128 bytes for every row (column) of the tile; the banks are 256 bytes wide.  KC: rows of
+// 128 bytes, piece p of row r at p ^ swizzle_kc(r), so that a fragment read of 16 rows covers all banks.  KR, bf16: rows
+// of the tile's width, piece p of row r at p ^ swizzle_kr(r), so that the 64 bytes that half a wave reads of each of
+// 4 rows do; fp32 fragments are read along the rows and need none.
+__device__ __forceinline__ int swizzle_kc(int r) { return (r >> 1) & 7; }
 template <class E>
 __device__ __forceinline__ int swizzle_kr(int r, int pieces) {
-  return sizeof(E) == 2 ? (((r & 3) << 1) | (r & 8)) & (pieces - 1) : 0;
+  return sizeof(E) != 2 ? 0 : pieces == 8 ? (r & 2) << 1 : (r & 3) << 2;
 }
 
 // A piece at (row, col), zeros past the rows and the width, at any alignment of the element.
@@ -103,7 +104,7 @@ struct HeadOperand {
   uint32_t off[VEC ? P : 1];           // byte offsets of the thread's pieces in a slab
   uint4 reg[VEC ? 1 : P];
 
-  static __device__ __forceinline__ int kc_col(int s) { return EP * ((s & 7) ^ ((s >> 3) & 7)); }
+  static __device__ __forceinline__ int kc_col(int s) { return EP * ((s & 7) ^ swizzle_kc(s >> 3)); }
   static __device__ __forceinline__ int kr_col(int s) { return EP * ((s % RP) ^ swizzle_kr<E>(s / RP, RP)); }
 
   __device__ __forceinline__ HeadOperand(const HeadRows& X_, int64_t t) : X(X_), t0(t) {
@@ -163,7 +164,7 @@ struct HeadOperand {
     const int l32 = lane & 31, half = lane >> 5;
     if constexpr (!KR) {
       const int row = b + l32;
-      return *reinterpret_cast<const uint4*>(&lds[row * TL::slab + EP * ((2 * ks + half) ^ (row & 7))]);
+      return *reinterpret_cast<const uint4*>(&lds[row * TL::slab + EP * ((2 * ks + half) ^ swizzle_kc(row))]);
     } else if constexpr (sizeof(E) == 2) {
       // lane group g reads rows 8 (g / 2) + r4 (+ 4) of columns 16 (g % 2) + 4 c4 .. of the block
       const int g = lane >> 4, r4 = (lane & 15) >> 2, c4 = lane & 3;
@@ -487,7 +488,7 @@ __device__ __forceinline__ void head_targets(const HeadMulArgs& a, int split, in
     __syncthreads();
     if (in) {                                           // (at most the first 64 threads)
       const int at = AKR ? tid * TL::MT + 8 * ((row >> 3) ^ swizzle_kr<uint16_t>(tid, TL::MT / 8)) + (row & 7)
-                         : row * TL::slab + 8 * ((tid >> 3) ^ (row & 7)) + (tid & 7);
+                         : row * TL::slab + 8 * ((tid >> 3) ^ swizzle_kc(row)) + (tid & 7);
       la0[at] = __builtin_bit_cast(uint16_t, (__bf16)lo);
     }
     __syncthreads();
