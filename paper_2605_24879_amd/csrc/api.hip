@@ -2163,6 +2163,9 @@ dprc_status dprc_rotary(const dprc_rope* R, const dprc_heads* heads, int32_t cou
 namespace {
 
 constexpr int64_t kGradBlocks = 1024;       // workgroups, and parts of the sum, of a call
+// (8 tensors of 2^17, 2^19, 2^21 values in all, GPU us with chunks of at least 1024: 11.7, 12.4, 14.6;
+// 4096: 12.1, 12.2, 13.2; 16384: 12.9, 13.9, 14.6.  2^28 values with at most 8192: 518, 16384: 500.)
+constexpr int64_t kGradChunkLeast = 4096, kGradChunkMost = 16384;
 constexpr int64_t kGradSmall = 1 << 14;     // elements that one workgroup clips (79047 take 19 us so, 13 in two launches)
 constexpr int64_t kGradStream = (int64_t)300 << 20;   // bytes of tensors from which on they go past the caches
 constexpr int64_t kGradKeep = 3000;         // chunks at a launch's end that do not (188 MiB of fp32: 243 million values 500 us; 0, 1000, 2048: 514, 514, 505)
@@ -2171,6 +2174,14 @@ int64_t grad_bytes(const dprc_tensor* t, int32_t count) {
   int64_t n = 0;
   for (int32_t i = 0; i < count; ++i) n += t[i].rows * t[i].cols * (int64_t)elem_bytes(t[i].dtype);
   return n;
+}
+
+// Elements of a chunk: as many as leave every workgroup of the call one, between kGradChunkLeast and kGradChunkMost.
+int64_t grad_chunk_elements(const dprc_tensor* t, int32_t count) {
+  int64_t n = 0, chunk = kGradChunkMost;
+  for (int32_t i = 0; i < count; ++i) n += t[i].rows * t[i].cols;
+  while (chunk > kGradChunkLeast && n < chunk * kGradBlocks) chunk /= 2;
+  return chunk;
 }
 
 dprc_status check_tensors(const dprc_tensor* t, int32_t count, bool out) {
@@ -2200,6 +2211,7 @@ dprc_status grad_launches(const dprc_tensor* t, int32_t count, GradArgs& a, F&& 
   const int64_t launches = ceil_div(filled, kGradTensors);
   const bool past = grad_bytes(t, count) > kGradStream;
   int32_t part0 = 0;
+  a.chunk = grad_chunk_elements(t, count);
   for (int32_t i = 0; i < count;) {
     a.count = 0;
     a.chunks = 0;
@@ -2214,7 +2226,7 @@ dprc_status grad_launches(const dprc_tensor* t, int32_t count, GradArgs& a, F&& 
         g.rows = 1;
       }
       g.chunk0 = a.chunks;
-      a.chunks += g.cols >= kGradChunk ? g.rows * ceil_div(g.cols, kGradChunk) : ceil_div(g.rows, kGradChunk / g.cols);
+      a.chunks += g.cols >= a.chunk ? g.rows * ceil_div(g.cols, a.chunk) : ceil_div(g.rows, a.chunk / g.cols);
     }
     if (a.count == 0) break;
     a.blocks = (int32_t)std::min<int64_t>(a.chunks, std::max<int64_t>(64, kGradBlocks / launches));

@@ -21,13 +21,13 @@ __device__ __forceinline__ GradChunk grad_chunk(const GradArgs& a, int64_t c) {
   const GradTensor& t = a.t[i];
   c -= t.chunk0;
   GradChunk k{i, 0, 1, 0, 0};
-  if (t.cols >= kGradChunk) {
-    const int64_t per = (t.cols + kGradChunk - 1) / kGradChunk;
+  if (t.cols >= a.chunk) {
+    const int64_t per = (t.cols + a.chunk - 1) / a.chunk;
     k.row = c / per;
-    k.col = (c - k.row * per) * kGradChunk;
-    k.cols = min(kGradChunk, t.cols - k.col);
+    k.col = (c - k.row * per) * a.chunk;
+    k.cols = min(a.chunk, t.cols - k.col);
   } else {
-    const int64_t rows = kGradChunk / t.cols;
+    const int64_t rows = a.chunk / t.cols;
     k.row = c * rows;
     k.rows = min(rows, t.rows - k.row);
     k.cols = t.cols;

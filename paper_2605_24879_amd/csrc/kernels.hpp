@@ -529,8 +529,7 @@ struct RotaryArgs {
 hipError_t launch_rotary(RotaryArgs a, hipStream_t st);
 
 // The joint norm of many tensors and their clipping (see dprc_grad_clip).  A tensor is rows of cols
-// elements; its chunks of about kGradChunk elements are numbered from chunk0 on.
-constexpr int64_t kGradChunk = 16384;
+// elements; its chunks of about GradArgs::chunk elements are numbered from chunk0 on.
 constexpr int kGradTensors = 48;     // of a launch: 2.8 KB of kernel arguments
 struct GradTensor {
   const void* x;
@@ -540,7 +539,7 @@ struct GradTensor {
 };
 struct GradArgs {
   int32_t count, blocks;
-  int64_t chunks;
+  int64_t chunk, chunks;             // elements of a chunk; how many there are
   double* part;                      // [parts], this launch's from part0 on
   int32_t part0, parts;
   int64_t keep;                      // the first chunk that is kept in the caches; 0: all are
