@@ -1840,6 +1840,15 @@ dprc_status head_blocks(const dprc_head& H, const HeadBufs& b, int64_t v0, int64
   return DPRC_SUCCESS;
 }
 
+// The products that give a piece's nv rows of dW: f(first row, rows, plan) for each.
+template <class F>
+dprc_status head_weight_parts(const dprc_head& H, int64_t nv, F&& f) {
+  const int bf16 = H.dtype == DPRC_BF16;
+  const int64_t whole = head_mul_rounds(nv, H.d, H.B * H.T, bf16);
+  const dprc_status s = f(0, whole, head_mul_plan(whole, H.d, H.B * H.T, bf16));
+  return s != DPRC_SUCCESS || whole == nv ? s : f(whole, nv - whole, head_mul_plan(nv - whole, H.d, H.B * H.T, bf16));
+}
+
 size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_head_norms* norms, void* ws, HeadBufs& b) {
   const size_t e = elem_bytes(H.dtype);
   Arena ar(ws);
@@ -1855,8 +1864,8 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
   // buffers of a shape to ask for sizes with: only their alignment counts
   HeadBufs probe = b;
   probe.rows = probe.E = reinterpret_cast<void*>((uintptr_t)kAlign);
-  const int bf16 = H.dtype == DPRC_BF16;
   if (dh) {
+    const int bf16 = H.dtype == DPRC_BF16;
     b.dh = head_mul_plan(b.N, H.d, b.piece, bf16);
     if (b.dh.S > 1 || b.piece < H.V) b.dh_planes = ar.take<float>((size_t)b.dh.S * b.N * H.d);
   }
@@ -1864,10 +1873,11 @@ size_t head_layout(const dprc_head& H, bool dh, bool dW, bool clip, const dprc_h
   int64_t dW_floats = 0;
   for (const int64_t nv : {b.piece, rest}) {
     if (nv == 0) continue;
-    if (dW) {
-      const int32_t S = head_mul_plan(nv, H.d, b.N, bf16).S;
-      if (S > 1) dW_floats = std::max(dW_floats, S * nv * H.d);
-    }
+    if (dW)
+      head_weight_parts(H, nv, [&](int64_t, int64_t rows, const HeadMulPlan& plan) {
+        if (plan.S > 1) dW_floats = std::max(dW_floats, plan.S * rows * H.d);
+        return DPRC_SUCCESS;
+      });
     if (clip) {
       const dprc_layer L = head_layer(H, probe, 0, nv, 0);
       b.acc_bytes = std::max(b.acc_bytes, dprc_clip_accumulate_workspace(&L));
@@ -2085,20 +2095,19 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
       if (!b.dh_planes) { a.out = dh; a.ldo = lddh; }
       if ((s = multiply(a, v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16), v0, DPRC_KERNEL_HEAD_BACK)) != DPRC_SUCCESS) return s;
     }
-    if (dW) {
-      const HeadMulPlan plan = head_mul_plan(nv, H->d, b.N, bf16);
-      char* out = static_cast<char*>(dW) + v0 * lddw * (int64_t)e;
+    if (!dW) return DPRC_SUCCESS;
+    return head_weight_parts(*H, nv, [&](int64_t r0, int64_t rows, const HeadMulPlan& plan) -> dprc_status {
+      char* out = static_cast<char*>(dW) + (v0 + r0) * lddw * (int64_t)e;
       HeadMulArgs a{};
-      a.A = HeadRows{b.E, b.lde, b.N, nv};
+      a.A = HeadRows{static_cast<const char*>(b.E) + r0 * (int64_t)e, b.lde, b.N, rows};
       a.B = head_rows(*H, b);
-      a.rows = nv; a.cols = H->d; a.K = b.N;
+      a.rows = rows; a.cols = H->d; a.K = b.N;
       a.akr = 1; a.vec_b = 1;
       a.planes = b.dW_planes;
       if (plan.S == 1) { a.out = out; a.ldo = lddw; }
-      if ((s = multiply(a, plan, v0, DPRC_KERNEL_HEAD_WEIGHT)) != DPRC_SUCCESS) return s;
-      if (plan.S > 1 && (s = round(b.dW_planes, plan.S, nv, out, lddw)) != DPRC_SUCCESS) return s;
-    }
-    return DPRC_SUCCESS;
+      const dprc_status s = multiply(a, plan, v0 + r0, DPRC_KERNEL_HEAD_WEIGHT);
+      return s != DPRC_SUCCESS || plan.S == 1 ? s : round(b.dW_planes, plan.S, rows, out, lddw);
+    });
   });
   if (st != DPRC_SUCCESS || !b.dh_planes) return st;
   return round(b.dh_planes, b.dh.S, b.N, dh, lddh);

@@ -842,6 +842,18 @@ HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16) {
   return split_plan(K, want, side, bf16);
 }
 
+// Rows that whole rounds of large tiles over the CUs take; the others, a last round of few tiles otherwise, are a
+// product of their own with a plan of its own.  Errors and dW of 3 rounds and 8, 40, 80, 104, 128 tiles, d 1024, 2048
+// tokens, us with and without: 505, 514, 524, 542, 548 and 540, 536, 541, 548, 550; of 1 round 199, 208, 214, 224, 245 and
+// 222, 216, 218, 222, 225.
+constexpr int64_t kHeadLastRound = 80;
+int64_t head_mul_rounds(int64_t rows, int64_t cols, int64_t K, int bf16) {
+  const HeadMulPlan p = head_mul_plan(rows, cols, K, bf16);
+  const int64_t tm = ceil_div(rows, 256), tn = ceil_div(cols, 256), over = tm * tn % 256;
+  if (!bf16 || p.side != 256 || p.S != 1 || tm * tn < 256 || over > kHeadLastRound) return rows;
+  return std::min(rows, 256 * (tm - ceil_div(over, tn)));
+}
+
 HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16) { return split_plan(K, p.S, p.side, bf16); }
 
 template <bool AKR>

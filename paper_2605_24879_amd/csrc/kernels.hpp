@@ -500,6 +500,7 @@ struct HeadMulPlan {
   int32_t S, side;
 };
 HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16);
+int64_t head_mul_rounds(int64_t rows, int64_t cols, int64_t K, int bf16);
 // of a shorter contraction: the same tiles, at most as many splits
 HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16);
 hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st);

@@ -152,6 +152,15 @@ def test_pieces(D, V, piece, dtype):
     check_backward(D, h, W, target, g, dtype, piece=piece)
 
 
+@pytest.mark.parametrize("T,V", [(70, 66565), (700, 65700)])
+def test_weight_rows_past_whole_rounds_of_tiles(D, T, V):
+    """256 tiles and a few more, whose rows of dW are a product of their own (split and rounded, for 700 tokens), with
+    targets on both sides of the border."""
+    h, W, target, g = make(1, T, 48, V, "bf16", seed=T)
+    target[0, :6] = torch.tensor([65535, 65536, 65537, V - 1, 65535, 0], device="cuda")
+    check_backward(D, h, W, target, g, "bf16")
+
+
 @pytest.mark.parametrize("B,T,d,V,wpad,piece", [(1, 1, 64, 300, 0, 0), (2, 77, 72, 1000, 0, 0), (2, 77, 72, 1000, 3, 0),
                                                 (1, 700, 264, 20000, 0, 8192), (1, 300, 136, 9000, 0, 0), (4, 600, 520, 600, 0, 0)])
 def test_the_targets_entry_enters_to_16_bits(D, B, T, d, V, wpad, piece):
