@@ -572,7 +572,7 @@ typedef enum {
   DPRC_KERNEL_HEAD_SUMS = 29,         /* head: logit tiles' maxima and sums      */
   DPRC_KERNEL_HEAD_JOIN = 30,         /* head: losses and log-sum-exps           */
   DPRC_KERNEL_HEAD_ERRORS = 31,       /* head: E of a piece of the vocabulary    */
-  DPRC_KERNEL_HEAD_BACK = 32,         /* head: E W                               */
+  DPRC_KERNEL_HEAD_BACK = 32,         /* head: E W (for few tokens with E^T h)    */
   DPRC_KERNEL_HEAD_ROWS = 33,         /* head: rows laid out, sums rounded       */
   DPRC_KERNEL_ROTARY = 34,
   DPRC_KERNEL_GRAD_SQUARES = 35,      /* joint norm of many tensors              */

@@ -2065,9 +2065,11 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
   head_layout(*H, dh, dW, false, norms, ws, b);
   const int bf16 = H->dtype == DPRC_BF16;
   // a product's sums in planes, or with one split of all of them in the result; then the planes rounded
-  auto multiply = [&](HeadMulArgs& a, const HeadMulPlan& plan, int64_t v0, int kind) -> dprc_status {
+  auto planned = [&](HeadMulArgs& a, const HeadMulPlan& plan, int64_t v0) {
     a.lo = b.lo; a.target = H->target; a.v0 = v0;
     a.per_split = plan.per_split; a.S = plan.S; a.side = plan.side; a.bf16 = bf16;
+  };
+  auto multiply = [&](const HeadMulArgs& a, int kind) {
     return hip_status(traced(kind, stream, [&] { return launch_head_mul(a, stream); }));
   };
   auto round = [&](const float* planes, int S, int64_t rows, void* out, int64_t ld) {
@@ -2084,28 +2086,37 @@ dprc_status dprc_head_backward(const dprc_head* H, const float* lse, const float
       });
       if (s != DPRC_SUCCESS) return s;
     }
+    HeadMulArgs x{};
+    HeadMulPlan plan_x{};
     if (dh) {                                          // (E's columns behind nv are zeros, and meet none of W's rows)
-      HeadMulArgs a{};
-      a.A = HeadRows{b.E, b.lde, b.N, round_up(nv, 8)};
-      a.B = formed.W;
-      a.rows = b.N; a.cols = H->d; a.K = nv;
-      a.vec_b = formed.vec_w;
-      a.add = v0 > 0;
-      a.planes = b.dh_planes;
-      if (!b.dh_planes) { a.out = dh; a.ldo = lddh; }
-      if ((s = multiply(a, v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16), v0, DPRC_KERNEL_HEAD_BACK)) != DPRC_SUCCESS) return s;
+      x.A = HeadRows{b.E, b.lde, b.N, round_up(nv, 8)};
+      x.B = formed.W;
+      x.rows = b.N; x.cols = H->d; x.K = nv;
+      x.vec_b = formed.vec_w;
+      x.add = v0 > 0;
+      x.planes = b.dh_planes;
+      if (!b.dh_planes) { x.out = dh; x.ldo = lddh; }
+      plan_x = v0 == 0 ? b.dh : head_mul_plan_like(b.dh, nv, bf16);
+      planned(x, plan_x, v0);
     }
-    if (!dW) return DPRC_SUCCESS;
+    if (!dW) return dh ? multiply(x, DPRC_KERNEL_HEAD_BACK) : DPRC_SUCCESS;
     return head_weight_parts(*H, nv, [&](int64_t r0, int64_t rows, const HeadMulPlan& plan) -> dprc_status {
       char* out = static_cast<char*>(dW) + (v0 + r0) * lddw * (int64_t)e;
-      HeadMulArgs a{};
-      a.A = HeadRows{static_cast<const char*>(b.E) + r0 * (int64_t)e, b.lde, b.N, rows};
-      a.B = head_rows(*H, b);
-      a.rows = rows; a.cols = H->d; a.K = b.N;
-      a.akr = 1; a.vec_b = 1;
-      a.planes = b.dW_planes;
-      if (plan.S == 1) { a.out = out; a.ldo = lddw; }
-      const dprc_status s = multiply(a, plan, v0 + r0, DPRC_KERNEL_HEAD_WEIGHT);
+      HeadMulArgs y{};
+      y.A = HeadRows{static_cast<const char*>(b.E) + r0 * (int64_t)e, b.lde, b.N, rows};
+      y.B = head_rows(*H, b);
+      y.rows = rows; y.cols = H->d; y.K = b.N;
+      y.akr = 1; y.vec_b = 1;
+      y.planes = b.dW_planes;
+      if (plan.S == 1) { y.out = out; y.ldo = lddw; }
+      planned(y, plan, v0 + r0);
+      dprc_status s = DPRC_SUCCESS;
+      if (dh && r0 == 0 && head_mul_pairs(plan_x, plan)) {
+        s = hip_status(traced(DPRC_KERNEL_HEAD_BACK, stream, [&] { return launch_head_pair(x, y, stream); }));
+      } else {
+        if (dh && r0 == 0) s = multiply(x, DPRC_KERNEL_HEAD_BACK);
+        if (s == DPRC_SUCCESS) s = multiply(y, DPRC_KERNEL_HEAD_WEIGHT);
+      }
       return s != DPRC_SUCCESS || plan.S == 1 ? s : round(b.dW_planes, plan.S, rows, out, lddw);
     });
   });

@@ -625,7 +625,20 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   }
 }
 
-// Tiles of A B, blockIdx.z the split of the contraction.  B's rows are the contraction's; so are A's with AKR.
+// A tile of A B, of one split of the contraction.  B's rows are the contraction's; so are A's with AKR.
+template <class TL, bool AKR, bool VB>
+__device__ __forceinline__ void head_mul(const HeadMulArgs& a, int64_t tm, int64_t tn, int split, typename TL::elem* la0,
+                                         typename TL::elem* la1, typename TL::elem* lb0, typename TL::elem* lb1) {
+  const int64_t k0 = split * a.per_split, k1 = min(a.K, k0 + a.per_split);
+  f32x16_t acc[TL::XB][TL::YB];
+  head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
+                   HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
+  if constexpr (sizeof(typename TL::elem) == 2)
+    head_targets<TL, AKR, VB>(a, split, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
+  head_store<TL>(a, split, tm * TL::MT, tn * TL::NT, acc);
+}
+
+// blockIdx.z the split.
 template <class TL, bool AKR, bool VB>
 __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
   DPRC_HEAD_SLABS(TL);
@@ -634,13 +647,31 @@ __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
   if (wg >= tm_n * tn_n) return;
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
-  const int64_t k0 = blockIdx.z * a.per_split, k1 = min(a.K, k0 + a.per_split);
-  f32x16_t acc[TL::XB][TL::YB];
-  head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
-                   HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
-  if constexpr (sizeof(typename TL::elem) == 2)
-    head_targets<TL, AKR, VB>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
-  head_store<TL>(a, blockIdx.z, tm * TL::MT, tn * TL::NT, acc);
+  head_mul<TL, AKR, VB>(a, tm, tn, blockIdx.z, la0, la1, lb0, lb1);
+}
+
+// dh and dW in one launch, the tiles of every split of x, then those of y, where neither has tiles enough to fill the CUs
+// for long.  Gradients of N x d x V = 150 x 136 x 1009, 200 x 512 x 8000, 2000 x 512 x 8000 bf16 19, 33, 108 us, in two
+// launches 25, 44, 141; fp32 24, 75, 422 and 30, 84, 421.
+template <class TX, class TY, bool VB>
+__global__ __launch_bounds__(TY::threads) void head_pair_kernel(HeadMulArgs x, HeadMulArgs y) {
+  static_assert(TX::threads == TY::threads && TX::MT <= TY::MT && TX::NT <= TY::NT);
+  DPRC_HEAD_SLABS(TY);
+  auto tile = [&](auto t, const HeadMulArgs& a, int64_t wg, auto f) __attribute__((always_inline)) {
+    typedef decltype(t) TL;
+    const int64_t tm_n = (a.rows + TL::MT - 1) / TL::MT, tn_n = (a.cols + TL::NT - 1) / TL::NT, tiles = tm_n * tn_n;
+    if (wg >= tiles * a.S) return wg - tiles * a.S;
+    const int split = (int)(wg / tiles);
+    int64_t tm, tn;
+    tile_of(wg - split * tiles, tm_n, tn_n, tm, tn);
+    f(tm, tn, split);
+    return (int64_t)-1;
+  };
+  const int64_t wg = tile(TX{}, x, flat_block(), [&](int64_t tm, int64_t tn, int split) __attribute__((always_inline)) {
+    head_mul<TX, false, VB>(x, tm, tn, split, la0, la1, lb0, lb1); });
+  if (wg >= 0)
+    tile(TY{}, y, wg, [&](int64_t tm, int64_t tn, int split) __attribute__((always_inline)) {
+      head_mul<TY, true, true>(y, tm, tn, split, la0, la1, lb0, lb1); });
 }
 
 // Joins the tiles' maxima and sums in a fixed order and takes the target's logit, summed in fp32.  TPB tokens per
@@ -880,6 +911,23 @@ static void launch_mul(const HeadMulArgs& a, hipStream_t st) {
 hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st) {
   if (a.akr) launch_mul<true>(a, st);
   else launch_mul<false>(a, st);
+  return hipGetLastError();
+}
+
+bool head_mul_pairs(const HeadMulPlan& x, const HeadMulPlan& y) { return x.side == 64 && y.side <= 128; }
+
+hipError_t launch_head_pair(HeadMulArgs x, HeadMulArgs y, hipStream_t st) {
+  auto go = [&](auto tx, auto ty) {
+    typedef decltype(tx) TX;
+    typedef decltype(ty) TY;
+    const int64_t blocks = ceil_div(x.rows, TX::MT) * ceil_div(x.cols, TX::NT) * x.S + ceil_div(y.rows, TY::MT) * ceil_div(y.cols, TY::NT) * y.S;
+    if (x.vec_b) DPRC_LAUNCH((head_pair_kernel<TX, TY, true>), flat_grid(blocks), dim3(TY::threads), 0, st, x, y);
+    else DPRC_LAUNCH((head_pair_kernel<TX, TY, false>), flat_grid(blocks), dim3(TY::threads), 0, st, x, y);
+  };
+  if (x.bf16 && y.side == 128) go(TileSmall{}, TileMid{});
+  else if (x.bf16) go(TileSmall{}, TileSmall{});
+  else if (y.side == 128) go(TileSmallF32{}, TileMidF32{});
+  else go(TileSmallF32{}, TileSmallF32{});
   return hipGetLastError();
 }
 

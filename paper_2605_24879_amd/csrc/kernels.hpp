@@ -504,6 +504,8 @@ int64_t head_mul_rounds(int64_t rows, int64_t cols, int64_t K, int bf16);
 // of a shorter contraction: the same tiles, at most as many splits
 HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16);
 hipError_t launch_head_mul(HeadMulArgs a, hipStream_t st);
+bool head_mul_pairs(const HeadMulPlan& x, const HeadMulPlan& y);   // whether dh and dW go in one launch
+hipError_t launch_head_pair(HeadMulArgs x, HeadMulArgs y, hipStream_t st);
 hipError_t launch_head_rows(const HeadRows& X, int bf16, const int64_t* target, void* out, int64_t ldo, hipStream_t st);
 hipError_t launch_head_round(const float* planes, int S, int64_t rows, int64_t cols, int bf16, void* out, int64_t ldo,
                              hipStream_t st);

@@ -128,6 +128,17 @@ def test_backward(D, B, T, d, V, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V,wpad", [(150, 136, 1009, 0), (40, 72, 900, 3), (900, 264, 3000, 0), (700, 520, 12000, 1)])
+def test_gradients_alone(D, T, d, V, wpad, dtype):
+    """dh and dW by themselves are those of the call for both."""
+    h, W, target, g = make(2, T, d, V, dtype, seed=T, wpad=wpad)
+    lse = D.dprc_head_loss(h, W, target)[1]
+    dh, dW = D.dprc_head_backward(h, W, target, lse, g)
+    assert torch.equal(D.dprc_head_backward(h, W, target, lse, g, weight_grad=False)[0], dh)
+    assert torch.equal(D.dprc_head_backward(h, W, target, lse, g, hidden_grad=False)[1], dW)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("pad,wpad,d", [(3, 0, 128), (8, 8, 128), (0, 5, 64), (1, 1, 131), (0, 0, 131), (4, 4, 132)])
 def test_strides(D, pad, wpad, d, dtype):
     h, W, target, g = make(2, 90, d, 600, dtype, seed=pad, pad=pad, wpad=wpad)
