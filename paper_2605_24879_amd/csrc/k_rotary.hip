@@ -6,7 +6,7 @@
 // Bounded by memory, or by a launch's latency for the few tokens of a serving step.  A workgroup takes whole
 // tokens: their cosines and sines are made once for all heads of all tensors and kept in LDS.
 // The angle is reduced to a fraction of a turn in 64 bits (in 32 a position of 10^6 would lose 0.06 of a
-// radian); sine and cosine of the fraction are taken in 32.
+// radian), to an eighth of a turn beside whole quarters; sine and cosine of that are taken in 32.
 // A thread takes eight pairs at a time, two 16-byte loads of bfloat16; the r mod 8 pairs left at the end of a head go as
 // 4, 2 and 1 (one at a time: 138 us for 16+4 heads of 96 with r 13 and 2^16 tokens, so 112).  32 + 8 heads of 64
 // bfloat16 features, 2^15 tokens: 72 us, 4.6 TB/s; with non-temporal loads and stores 77.  A step of 64 tokens: 3.6 us.
@@ -147,8 +147,11 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const double pos = (double)(a.pos ? a.pos[t] : a.start + t % a.T);
     double turns = pos * a.freqs[s - k * r] * 0.15915494309189533577;
     turns -= rint(turns);
-    float sn, c;
-    sincospif(2.f * (float)turns, &sn, &c);
+    const double quarter = rint(4.0 * turns);            // an eighth of a turn at most is left to round to 32 bits
+    float u, v;
+    sincospif(2.f * (float)(turns - 0.25 * quarter), &u, &v);
+    const int n = (int)quarter & 3;
+    const float sn = n == 0 ? u : n == 1 ? v : n == 2 ? -u : -v, c = n == 0 ? v : n == 1 ? -u : n == 2 ? -v : u;
     cs[s] = float2{a.scale * c, a.inverse ? -a.scale * sn : a.scale * sn};
   }
   __syncthreads();
