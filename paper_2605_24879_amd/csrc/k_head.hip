@@ -457,7 +457,7 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
 
 // ---- the target's entries to 16 bits ---------------------------------------------------------------
 // E_t,y(t) = g_t (p - 1) is by far the largest entry of most rows, and tokens of one sample share g: its rounding
-// to bf16 would be an error of up to 2^-9 of dh_t, and of a row of dW alike, in one direction for whole samples (an
+// to bf16 would be an error of up to 2^-8 of dh_t, and of a row of dW alike, in one direction for whole samples (an
 // error of 0.0022 to 0.0028 of all of dh and dW where the results' own rounding is 0.0017).  What it loses, lo_t, joins
 // the products as slabs of their own, formed in LDS:
 //   dh:  64 tokens of the tile at a time, A their diagonal of lo_t, B the rows W_y(t);
