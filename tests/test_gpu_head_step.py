@@ -215,3 +215,30 @@ def test_a_captured_pass(mods):
         # the embedding's gradient adds with atomics
         for (name, _), a, b in zip(model.named_parameters(), got[1:], want[1:]):
             assert torch.equal(a, b) or (name == "embed.weight" and (a - b).abs().max() <= 0.02 * b.abs().max()), name
+
+
+def test_launches_are_traced(mods):
+    from test_gpu_trace import _trace
+    D = mods[0]
+    bf = lambda *s: torch.randn(*s, device="cuda").bfloat16()
+    tokens = lambda T, V: torch.randint(0, V, (1, T), device="cuda")
+    ones = lambda T: torch.ones(1, T, device="cuda")
+    small, large = torch.randn(100, device="cuda"), torch.randn(100000, device="cuda")
+
+    def back(T, d, V, **kw):
+        h, W, y = bf(1, T, d), bf(V, d) * 0.1, tokens(T, V)
+        lse = D.dprc_head_loss(h, W, y)[1]
+        return lambda: D.dprc_head_backward(h, W, y, lse, ones(T), **kw)
+    for call, kinds in (
+            (lambda: D.dprc_head_loss(bf(1, 9, 64), bf(300, 64), tokens(9, 300)), ["head_sums", "head_join"]),
+            (lambda: D.dprc_head_loss(bf(1, 9, 65), bf(300, 65), tokens(9, 300)), ["head_rows", "head_sums", "head_join"]),
+            (back(40, 64, 500, hidden_grad=False), ["head_rows", "head_errors", "head_weight"]),
+            (back(40, 64, 200, weight_grad=False), ["head_rows", "head_errors", "head_back"]),
+            (back(40, 64, 200), ["head_rows", "head_errors", "head_back"]),                        # one launch for both
+            (back(40, 64, 50000), ["head_rows", "head_errors", "head_back", "head_weight", "head_rows"]),
+            (lambda: D.dprc_rotary([bf(1, 5, 2, 8), bf(1, 5, 1, 8)], torch.ones(4, dtype=torch.float64, device="cuda")), ["rotary"]),
+            (lambda: D.dprc_grad_clip([small], 1.0), ["grad_scale"]),
+            (lambda: D.dprc_grad_clip([large, small], 1.0), ["grad_squares", "grad_scale"]),
+            (lambda: D.dprc_grad_norm([small]), ["grad_squares", "grad_squares"])):
+        names, ms = _trace(D, call)
+        assert names == kinds and all(0 < m < 1000 for m in ms), (names, kinds)
