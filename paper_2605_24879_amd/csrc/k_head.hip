@@ -795,6 +795,16 @@ static int tile_side(int64_t m, int64_t n, int bf16) {
   return ceil_div(m, 128) * ceil_div(n, 128) >= 192 ? 128 : 64;
 }
 
+// Rows of an m x n result that whole rounds of 256 x 256 tiles over the CUs take, or all of them where the last round is not
+// nearly empty (they are then launches of their own, of smaller tiles).  3 rounds and 8, 40, 80, 104, 128 tiles, 2048 tokens,
+// us with and without: d 2048, loss 189, 194, 200, 210, 211 and 206, 207, 209, 210, 211, errors and dW 452, 468, 491, 505, 510 and
+// 491, 493, 502, 520, 502; d 1024, loss 192, 198, 206, 205, 210 and 200, 200, 202, 208, 208.
+constexpr int64_t kHeadLastRound = 80;
+static int64_t whole_rounds(int64_t m, int64_t n) {
+  const int64_t tm = ceil_div(m, 256), tn = ceil_div(n, 256), last = ceil_div(tm * tn % 256, tn);   // rows of tiles
+  return tm * tn < 256 || last * tn > kHeadLastRound || (tm - last) * tn < 192 ? m : std::min(m, 256 * (tm - last));
+}
+
 // Up to 64 tokens (32 in fp32) of a large vocabulary: tiles of all tokens and 256 rows of W, which bounds the call and
 // is read past the caches.  64 tokens of 128256 x 2048 bf16 114 us (525 MB); with three and four slabs of loads under
 // way and one such workgroup a CU 115, with every wave reading rows of its own into registers 313.
@@ -807,8 +817,19 @@ static int logits_side(int64_t N, int64_t nv, int bf16) {
   return bf16 ? (N <= 128 ? std::min(side, 128) : side) : (N <= 64 ? 64 : side);
 }
 
+// Columns that whole rounds of large tiles over the CUs take; a last round of few tiles is a launch of its own, of smaller
+// ones.
+static int64_t logits_rounds(int64_t N, int64_t nv, int bf16) {
+  return logits_side(N, nv, bf16) == 256 ? whole_rounds(nv, N) : nv;
+}
+
+static int64_t logits_tiles(int64_t N, int64_t nv, int bf16) {
+  const int side = logits_side(N, nv, bf16);
+  return ceil_div(nv, side == 0 ? 256 : side);
+}
+
 template <bool ERRORS>
-static hipError_t launch_head_logits(const HeadArgs& a, hipStream_t st) {
+static void launch_logits_part(const HeadArgs& a, hipStream_t st) {
   auto tiles = [&](auto tile) {
     typedef decltype(tile) TL;
     const dim3 grid = flat_grid(ceil_div(a.nv, TL::MT) * ceil_div(a.N, TL::NT));
@@ -826,13 +847,31 @@ static hipError_t launch_head_logits(const HeadArgs& a, hipStream_t st) {
     else if (side == 128) tiles(TileMidF32{});
     else tiles(TileSmallF32{});
   }
+}
+
+template <bool ERRORS>
+static hipError_t launch_head_logits(const HeadArgs& all, hipStream_t st) {
+  const int64_t whole = logits_rounds(all.N, all.nv, all.bf16), e = all.bf16 ? 2 : 4;
+  HeadArgs a = all;
+  if (whole < all.nv) {
+    a.nv = a.W.rows = a.width = whole;
+    launch_logits_part<ERRORS>(a, st);
+    a = all;
+    a.nv = a.W.rows = all.nv - whole;
+    a.v0 += whole;
+    a.width -= whole;
+    a.W.p = static_cast<const char*>(a.W.p) + whole * a.W.ld * e;
+    if (ERRORS) a.E = static_cast<char*>(a.E) + whole * e;
+    else a.part += logits_tiles(a.N, whole, a.bf16) * a.N;
+  }
+  launch_logits_part<ERRORS>(a, st);
   return hipGetLastError();
 }
 
 // tiles of the vocabulary that the sums leave
 int64_t head_sum_tiles(int64_t N, int64_t nv, int bf16) {
-  const int side = logits_side(N, nv, bf16);
-  return ceil_div(nv, side == 0 ? 256 : side);
+  const int64_t whole = logits_rounds(N, nv, bf16);
+  return logits_tiles(N, whole, bf16) + (whole < nv ? logits_tiles(N, nv - whole, bf16) : 0);
 }
 
 hipError_t launch_head_sums(const HeadArgs& a, hipStream_t st) { return launch_head_logits<false>(a, st); }
@@ -876,16 +915,10 @@ HeadMulPlan head_mul_plan(int64_t rows, int64_t cols, int64_t K, int bf16) {
   return split_plan(K, want, side, bf16);
 }
 
-// Rows that whole rounds of large tiles over the CUs take; the others, a last round of few tiles otherwise, are a
-// product of their own with a plan of its own.  Errors and dW of 3 rounds and 8, 40, 80, 104, 128 tiles, d 1024, 2048
-// tokens, us with and without: 505, 514, 524, 542, 548 and 540, 536, 541, 548, 550; of 1 round 199, 208, 214, 224, 245 and
-// 222, 216, 218, 222, 225.
-constexpr int64_t kHeadLastRound = 80;
+// Rows that go with whole rounds of large tiles; the others are a product of their own with a plan of its own.
 int64_t head_mul_rounds(int64_t rows, int64_t cols, int64_t K, int bf16) {
   const HeadMulPlan p = head_mul_plan(rows, cols, K, bf16);
-  const int64_t tm = ceil_div(rows, 256), tn = ceil_div(cols, 256), over = tm * tn % 256;
-  if (!bf16 || p.side != 256 || p.S != 1 || tm * tn < 256 || over > kHeadLastRound) return rows;
-  return std::min(rows, 256 * (tm - ceil_div(over, tn)));
+  return bf16 && p.side == 256 && p.S == 1 ? whole_rounds(rows, cols) : rows;
 }
 
 HeadMulPlan head_mul_plan_like(const HeadMulPlan& p, int64_t K, int bf16) { return split_plan(K, p.S, p.side, bf16); }

@@ -83,17 +83,21 @@ SHAPES = [(1, 1, 1, 1), (1, 1, 8, 2), (2, 3, 5, 7), (1, 1, 64, 300), (2, 37, 72,
           (65, 1, 200, 513), (1, 300, 129, 777), (2, 130, 320, 2050), (1, 257, 1030, 260)]
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("B,T,d,V", SHAPES)
-def test_loss(D, B, T, d, V, dtype):
-    h, W, target, _ = make(B, T, d, V, dtype, seed=V)
+def check_loss(D, h, W, target):
     loss, lse = D.dprc_head_loss(h, W, target)
     hn, Wn, tn = f64(h), f64(W), target.cpu().numpy()
     rl, rz = O.loss(hn, Wn, tn)
     big = np.abs(hn @ Wn.T).max(-1)
-    tz = delta(hn, Wn) + 8 * U * big + (170 + V / 128) * U + 4 * U * np.abs(rz)
+    tz = delta(hn, Wn) + 8 * U * big + (170 + W.shape[0] / 128) * U + 4 * U * np.abs(rz)
     within(lse, rz, tz, "lse")
     within(loss, rl, np.where(tn < 0, 0.0, tz + delta(hn, Wn) + 2 * U * (np.abs(rz) + big)), "loss")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,d,V", SHAPES)
+def test_loss(D, B, T, d, V, dtype):
+    h, W, target, _ = make(B, T, d, V, dtype, seed=V)
+    check_loss(D, h, W, target)
 
 
 def check_backward(D, h, W, target, g, dtype, **kw):
@@ -164,11 +168,13 @@ def test_pieces(D, V, piece, dtype):
 
 
 @pytest.mark.parametrize("T,V", [(70, 66565), (700, 65700)])
-def test_weight_rows_past_whole_rounds_of_tiles(D, T, V):
-    """256 tiles and a few more, whose rows of dW are a product of their own (split and rounded, for 700 tokens), with
-    targets on both sides of the border."""
+def test_rows_past_whole_rounds_of_tiles(D, T, V):
+    """Rounds of 256 tiles and a few more, whose rows of W are products of their own (dW's for 70 tokens; the logits' and
+    dW's, split and rounded, for 700), with targets on both sides of the border and the largest logits past it."""
     h, W, target, g = make(1, T, 48, V, "bf16", seed=T)
+    W[65500:] *= 3
     target[0, :6] = torch.tensor([65535, 65536, 65537, V - 1, 65535, 0], device="cuda")
+    check_loss(D, h, W, target)
     check_backward(D, h, W, target, g, "bf16")
 
 
