@@ -39,10 +39,11 @@ __device__ __forceinline__ void tile_of(int64_t wg, int64_t tm_n, int64_t tn_n, 
 // Accumulators as the 32 x 32 MFMAs hold them: WM x WN waves of XB x YB blocks; lane l of block (x, y) has
 // rows 8 (q / 4) + 4 (l / 32) + q % 4, q < 16, of column l % 32.
 
-template <class E, int WM_, int WN_, int XB_, int YB_>
+template <class E, int WM_, int WN_, int XB_, int YB_, int RING = 2>
 struct HeadTile {
   typedef E elem;
   static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_;
+  static constexpr int ring = RING;                     // slabs in LDS
   static constexpr int MT = 32 * XB * WM, NT = 32 * YB * WN, threads = 64 * WM * WN;
   static constexpr int EP = kPiece<E>;                  // elements of a 16-byte piece
   static constexpr int slab = 8 * EP;                   // contraction elements of a slab: 64 bf16, 32 fp32
@@ -86,6 +87,21 @@ __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, void* lds,
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_void_t*)lds, 16, (int)off, 0, 0, NT ? kCachePolicyNT : 0);
 }
 
+// A workgroup's slabs, an array each: the compiler then knows that loads into one do not reach reads of another, and does
+// not wait for them.
+template <class TL>
+struct HeadLds {
+  typename TL::elem *a[TL::ring], *b[TL::ring];
+};
+template <class TL>
+__device__ __forceinline__ HeadLds<TL> head_lds(typename TL::elem* a0, typename TL::elem* a1, typename TL::elem* a2,
+                                                typename TL::elem* a3, typename TL::elem* b0, typename TL::elem* b1,
+                                                typename TL::elem* b2, typename TL::elem* b3) {
+  if constexpr (TL::ring == 2) return HeadLds<TL>{{a0, a1}, {b0, b1}};
+  else if constexpr (TL::ring == 3) return HeadLds<TL>{{a0, a1, a2}, {b0, b1, b2}};
+  else return HeadLds<TL>{{a0, a1, a2, a3}, {b0, b1, b2, b3}};
+}
+
 template <int V>
 struct HInt {
   static constexpr int value = V;
@@ -98,6 +114,7 @@ template <class TL, int T, bool KR, bool VEC, bool NT = false>
 struct HeadOperand {
   typedef typename TL::elem E;
   static constexpr int EP = TL::EP, P = T * 8 / TL::threads, RP = T / EP;    // pieces of a thread; of a KR row
+  static constexpr bool direct = VEC;
   static_assert(T * 8 % TL::threads == 0);
   const HeadRows& X;
   int64_t t0;
@@ -134,7 +151,7 @@ struct HeadOperand {
       for (int r = 0; r < P; ++r) load_to_lds<NT>(r0, lds + EP * (wave0 + TL::threads * r), off[r]);
     } else if constexpr (VEC) {
       const __amdgpu_buffer_rsrc_t r0 = rsrc(t0, T, k);
-      if (k + TL::slab > X.width) {                      // columns past the rows' end
+      if (TL::ring > 2 || k + TL::slab > X.width) {      // columns past the rows' end
 #pragma unroll
         for (int r = 0; r < P; ++r)
           load_to_lds<NT>(r0, lds + EP * (wave0 + TL::threads * r),
@@ -204,32 +221,37 @@ __device__ __forceinline__ void head_mfma(const uint4 (&av)[XB], const uint4 (&b
 }
 
 // acc = sum over k in [k0, k1) of A[i][k] B[j][k], i and j the tile's rows and columns; k0 a multiple of the
-// slab.  fp32 products and sums (bf16 products are exact).  Slabs are double-buffered: while one is
-// multiplied the next is loaded.  A wave has the next fragments in registers ahead of their products, also
-// across the slab's one barrier, and reads and products are issued in turn.  Four LDS arrays and not one: the
-// compiler then knows that loads into one do not reach reads of another, and does not wait for them.
+// slab.  fp32 products and sums (bf16 products are exact).  While a slab is multiplied the next TL::ring - 1 are
+// on their way.  A wave has the next fragments in registers ahead of their products, also
+// across the slab's one barrier, and reads and products are issued in turn.
 // bf16, 256 x 256 tiles of 128000 x 8192 x 2048: 1330 TFLOP/s (the same loop as the compiler orders it 1146, all
 // reads before all products 1270, four waves of 128 x 128 1217, tiles of 128 x 128 1093).
 template <class TL, class OA, class OB>
 __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1, f32x16_t (&acc)[TL::XB][TL::YB],
-                                             typename TL::elem* la0, typename TL::elem* la1, typename TL::elem* lb0,
-                                             typename TL::elem* lb1) {
+                                             const HeadLds<TL>& lds) {
   typedef typename TL::elem E;
-  constexpr int XB = TL::XB, YB = TL::YB;
+  constexpr int XB = TL::XB, YB = TL::YB, RING = TL::ring;
+  // loads that may still be under way when a slab is needed (all of them wait where a register is between)
+  constexpr int later = OA::direct && OB::direct ? (RING - 2) * (OA::P + OB::P) : 0;
+  static_assert(later < 64 && (RING == 2 || (OA::direct && OB::direct)));
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int wm = wv / TL::WN, wn = wv % TL::WN;
   auto gload = [&](int64_t k, auto u) __attribute__((always_inline)) {
-    A.load(k, decltype(u)::value ? la1 : la0);
-    B.load(k, decltype(u)::value ? lb1 : lb0);
+    A.load(k < k1 ? k : (int64_t)1 << 40, lds.a[decltype(u)::value]);      // past the end: zeros
+    B.load(k < k1 ? k : (int64_t)1 << 40, lds.b[decltype(u)::value]);
   };
-  // what went through registers to LDS, then every wave's slab is there and the other's reads are done
+  // what went through registers to LDS, then every wave's slab is there and the reads of the one before it are done
   auto arrive = [&](auto u) __attribute__((always_inline)) {
-    A.arrive(decltype(u)::value ? la1 : la0);
-    B.arrive(decltype(u)::value ? lb1 : lb0);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
-    __builtin_amdgcn_s_waitcnt(0);
-    __builtin_amdgcn_s_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    A.arrive(lds.a[decltype(u)::value]);
+    B.arrive(lds.b[decltype(u)::value]);
+    if constexpr (later > 0) {
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(later) : "memory");
+    } else {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+      __builtin_amdgcn_s_waitcnt(0);
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+    }
   };
 #pragma unroll
   for (int x = 0; x < XB; ++x)
@@ -239,8 +261,8 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
       for (int q = 0; q < 16; ++q) acc[x][y][q] = 0.f;
   uint4 f0a[XB], f0b[YB], f1a[XB], f1b[YB];
   auto frag = [&](uint4 (&av)[XB], uint4 (&bv)[YB], auto u, int ks) __attribute__((always_inline)) {
-    const E* la = decltype(u)::value ? la1 : la0;
-    const E* lb = decltype(u)::value ? lb1 : lb0;
+    const E* la = lds.a[decltype(u)::value];
+    const E* lb = lds.b[decltype(u)::value];
 #pragma unroll
     for (int y = 0; y < YB; ++y) bv[y] = OB::frag(lb, 32 * (wn * YB + y), ks, lane);
 #pragma unroll
@@ -261,23 +283,28 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
   };
   // the slab at k in buffers u, its first fragments in registers
   auto step = [&](int64_t k, auto u) __attribute__((always_inline)) {
-    constexpr HInt<decltype(u)::value ^ 1> other{};
-    gload(k + TL::slab < k1 ? k + TL::slab : (int64_t)1 << 40, other);     // past the end: zeros
+    constexpr HInt<(decltype(u)::value + 1) % RING> next{};
+    gload(k + (RING - 1) * TL::slab, HInt<(decltype(u)::value + RING - 1) % RING>{});
     __builtin_amdgcn_sched_barrier(0);
     phase(f1a, f1b, u, 1, f0a, f0b);
     phase(f0a, f0b, u, 2, f1a, f1b);
     phase(f1a, f1b, u, 3, f0a, f0b);
-    arrive(other);
-    phase(f0a, f0b, other, 0, f1a, f1b);
+    arrive(next);
+    phase(f0a, f0b, next, 0, f1a, f1b);
   };
   gload(k0, HInt<0>{});
+  if constexpr (RING > 2) gload(k0 + TL::slab, HInt<1>{});
+  if constexpr (RING > 3) gload(k0 + 2 * TL::slab, HInt<2>{});
   arrive(HInt<0>{});
   frag(f0a, f0b, HInt<0>{}, 0);
-  for (int64_t k = k0; k < k1; k += 2 * TL::slab) {  // (an odd number of slabs: the last one is zeros)
+  for (int64_t k = k0; k < k1; k += RING * TL::slab) {  // (slabs past the end: zeros)
     step(k, HInt<0>{});
     step(k + TL::slab, HInt<1>{});
+    if constexpr (RING > 2) step(k + 2 * TL::slab, HInt<2>{});
+    if constexpr (RING > 3) step(k + 3 * TL::slab, HInt<3>{});
   }
-  __syncthreads();                                     // all reads are done
+  if constexpr (later > 0) __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();                                     // all loads have arrived, all reads are done
 }
 
 // ---- what becomes of a tile -----------------------------------------------------------------------
@@ -595,16 +622,22 @@ __device__ __forceinline__ void head_store(const HeadMulArgs& a, int split, int6
 
 // ---- kernels --------------------------------------------------------------------------------------
 
-#define DPRC_HEAD_SLABS(TL)                                                                     \
-  __shared__ __attribute__((aligned(16))) typename TL::elem la0[TL::MT * TL::slab];             \
-  __shared__ __attribute__((aligned(16))) typename TL::elem la1[TL::MT * TL::slab];             \
-  __shared__ __attribute__((aligned(16))) typename TL::elem lb0[TL::NT * TL::slab];             \
-  __shared__ __attribute__((aligned(16))) typename TL::elem lb1[TL::NT * TL::slab]
+// arrays for slabs of MT rows and NT columns, two or four of each
+#define DPRC_HEAD_SLABS(E, MT, NT, SLAB, RING)                                        \
+  __shared__ __attribute__((aligned(16))) E la0[MT * SLAB];                           \
+  __shared__ __attribute__((aligned(16))) E la1[MT * SLAB];                           \
+  __shared__ __attribute__((aligned(16))) E la2[RING > 2 ? MT * SLAB : 8];            \
+  __shared__ __attribute__((aligned(16))) E la3[RING > 3 ? MT * SLAB : 8];            \
+  __shared__ __attribute__((aligned(16))) E lb0[NT * SLAB];                           \
+  __shared__ __attribute__((aligned(16))) E lb1[NT * SLAB];                           \
+  __shared__ __attribute__((aligned(16))) E lb2[RING > 2 ? NT * SLAB : 8];            \
+  __shared__ __attribute__((aligned(16))) E lb3[RING > 3 ? NT * SLAB : 8]
+#define DPRC_HEAD_LDS(TL) head_lds<TL>(la0, la1, la2, la3, lb0, lb1, lb2, lb3)
 
 // The logits' tiles.  Rows of W in 16-byte pieces (VW) or at any alignment; h always in pieces.
 template <class TL, bool ERRORS, bool VW>
 __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
-  DPRC_HEAD_SLABS(TL);
+  DPRC_HEAD_SLABS(typename TL::elem, TL::MT, TL::NT, TL::slab, TL::ring);
   const int64_t tm_n = (a.nv + TL::MT - 1) / TL::MT, tn_n = (a.N + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
   if (wg >= tm_n * tn_n) return;
@@ -614,7 +647,7 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
   constexpr bool STREAM = TL::NT < TL::MT;              // few tokens: every row of W is read once
   auto product = [&] {
     head_product<TL>(HeadOperand<TL, TL::MT, false, VW, STREAM>(a.W, tm * TL::MT),
-                     HeadOperand<TL, TL::NT, false, true>(a.h, tn * TL::NT), 0, a.W.width, acc, la0, la1, lb0, lb1);
+                     HeadOperand<TL, TL::NT, false, true>(a.h, tn * TL::NT), 0, a.W.width, acc, DPRC_HEAD_LDS(TL));
   };
   if constexpr (ERRORS) {
     const HeadTokens<TL> tok(a, tn * TL::NT);
@@ -628,27 +661,26 @@ __global__ __launch_bounds__(TL::threads) void head_logits_kernel(HeadArgs a) {
 
 // A tile of A B, of one split of the contraction.  B's rows are the contraction's; so are A's with AKR.
 template <class TL, bool AKR, bool VB>
-__device__ __forceinline__ void head_mul(const HeadMulArgs& a, int64_t tm, int64_t tn, int split, typename TL::elem* la0,
-                                         typename TL::elem* la1, typename TL::elem* lb0, typename TL::elem* lb1) {
+__device__ __forceinline__ void head_mul(const HeadMulArgs& a, int64_t tm, int64_t tn, int split, const HeadLds<TL>& lds) {
   const int64_t k0 = split * a.per_split, k1 = min(a.K, k0 + a.per_split);
   f32x16_t acc[TL::XB][TL::YB];
   head_product<TL>(HeadOperand<TL, TL::MT, AKR, true>(a.A, tm * TL::MT),
-                   HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, la0, la1, lb0, lb1);
+                   HeadOperand<TL, TL::NT, true, VB>(a.B, tn * TL::NT), k0, k1, acc, lds);
   if constexpr (sizeof(typename TL::elem) == 2)
-    head_targets<TL, AKR, VB>(a, split, tm * TL::MT, tn * TL::NT, k0, k1, acc, la0, la1, lb0);
+    head_targets<TL, AKR, VB>(a, split, tm * TL::MT, tn * TL::NT, k0, k1, acc, lds.a[0], lds.a[1], lds.b[0]);
   head_store<TL>(a, split, tm * TL::MT, tn * TL::NT, acc);
 }
 
 // blockIdx.z the split.
 template <class TL, bool AKR, bool VB>
 __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
-  DPRC_HEAD_SLABS(TL);
+  DPRC_HEAD_SLABS(typename TL::elem, TL::MT, TL::NT, TL::slab, TL::ring);
   const int64_t tm_n = (a.rows + TL::MT - 1) / TL::MT, tn_n = (a.cols + TL::NT - 1) / TL::NT;
   const int64_t wg = flat_block();
   if (wg >= tm_n * tn_n) return;
   int64_t tm, tn;
   tile_of(wg, tm_n, tn_n, tm, tn);
-  head_mul<TL, AKR, VB>(a, tm, tn, blockIdx.z, la0, la1, lb0, lb1);
+  head_mul<TL, AKR, VB>(a, tm, tn, blockIdx.z, DPRC_HEAD_LDS(TL));
 }
 
 // dh and dW in one launch, the tiles of every split of x, then those of y: neither's last round leaves CUs idle.  Gradients
@@ -656,9 +688,9 @@ __global__ __launch_bounds__(TL::threads) void head_mul_kernel(HeadMulArgs a) {
 // 24, 75, 412 and 30, 84, 425.
 template <class TX, class TY, bool VB>
 __global__ __launch_bounds__(TY::threads) void head_pair_kernel(HeadMulArgs x, HeadMulArgs y) {
-  static_assert(TX::threads == TY::threads);
+  static_assert(TX::threads == TY::threads && TX::ring == TY::ring);
   typedef typename std::conditional<(TX::MT > TY::MT), TX, TY>::type TL;
-  DPRC_HEAD_SLABS(TL);
+  DPRC_HEAD_SLABS(typename TL::elem, TL::MT, TL::NT, TL::slab, TL::ring);
   auto tile = [&](auto t, const HeadMulArgs& a, int64_t wg, auto f) __attribute__((always_inline)) {
     typedef decltype(t) TL;
     const int64_t tm_n = (a.rows + TL::MT - 1) / TL::MT, tn_n = (a.cols + TL::NT - 1) / TL::NT, tiles = tm_n * tn_n;
@@ -670,10 +702,10 @@ __global__ __launch_bounds__(TY::threads) void head_pair_kernel(HeadMulArgs x, H
     return (int64_t)-1;
   };
   const int64_t wg = tile(TX{}, x, flat_block(), [&](int64_t tm, int64_t tn, int split) __attribute__((always_inline)) {
-    head_mul<TX, false, VB>(x, tm, tn, split, la0, la1, lb0, lb1); });
+    head_mul<TX, false, VB>(x, tm, tn, split, DPRC_HEAD_LDS(TX)); });
   if (wg >= 0)
     tile(TY{}, y, wg, [&](int64_t tm, int64_t tn, int split) __attribute__((always_inline)) {
-      head_mul<TY, true, true>(y, tm, tn, split, la0, la1, lb0, lb1); });
+      head_mul<TY, true, true>(y, tm, tn, split, DPRC_HEAD_LDS(TY)); });
 }
 
 // Joins the tiles' maxima and sums in a fixed order and takes the target's logit, summed in fp32.  TPB tokens per
@@ -784,10 +816,28 @@ __global__ __launch_bounds__(256) void head_round_kernel(const float* planes, in
 typedef HeadTile<uint16_t, 2, 4, 4, 2> TileWide;       // 256 x 256, eight waves of 128 x 64
 typedef HeadTile<uint16_t, 2, 2, 2, 2> TileMid;        // 128 x 128, four waves of 64 x 64
 typedef HeadTile<uint16_t, 2, 2, 1, 1> TileSmall;      // 64 x 64, four waves of 32 x 32
+typedef HeadTile<uint16_t, 2, 2, 2, 2, 4> TileMidRing;
+typedef HeadTile<uint16_t, 2, 2, 1, 1, 4> TileSmallRing;
 typedef HeadTile<float, 2, 2, 2, 2> TileMidF32;
 typedef HeadTile<float, 2, 2, 1, 1> TileSmallF32;
-typedef HeadTile<uint16_t, 8, 1, 1, 2> TileFew;        // 256 x 64, eight waves of 32 x 64
+typedef HeadTile<uint16_t, 4, 1, 1, 2> TileFew;        // 128 x 64, four waves of 32 x 64
+typedef HeadTile<uint16_t, 4, 1, 1, 2, 3> TileFewRing;
 typedef HeadTile<float, 4, 1, 2, 1> TileFewF32;        // 256 x 32, four waves of 64 x 32
+
+// Four slabs in LDS for bf16 tiles so few that they all run at once with them, and a contraction of 8 slabs or more: a slab
+// is on its way while three are multiplied.  Loss of N x d x V = 100 x 2048 x 32000, 64 x 2048 x 8000 36, 25 us, with two
+// 47, 32; dh of 500 x 1024 x 20000 with errors 98 and 104.  Shorter ones lose by it (dW of 8 tokens 33 and 31), fp32 products are
+// as fast without.
+static bool ring_tiles(int64_t m, int64_t n, int64_t K, int64_t S, int side, int bf16) {
+  return bf16 && K >= 8 * TileMid::slab && ceil_div(m, side) * ceil_div(n, side) * S <= (side == 64 ? 512 : side == 128 ? 256 : 0);
+}
+
+// f(tile) with the ring's tile or the other.
+template <class T, class R, class F>
+static void ring_if(bool ring, T tile, R ringed, F&& f) {
+  if (ring) f(ringed);
+  else f(tile);
+}
 
 // The side of the tiles of an m x n result: the largest that leaves no CU without a tile, else small ones.
 static int tile_side(int64_t m, int64_t n, int bf16) {
@@ -805,9 +855,10 @@ static int64_t whole_rounds(int64_t m, int64_t n) {
   return tm * tn < 256 || last * tn > kHeadLastRound || (tm - last) * tn < 192 ? m : std::min(m, 256 * (tm - last));
 }
 
-// Up to 64 tokens (32 in fp32) of a large vocabulary: tiles of all tokens and 256 rows of W, which bounds the call and
-// is read past the caches.  64 tokens of 128256 x 2048 bf16 114 us (525 MB); with three and four slabs of loads under
-// way and one such workgroup a CU 115, with every wave reading rows of its own into registers 313.
+// Up to 64 tokens (32 in fp32) of a large vocabulary: tiles of all tokens and 128 (256) rows of W, which bounds the call and
+// is read past the caches; bf16 with three slabs in LDS, two workgroups a CU.  64 tokens of 2048 and V 128256, 65536, 32000
+// (32 tokens) bf16 96, 61, 37 us; two slabs 111, 67, 41, four (one workgroup a CU) 102, 66, 35; 256 rows and two slabs
+// 102, 67, 53; d 512 and V 250000 53, with 256 rows 49.  Every wave reading rows of its own into registers: 3 times as slow.
 static bool few_tokens(int64_t N, int64_t nv, int bf16) { return N <= (bf16 ? 64 : 32) && nv >= 64 * 256; }
 
 static int logits_side(int64_t N, int64_t nv, int bf16) {
@@ -825,7 +876,7 @@ static int64_t logits_rounds(int64_t N, int64_t nv, int bf16) {
 
 static int64_t logits_tiles(int64_t N, int64_t nv, int bf16) {
   const int side = logits_side(N, nv, bf16);
-  return ceil_div(nv, side == 0 ? 256 : side);
+  return ceil_div(nv, side > 0 ? side : bf16 ? TileFew::MT : TileFewF32::MT);
 }
 
 template <bool ERRORS>
@@ -834,14 +885,15 @@ static void launch_logits_part(const HeadArgs& a, hipStream_t st) {
     typedef decltype(tile) TL;
     const dim3 grid = flat_grid(ceil_div(a.nv, TL::MT) * ceil_div(a.N, TL::NT));
     if (a.vec_w) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, true>), grid, dim3(TL::threads), 0, st, a);
-    else DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false>), grid, dim3(TL::threads), 0, st, a);
+    else if constexpr (TL::ring == 2) DPRC_LAUNCH((head_logits_kernel<TL, ERRORS, false>), grid, dim3(TL::threads), 0, st, a);
   };
   const int side = logits_side(a.N, a.nv, a.bf16);
+  const bool ring = side > 0 && a.vec_w && ring_tiles(a.nv, a.N, a.W.width, 1, side, a.bf16);
   if (a.bf16) {
-    if (side == 0) tiles(TileFew{});
+    if (side == 0) ring_if(a.vec_w, TileFew{}, TileFewRing{}, tiles);
     else if (side == 256) tiles(TileWide{});
-    else if (side == 128) tiles(TileMid{});
-    else tiles(TileSmall{});
+    else if (side == 128) ring_if(ring, TileMid{}, TileMidRing{}, tiles);
+    else ring_if(ring, TileSmall{}, TileSmallRing{}, tiles);
   } else {
     if (side == 0) tiles(TileFewF32{});
     else if (side == 128) tiles(TileMidF32{});
@@ -935,11 +987,12 @@ static void launch_mul(const HeadMulArgs& a, hipStream_t st) {
     typedef decltype(tile) TL;
     if constexpr (AKR) go(head_mul_kernel<TL, true, true>, tile);      // h's copy
     else if (a.vec_b) go(head_mul_kernel<TL, false, true>, tile);
-    else go(head_mul_kernel<TL, false, false>, tile);
+    else if constexpr (TL::ring == 2) go(head_mul_kernel<TL, false, false>, tile);
   };
+  const bool ring = a.vec_b && ring_tiles(a.rows, a.cols, a.per_split, a.S, a.side, a.bf16);
   if (a.bf16 && a.side == 256) rows(TileWide{});
-  else if (a.bf16 && a.side == 128) rows(TileMid{});
-  else if (a.bf16) rows(TileSmall{});
+  else if (a.bf16 && a.side == 128) ring_if(ring, TileMid{}, TileMidRing{}, rows);
+  else if (a.bf16) ring_if(ring, TileSmall{}, TileSmallRing{}, rows);
   else if (a.side == 128) rows(TileMidF32{});
   else rows(TileSmallF32{});
 }
@@ -958,7 +1011,7 @@ hipError_t launch_head_pair(HeadMulArgs x, HeadMulArgs y, hipStream_t st) {
     typedef decltype(ty) TY;
     const int64_t blocks = ceil_div(x.rows, TX::MT) * ceil_div(x.cols, TX::NT) * x.S + ceil_div(y.rows, TY::MT) * ceil_div(y.cols, TY::NT) * y.S;
     if (x.vec_b) DPRC_LAUNCH((head_pair_kernel<TX, TY, true>), flat_grid(blocks), dim3(TY::threads), 0, st, x, y);
-    else DPRC_LAUNCH((head_pair_kernel<TX, TY, false>), flat_grid(blocks), dim3(TY::threads), 0, st, x, y);
+    else if constexpr (TX::ring == 2) DPRC_LAUNCH((head_pair_kernel<TX, TY, false>), flat_grid(blocks), dim3(TY::threads), 0, st, x, y);
   };
   auto sides = [&](auto small, auto mid) {
     if (x.side == 128 && y.side == 128) go(mid, mid);
@@ -966,7 +1019,9 @@ hipError_t launch_head_pair(HeadMulArgs x, HeadMulArgs y, hipStream_t st) {
     else if (y.side == 128) go(small, mid);
     else go(small, small);
   };
-  if (x.bf16) sides(TileSmall{}, TileMid{});
+  const auto ring = [](const HeadMulArgs& a) { return a.side == 64 && a.vec_b && ring_tiles(a.rows, a.cols, a.per_split, a.S, 64, a.bf16); };
+  if (ring(x) && ring(y)) go(TileSmallRing{}, TileSmallRing{});
+  else if (x.bf16) sides(TileSmall{}, TileMid{});
   else sides(TileSmallF32{}, TileMidF32{});
   return hipGetLastError();
 }
