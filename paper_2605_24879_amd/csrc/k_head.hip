@@ -39,12 +39,13 @@ __device__ __forceinline__ void tile_of(int64_t wg, int64_t tm_n, int64_t tn_n, 
 // Accumulators as the 32 x 32 MFMAs hold them: WM x WN waves of XB x YB blocks; lane l of block (x, y) has
 // rows 8 (q / 4) + 4 (l / 32) + q % 4, q < 16, of column l % 32.
 
-template <class E, int WM_, int WN_, int XB_, int YB_, int RING = 2>
+// WK groups of waves take a part of every slab's contraction each.
+template <class E, int WM_, int WN_, int XB_, int YB_, int RING = 2, int WK_ = 1>
 struct HeadTile {
   typedef E elem;
-  static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_;
+  static constexpr int WM = WM_, WN = WN_, XB = XB_, YB = YB_, WK = WK_;
   static constexpr int ring = RING;                     // slabs in LDS
-  static constexpr int MT = 32 * XB * WM, NT = 32 * YB * WN, threads = 64 * WM * WN;
+  static constexpr int MT = 32 * XB * WM, NT = 32 * YB * WN, threads = 64 * WM * WN * WK;
   static constexpr int EP = kPiece<E>;                  // elements of a 16-byte piece
   static constexpr int slab = 8 * EP;                   // contraction elements of a slab: 64 bf16, 32 fp32
 };
@@ -235,7 +236,7 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
   constexpr int later = OA::direct && OB::direct ? (RING - 2) * (OA::P + OB::P) : 0;
   static_assert(later < 64 && (RING == 2 || (OA::direct && OB::direct)));
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  const int wm = wv / TL::WN, wn = wv % TL::WN;
+  const int wm = wv / TL::WN % TL::WM, wn = wv % TL::WN;
   auto gload = [&](int64_t k, auto u) __attribute__((always_inline)) {
     A.load(k < k1 ? k : (int64_t)1 << 40, lds.a[decltype(u)::value]);      // past the end: zeros
     B.load(k < k1 ? k : (int64_t)1 << 40, lds.b[decltype(u)::value]);
@@ -296,6 +297,35 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
   if constexpr (RING > 2) gload(k0 + TL::slab, HInt<1>{});
   if constexpr (RING > 3) gload(k0 + 2 * TL::slab, HInt<2>{});
   arrive(HInt<0>{});
+  if constexpr (TL::WK > 1) {
+    static_assert(TL::WK == 4 && TL::WM * TL::WN * XB * YB == 1 && TL::MT * TL::slab * sizeof(E) == 4096);
+    auto quarter = [&](int64_t k, auto u) __attribute__((always_inline)) {
+      gload(k + (RING - 1) * TL::slab, HInt<(decltype(u)::value + RING - 1) % RING>{});
+      frag(f0a, f0b, u, wv);
+      head_mfma<E, XB, YB>(f0a, f0b, acc);
+      arrive(HInt<(decltype(u)::value + 1) % RING>{});
+    };
+    for (int64_t k = k0; k < k1; k += RING * TL::slab) {
+      quarter(k, HInt<0>{});
+      quarter(k + TL::slab, HInt<1>{});
+      if constexpr (RING > 2) quarter(k + 2 * TL::slab, HInt<2>{});
+      if constexpr (RING > 3) quarter(k + 3 * TL::slab, HInt<3>{});
+    }
+    __builtin_amdgcn_s_waitcnt(0);
+    __syncthreads();
+    // every wave has the sum of the four, in their order
+    float* part[4] = {reinterpret_cast<float*>(lds.a[0]), reinterpret_cast<float*>(lds.a[1]),
+                      reinterpret_cast<float*>(lds.b[0]), reinterpret_cast<float*>(lds.b[1])};
+    float* own = wv == 0 ? part[0] : wv == 1 ? part[1] : wv == 2 ? part[2] : part[3];
+#pragma unroll
+    for (int q = 0; q < 16; ++q) own[64 * q + lane] = acc[0][0][q];
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < 16; ++q)
+      acc[0][0][q] = part[0][64 * q + lane] + part[1][64 * q + lane] + part[2][64 * q + lane] + part[3][64 * q + lane];
+    __syncthreads();
+    return;
+  }
   frag(f0a, f0b, HInt<0>{}, 0);
   for (int64_t k = k0; k < k1; k += RING * TL::slab) {  // (slabs past the end: zeros)
     step(k, HInt<0>{});
@@ -322,7 +352,7 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 template <class TL>
 __device__ __forceinline__ void head_sums(const HeadArgs& a, int64_t tm, int64_t t0, f32x16_t (&acc)[TL::XB][TL::YB],
                                           float2* lds) {
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN % TL::WM, wn = wv % TL::WN;
   const int64_t v0 = tm * TL::MT + 32 * TL::XB * wm;
   if (v0 + 32 * TL::XB > a.nv) {
 #pragma unroll
@@ -400,7 +430,7 @@ __device__ __forceinline__ void head_errors(const HeadArgs& a, int64_t tm, int64
                                             f32x16_t (&acc)[TL::XB][TL::YB], const HeadStage<TL>& stage) {
   typedef typename TL::elem E;
   constexpr int EP = TL::EP, PPR = TL::MT / EP;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN % TL::WM, wn = wv % TL::WN;
   const int64_t vt = tm * TL::MT;                       // the tile's first column of this piece
   const int v0 = 32 * TL::XB * wm;                      // the wave's first in the tile
   const int end = (int)min((int64_t)TL::MT, a.nv - vt); // the tile's columns before the vocabulary's end
@@ -496,7 +526,7 @@ __device__ __forceinline__ void head_targets(const HeadMulArgs& a, int split, in
   constexpr int TH = TL::threads, NW = TH / 64, PA = TL::MT * 8 / TH, PB = TL::NT * 8 / TH, RP = TL::NT / 8;
   typedef HeadOperand<TL, TL::MT, AKR, true> OA;
   typedef HeadOperand<TL, TL::NT, true, true> OB;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6, wm = wv / TL::WN % TL::WM, wn = wv % TL::WN;
   // A's slab: the k-th entry, zero where there is none, at row `row` of the tile; B's: row(k) of the operand
   auto slab = [&](auto row_of, bool in, int row, float lo) __attribute__((always_inline)) {
     uint4 v[PB];
@@ -595,7 +625,7 @@ template <class TL>
 __device__ __forceinline__ void head_store(const HeadMulArgs& a, int split, int64_t m0, int64_t n0,
                                            f32x16_t (&acc)[TL::XB][TL::YB]) {
   typedef typename TL::elem E;
-  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN, wn = wv % TL::WN;
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6, wm = wv / TL::WN % TL::WM, wn = wv % TL::WN;
   float* plane = a.planes + split * a.rows * a.cols;
 #pragma unroll
   for (int x = 0; x < TL::XB; ++x)
@@ -820,6 +850,8 @@ typedef HeadTile<uint16_t, 2, 2, 2, 2, 4> TileMidRing;
 typedef HeadTile<uint16_t, 2, 2, 1, 1, 4> TileSmallRing;
 typedef HeadTile<float, 2, 2, 2, 2> TileMidF32;
 typedef HeadTile<float, 2, 2, 1, 1> TileSmallF32;
+typedef HeadTile<float, 1, 1, 1, 1, 2, 4> TileLeastF32;  // 32 x 32, four waves of a quarter of the contraction
+typedef HeadTile<float, 1, 1, 1, 1, 4, 4> TileLeastRingF32;
 typedef HeadTile<uint16_t, 4, 1, 1, 2> TileFew;        // 128 x 64, four waves of 32 x 64
 typedef HeadTile<uint16_t, 4, 1, 1, 2, 3> TileFewRing;
 typedef HeadTile<float, 4, 1, 2, 1> TileFewF32;        // 256 x 32, four waves of 64 x 32
@@ -861,10 +893,16 @@ static int64_t whole_rounds(int64_t m, int64_t n) {
 // 102, 67, 53; d 512 and V 250000 53, with 256 rows 49.  Every wave reading rows of its own into registers: 3 times as slow.
 static bool few_tokens(int64_t N, int64_t nv, int bf16) { return N <= (bf16 ? 64 : 32) && nv >= 64 * 256; }
 
+// So few fp32 tiles of 64 x 64 that their contraction's length bounds them take 32 x 32, a quarter of it for each wave.  Loss of
+// N x d x V = 16 x 4096 x 300, 64 x 2048 x 4096, 200 x 2048 x 2000 43, 30, 38 us, in tiles of 64 92, 54, 53; up to 256 of
+// them 64 x 1024 x 12000 31 and 36, but 100 x 512 x 8000 24 and 22.
+constexpr int64_t kHeadLeast = 128;
+
 static int logits_side(int64_t N, int64_t nv, int bf16) {
   if (few_tokens(N, nv, bf16)) return 0;
   // one column of tiles: narrow ones, of which two share a CU
   const int side = tile_side(nv, N, bf16);
+  if (!bf16 && side == 64 && ceil_div(nv, 64) * ceil_div(N, 64) <= kHeadLeast) return 32;
   return bf16 ? (N <= 128 ? std::min(side, 128) : side) : (N <= 64 ? 64 : side);
 }
 
@@ -897,7 +935,8 @@ static void launch_logits_part(const HeadArgs& a, hipStream_t st) {
   } else {
     if (side == 0) tiles(TileFewF32{});
     else if (side == 128) tiles(TileMidF32{});
-    else tiles(TileSmallF32{});
+    else if (side == 64) tiles(TileSmallF32{});
+    else ring_if(a.vec_w, TileLeastF32{}, TileLeastRingF32{}, tiles);
   }
 }
 

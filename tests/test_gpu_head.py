@@ -167,6 +167,16 @@ def test_pieces(D, V, piece, dtype):
     check_backward(D, h, W, target, g, dtype, piece=piece)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,d,V,wpad", [(16, 1544, 300, 0), (33, 1030, 1000, 2), (70, 2050, 600, 2), (100, 776, 17000, 0), (40, 1000, 17000, 0),
+                                        (32, 776, 17000, 1), (200, 1544, 300, 0)])
+def test_long_contractions_of_few_tiles(D, T, d, V, wpad, dtype):
+    """Slabs three ahead, contractions over the waves, narrow tiles, and W off the boundaries for each."""
+    h, W, target, g = make(1, T, d, V, dtype, seed=T + d, wpad=wpad)
+    check_loss(D, h, W, target)
+    check_backward(D, h, W, target, g, dtype)
+
+
 @pytest.mark.parametrize("T,V", [(70, 66565), (700, 65700)])
 def test_rows_past_whole_rounds_of_tiles(D, T, V):
     """Rounds of 256 tiles and a few more, whose rows of W are products of their own (dW's for 70 tokens; the logits' and
