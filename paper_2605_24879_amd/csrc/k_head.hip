@@ -222,8 +222,8 @@ __device__ __forceinline__ void head_mfma(const uint4 (&av)[XB], const uint4 (&b
 }
 
 // acc = sum over k in [k0, k1) of A[i][k] B[j][k], i and j the tile's rows and columns; k0 a multiple of the
-// slab.  fp32 products and sums (bf16 products are exact).  While a slab is multiplied the next TL::ring - 1 are
-// on their way.  A wave has the next fragments in registers ahead of their products, also
+// slab.  fp32 products and sums (bf16 products are exact).  While a slab is multiplied the next TL::ring - 1 are on
+// their way.  A wave has the next fragments in registers ahead of their products, also
 // across the slab's one barrier, and reads and products are issued in turn.
 // bf16, 256 x 256 tiles of 128000 x 8192 x 2048: 1330 TFLOP/s (the same loop as the compiler orders it 1146, all
 // reads before all products 1270, four waves of 128 x 128 1217, tiles of 128 x 128 1093).
@@ -245,7 +245,7 @@ __device__ __forceinline__ void head_product(OA A, OB B, int64_t k0, int64_t k1,
   auto arrive = [&](auto u) __attribute__((always_inline)) {
     A.arrive(lds.a[decltype(u)::value]);
     B.arrive(lds.b[decltype(u)::value]);
-    if constexpr (later > 0) {
+    if constexpr (later > 0) {                          // (with the fences all loads would be waited for)
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(later) : "memory");
     } else {
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
