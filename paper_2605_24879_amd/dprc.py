@@ -864,10 +864,9 @@ def _tensors(tensors, outs):
                 if y.shape != t.shape or y.dtype != t.dtype or y.get_device() != index:
                     raise ValueError("every result must have its tensor's shape, dtype and device")
                 r, _, ldo = _tensor_rows(y, "a result")
-                if r != rows:                  # one of them is contiguous
-                    n = rows * cols
+                if r != rows:                  # one of them is contiguous, given as one row
+                    ldx, ldo = (t.shape[1], ldo) if rows == 1 else (ldx, t.shape[1])
                     rows, cols = t.shape
-                    ldx, ldo = ldx if ldx != n else cols, ldo if ldo != n else cols
             if place in places and t.numel():
                 raise ValueError("a result is listed twice")
             places.add(place)

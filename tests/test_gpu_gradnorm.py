@@ -82,6 +82,22 @@ def test_strided_rows(D):
     assert (base[2][:, 2:] == 9).all()
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("R,C", [(2, 4), (3, 70), (5, 9000)])
+def test_rows_as_far_apart_as_the_tensor_is_long(D, R, C, dtype):
+    """A row stride of R C elements, on either side of a contiguous tensor: nothing between the rows is read or written."""
+    n, x = R * C, make([(R, C)], seed=C, dtypes=(dtype,))[0]
+    want, norm = D.dprc_grad_clip([x], 0.5, outs=[torch.empty_like(x)])
+    buf = torch.full((R, n), 7.0, dtype=dtype, device="cuda")
+    out, m = D.dprc_grad_clip([x], 0.5, outs=[buf[:, :C]])
+    assert torch.equal(out[0], want[0]) and torch.equal(m, norm) and (buf[:, C:] == 7).all()
+    buf = torch.full((R, n), float("nan"), dtype=dtype, device="cuda")
+    buf[:, :C] = x
+    out, m = D.dprc_grad_clip([buf[:, :C]], 0.5, outs=[torch.empty_like(x)])
+    assert torch.equal(out[0], want[0]) and torch.equal(m, D.dprc_grad_norm([buf[:, :C]]))
+    check(D, [buf[:, :C]], 0.5, [torch.empty_like(x)])
+
+
 def test_odd_addresses(D):
     buf, out = torch.randn(5003, device="cuda").bfloat16(), torch.zeros(5003, device="cuda").bfloat16()
     check(D, [buf[1:], buf[:1]], 3.0, [out[1:], out[:1]])

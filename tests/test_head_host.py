@@ -241,6 +241,19 @@ def test_binding_refuses_mismatched_tensors(calls):
     assert [t[2:6] for t in dprc.TENSOR.iter_unpack(words)] == [(4, 5, 5, 9), (4, 5, 9, 5), (1, 20, 20, 20)]
 
 
+@pytest.mark.parametrize("R,C,wide", [(2, 4, 8), (2, 1, 2), (3, 5, 15), (3, 5, 7), (3, 5, 5 * 15)])
+def test_rows_beside_a_contiguous_tensor_keep_their_stride(calls, R, C, wide):
+    """A matrix whose rows lie any number of elements apart (its own number of elements, too) beside a contiguous one, as
+    the tensor or as the result, is packed with both strides."""
+    t, rows = torch.ones(R, C), torch.zeros(R, wide)[:, :C]
+    shape = lambda *a: [w[2:6] for w in dprc.TENSOR.iter_unpack(dprc._tensors(*a))]
+    assert shape([t], [rows]) == [(R, C, C, wide)]
+    assert shape([rows], [t]) == [(R, C, wide, C)]
+    assert shape([rows], [torch.zeros(R, wide + 1)[:, :C]]) == [(R, C, wide, wide + 1)]
+    assert shape([rows], None) == [(R, C, wide, wide)]
+    assert shape([t], [torch.zeros(R, C)]) == [(1, R * C, R * C, R * C)]
+
+
 def test_oracle_against_torch():
     rng = np.random.default_rng(0)
     h, W = rng.standard_normal((2, 5, 7)), rng.standard_normal((11, 7))
