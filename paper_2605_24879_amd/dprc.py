@@ -871,6 +871,10 @@ def _tensors(tensors, outs):
                 raise ValueError("a result is listed twice")
             places.add(place)
         parts.append(pack(t.data_ptr(), place, rows, cols, ldx, ldo, code))
+    if sources is not None and len(sources) < len(tensors):     # a tensor is listed twice (or several are empty)
+        at = [t.data_ptr() for t in tensors if t.numel()]
+        if any(t.numel() and y.data_ptr() == t.data_ptr() and at.count(y.data_ptr()) > 1 for t, y in zip(tensors, outs)):
+            raise ValueError("a result lies where another tensor does")
     return b"".join(parts)
 
 

@@ -254,6 +254,19 @@ def test_rows_beside_a_contiguous_tensor_keep_their_stride(calls, R, C, wide):
     assert shape([t], [torch.zeros(R, C)]) == [(1, R * C, R * C, R * C)]
 
 
+def test_binding_refuses_a_result_over_another_entrys_tensor(calls):
+    """A tensor listed twice may be scaled in place by neither entry: the other one still reads it."""
+    a, b, e = torch.ones(4, 5), torch.ones(4, 5), torch.zeros(0)
+    rows = torch.ones(4, 9)[:, :5]
+    for ts, outs in (([a, a], [a, b]), ([a, a], [b, a]), ([a, rows, rows], [b, rows, torch.ones(4, 5)]), ([e, e, a, a], [e, e, a.view(4, 5), b])):
+        with pytest.raises(ValueError, match="another"):
+            dprc.dprc_grad_clip(ts, 1.0, outs=outs)
+    assert not calls
+    dprc.dprc_grad_clip([a, a], 1.0, outs=[b, torch.ones(4, 5)])        # read twice, written elsewhere
+    dprc.dprc_grad_clip([e, a, e, b], 1.0, outs=[e, a, torch.zeros(0), torch.ones(4, 5)])
+    assert len(calls) == 2
+
+
 def test_oracle_against_torch():
     rng = np.random.default_rng(0)
     h, W = rng.standard_normal((2, 5, 7)), rng.standard_normal((11, 7))
