@@ -275,3 +275,14 @@ def test_rotary_module():
     with torch.inference_mode():                            # then trained
         first(torch.zeros(1, 1, 1, 8, dtype=torch.float64))
     torch.autograd.grad(first(q).sum(), q)
+
+
+def test_tables_are_made_where_they_are_read(monkeypatch):
+    """The stack's own cosines and sines are for blocks without a rotary module."""
+    made, tables, tok = [], llama._rope_tables, tokens()
+    monkeypatch.setattr(llama, "_rope_tables", lambda *a: made.append(a) or tables(*a))
+    plain = llama.build(seed=3, device="cpu", dtype=torch.float32, **SIZES)
+    loss_of(stack(), tok)()
+    assert not made
+    plain(tok[:, :-1])
+    assert len(made) == 1

@@ -132,6 +132,7 @@ class LlamaShaped(nn.Module):
             with torch.device("cpu"):           # frequencies are values, whatever device the model is laid out on
                 rot = Rotary(hidden // heads, base=rope_base)
         self.blocks = nn.ModuleList([block(hidden, mlp, heads, kv_heads, make_norm, make_drop, rot) for _ in range(layers)])
+        self.tables = rot is None
         self.norm = make_norm(hidden)
         self.lm_head = nn.Linear(hidden, vocab, bias=False)
         head_of = None
@@ -159,7 +160,7 @@ class LlamaShaped(nn.Module):
         if targets is not None and self.head is None:
             raise ValueError("losses come with head=True")
         B, T = tokens.shape
-        cos, sin = _rope_tables(T, self.hd, self.rope_base, tokens.device)
+        cos, sin = _rope_tables(T, self.hd, self.rope_base, tokens.device) if self.tables else (None, None)
         mask = torch.full((T, T), float("-inf"), device=tokens.device).triu(1)
         x = self.embed(tokens)
         if self.junctions:
