@@ -37,9 +37,9 @@ SIDE_OUT, SIDE_IN, SIDE_AUTO = 0, 1, 2
 
 
 def as_f64(x):
-    """Widen an input array (float32, float64, or a torch tensor of bf16/fp32) exactly."""
-    if hasattr(x, "detach"):                      # torch tensor: bf16 -> fp32 is exact
-        x = x.detach().to("cpu").float().numpy()
+    """Widen an input (a float32 or float64 array, or a torch tensor of bf16, fp32 or fp64) exactly."""
+    if hasattr(x, "detach"):
+        x = x.detach().to("cpu").double().numpy()
     return np.asarray(x, dtype=np.float64)
 
 

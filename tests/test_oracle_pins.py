@@ -371,3 +371,11 @@ def test_private_gradient_composition():
     assert np.allclose(g, est.clip_accumulate(A, E, c) / 3, rtol=1e-15)
     g = est.private_gradient(A, E, c, 0.7, 2.0, 9, 4, 3)
     assert np.allclose(g, est.add_noise(est.clip_accumulate(A, E, c), 0.7, 2.0, 9, 4) / 3, rtol=1e-15)
+
+
+def test_widening_is_exact():
+    x = 1.0 + torch.arange(1, 40, dtype=torch.float64) * 2.0 ** -50
+    assert (est.as_f64(x) == x.numpy()).all() and (est.as_f64(x.numpy()) == x.numpy()).all()
+    for t in (torch.float32, torch.bfloat16):
+        y = torch.tensor([1.0, -3.0e38, 2.0 ** -126, float("inf")]).to(t).requires_grad_()
+        assert est.as_f64(y).dtype == np.float64 and (torch.from_numpy(est.as_f64(y)) == y.detach().double()).all()
