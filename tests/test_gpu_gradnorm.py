@@ -128,6 +128,28 @@ def test_extremes(D):
     assert D.dprc_grad_clip([torch.empty(0, device="cuda")], 1.0)[1].item() == 0
 
 
+@pytest.mark.parametrize("dtypes", [(torch.float32,), (torch.bfloat16,), (torch.bfloat16, torch.float32)])
+def test_several_launches_past_the_caches(D, dtypes):
+    """More tensors than a launch takes and more than 300 MiB: every launch reads past the caches but for its end."""
+    gen = torch.Generator(device="cuda").manual_seed(len(dtypes))
+    shapes = [(1201, 1571 + 4 * k) if k % 7 else (3 * k + 1,) for k in range(110)]
+    xs = [torch.randn(s, generator=gen, device="cuda").to(dtypes[i % len(dtypes)]) for i, s in enumerate(shapes)]
+    assert sum(x.numel() * x.element_size() for x in xs) > 300 << 20
+    norm = math.sqrt(sum(x.double().square().sum().item() for x in xs))
+    want = D.dprc_grad_norm(xs)
+    assert abs(want.item() - norm) <= 1.01 * U * norm
+    for max_norm in (0.3 * norm, 10.0 * norm):
+        c = min(1.0, max_norm / norm)
+        outs, n = D.dprc_grad_clip(xs, max_norm, outs=[torch.full_like(x, 9.0) for x in xs])
+        assert torch.equal(n, want)
+        for x, y in zip(xs, outs):
+            z = c * x.double()
+            assert ((y.double() - z).abs() <= (3.01 * U + R[x.dtype]) * z.abs() + 2.0 ** -149).all()
+    ys, _ = D.dprc_grad_clip([x.clone() for x in xs], 0.3 * norm)       # in place
+    outs, _ = D.dprc_grad_clip(xs, 0.3 * norm, outs=[torch.empty_like(x) for x in xs])
+    assert all(torch.equal(a, b) for a, b in zip(ys, outs))
+
+
 def test_past_32_bits(D):
     """More than 2^31 elements in one tensor, and rows more than 2^31 elements apart."""
     big = torch.zeros(2 ** 31 + 20000, dtype=torch.bfloat16, device="cuda")

@@ -177,6 +177,15 @@ def test_long_contractions_of_few_tiles(D, T, d, V, wpad, dtype):
     check_backward(D, h, W, target, g, dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,T,d,V,wpad", [(1, 32, 776, 17000, 0), (1, 1, 132, 16388, 0), (31, 1, 136, 16385, 0), (7, 1, 131, 16400, 0)])
+def test_few_tokens_of_a_large_vocabulary(D, B, T, d, V, wpad, dtype):
+    """One column of narrow tiles, W in whole pieces straight to LDS or off its boundaries, a last tile of few rows."""
+    h, W, target, g = make(B, T, d, V, dtype, seed=V, wpad=wpad)
+    check_loss(D, h, W, target)
+    check_backward(D, h, W, target, g, dtype)
+
+
 @pytest.mark.parametrize("T,V", [(70, 66565), (700, 65700)])
 def test_rows_past_whole_rounds_of_tiles(D, T, V):
     """Rounds of 256 tiles and a few more, whose rows of W are products of their own (dW's for 70 tokens; the logits' and

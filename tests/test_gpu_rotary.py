@@ -65,6 +65,24 @@ def test_shapes(D, B, T, H, Dh, r, dtype, out, interleaved):
     check(D.dprc_rotary(x, f, pos=pos.cuda(), inverse=True, **kw), x, f, pos.numpy(), out, 1.0, interleaved, True)
 
 
+@pytest.mark.parametrize("interleaved", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,H,Dh,r", [(3, 2, 8192, 4096), (2, 1, 1 << 20, 4096), (2, 1, 1 << 20, 1), (2, 1 << 16, 16, 8), (3, 1 << 16, 3, 1)])
+def test_ends_of_the_ranges(D, T, H, Dh, r, dtype, interleaved):
+    """The most pairs, the widest head, the most heads.  (The product and the reduction of an angle are off by about 2^-52
+    of it: 2^-32 of a radian at a position of 10^6, far below the roundings to 32 bits.)"""
+    x, f = make(1, T, H, Dh, dtype, seed=r), freqs(r).cuda()
+    pos = torch.tensor([[1_000_000, 3, 77]])[:, :T]
+    check(D.dprc_rotary(x, f, pos=pos.cuda(), interleaved=interleaved), x, f, pos.numpy(), dtype, interleaved=interleaved)
+    want = D.dprc_rotary(x, f, start=5, inverse=True, interleaved=interleaved)
+    check(want, x, f, 5 + np.arange(T)[None], dtype, interleaved=interleaved, inverse=True)
+    if H > 2:                                            # as many in two tensors
+        a, b = D.dprc_rotary([x[:, :, :-1], x[:, :, -1:]], f, start=5, inverse=True, interleaved=interleaved)
+        assert torch.equal(torch.cat([a, b], 2), want)
+    D.dprc_rotary(x, f, start=5, inverse=True, interleaved=interleaved, out=x)
+    assert torch.equal(x, want)
+
+
 def test_far_positions(D):
     """Angles of 2^40 radians and more."""
     x, f = make(1, 4, 2, 64, "f32"), freqs(32).cuda()
