@@ -343,7 +343,8 @@ dprc_status dprc_clip_accumulate_vectors(const float* G, int64_t ldg, const floa
  * with that lse every gradient of the token.  Products are summed in fp32, exponentials taken in fp32 (logits of
  * 1e38 or more give infinities or NaN); E is rounded to the head's dtype once (as the gradient of stored logits is),
  * then enters the products.  In dh and dW of bf16 heads the target's entry of E, by far the largest of its row, enters
- * as two bf16 numbers: the rounded one and what its rounding lost.
+ * as two bf16 numbers: the rounded one and what its rounding lost.  The norms and the clipped sum take E rounded once, as
+ * dprc_head_errors gives it: they are those of one and the same per-sample gradient.
  *
  * The last four go through the vocabulary in pieces of `piece` columns, of which E is held in the workspace:
  * a positive multiple of DPRC_HEAD_BLOCK, or 0 for as many as E of 1 GiB holds (at least one block).  dh, dW

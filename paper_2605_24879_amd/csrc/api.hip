@@ -2188,7 +2188,9 @@ constexpr int64_t kGradBlocks = 1024;       // workgroups, and parts of the sum,
 constexpr int64_t kGradChunkLeast = 4096, kGradChunkMost = 16384;
 constexpr int64_t kGradSmall = 1 << 14;     // elements that one workgroup clips (79047 take 19 us so, 13 in two launches)
 constexpr int64_t kGradStream = (int64_t)300 << 20;   // bytes of tensors from which on they go past the caches
-constexpr int64_t kGradKeep = 3000;         // chunks at a launch's end that do not (188 MiB of fp32: 243 million values 500 us; 0, 1000, 2048: 514, 514, 505)
+// chunks at a launch's end that do not: 188 MiB of fp32 in whole chunks, 94 of bf16 (243 million fp32 values 500 us; 0, 1000,
+// 2048: 514, 514, 505)
+constexpr int64_t kGradKeep = 3000;
 
 int64_t grad_bytes(const dprc_tensor* t, int32_t count) {
   int64_t n = 0;

@@ -98,7 +98,10 @@ __device__ __forceinline__ double block_sum(double t) {
   return t;
 }
 
-// Chunks before a.keep are read past the caches, which then hold the last ones when the scaling begins.
+// Chunks before a.keep are read past the caches, which then hold the last ones when the scaling begins.  So for one launch
+// (kGradTensors tensors).  Of several each keeps its own end, and they are scaled in the order of the squares: the later
+// ones have pushed out what the first left.  113 fp32 tensors of 4.9 GB: 3063 us, norm alone 1143; 160 bf16 tensors of
+// 512 MB: 578, norm alone 263 (launches of 256 workgroups one after the other).
 __global__ __launch_bounds__(256) void grad_squares_kernel(GradArgs a) {
   double t = 0.0;
   for (int64_t c = blockIdx.x; c < a.chunks; c += gridDim.x) {
@@ -190,7 +193,7 @@ __device__ __forceinline__ void chunk_scale(const GradTensor& g, const GradChunk
   }
 }
 
-// From the last chunk on: what the squares read last is still in the caches.
+// From the launch's last chunk on: where it is the only launch, what the squares read last is still in the caches.
 __global__ __launch_bounds__(256) void grad_scale_kernel(GradArgs a) {
   const double norm = sqrt(grad_total(a)), c = grad_factor(a, norm);
   if (a.norm && blockIdx.x == 0 && threadIdx.x == 0) *a.norm = (float)norm;

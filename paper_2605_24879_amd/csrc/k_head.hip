@@ -652,7 +652,7 @@ __device__ __forceinline__ void head_store(const HeadMulArgs& a, int split, int6
 
 // ---- kernels --------------------------------------------------------------------------------------
 
-// arrays for slabs of MT rows and NT columns, two or four of each
+// arrays for slabs of MT rows and NT columns, RING (2 to 4) of each
 #define DPRC_HEAD_SLABS(E, MT, NT, SLAB, RING)                                        \
   __shared__ __attribute__((aligned(16))) E la0[MT * SLAB];                           \
   __shared__ __attribute__((aligned(16))) E la1[MT * SLAB];                           \

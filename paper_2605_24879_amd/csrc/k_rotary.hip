@@ -8,8 +8,10 @@
 // The angle is reduced to a fraction of a turn in 64 bits (in 32 a position of 10^6 would lose 0.06 of a
 // radian), to an eighth of a turn beside whole quarters; sine and cosine of that are taken in 32.
 // A thread takes eight pairs at a time, two 16-byte loads of bfloat16; the r mod 8 pairs left at the end of a head go as
-// 4, 2 and 1 (one at a time: 138 us for 16+4 heads of 96 with r 13 and 2^16 tokens, so 112).  32 + 8 heads of 64
-// bfloat16 features, 2^15 tokens: 72 us, 4.6 TB/s; with non-temporal loads and stores 77.  A step of 64 tokens: 3.6 us.
+// 4, 2 and 1 (one at a time: 138 us for 16 + 4 heads of 96 with r 13 and 2^15 tokens, results heads first, so 112;
+// tokens first 88, with r 16 44).  32 + 8 heads of 64 bfloat16 features, 2^15 tokens: 72 us, 4.6 TB/s; with
+// non-temporal loads and stores 77.  A step of 64 tokens: 3.8 us.  A workgroup reads x behind its angles' barrier, which
+// adds their latencies: 12 us for 3063 tokens of 12 + 4 fp32 heads of 80, twice their bytes' time.
 #include <algorithm>
 #include "device.hpp"
 #include "kernels.hpp"

@@ -533,7 +533,7 @@ hipError_t launch_rotary(RotaryArgs a, hipStream_t st);
 
 // The joint norm of many tensors and their clipping (see dprc_grad_clip).  A tensor is rows of cols
 // elements; its chunks of about GradArgs::chunk elements are numbered from chunk0 on.
-constexpr int kGradTensors = 48;     // of a launch: 2.8 KB of kernel arguments
+constexpr int kGradTensors = 48;     // of a launch: 3136 bytes of kernel arguments
 struct GradTensor {
   const void* x;
   void* out;
@@ -545,7 +545,7 @@ struct GradArgs {
   int64_t chunk, chunks;             // elements of a chunk; how many there are
   double* part;                      // [parts], this launch's from part0 on
   int32_t part0, parts;
-  int64_t keep;                      // the first chunk that is kept in the caches; 0: all are
+  int64_t keep;                      // the first chunk of the launch that is kept in the caches; 0: all are
   double max_norm;
   float* norm;                       // may be null
   GradTensor t[kGradTensors];

@@ -892,7 +892,8 @@ def dprc_grad_norm(tensors, norm=None, ws=None):
 
 def dprc_grad_clip(tensors, max_norm, outs=None, norm=None, ws=None):
     """Every tensor times min(1, max_norm / the joint norm), into outs (by default the tensors themselves): returns
-    (outs, norm [1]).  A norm that is not finite gives zeros."""
+    (outs, norm [1]).  A norm that is not finite gives zeros.  A result lies over its own tensor or over none; a tensor
+    that is listed twice has results elsewhere."""
     outs = list(tensors if outs is None else outs)
     if len(outs) != len(tensors):
         raise ValueError("one result per tensor")
