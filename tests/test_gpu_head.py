@@ -283,6 +283,34 @@ def test_targets_past_the_vocabulary_and_infinite_logits(D, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 67])
+def test_a_sample_whose_errors_are_not_finite_is_clipped_to_nothing(D, d, dtype):
+    """The largest and the smallest target there are, an infinite weight of a loss: of other samples nothing changes, and with
+    the factor that the estimates give the clipped sum is theirs."""
+    B, T, V = 4, 70, 9001
+    h, W, target, g = make(B, T, d, V, dtype, seed=d, ignored="none")
+    target[0, 3], target[0, 66] = -2 ** 63, -1
+    clean = target.clone()
+    target[1, 5], target[2, 64] = 2 ** 63 - 1, V
+    loss, lse = D.dprc_head_loss(h, W, target)
+    l0, z0 = D.dprc_head_loss(h, W, clean)
+    bad = target != clean
+    assert torch.equal(loss.isnan(), bad) and torch.equal(lse.isnan(), bad) and loss[0, 3] == 0 and loss[0, 66] == 0
+    assert torch.equal(loss[~bad], l0[~bad]) and torch.equal(lse[~bad], z0[~bad])
+    dh, _, n2 = D.dprc_head_backward(h, W, target, lse, g, weight_grad=False, k=8, seed=3)
+    r, _, m2 = D.dprc_head_backward(h, W, clean, z0, g, weight_grad=False, k=8, seed=3)
+    assert torch.equal(dh[~bad], r[~bad]) and dh[bad].isnan().all()
+    gi = g.clone()
+    gi[3, 7] = float("inf")
+    n2 = torch.cat([n2[:3], D.dprc_head_backward(h, W, clean, z0, gi, hidden_grad=False, weight_grad=False, k=8, seed=3)[2][3:]])
+    assert torch.equal(n2[:1], m2[:1]) and not n2[1:].isfinite().any()
+    c = D.dprc_clip_scale(n2, 0.5)
+    assert c[0] > 0 and not c[1:].any()
+    got = D.dprc_head_clip_accumulate(h, W, target, lse, gi, c)
+    assert got.isfinite().all() and torch.equal(got, D.dprc_head_clip_accumulate(h, W, clean, z0, g, c))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("side", [0, 1, 2])
 @pytest.mark.parametrize("probe,k", [(0, 16), (2, 8), (0, 33)])
 def test_private(D, dtype, side, probe, k):

@@ -112,6 +112,29 @@ def test_rotary_module_gradients(mods, dtype):
     assert torch.equal(one, whole[:, -1:])
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_modules_of_broadcast_inputs(mods, dtype):
+    """One sample's hidden states and one head's features for all: gradients are the sums over what shares them."""
+    _, _, head, rotary = mods
+    g = torch.Generator().manual_seed(9)
+    mod = head.Head(torch.nn.Linear(40, 300, bias=False, device="cuda", dtype=dtype))
+    h = torch.randn(1, 13, 40, generator=g).to(dtype).cuda().requires_grad_()
+    y = torch.randint(0, 300, (3, 13), generator=g).cuda()
+    whole = h.detach().expand(3, 13, 40).contiguous().requires_grad_()
+    assert torch.equal(mod(h.expand(3, 13, 40), y), mod(whole, y))
+    a, = torch.autograd.grad(mod(h.expand(3, 13, 40), y).mean(), h)      # a broadcast gradient of the losses, too
+    b, = torch.autograd.grad(mod(whole, y).mean(), whole)
+    assert torch.equal(a, b.sum(0, keepdim=True))
+    rot = rotary.Rotary(20, dim=12)
+    k = torch.randn(2, 9, 1, 20, generator=g).to(dtype).cuda().requires_grad_()
+    w = torch.randn(2, 9, 5, 20, generator=g).to(dtype).cuda()
+    each = k.detach().expand(2, 9, 5, 20).contiguous().requires_grad_()
+    assert torch.equal(rot(k.expand(2, 9, 5, 20)), rot(each))
+    a, = torch.autograd.grad((rot(k.expand(2, 9, 5, 20)) * w).sum(), k)
+    b, = torch.autograd.grad((rot(each) * w).sum(), each)
+    assert torch.equal(a, b.sum(2, keepdim=True))
+
+
 def test_private_step_with_a_head(mods):
     """Estimates and clipped sums of the head against those of its stored gradient, and the update of its weight."""
     D, dpsgd, _, _ = mods
